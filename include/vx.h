@@ -381,9 +381,10 @@ vx_status vx_topk_select(const float* scores, int32_t score_stride, int32_t num_
  * the split kernel, by the pair's last split; for MLA by a merge launch).  Logical ids
  * outside [0, P_i) are skipped.  max_sel above 2^24 returns VX_ERR_UNSUPPORTED.
  * workspace: device buffer of at least vx_workspace_size(VX_STAGE_DECODE) bytes.  It starts
- * with one 32-bit split counter per (request, KV head) pair, which must be zero before the
+ * with the 32-bit split counters of the (request, KV head) pairs, which must be zero before the
  * first call: zero-fill the buffer once after allocating it.  Every call leaves the counters
- * zero again; the rest of the buffer is scratch.  Do not use the buffer for anything else. */
+ * zero again; the rest of the buffer is scratch.  Batches of any size and geometry may take turns
+ * on one buffer that is large enough.  Do not use the buffer for anything else. */
 vx_status vx_sparse_paged_decode(const void* q, int32_t num_q_heads,
                                  const vx_paged_cache* kv, const vx_batch* b,
                                  const int32_t* sel_pages, const int32_t* sel_count,

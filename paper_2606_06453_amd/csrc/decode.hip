@@ -1197,9 +1197,10 @@ DecodeLayout decode_layout(int batch, int num_kv_heads, int group, int head_dim_
   }
   auto al = [](size_t x) { return (x + 255) & ~(size_t)255; };
   const long long rows = pairs * L.splits;
-  size_t off = 0;
-  L.off_ctr = off;
-  off = al(off + sizeof(uint32_t) * (size_t)(mla ? 0 : pairs));
+  // Only batches of fewer than kGqaTargetWgs pairs split any, and the counters keep their place in
+  // every layout: a buffer that batches of other sizes have used still has them at zero.
+  L.off_ctr = 0;
+  size_t off = al(sizeof(uint32_t) * kGqaTargetWgs);
   L.off_lse = off;
   off = al(off + sizeof(float) * (size_t)rows * group);
   L.off_o = off;

@@ -13,8 +13,8 @@ namespace vx {
 // of a split pair merge in the split kernel through the pair's counter.
 // MLA: `splits` workgroups per request over fixed slot ranges, merged by a merge launch.
 // Partials: fp32 output and log2-sum-exp per query head, `splits` rows per pair.
-// Workspace: [pairs] uint32 split counters (GQA; zero before the first call, every call leaves
-// them zero), then the partials.
+// Workspace: 512 uint32 split counters (GQA; zero before the first call, every call leaves them
+// zero), then the partials.
 struct DecodeLayout {
   int32_t splits;             // workgroups (partial rows) per pair
   int32_t split_slots;        // GQA: selection slots per split
