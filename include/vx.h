@@ -13,6 +13,9 @@
  *      inside the selection's top-K launch: steps 1 and 2 in two launches)
  *   3. vx_sparse_paged_decode  attention over the selected pages only (Eq. 4), as split-K
  *                              online softmax plus a merge, over a ragged batch.
+ * Around the step, the cache's own operators: vx_page_extend gives a step's tokens their pages,
+ * page list and slots and vx_page_release takes pages back; vx_kv_write puts whole prompts' rows
+ * into the cache by slot and vx_kv_read gives rows back as bf16.
  *
  * Conventions shared by every call
  * ---------------------------------
@@ -41,11 +44,20 @@
  *   fp8 entry is the fp32 product scale * code value; summaries, scores and attention all use
  *   that value.  For an MLA latent (V aliased to its first head_dim_v channels) the V values
  *   are the latent's, at the K scale; v_scale is then unused.
+ *   Or half a byte per element in the OCP microscaling format MXFP4: E2M1 codes (0, 0.5, 1, 1.5,
+ *   2, 3, 4, 6 and their negatives) and, for every 32 channels of a token, one E8M0 scale byte E;
+ *   the value of an entry is code * 2^(E - 127), NaN where E = 255 (scales the kernels write are 8
+ *   to 252, or 255).  k_scale and v_scale are unused.  GQA geometry only, caches 16-byte aligned.
  * - Paged KV cache (Appendix A), "HND": one (page, head) slice is one contiguous run.
  *       k  [num_phys_pages][num_kv_heads][page_size][head_dim_qk]
  *       v  [num_phys_pages][num_kv_heads][page_size][head_dim_v], or NULL when V is the first
  *          head_dim_v channels of K (absorbed-weight MLA latent, Sec. 6.2).
  *   Elements are bf16 or fp8 codes (kv_dtype); k and v have the same element type.
+ *   An mxfp4 slice is page_size * D / 2 bytes of codes, then page_size * D / 32 scale bytes, D the
+ *   head dim; two codes a byte, the even channel in the low nibble:
+ *       K  codes [token][D / 2], scales [token][D / 32];
+ *       V  codes [token / 4][16][token % 4][D / 32] (16 pieces of D / 16 channels, four tokens of a
+ *          piece side by side), scales [token / 4][D / 32][token % 4].
  * - Batch (Sec. 4.1, C = (b, p, I)): page_indptr [batch+1] with page_indptr[0] = 0, and
  *   page_indices [page_indptr[batch]] physical page ids.  The logical page j of request i is
  *   page_indices[page_indptr[i] + j].  Ids may repeat across requests (prefix sharing); a
@@ -139,7 +151,8 @@ typedef enum {
 typedef enum {
   VX_KV_BF16 = 0,
   VX_KV_FP8_E4M3 = 1,   /* OCP E4M3: bias 7, no infinities, S.1111.111 is NaN */
-  VX_KV_FP8_E5M2 = 2    /* OCP E5M2: bias 15 */
+  VX_KV_FP8_E5M2 = 2,   /* OCP E5M2: bias 15 */
+  VX_KV_MXFP4 = 3       /* OCP MXFP4: E2M1 codes, an E8M0 scale per 32 channels of a token */
 } vx_kv_dtype;
 
 typedef enum {
@@ -213,7 +226,8 @@ vx_status vx_page_summarize(const vx_paged_cache* kv, const vx_batch* b,
  * (L_i - 1) mod page_size of logical page (L_i - 1) / page_size:
  *   K[p][h][slot][:] = k_new[i][h][:]   k_new [batch][num_kv_heads][head_dim_qk]
  *   V[p][h][slot][:] = v_new[i][h][:]   v_new [batch][num_kv_heads][head_dim_v]
- * (kv_dtype elements: bf16, or fp8 codes already quantised with the cache's scales).  With V
+ * (kv_dtype elements: bf16, or fp8 codes already quantised with the cache's scales; for an mxfp4
+ * cache bf16 rows, quantised here exactly as vx_kv_write quantises them).  With V
  * aliased (kv->v NULL, MLA) v_new must be NULL and only K is written.  Then the summaries of
  * that page are written exactly as vx_page_summarize with first_page[i] = (L_i - 1) / page_size
  * writes them (bit-identical), to whichever of the four outputs are non-NULL.
@@ -407,6 +421,86 @@ vx_status vx_sparse_paged_decode_noalloc(const void* q, int32_t num_q_heads,
                                          const int32_t* sel_pages, const int32_t* sel_count,
                                          int32_t max_sel, float sm_scale,
                                          void* out, hipStream_t stream);
+
+/* ---- pages, block table and slots of growing requests ---------------------------------------
+ * A pool of physical pages and the requests that hold them, all device memory of the caller:
+ *   free_pages [num_phys_pages]   stack of the free pages' ids, free_pages[0 .. *free_count)
+ *   free_count [1]
+ *   table [table_rows][table_stride]   row r's pages in order, ceil(lens[r] / page_size) of them
+ *   lens  [table_rows]            tokens of each row (0 for a row that holds no request)
+ * table_stride * page_size must fit 31 bits.  block_size as in vx_paged_cache. */
+typedef struct {
+  int32_t* free_pages;
+  int32_t* free_count;
+  int32_t* table;
+  int32_t* lens;
+  int32_t num_phys_pages;
+  int32_t table_rows;
+  int32_t table_stride;
+  int32_t page_size;
+  int32_t block_size;
+} vx_page_pool;
+
+/* Host-only: workspace bytes of vx_page_extend and vx_page_release for a batch. */
+vx_status vx_page_workspace_size(int32_t batch, size_t* bytes);
+
+/* A step's tokens get their pages and slots (Sec. 4.1, C = (b, p, I)).  Request i is row rows[i]
+ * of the table, L_i = lens[rows[i]] tokens long, and asks for new_lens[i] >= 0 tokens, i.e. for
+ * need_i = ceil((L_i + n_i) / page_size) - ceil(L_i / page_size) pages.  In the order of the batch
+ * a request is granted its tokens when its row has room for them and either need_i = 0 or the
+ * needs up to and with it sum to at most *free_count (requests whose row has no room need
+ * nothing); else none of them.  The p-th page granted, over all requests in order, is
+ * free_pages[*free_count - 1 - p].  Then
+ *   table, lens, free_count       hold the new state
+ *   granted [batch]               n_i, or 0 for a refused request
+ *   seq_lens [batch]              L_i + granted[i]
+ *   page_indptr [batch+1], page_indices [page_indices_cap]   the page lists of seq_lens, as vx_batch
+ *                                 takes them; lists past the capacity are cut, and page_indptr with
+ *                                 them; entries behind the last list are left as they were
+ *   token_indptr [batch+1]        running sums of new_lens (refused ones too): request i's tokens are
+ *                                 rows token_indptr[i] .. of the step's packed K/V rows
+ *   slots [slots_cap]             slot (page * page_size + token in the page) of every packed row; -1
+ *                                 for rows of refused requests and for entries behind the last row
+ *   first_block [batch] or NULL   L_i / block_size: the first block whose summary changes
+ *                                 (first_page of vx_page_summarize)
+ * rows must differ from each other; a row outside the table is refused and has no pages.  An empty
+ * batch writes nothing.  seq_lens must not be pool->lens. */
+vx_status vx_page_extend(const vx_page_pool* pool, int32_t batch, const int32_t* rows, const int32_t* new_lens,
+                         int32_t* seq_lens, int32_t* page_indptr, int32_t* page_indices, int32_t page_indices_cap,
+                         int32_t* token_indptr, int64_t* slots, int32_t slots_cap, int32_t* granted,
+                         int32_t* first_block, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Row rows[i] keeps its first min(keep_lens[i], lens) tokens (keep_lens NULL: none, the request has
+ * ended); its pages past them go back to the stack, the first one listed (in the order of the batch
+ * and of each row) on top, so that a release to the former lengths takes a vx_page_extend of the same
+ * rows back exactly.  rows must differ from each other; rows outside the table are skipped.  A page
+ * that other rows or requests still use must not be released here. */
+vx_status vx_page_release(const vx_page_pool* pool, int32_t batch, const int32_t* rows, const int32_t* keep_lens,
+                          void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Rows into the cache by slot: row n of k_new and v_new, bf16, goes to token slots[n] % page_size of
+ * page slots[n] / page_size, for every KV head.
+ *   k_new[n * k_row_stride + h * k_head_stride + c], v_new alike (strides in elements, any sign,
+ *   multiples of 8; rows 16-byte aligned); v_new NULL when V is aliased.
+ *   bf16   the value itself
+ *   fp8    the code nearest to the fp32 quotient value / scale, ties to the even code; larger
+ *          magnitudes, infinities too, become the largest finite one; NaN stays NaN
+ *   mxfp4  per group of 32 channels E - 127 is the exponent of the group's largest magnitude rounded
+ *          to one mantissa bit (half up), less 2, E held within 8 .. 252; then the code nearest to
+ *          value / 2^(E - 127), ties to the even code, at most 6.  A group with an infinity or a NaN
+ *          gets E = 255 and reads as NaN.
+ * Slots below 0 or past the cache are skipped, so padded rows may carry -1; the others must differ
+ * from each other.  The summaries are the caller's to refresh (vx_page_summarize). */
+vx_status vx_kv_write(const vx_paged_cache* kv, const void* k_new, int64_t k_row_stride, int64_t k_head_stride,
+                      const void* v_new, int64_t v_row_stride, int64_t v_head_stride, const int64_t* slots,
+                      int32_t num_rows, hipStream_t stream);
+
+/* Rows out of the cache by slot: the values of token slots[n], rounded to bf16 (exact for bf16 and
+ * mxfp4 caches), to k_out and v_out laid out as the rows of vx_kv_write; zeros for a slot below 0
+ * or past the cache.  Slots may repeat. */
+vx_status vx_kv_read(const vx_paged_cache* kv, void* k_out, int64_t k_row_stride, int64_t k_head_stride, void* v_out,
+                     int64_t v_row_stride, int64_t v_head_stride, const int64_t* slots, int32_t num_rows,
+                     hipStream_t stream);
 
 /* Measurement utility, not a step of the path: reads `bytes` (a positive multiple of 16) from
  * the 16-byte aligned device buffer `buf` with 16-byte loads carrying the non-temporal hint (the

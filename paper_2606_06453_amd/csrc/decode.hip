@@ -43,6 +43,7 @@
 #include <mutex>
 #include <type_traits>
 
+#include "mxfp4.h"
 #include "vx_device.h"
 #include "vx_internal.h"
 
@@ -328,6 +329,60 @@ __device__ __forceinline__ void widen_tile(const Tile8<D>& s, Tile<D>& t) {
   }
 }
 
+// The same tile from an mxfp4 cache: codes and scales as loaded, converted to the bf16 Tile just before
+// use (a code times its scale is a bf16 value).
+template <int D>
+struct Tile4 {
+  static constexpr int KW = D / 32, VW = D / 32;   // 32-bit words of codes per lane
+  uint32_t k[KW];                      // D/4 codes of token col: channels D/4 * grp ..
+  uint32_t v[VW];                      // token rows 4*grp + r, piece col (D/16 channels), r by r
+  uint32_t ke, ve;                     // the scale of k; the scales of the four rows of v
+};
+
+template <int D>
+__device__ __forceinline__ void load_tile4(const uint8_t* __restrict__ ks, const uint8_t* __restrict__ vs, int t0,
+                                           int ps, int col, int grp, Tile4<D>& t) {
+  const uint8_t* kc = ks + (t0 + col) * (D / 2) + grp * (D / 8);
+  const uint8_t* vc = vs + t0 * (D / 2) + grp * (2 * D) + col * (D / 8);
+  if constexpr (D == 128) {
+    const uint4 a = load_stream_u4(kc), b = load_stream_u4(vc);
+    t.k[0] = a.x; t.k[1] = a.y; t.k[2] = a.z; t.k[3] = a.w;
+    t.v[0] = b.x; t.v[1] = b.y; t.v[2] = b.z; t.v[3] = b.w;
+  } else {
+    const uint2 a = load_stream_u2(kc), b = load_stream_u2(vc);
+    t.k[0] = a.x; t.k[1] = a.y;
+    t.v[0] = b.x; t.v[1] = b.y;
+  }
+  const int sc = ps * (D / 2) + t0 * (D / 32);
+  t.ke = ks[sc + col * (D / 32) + grp * D / 128];
+  t.ve = *reinterpret_cast<const uint32_t*>(vs + sc + grp * (D / 8) + col / (512 / D) * 4);
+}
+
+template <int D>
+__device__ __forceinline__ void widen_tile4(const Tile4<D>& s, Tile<D>& t) {
+  const float ksc = mx::scale_value(s.ke);
+#pragma unroll
+  for (int kk = 0; kk < D / 32; kk++) {
+    const u32x4_t w = {mx::pair_bf16<0>(s.k[kk], ksc), mx::pair_bf16<1>(s.k[kk], ksc), mx::pair_bf16<2>(s.k[kk], ksc),
+                       mx::pair_bf16<3>(s.k[kk], ksc)};
+    t.k[kk] = __builtin_bit_cast(bf16x8_t, w);
+  }
+#pragma unroll
+  for (int r = 0; r < 4; r++) {
+    const float vsc = mx::scale_value((s.ve >> (8 * r)) & 0xffu);
+    if constexpr (D == 128) {
+      t.v[r][0] = mx::pair_bf16<0>(s.v[r], vsc);
+      t.v[r][1] = mx::pair_bf16<1>(s.v[r], vsc);
+      t.v[r][2] = mx::pair_bf16<2>(s.v[r], vsc);
+      t.v[r][3] = mx::pair_bf16<3>(s.v[r], vsc);
+    } else {
+      const uint32_t w = s.v[r >> 1];
+      t.v[r][0] = (r & 1) ? mx::pair_bf16<2>(w, vsc) : mx::pair_bf16<0>(w, vsc);
+      t.v[r][1] = (r & 1) ? mx::pair_bf16<3>(w, vsc) : mx::pair_bf16<1>(w, vsc);
+    }
+  }
+}
+
 template <int D>
 __device__ __forceinline__ void compute_tile(Tile<D>& t, const bf16x8_t (&qv)[D / 32], int valid, int grp,
                                              float scale_log2, float& m, float& lsum, f32x4_t (&acc)[D / 16]) {
@@ -399,10 +454,19 @@ __device__ __forceinline__ void compute_tile(Tile<D>& t, const bf16x8_t (&qv)[D 
 template <int D, int KT>
 struct TileOps {
   using Elem = typename std::conditional<KT == kKvBf16, uint16_t, uint8_t>::type;
-  using T = typename std::conditional<KT == kKvBf16, Tile<D>, Tile8<D>>::type;
-  __device__ static __forceinline__ void load(const Elem* kt, const Elem* vt, int col, int grp, T& t) {
-    if constexpr (KT == kKvBf16) load_tile<D>(kt, vt, col, grp, t);
-    else load_tile8<D>(kt, vt, col, grp, t);
+  using T = typename std::conditional<
+      KT == kKvBf16, Tile<D>, typename std::conditional<KT == kKvMxFp4, Tile4<D>, Tile8<D>>::type>::type;
+  // tile t16 (16 tokens) of slice `sl` = page * H + head
+  __device__ static __forceinline__ void load(const Elem* k, const Elem* v, int64_t sl, int t16, int ps, int col,
+                                              int grp, T& t) {
+    if constexpr (KT == kKvMxFp4) {
+      const int64_t at = sl * mx::slice_bytes(ps, D);
+      load_tile4<D>(k + at, v + at, 16 * t16, ps, col, grp, t);
+    } else {
+      const int64_t at = sl * ps * D + (int64_t)t16 * 16 * D;
+      if constexpr (KT == kKvBf16) load_tile<D>(k + at, v + at, col, grp, t);
+      else load_tile8<D>(k + at, v + at, col, grp, t);
+    }
   }
   __device__ static __forceinline__ void compute(T& t, const bf16x8_t (&qv)[D / 32], int valid, int grp,
                                                  float scale_log2, float& m, float& lsum, f32x4_t (&acc)[D / 16]) {
@@ -410,7 +474,8 @@ struct TileOps {
       compute_tile<D>(t, qv, valid, grp, scale_log2, m, lsum, acc);
     } else {
       Tile<D> w;
-      widen_tile<D, KT>(t, w);
+      if constexpr (KT == kKvMxFp4) widen_tile4<D>(t, w);
+      else widen_tile<D, KT>(t, w);
       compute_tile<D>(w, qv, valid, grp, scale_log2, m, lsum, acc);
     }
   }
@@ -458,8 +523,6 @@ __device__ __forceinline__ void gqa_wave_slots(const DecodeArgs& a, int i, int h
   cnt_all = min(max(cnt_raw, 0), a.max_sel);
   const int cnt = min(cnt_all, hi_fixed);                       // end of this split's slots
   const int P = num_pages(L, a.bs, list_len * a.r, INT_MAX);     // blocks of the request
-  const int64_t head_off = (int64_t)h * a.ps * D;
-  const int64_t page_stride = (int64_t)a.H * a.ps * D;
 
   // windows of 64 of the wave's slots (one per lane); the first was loaded above
   for (int w0 = 0; lo + w + U * w0 < cnt; w0 += kWave) {
@@ -481,15 +544,13 @@ __device__ __forceinline__ void gqa_wave_slots(const DecodeArgs& a, int i, int h
     int ls = 0, ltt = 0;
     while (ls < nb && __builtin_amdgcn_readlane(my_n, ls) <= 0) ls++;
     if (ls >= nb) continue;
-    auto tile_ptr_k = [&](int p, int t16) { return kbase + p * page_stride + head_off + (int64_t)t16 * 16 * D; };
-    auto tile_ptr_v = [&](int p, int t16) { return vbase + p * page_stride + head_off + (int64_t)t16 * 16 * D; };
     auto fetch = [&](typename Ops::T& buf) -> int {
       if (ls >= nb) return 0;
       int n = __builtin_amdgcn_readlane(my_n, ls);
       const int t0 = n >> 16;
       n &= 0xffff;
       const int p = __builtin_amdgcn_readlane(my_p, ls);
-      Ops::load(tile_ptr_k(p, t0 + ltt), tile_ptr_v(p, t0 + ltt), col, grp, buf);
+      Ops::load(kbase, vbase, (int64_t)p * a.H + h, t0 + ltt, a.ps, col, grp, buf);
       const int valid = min(16, n - 16 * ltt);
       if (++ltt * 16 >= n) {
         ltt = 0;
@@ -1304,6 +1365,7 @@ hipError_t launch_decode(const Geometry& g, const uint16_t* q, int Hq, const int
   do {                                                       \
     if (g.kv_dtype == kKvFp8E4M3) VX_GQA(D, NW, kKvFp8E4M3); \
     else if (g.kv_dtype == kKvFp8E5M2) VX_GQA(D, NW, kKvFp8E5M2); \
+    else if (g.kv_dtype == kKvMxFp4) VX_GQA(D, NW, kKvMxFp4); \
     else VX_GQA(D, NW, kKvBf16);                             \
   } while (0)
     if (g.Dqk == 128) {

@@ -1,0 +1,252 @@
+// Rows into and out of the paged cache by slot (slot = page * page_size + token in the page).
+//
+// vx_kv_write rounds bf16 rows to the cache's type; vx_kv_read gives the cache's values as bf16.
+// A task is 8 consecutive channels of one row and head, K and V side by side.  Four consecutive rows
+// of a head share a wave (16 chunks each), so that rows of consecutive slots, whose V codes of an
+// mxfp4 cache interleave by four, fill whole lines together.  Bound by HBM: a row of D channels is
+// 2 D bytes of bf16 and 2 D (bf16), D (fp8) or 17 D / 32 (mxfp4) bytes of cache, for K and V each.
+#include "mxfp4.h"
+#include "vx_device.h"
+#include "vx_internal.h"
+
+namespace vx {
+namespace {
+
+constexpr int kRowThreads = 256;
+
+struct RowArgs {
+  uint8_t* k;
+  uint8_t* v;
+  const uint16_t* k_in;
+  const uint16_t* v_in;
+  uint16_t* k_out;
+  uint16_t* v_out;
+  int64_t k_row, k_head, v_row, v_head;    // strides of the bf16 rows, in elements
+  const int64_t* slots;
+  int n, H, ps, ps_shift, num_phys;
+  float k_scale, v_scale;
+};
+
+// Task x: row, head and chunk; false past the last row.
+template <int D>
+__device__ __forceinline__ bool row_task(const RowArgs& a, int64_t x, int& n, int& h, int& c8) {
+  constexpr int CH = D / 8;
+  c8 = (int)(x % CH);
+  const int64_t y = x / CH;
+  const int64_t z = y >> 2;
+  const int64_t nq = z / a.H;
+  h = (int)(z - nq * a.H);
+  const int64_t row = nq * 4 + (y & 3);
+  n = (int)row;
+  return row < a.n;
+}
+
+// Page and token of a slot; false for a slot outside the cache.
+__device__ __forceinline__ bool slot_place(const RowArgs& a, int64_t slot, int64_t& page, int& t) {
+  page = slot >> a.ps_shift;
+  t = (int)(slot & (a.ps - 1));
+  return slot >= 0 && page < a.num_phys;
+}
+
+// 8 values of a row as fp8 codes: value / scale, to the nearest even code, finite values and
+// infinities at most the format's largest.
+template <int KT>
+__device__ __forceinline__ uint2 encode_fp8(const uint4& w, float scale) {
+  constexpr float kTop = KT == kKvFp8E4M3 ? 448.f : 57344.f;
+  const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+  float x[8];
+#pragma unroll
+  for (int e = 0; e < 4; e++) {
+    x[2 * e] = bf16lo(ws[e]) / scale;
+    x[2 * e + 1] = bf16hi(ws[e]) / scale;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; e++) x[e] = x[e] != x[e] ? x[e] : fminf(fmaxf(x[e], -kTop), kTop);
+  int lo = 0, hi = 0;
+  if constexpr (KT == kKvFp8E4M3) {
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], lo, false);
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], lo, true);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[4], x[5], hi, false);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[6], x[7], hi, true);
+  } else {
+    lo = __builtin_amdgcn_cvt_pk_bf8_f32(x[0], x[1], lo, false);
+    lo = __builtin_amdgcn_cvt_pk_bf8_f32(x[2], x[3], lo, true);
+    hi = __builtin_amdgcn_cvt_pk_bf8_f32(x[4], x[5], hi, false);
+    hi = __builtin_amdgcn_cvt_pk_bf8_f32(x[6], x[7], hi, true);
+  }
+  return make_uint2((uint32_t)lo, (uint32_t)hi);
+}
+
+template <int KT>
+__device__ __forceinline__ uint4 decode_fp8(const uint2& w, float scale) {
+  const int ws[2] = {(int)w.x, (int)w.y};
+  uint32_t o[4];
+#pragma unroll
+  for (int h = 0; h < 2; h++) {
+    float2_t lo, hi;
+    if constexpr (KT == kKvFp8E4M3) {
+      lo = __builtin_amdgcn_cvt_pk_f32_fp8(ws[h], false);
+      hi = __builtin_amdgcn_cvt_pk_f32_fp8(ws[h], true);
+    } else {
+      lo = __builtin_amdgcn_cvt_pk_f32_bf8(ws[h], false);
+      hi = __builtin_amdgcn_cvt_pk_f32_bf8(ws[h], true);
+    }
+    o[2 * h] = f32_to_bf16_rne(lo[0] * scale) | (f32_to_bf16_rne(lo[1] * scale) << 16);
+    o[2 * h + 1] = f32_to_bf16_rne(hi[0] * scale) | (f32_to_bf16_rne(hi[1] * scale) << 16);
+  }
+  return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+// Largest of the four adjacent lanes that hold a group.
+__device__ __forceinline__ uint32_t quad_max(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xf, 0xf, false));
+  return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xf, 0xf, false));
+}
+
+template <int D, int KT>
+__device__ __forceinline__ void write_chunk(const RowArgs& a, bool v, int64_t page, int t, int h, int c8, bool ok,
+                                            const uint4& w) {
+  uint8_t* base = v ? a.v : a.k;
+  if constexpr (KT == kKvMxFp4) {
+    const uint32_t e = mx::group_scale(quad_max(mx::amax_bits(w)));   // every lane of the quad takes part
+    if (!ok) return;
+    uint8_t* slice = base + (page * a.H + h) * mx::slice_bytes(a.ps, D);
+    const uint32_t codes = mx::encode8(w, e);
+    if (v) mx::put_v_codes(slice, t, c8, D, codes);
+    else *reinterpret_cast<uint32_t*>(slice + mx::k_code(t, c8, D)) = codes;
+    if ((c8 & 3) == 0)
+      slice[mx::codes_bytes(a.ps, D) + (v ? mx::v_scale(t, c8 >> 2, D) : mx::k_scale(t, c8 >> 2, D))] = (uint8_t)e;
+  } else if (ok) {
+    const int64_t at = ((page * a.H + h) * a.ps + t) * D + 8 * c8;
+    if constexpr (KT == kKvBf16) *reinterpret_cast<uint4*>(base + 2 * at) = w;
+    else *reinterpret_cast<uint2*>(base + at) = encode_fp8<KT>(w, v ? a.v_scale : a.k_scale);
+  }
+}
+
+template <int D, int KT>
+__global__ __launch_bounds__(kRowThreads) void write_kernel(const RowArgs a) {
+  int n, h, c8;
+  const bool in = row_task<D>(a, (int64_t)blockIdx.x * kRowThreads + threadIdx.x, n, h, c8);
+  int64_t page = 0;
+  int t = 0;
+  const bool ok = in && slot_place(a, a.slots[n], page, t);
+  uint4 wk{}, wv{};
+  if (ok) {
+    wk = load_stream_u4(a.k_in + n * a.k_row + h * a.k_head + 8 * c8);
+    if (a.v) wv = load_stream_u4(a.v_in + n * a.v_row + h * a.v_head + 8 * c8);
+  }
+  write_chunk<D, KT>(a, false, page, t, h, c8, ok, wk);
+  if (a.v) write_chunk<D, KT>(a, true, page, t, h, c8, ok, wv);
+}
+
+template <int D, int KT>
+__device__ __forceinline__ uint4 read_chunk(const RowArgs& a, bool v, int64_t page, int t, int h, int c8) {
+  const uint8_t* base = v ? a.v : a.k;
+  if constexpr (KT == kKvMxFp4) {
+    const uint8_t* slice = base + (page * a.H + h) * mx::slice_bytes(a.ps, D);
+    const uint32_t w = v ? mx::get_v_codes(slice, t, c8, D)
+                         : *reinterpret_cast<const uint32_t*>(slice + mx::k_code(t, c8, D));
+    const float s = mx::scale_value(
+        slice[mx::codes_bytes(a.ps, D) + (v ? mx::v_scale(t, c8 >> 2, D) : mx::k_scale(t, c8 >> 2, D))]);
+    return make_uint4(mx::pair_bf16<0>(w, s), mx::pair_bf16<1>(w, s), mx::pair_bf16<2>(w, s), mx::pair_bf16<3>(w, s));
+  } else {
+    const int64_t at = ((page * a.H + h) * a.ps + t) * D + 8 * c8;
+    if constexpr (KT == kKvBf16) return *reinterpret_cast<const uint4*>(base + 2 * at);
+    else return decode_fp8<KT>(*reinterpret_cast<const uint2*>(base + at), v ? a.v_scale : a.k_scale);
+  }
+}
+
+template <int D, int KT>
+__global__ __launch_bounds__(kRowThreads) void read_kernel(const RowArgs a) {
+  int n, h, c8;
+  if (!row_task<D>(a, (int64_t)blockIdx.x * kRowThreads + threadIdx.x, n, h, c8)) return;
+  int64_t page = 0;
+  int t = 0;
+  uint4 wk{}, wv{};
+  if (slot_place(a, a.slots[n], page, t)) {
+    wk = read_chunk<D, KT>(a, false, page, t, h, c8);
+    if (a.v) wv = read_chunk<D, KT>(a, true, page, t, h, c8);
+  }
+  *reinterpret_cast<uint4*>(a.k_out + n * a.k_row + h * a.k_head + 8 * c8) = wk;
+  if (a.v) *reinterpret_cast<uint4*>(a.v_out + n * a.v_row + h * a.v_head + 8 * c8) = wv;
+}
+
+template <int D, int KT>
+hipError_t launch(const RowArgs& all, bool write, hipStream_t stream) {
+  // a launch has fewer than 2^32 threads
+  const int most = (1 << 30) / (all.H * (D / 8)) & ~3;
+  RowArgs a = all;
+  for (int done = 0; done < all.n; done += a.n) {
+    a.n = all.n - done < most ? all.n - done : most;
+    a.slots = all.slots + done;
+    if (write) {
+      a.k_in = all.k_in + done * all.k_row;
+      if (a.v) a.v_in = all.v_in + done * all.v_row;
+    } else {
+      a.k_out = all.k_out + done * all.k_row;
+      if (a.v) a.v_out = all.v_out + done * all.v_row;
+    }
+    const int64_t tasks = ((int64_t)a.n + 3) / 4 * 4 * a.H * (D / 8);
+    const dim3 grid((unsigned)((tasks + kRowThreads - 1) / kRowThreads));
+    if (write) hipLaunchKernelGGL((write_kernel<D, KT>), grid, dim3(kRowThreads), 0, stream, a);
+    else hipLaunchKernelGGL((read_kernel<D, KT>), grid, dim3(kRowThreads), 0, stream, a);
+  }
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_kt(const RowArgs& a, int kt, bool write, hipStream_t stream) {
+  if (kt == kKvFp8E4M3) return launch<D, kKvFp8E4M3>(a, write, stream);
+  if (kt == kKvFp8E5M2) return launch<D, kKvFp8E5M2>(a, write, stream);
+  if constexpr (D != 576) {
+    if (kt == kKvMxFp4) return launch<D, kKvMxFp4>(a, write, stream);
+  }
+  return launch<D, kKvBf16>(a, write, stream);
+}
+
+hipError_t launch_rows(const Geometry& g, RowArgs& a, bool write, hipStream_t stream) {
+  if (a.n == 0) return hipSuccess;
+  a.k = static_cast<uint8_t*>(const_cast<void*>(g.k));
+  a.v = static_cast<uint8_t*>(const_cast<void*>(g.v));
+  a.H = g.H;
+  a.ps = g.ps;
+  a.ps_shift = __builtin_ctz((unsigned)g.ps);
+  a.num_phys = g.num_phys_pages;
+  a.k_scale = g.k_scale;
+  a.v_scale = g.v_scale;
+  if (g.Dqk == 128) return launch_kt<128>(a, g.kv_dtype, write, stream);
+  if (g.Dqk == 64) return launch_kt<64>(a, g.kv_dtype, write, stream);
+  return launch_kt<576>(a, g.kv_dtype, write, stream);
+}
+
+}  // namespace
+
+hipError_t launch_kv_write(const Geometry& g, const RowView& k, const RowView& v, const int64_t* slots, int n,
+                           hipStream_t stream) {
+  RowArgs a{};
+  a.k_in = static_cast<const uint16_t*>(k.rows);
+  a.v_in = static_cast<const uint16_t*>(v.rows);
+  a.k_row = k.row_stride;
+  a.k_head = k.head_stride;
+  a.v_row = v.row_stride;
+  a.v_head = v.head_stride;
+  a.slots = slots;
+  a.n = n;
+  return launch_rows(g, a, true, stream);
+}
+
+hipError_t launch_kv_read(const Geometry& g, const RowView& k, const RowView& v, const int64_t* slots, int n,
+                          hipStream_t stream) {
+  RowArgs a{};
+  a.k_out = static_cast<uint16_t*>(const_cast<void*>(k.rows));
+  a.v_out = static_cast<uint16_t*>(const_cast<void*>(v.rows));
+  a.k_row = k.row_stride;
+  a.k_head = k.head_stride;
+  a.v_row = v.row_stride;
+  a.v_head = v.head_stride;
+  a.slots = slots;
+  a.n = n;
+  return launch_rows(g, a, false, stream);
+}
+
+}  // namespace vx

@@ -2766,7 +2766,7 @@ hipError_t launch_score_topk(const Geometry& g, const uint16_t* q, int Hq, int k
   // radix path is not fused).
   AppendStep ap{};
   if (sa.k_new) {
-    if (approx || g.max_pages > kTwoPassMaxPages || flow) {
+    if (approx || g.max_pages > kTwoPassMaxPages || flow || g.kv_dtype == kKvMxFp4) {
       const hipError_t e =
           launch_kv_append_summarize(g, sa.k_new, sa.v_new, sa.mean, sa.mean_bf, sa.maxo, sa.mino, stream);
       if (e != hipSuccess) return e;

@@ -101,6 +101,7 @@ void dispatch(const Geometry& g, const int32_t* first_page, float* mean, uint16_
                      mean, mean_bf, maxo, mino, ppb, split, app)
   if (g.kv_dtype == kKvFp8E4M3) VX_SUMMARIZE(kKvFp8E4M3);
   else if (g.kv_dtype == kKvFp8E5M2) VX_SUMMARIZE(kKvFp8E5M2);
+  else if (g.kv_dtype == kKvMxFp4) VX_SUMMARIZE(kKvMxFp4);
   else VX_SUMMARIZE(kKvBf16);
 #undef VX_SUMMARIZE
 }

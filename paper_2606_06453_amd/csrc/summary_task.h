@@ -8,6 +8,7 @@
 #pragma once
 #include <type_traits>
 
+#include "mxfp4.h"
 #include "vx_device.h"
 #include "vx_internal.h"
 
@@ -70,6 +71,28 @@ struct RowChunk {
   }
 };
 
+// mxfp4: the 8 codes and their group's scale byte.
+template <>
+struct RowChunk<kKvMxFp4> {
+  struct Raw {
+    uint32_t codes, e;
+  };
+  static constexpr int kBytes = 4;
+  __device__ static __forceinline__ void values(const Raw& w, float, float (&x)[8]) {
+    const float s = mx::scale_value(w.e);
+    const float2_t v[4] = {mx::pair_f32<0>(w.codes, s), mx::pair_f32<1>(w.codes, s), mx::pair_f32<2>(w.codes, s),
+                           mx::pair_f32<3>(w.codes, s)};
+#pragma unroll
+    for (int e = 0; e < 8; e++) x[e] = v[e >> 1][e & 1];
+  }
+};
+
+// Largest over the four tasks of a group of 32 channels, whose lanes are 4 apart in a DPP row.
+__device__ __forceinline__ uint32_t group_max(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x124, 0xf, 0xf, false));
+  return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x128, 0xf, 0xf, false));
+}
+
 // Append mode: the step's rows, k_new [batch][H][D] and v_new [batch][H][Dv] (v_new null: V
 // aliased), and the caches they are written to (the same buffers the kernel reads k from).
 struct AppendArgs {
@@ -100,16 +123,34 @@ __device__ __forceinline__ void task(const void* __restrict__ kv, float k_scale,
   const int n = active ? min(bs, L - j * bs) : 0;
   using RC = RowChunk<KT>;
   // element offset of the block's first token row, channel chunk c8
+  constexpr bool kMx = KT == kKvMxFp4;
   const int64_t row0 = (p * H + h) * (int64_t)ps * D + (int64_t)blk * bs * D + c8 * 8;
-  const char* src = static_cast<const char*>(kv) + row0 * (RC::kBytes / 8);
-  const int64_t row_bytes = (int64_t)D * (RC::kBytes / 8);
+  const int64_t mxs = kMx ? (p * H + h) * mx::slice_bytes(ps, D) : 0;
+  const char* src = static_cast<const char*>(kv) + (kMx ? mxs + mx::k_code(blk * bs, c8, D) : row0 * (RC::kBytes / 8));
+  const int64_t row_bytes = kMx ? D / 2 : (int64_t)D * (RC::kBytes / 8);
+  const uint8_t* scales = static_cast<const uint8_t*>(kv) + mxs + mx::codes_bytes(ps, D) +
+                          mx::k_scale(blk * bs, c8 >> 2, D);                       // mxfp4
+  auto load_row = [&](int t) {
+    if constexpr (kMx)
+      return typename RC::Raw{*reinterpret_cast<const uint32_t*>(src + t * row_bytes), scales[t * (D / mx::kGroup)]};
+    else return RC::template load<STREAM>(src + (int64_t)t * row_bytes);
+  };
   // append: the new token is row n - 1 of this page; its chunk comes from the step's input
   const int n_mem = APPEND ? n - 1 : n;
   // append: the step's K (and V) chunk load first; they are written to row n - 1 after the
   // block's other rows are in flight (nothing in this launch reads row n - 1)
   typename RC::Raw new_row{}, new_v{};
   const bool writer = APPEND && active && slice == 0;
-  if constexpr (APPEND) {
+  if constexpr (APPEND && kMx) {
+    static_assert(!APPEND || TS == 4, "a group's tasks are 4 lanes apart");
+    const int64_t in = (((int64_t)i * H + h) * D + c8 * 8) * 2;
+    const uint4 k16 = *reinterpret_cast<const uint4*>(static_cast<const char*>(app.knew) + in);
+    const uint4 v16 = *reinterpret_cast<const uint4*>(static_cast<const char*>(app.vnew) + in);
+    new_row.e = mx::group_scale(group_max(mx::amax_bits(k16)));
+    new_row.codes = mx::encode8(k16, new_row.e);
+    new_v.e = mx::group_scale(group_max(mx::amax_bits(v16)));
+    new_v.codes = mx::encode8(v16, new_v.e);
+  } else if constexpr (APPEND) {
     const int64_t in = (((int64_t)i * H + h) * D + c8 * 8) * (RC::kBytes / 8);
     new_row = *reinterpret_cast<const typename RC::Raw*>(static_cast<const char*>(app.knew) + in);
     if (writer && app.vnew)   // V rows have D channels too (GQA); an aliased V has no rows of its own
@@ -128,7 +169,7 @@ __device__ __forceinline__ void task(const void* __restrict__ kv, float k_scale,
     typename RC::Raw w[KB];
 #pragma unroll
     for (int b = 0; b < KB; b++)
-      w[b] = RC::template load<STREAM>(src + (int64_t)min(t0 + TS * b, n_mem - 1) * row_bytes);
+      w[b] = load_row(min(t0 + TS * b, n_mem - 1));
     // The rows past the block's end are masked instead of skipped: a branch per row would let the
     // compiler sink each load into it, one round trip per row.  Adding +0 leaves s unchanged (s
     // starts at +0 and round-to-nearest never makes it -0), and -inf / +inf leave the max / min
@@ -157,7 +198,19 @@ __device__ __forceinline__ void task(const void* __restrict__ kv, float k_scale,
     else add_rows(std::true_type{});
   }
   if constexpr (APPEND) {
-    if (writer) {
+    if constexpr (kMx) {
+      if (writer) {
+        const int t = blk * bs + n - 1, sc = mx::codes_bytes(ps, D);
+        uint8_t* ks = static_cast<uint8_t*>(app.kw) + mxs;
+        uint8_t* vs = static_cast<uint8_t*>(app.vw) + mxs;
+        *reinterpret_cast<uint32_t*>(ks + mx::k_code(t, c8, D)) = new_row.codes;
+        mx::put_v_codes(vs, t, c8, D, new_v.codes);
+        if ((c8 & 3) == 0) {
+          ks[sc + mx::k_scale(t, c8 >> 2, D)] = (uint8_t)new_row.e;
+          vs[sc + mx::v_scale(t, c8 >> 2, D)] = (uint8_t)new_v.e;
+        }
+      }
+    } else if (writer) {
       const int64_t out = (row0 + (int64_t)(n - 1) * D) * (RC::kBytes / 8);
       *reinterpret_cast<typename RC::Raw*>(static_cast<char*>(app.kw) + out) = new_row;
       if (app.vnew) *reinterpret_cast<typename RC::Raw*>(static_cast<char*>(app.vw) + out) = new_v;

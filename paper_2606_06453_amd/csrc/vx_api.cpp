@@ -69,9 +69,16 @@ vx_status check_cache(const vx_paged_cache* kv, bool need_v) {
       !((kv->block_size == 16 || kv->block_size == 32) && kv->page_size % kv->block_size == 0))
     return fail(VX_ERR_UNSUPPORTED, "block_size %d must be 0, page_size, or 16 or 32 dividing page_size %d",
                 kv->block_size, kv->page_size);
-  if (kv->kv_dtype != VX_KV_BF16 && kv->kv_dtype != VX_KV_FP8_E4M3 && kv->kv_dtype != VX_KV_FP8_E5M2)
+  if (kv->kv_dtype != VX_KV_BF16 && kv->kv_dtype != VX_KV_FP8_E4M3 && kv->kv_dtype != VX_KV_FP8_E5M2 &&
+      kv->kv_dtype != VX_KV_MXFP4)
     return fail(VX_ERR_INVALID_ARG, "kv_dtype %d is not a vx_kv_dtype", kv->kv_dtype);
-  if (kv->kv_dtype != VX_KV_BF16) {
+  if (kv->kv_dtype == VX_KV_MXFP4) {
+    if (is_mla(kv))
+      return fail(VX_ERR_UNSUPPORTED, "an mxfp4 cache needs the GQA geometry (head_dim_qk 64 or 128)");
+    if ((reinterpret_cast<uintptr_t>(kv->k) & 15) != 0 || (reinterpret_cast<uintptr_t>(kv->v) & 15) != 0)
+      return fail(VX_ERR_INVALID_ARG, "mxfp4 caches must be 16-byte aligned");
+  }
+  if (kv->kv_dtype == VX_KV_FP8_E4M3 || kv->kv_dtype == VX_KV_FP8_E5M2) {
     if (!(kv->k_scale > 0.f) || !(kv->v_scale > 0.f) || std::isinf(kv->k_scale) || std::isinf(kv->v_scale))
       return fail(VX_ERR_INVALID_ARG, "fp8 caches need finite scales > 0 (got %g, %g)", (double)kv->k_scale,
                   (double)kv->v_scale);
@@ -138,8 +145,9 @@ vx::Geometry geometry(const vx_paged_cache* kv, const vx_batch* b) {
   g.k = kv->k;
   g.v = kv->v;
   g.kv_dtype = kv->kv_dtype;
-  g.k_scale = kv->kv_dtype == VX_KV_BF16 ? 1.f : kv->k_scale;
-  g.v_scale = kv->kv_dtype == VX_KV_BF16 ? 1.f : kv->v_scale;
+  const bool scaled = kv->kv_dtype == VX_KV_FP8_E4M3 || kv->kv_dtype == VX_KV_FP8_E5M2;
+  g.k_scale = scaled ? kv->k_scale : 1.f;
+  g.v_scale = scaled ? kv->v_scale : 1.f;
   g.num_phys_pages = kv->num_phys_pages;
   g.H = kv->num_kv_heads;
   g.ps = kv->page_size;
@@ -412,6 +420,122 @@ vx_status vx_sparse_paged_decode_noalloc(const void* q, int32_t num_q_heads, con
                                       sel_count, max_sel, sm_scale, static_cast<uint16_t*>(out), scratch, lay,
                                       stream),
                     "vx_sparse_paged_decode_noalloc");
+}
+
+namespace {
+
+// Rows of vx_kv_write and vx_kv_read: 16-byte accesses of 8 channels.
+vx_status check_rows(const char* name, const void* rows, int64_t row_stride, int64_t head_stride) {
+  if (!rows) return fail(VX_ERR_INVALID_ARG, "%s must be non-NULL", name);
+  if ((reinterpret_cast<uintptr_t>(rows) & 15) != 0 || row_stride % 8 != 0 || head_stride % 8 != 0)
+    return fail(VX_ERR_INVALID_ARG, "%s must be 16-byte aligned with strides of whole 8 elements", name);
+  return VX_OK;
+}
+
+vx_status kv_rows(const vx_paged_cache* kv, const void* k, int64_t k_row, int64_t k_head, const void* v, int64_t v_row,
+                  int64_t v_head, const int64_t* slots, int32_t n, bool write, hipStream_t stream, const char* name) {
+  vx_status s;
+  if ((s = check_cache(kv, true)) != VX_OK) return s;
+  if (n < 0) return fail(VX_ERR_INVALID_ARG, "num_rows must be >= 0");
+  if (n == 0) return VX_OK;
+  if ((reinterpret_cast<uintptr_t>(kv->k) & 15) != 0 || (reinterpret_cast<uintptr_t>(kv->v) & 15) != 0)
+    return fail(VX_ERR_INVALID_ARG, "the caches must be 16-byte aligned");
+  if (!slots) return fail(VX_ERR_INVALID_ARG, "slots must be non-NULL");
+  if ((s = check_rows(write ? "k_new" : "k_out", k, k_row, k_head)) != VX_OK)
+    return s;
+  if (!kv->v && v) return fail(VX_ERR_INVALID_ARG, "V rows given but V is aliased to K (kv->v is NULL)");
+  if (kv->v &&
+      (s = check_rows(write ? "v_new" : "v_out", v, v_row, v_head)) != VX_OK)
+    return s;
+  vx_batch none{};
+  const vx::RowView kr{k, k_row, k_head}, vr{v, v_row, v_head};
+  const vx::Geometry g = geometry(kv, &none);
+  return hip_status(write ? vx::launch_kv_write(g, kr, vr, slots, n, stream)
+                          : vx::launch_kv_read(g, kr, vr, slots, n, stream),
+                    name);
+}
+
+vx_status check_pool(const vx_page_pool* p) {
+  if (!p) return fail(VX_ERR_INVALID_ARG, "pool is NULL");
+  if (!p->free_pages || !p->free_count || !p->table || !p->lens)
+    return fail(VX_ERR_INVALID_ARG, "free_pages, free_count, table and lens must be non-NULL");
+  if (p->num_phys_pages < 1 || p->table_rows < 1 || p->table_stride < 1)
+    return fail(VX_ERR_INVALID_ARG, "num_phys_pages, table_rows and table_stride must be >= 1");
+  if (p->page_size != 16 && p->page_size != 32 && p->page_size != 64)
+    return fail(VX_ERR_UNSUPPORTED, "page_size %d not in {16, 32, 64}", p->page_size);
+  if (p->table_stride > INT32_MAX / p->page_size)
+    return fail(VX_ERR_UNSUPPORTED, "table_stride * page_size must fit 31 bits");
+  if (p->block_size != 0 && p->block_size != p->page_size &&
+      !((p->block_size == 16 || p->block_size == 32) && p->page_size % p->block_size == 0))
+    return fail(VX_ERR_UNSUPPORTED, "block_size %d must be 0, page_size, or 16 or 32 dividing page_size %d",
+                p->block_size, p->page_size);
+  return VX_OK;
+}
+
+vx::PagePool pool_of(const vx_page_pool* p) {
+  return vx::PagePool{p->free_pages,     p->free_count, p->table,        p->lens,
+                      p->num_phys_pages, p->table_rows, p->table_stride, p->page_size,
+                      p->block_size > 0 ? p->block_size : p->page_size};
+}
+
+vx_status check_plan(const vx_page_pool* pool, int32_t batch, const int32_t* rows, const void* ws, size_t ws_bytes) {
+  vx_status s;
+  if ((s = check_pool(pool)) != VX_OK) return s;
+  if (batch < 0 || batch > 65535) return fail(VX_ERR_INVALID_ARG, "batch %d not in [0, 65535]", batch);
+  if (batch > 0 && !rows) return fail(VX_ERR_INVALID_ARG, "rows must be non-NULL");
+  const size_t need = vx::plan_workspace_bytes(batch);
+  if (!ws || ws_bytes < need)
+    return fail(VX_ERR_WORKSPACE, "page workspace needs %zu bytes (got %zu)", need, ws ? ws_bytes : 0);
+  return VX_OK;
+}
+
+}  // namespace
+
+vx_status vx_kv_write(const vx_paged_cache* kv, const void* k_new, int64_t k_row_stride, int64_t k_head_stride,
+                      const void* v_new, int64_t v_row_stride, int64_t v_head_stride, const int64_t* slots,
+                      int32_t num_rows, hipStream_t stream) {
+  return kv_rows(kv, k_new, k_row_stride, k_head_stride, v_new, v_row_stride, v_head_stride, slots, num_rows, true,
+                 stream, "vx_kv_write");
+}
+
+vx_status vx_kv_read(const vx_paged_cache* kv, void* k_out, int64_t k_row_stride, int64_t k_head_stride, void* v_out,
+                     int64_t v_row_stride, int64_t v_head_stride, const int64_t* slots, int32_t num_rows,
+                     hipStream_t stream) {
+  return kv_rows(kv, k_out, k_row_stride, k_head_stride, v_out, v_row_stride, v_head_stride, slots, num_rows, false,
+                 stream, "vx_kv_read");
+}
+
+vx_status vx_page_workspace_size(int32_t batch, size_t* bytes) {
+  if (!bytes) return fail(VX_ERR_INVALID_ARG, "bytes is NULL");
+  if (batch < 0 || batch > 65535) return fail(VX_ERR_INVALID_ARG, "batch %d not in [0, 65535]", batch);
+  *bytes = vx::plan_workspace_bytes(batch);
+  return VX_OK;
+}
+
+vx_status vx_page_extend(const vx_page_pool* pool, int32_t batch, const int32_t* rows, const int32_t* new_lens,
+                         int32_t* seq_lens, int32_t* page_indptr, int32_t* page_indices, int32_t page_indices_cap,
+                         int32_t* token_indptr, int64_t* slots, int32_t slots_cap, int32_t* granted,
+                         int32_t* first_block, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  const vx_status s = check_plan(pool, batch, rows, workspace, workspace_bytes);
+  if (s != VX_OK) return s;
+  if (page_indices_cap < 0 || slots_cap < 0)
+    return fail(VX_ERR_INVALID_ARG, "page_indices_cap and slots_cap must be >= 0");
+  if (batch > 0 && (!new_lens || !seq_lens || !page_indptr || !token_indptr || !granted ||
+                    (page_indices_cap > 0 && !page_indices) || (slots_cap > 0 && !slots)))
+    return fail(VX_ERR_INVALID_ARG, "new_lens, seq_lens, page_indptr, page_indices, token_indptr, slots and granted "
+                                    "must be non-NULL");
+  return hip_status(vx::launch_page_extend(pool_of(pool), batch, rows, new_lens, seq_lens, page_indptr, page_indices,
+                                           page_indices_cap, token_indptr, slots, slots_cap, granted, first_block,
+                                           workspace, stream),
+                    "vx_page_extend");
+}
+
+vx_status vx_page_release(const vx_page_pool* pool, int32_t batch, const int32_t* rows, const int32_t* keep_lens,
+                          void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  const vx_status s = check_plan(pool, batch, rows, workspace, workspace_bytes);
+  if (s != VX_OK) return s;
+  return hip_status(vx::launch_page_release(pool_of(pool), batch, rows, keep_lens, workspace, stream),
+                    "vx_page_release");
 }
 
 vx_status vx_stream_read(const void* buf, size_t bytes, uint32_t* sink, int32_t workgroups, hipStream_t stream) {

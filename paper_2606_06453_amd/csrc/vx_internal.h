@@ -35,7 +35,7 @@ DecodeLayout decode_layout(int batch, int num_kv_heads, int group, int head_dim_
 size_t score_workspace_bytes(int batch, int num_kv_heads, int num_q_heads, int max_pages);
 
 // KV cache element types (the values of vx_kv_dtype).
-constexpr int kKvBf16 = 0, kKvFp8E4M3 = 1, kKvFp8E5M2 = 2;
+constexpr int kKvBf16 = 0, kKvFp8E4M3 = 1, kKvFp8E5M2 = 2, kKvMxFp4 = 3;
 
 struct Geometry {
   const void* k;          // bf16 or fp8 codes (kv_dtype)
@@ -96,6 +96,33 @@ hipError_t launch_score_flow(int kind, const float* in, float* out, int stride, 
 hipError_t launch_topk_select(const float* scores, int stride, int H, int batch, const int32_t* items,
                               const int32_t* budget, int n_sink, int n_local, int max_sel, int remap, int tau_q,
                               uint32_t seed, int32_t* sel_pages, int32_t* sel_count, hipStream_t stream);
+
+// Rows by slot: bf16 rows [n][H][D] at element strides.
+struct RowView {
+  const void* rows;
+  int64_t row_stride, head_stride;
+};
+hipError_t launch_kv_write(const Geometry& g, const RowView& k, const RowView& v, const int64_t* slots, int n,
+                           hipStream_t stream);
+hipError_t launch_kv_read(const Geometry& g, const RowView& k, const RowView& v, const int64_t* slots, int n,
+                          hipStream_t stream);
+
+// The state of a page pool (vx_page_pool, checked).
+struct PagePool {
+  int32_t* free_pages;
+  int32_t* free_count;
+  int32_t* table;
+  int32_t* lens;
+  int num_phys, table_rows, table_stride, ps;
+  int bs;                 // block size (tokens)
+};
+size_t plan_workspace_bytes(int batch);
+hipError_t launch_page_extend(const PagePool& pool, int batch, const int32_t* rows, const int32_t* new_lens,
+                              int32_t* seq_lens, int32_t* page_indptr, int32_t* page_indices, int page_cap,
+                              int32_t* token_indptr, int64_t* slots, int slot_cap, int32_t* granted,
+                              int32_t* first_block, void* ws, hipStream_t stream);
+hipError_t launch_page_release(const PagePool& pool, int batch, const int32_t* rows, const int32_t* keep_lens, void* ws,
+                               hipStream_t stream);
 
 // Plain stream of 16-byte non-temporal loads over `bytes` (a multiple of 16) from buf.
 hipError_t launch_stream_read(const void* buf, int64_t bytes, uint32_t* sink, int workgroups, hipStream_t stream);

@@ -28,8 +28,9 @@ class SparseDecoder:
         approx = topk_options is not None and (topk_options.tolerate_ratio > 0 or topk_options.remap != 0)
         self.num_q_heads, self.kind = num_q_heads, kind
         self.n_sink, self.n_local, self.max_sel, self.sm_scale = n_sink, n_local, max_sel, sm_scale
-        P, H, ps, Dqk = kv.k.shape
-        Dv = kv.v.shape[3] if kv.v is not None else kv.head_dim_v
+        P, H, ps, _ = kv.k.shape
+        Dqk = kv.head_dim_qk
+        Dv = Dqk if kv.v is not None else kv.head_dim_v
         dev = kv.k.device
         B = batch.seq_lens.numel()
         r = ps // kv.block_size if kv.block_size else 1      # summaries per page (one per block)

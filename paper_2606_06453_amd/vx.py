@@ -24,15 +24,23 @@ TWO_PASS_KINDS = (MEAN_DOT, MEAN_DOT_CONTENT)                    # may pass the 
 NEEDS_MAX = (MAX_DOT, QUEST, QUEST_CONSENSUS, ENVELOPE_LOWER, QUEST_RECTIFIED)
 NEEDS_MIN = (QUEST, QUEST_CONSENSUS, ENVELOPE_LOWER)
 STAGE_SCORE_TOPK, STAGE_DECODE = 0, 1
-KV_BF16, KV_FP8_E4M3, KV_FP8_E5M2 = 0, 1, 2
+KV_BF16, KV_FP8_E4M3, KV_FP8_E5M2, KV_MXFP4 = 0, 1, 2, 3
 
 
 def kv_dtype_code(t: torch.Tensor) -> int:
-    """vx_kv_dtype of a cache tensor: bfloat16, float8_e4m3fn (OCP E4M3) or float8_e5m2."""
-    codes = {torch.bfloat16: KV_BF16, torch.float8_e4m3fn: KV_FP8_E4M3, torch.float8_e5m2: KV_FP8_E5M2}
+    """vx_kv_dtype of a cache tensor: bfloat16, float8_e4m3fn (OCP E4M3), float8_e5m2, or uint8 for
+    the slices of an mxfp4 cache (mxfp4_cache)."""
+    codes = {torch.bfloat16: KV_BF16, torch.float8_e4m3fn: KV_FP8_E4M3, torch.float8_e5m2: KV_FP8_E5M2,
+             torch.uint8: KV_MXFP4}
     if t.dtype not in codes:
-        raise TypeError(f"KV cache dtype {t.dtype} is not bfloat16, float8_e4m3fn or float8_e5m2")
+        raise TypeError(f"KV cache dtype {t.dtype} is not bfloat16, float8_e4m3fn, float8_e5m2 or uint8 (mxfp4)")
     return codes[t.dtype]
+
+
+def mxfp4_cache(num_pages: int, num_kv_heads: int, page_size: int, head_dim: int, device="cuda") -> torch.Tensor:
+    """An mxfp4 K or V cache of zeros, uint8 [P][H][page_size][17 D / 32]: codes and scales of a
+    (page, head) slice as include/vx.h lays them out."""
+    return torch.zeros((num_pages, num_kv_heads, page_size, head_dim * 17 // 32), dtype=torch.uint8, device=device)
 TWO_PASS_MAX_PAGES = 16384    # block-mean two-pass selection: blocks per request bound
 # Below this many summary rows (batch x blocks per request x KV heads) the decoder scores the
 # block mean in one pass: the bound pass saves half the summary bytes, but its re-scoring of the
@@ -55,6 +63,12 @@ class _Cache(ctypes.Structure):
                 ("num_kv_heads", ctypes.c_int32), ("page_size", ctypes.c_int32),
                 ("head_dim_qk", ctypes.c_int32), ("head_dim_v", ctypes.c_int32), ("kv_dtype", ctypes.c_int32),
                 ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float), ("block_size", ctypes.c_int32)]
+
+
+class _Pool(ctypes.Structure):
+    _fields_ = [("free_pages", ctypes.c_void_p), ("free_count", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("lens", ctypes.c_void_p), ("num_phys_pages", ctypes.c_int32), ("table_rows", ctypes.c_int32),
+                ("table_stride", ctypes.c_int32), ("page_size", ctypes.c_int32), ("block_size", ctypes.c_int32)]
 
 
 class _Batch(ctypes.Structure):
@@ -88,6 +102,14 @@ def lib():
         L.vx_kv_append_summarize.argtypes = [P, P, P, P, P, P, P, P, P]
         L.vx_sparse_paged_decode_noalloc.argtypes = [P, i32, P, P, P, P, i32, ctypes.c_float, P, P]
         L.vx_append_score_topk.argtypes = [P, P, P, P, P, P, P, P, P, i32, i32, P, i32, i32, i32, P, P, P, sz, P, P]
+        i64 = ctypes.c_int64
+        L.vx_page_workspace_size.argtypes = [i32, ctypes.POINTER(sz)]
+        L.vx_page_extend.argtypes = [P, i32, P, P, P, P, P, i32, P, P, i32, P, P, P, sz, P]
+        L.vx_page_release.argtypes = [P, i32, P, P, P, sz, P]
+        L.vx_kv_write.argtypes = [P, P, i64, i64, P, i64, i64, P, i32, P]
+        L.vx_kv_read.argtypes = [P, P, i64, i64, P, i64, i64, P, i32, P]
+        for f in (L.vx_page_workspace_size, L.vx_page_extend, L.vx_page_release, L.vx_kv_write, L.vx_kv_read):
+            f.restype = ctypes.c_int
         for f in (L.vx_workspace_size, L.vx_page_summarize, L.vx_page_score_topk, L.vx_sparse_paged_decode,
                   L.vx_page_score, L.vx_topk_select, L.vx_score_flow, L.vx_kv_append_summarize,
                   L.vx_stream_read, L.vx_sparse_paged_decode_noalloc, L.vx_append_score_topk):
@@ -120,8 +142,9 @@ def _stream(stream) -> Optional[int]:
 
 @dataclass
 class PagedKV:
-    """Paged KV cache: k [P][H][ps][Dqk], v [P][H][ps][Dv] or None (V = K[..., :Dv]); bf16, or
-    fp8 (float8_e4m3fn / float8_e5m2) codes whose values are k_scale * code and v_scale * code."""
+    """Paged KV cache: k [P][H][ps][Dqk], v [P][H][ps][Dv] or None (V = K[..., :Dv]); bf16,
+    fp8 (float8_e4m3fn / float8_e5m2) codes whose values are k_scale * code and v_scale * code, or
+    mxfp4 slices (uint8, mxfp4_cache)."""
     k: torch.Tensor
     v: Optional[torch.Tensor]
     head_dim_v: Optional[int] = None
@@ -135,8 +158,25 @@ class PagedKV:
         dt = kv_dtype_code(self.k)
         if self.v is not None and kv_dtype_code(self.v) != dt:
             raise TypeError("K and V caches must have the same dtype")
+        if dt == KV_MXFP4:
+            Dqk, Dv = self._mx_dim(Dqk), self._mx_dim(Dv) if self.v is not None else Dv
         return _Cache(_ptr(self.k), _ptr(self.v), P, H, ps, Dqk, Dv, dt, float(self.k_scale), float(self.v_scale),
                       int(self.block_size))
+
+    @staticmethod
+    def _mx_dim(row_bytes: int) -> int:
+        if row_bytes % 17:
+            raise ValueError(f"an mxfp4 cache has 17 bytes per 32 channels of a token (got rows of {row_bytes} bytes)")
+        return row_bytes // 17 * 32
+
+    @property
+    def head_dim_qk(self) -> int:
+        return self._mx_dim(self.k.shape[3]) if kv_dtype_code(self.k) == KV_MXFP4 else self.k.shape[3]
+
+    @property
+    def row_dtype(self) -> torch.dtype:
+        """Element type of new rows at a decode step: the cache's own, bf16 for an mxfp4 cache."""
+        return torch.bfloat16 if kv_dtype_code(self.k) == KV_MXFP4 else self.k.dtype
 
     def ref(self):
         """A by-reference argument holding this geometry, built once (the tensors must not be
@@ -167,6 +207,128 @@ class BatchSpec:
         return self._ref
 
 
+@dataclass
+class PagePool:
+    """Pages, block table and lengths of growing requests (vx_page_pool): int32 device tensors
+    free_pages [num_phys_pages], free_count [1], table [rows][stride] and lens [rows]."""
+    free_pages: torch.Tensor
+    free_count: torch.Tensor
+    table: torch.Tensor
+    lens: torch.Tensor
+    page_size: int
+    block_size: int = 0
+
+    @classmethod
+    def empty(cls, num_phys_pages: int, table_rows: int, table_stride: int, page_size: int, block_size: int = 0,
+              device="cuda") -> "PagePool":
+        """A pool whose pages are all free (page 0 is the first to go) and whose rows are empty."""
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(torch.arange(num_phys_pages - 1, -1, -1, **i32), torch.full((1,), num_phys_pages, **i32),
+                   torch.zeros((table_rows, table_stride), **i32), torch.zeros(table_rows, **i32), page_size, block_size)
+
+    def struct(self) -> _Pool:
+        for n in ("free_pages", "free_count", "table", "lens"):
+            _int32(getattr(self, n), n)
+        rows, stride = self.table.shape
+        if self.lens.numel() != rows:
+            raise ValueError(f"lens has {self.lens.numel()} entries for {rows} table rows")
+        return _Pool(_ptr(self.free_pages), _ptr(self.free_count), _ptr(self.table), _ptr(self.lens),
+                     self.free_pages.numel(), rows, stride, int(self.page_size), int(self.block_size))
+
+    def ref(self):
+        """A by-reference argument holding this pool, built once (see PagedKV.ref)."""
+        if getattr(self, "_ref", None) is None:
+            self._st = self.struct()
+            self._ref = ctypes.byref(self._st)
+        return self._ref
+
+
+def _on_gpu(*tensors) -> None:
+    """The kernels take device addresses of the current GPU: anything else would fault it."""
+    for t in tensors:
+        if t is not None and (t.device.type != "cuda" or t.device.index != torch.cuda.current_device()):
+            raise ValueError(f"tensors must be on the current GPU (got one on {t.device})")
+
+
+def _int32(t: torch.Tensor, name: str) -> torch.Tensor:
+    if t.dtype != torch.int32:
+        raise TypeError(f"{name} must be int32 (got {t.dtype})")
+    return t
+
+
+def page_workspace_size(batch: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().vx_page_workspace_size(int(batch), ctypes.byref(out)))
+    return int(out.value)
+
+
+def page_extend(pool: PagePool, rows: torch.Tensor, new_lens: torch.Tensor, batch: BatchSpec,
+                token_indptr: torch.Tensor, slots: torch.Tensor, granted: torch.Tensor, workspace: torch.Tensor,
+                first_block: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Gives request i (row rows[i] of the pool) its new_lens[i] tokens: batch's page_indptr,
+    page_indices and seq_lens are written for the lengths with them, and token_indptr, slots
+    (int64), granted and first_block as include/vx.h says."""
+    B = rows.numel()
+    for t, n, name in ((rows, B, "rows"), (new_lens, B, "new_lens"), (batch.seq_lens, B, "seq_lens"),
+                       (batch.page_indptr, B + 1, "page_indptr"), (token_indptr, B + 1, "token_indptr"),
+                       (granted, B, "granted"), (first_block, B, "first_block")):
+        if t is not None and _int32(t, name).numel() != n:
+            raise ValueError(f"{name} has {t.numel()} entries, {n} are needed")
+    _int32(batch.page_indices, "page_indices")
+    if slots.dtype != torch.int64:
+        raise TypeError(f"slots must be int64 (got {slots.dtype})")
+    _on_gpu(pool.table, pool.free_pages, pool.free_count, pool.lens, rows, new_lens, batch.seq_lens, batch.page_indptr,
+            batch.page_indices, token_indptr, slots, granted, first_block, workspace)
+    _check(lib().vx_page_extend(pool.ref(), B, _ptr(rows), _ptr(new_lens), _ptr(batch.seq_lens), _ptr(batch.page_indptr),
+                                _ptr(batch.page_indices), batch.page_indices.numel(), _ptr(token_indptr), _ptr(slots),
+                                slots.numel(), _ptr(granted), _ptr(first_block), _ptr(workspace),
+                                workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def page_release(pool: PagePool, rows: torch.Tensor, keep_lens: Optional[torch.Tensor], workspace: torch.Tensor,
+                 stream=None) -> None:
+    """Row rows[i] keeps its first keep_lens[i] tokens (None: none) and gives its other pages back."""
+    B = _int32(rows, "rows").numel()
+    if keep_lens is not None and _int32(keep_lens, "keep_lens").numel() != B:
+        raise ValueError(f"keep_lens has {keep_lens.numel()} entries, {B} are needed")
+    _on_gpu(pool.table, pool.free_pages, pool.free_count, pool.lens, rows, keep_lens, workspace)
+    _check(lib().vx_page_release(pool.ref(), B, _ptr(rows), _ptr(keep_lens), _ptr(workspace),
+                                 workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def _row_args(kv: PagedKV, t: Optional[torch.Tensor], n: int, dim: int, name: str):
+    """Address and strides of rows [n][H][dim], bf16, channels side by side."""
+    if t is None:
+        return None, 0, 0
+    if t.dtype != torch.bfloat16:
+        raise TypeError(f"{name} must be bfloat16 (got {t.dtype})")
+    if tuple(t.shape) != (n, kv.k.shape[1], dim) or (t.numel() > 0 and t.stride(2) != 1):
+        raise ValueError(f"{name} must be [{n}][{kv.k.shape[1]}][{dim}] with contiguous channels (got {tuple(t.shape)}, "
+                         f"strides {tuple(t.stride())})")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def _kv_rows(fn, kv: PagedKV, slots: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor], names, stream) -> None:
+    if slots.dtype != torch.int64:
+        raise TypeError(f"slots must be int64 (got {slots.dtype})")
+    n, c = slots.numel(), kv.ref()
+    rows = (*_row_args(kv, k, n, kv._st.head_dim_qk, names[0]), *_row_args(kv, v, n, kv._st.head_dim_v, names[1]))
+    _on_gpu(kv.k, kv.v, slots, k, v)
+    _check(fn(c, *rows, _ptr(slots), n, _stream(stream)))
+
+
+def kv_write(kv: PagedKV, k_new: torch.Tensor, v_new: Optional[torch.Tensor], slots: torch.Tensor, stream=None) -> None:
+    """Rows k_new [n][H][Dqk] and v_new [n][H][Dv] (bf16, strided) into the cache, rounded to its
+    type, at slots [n] (int64; negative: skipped)."""
+    _kv_rows(lib().vx_kv_write, kv, slots, k_new, v_new, ("k_new", "v_new"), stream)
+
+
+def kv_read(kv: PagedKV, slots: torch.Tensor, k_out: torch.Tensor, v_out: Optional[torch.Tensor], stream=None) -> None:
+    """The cache's values at slots [n] as bf16 rows k_out [n][H][Dqk] and v_out [n][H][Dv] (zeros for a
+    negative slot)."""
+    _kv_rows(lib().vx_kv_read, kv, slots, k_out, v_out, ("k_out", "v_out"), stream)
+
+
 def workspace_size(stage: int, kv: PagedKV, batch: BatchSpec, num_q_heads: int, max_sel: int) -> int:
     out = ctypes.c_size_t(0)
     c, b = kv.struct(), batch.struct()
@@ -191,8 +353,8 @@ def kv_append_summarize(kv: PagedKV, batch: BatchSpec, k_new: torch.Tensor, v_ne
     """Writes k_new [B][H][Dqk] / v_new [B][H][Dv] (the cache's dtype) at token seq_lens[i]-1 and
     refreshes that page's summaries, in one launch."""
     for t in (k_new, v_new):
-        if t is not None and t.dtype != kv.k.dtype:
-            raise TypeError(f"new rows must have the cache's dtype {kv.k.dtype} (got {t.dtype})")
+        if t is not None and t.dtype != kv.row_dtype:
+            raise TypeError(f"new rows must have the cache's dtype {kv.row_dtype} (got {t.dtype})")
     c, b = kv.struct(), batch.struct()
     _check(lib().vx_kv_append_summarize(ctypes.byref(c), ctypes.byref(b), _ptr(k_new), _ptr(v_new), _ptr(mean),
                                         _ptr(mean_bf16), _ptr(max), _ptr(min), _stream(stream)))
@@ -232,8 +394,8 @@ def append_score_topk(kv: PagedKV, batch: BatchSpec, k_new: torch.Tensor, v_new:
                       options: Optional[_TopkOptions] = None) -> None:
     """kv_append_summarize followed by page_score_topk, the append inside the top-K launch."""
     for t in (k_new, v_new):
-        if t is not None and t.dtype != kv.k.dtype:
-            raise TypeError(f"new rows must have the cache's dtype {kv.k.dtype} (got {t.dtype})")
+        if t is not None and t.dtype != kv.row_dtype:
+            raise TypeError(f"new rows must have the cache's dtype {kv.row_dtype} (got {t.dtype})")
     c, b = kv.struct(), batch.struct()
     _check(lib().vx_append_score_topk(ctypes.byref(c), ctypes.byref(b), _ptr(k_new), _ptr(v_new), _ptr(mean),
                                       _ptr(mean_bf16), _ptr(max), _ptr(min), _ptr(q), q.shape[1], kind,

@@ -3,7 +3,7 @@ import os
 import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-PROBES = {"dot2_probe.hip": "libdot2probe.so"}
+PROBES = {"dot2_probe.hip": "libdot2probe.so", "mx_probe.hip": "libmxprobe.so"}
 
 
 def build() -> None:

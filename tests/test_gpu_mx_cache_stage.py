@@ -1,0 +1,208 @@
+"""The cache stage on an mxfp4 cache: summaries against fp64, the decode step's append against a write by
+slot followed by a pass over the block (bit-identical), and the whole flow of a growing batch."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2606_06453_amd import vx
+from paper_2606_06453_amd.decoder import SparseDecoder
+from tests import _mx
+
+pytestmark = pytest.mark.gpu
+
+
+def _gpu(x):
+    return torch.from_numpy(np.ascontiguousarray(x, np.int32)).cuda()
+
+
+def _cache(P, H, ps, D, seed):
+    rng = np.random.default_rng(seed)
+    x = torch.from_numpy(rng.normal(size=(2, P, H, ps, D))).to(torch.bfloat16).double().numpy()
+    return _mx.pack(x[0], "k"), _mx.pack(x[1], "v")
+
+
+@pytest.mark.parametrize("H,D,ps,block", [(16, 128, 16, 0), (8, 128, 32, 16), (2, 64, 16, 0), (1, 64, 64, 32), (4, 128, 64, 0)])
+@pytest.mark.parametrize("bound", [7, 140000])        # blocks per request that the grid is laid out for
+@pytest.mark.parametrize("first", [False, True])
+def test_summaries(H, D, ps, block, bound, first):
+    bs = block or ps
+    r = ps // bs
+    lens = [ps * 3 + 1, 0, ps * 2, ps * 6 + ps - 1, 5]
+    pages = [-(-n // ps) for n in lens]
+    total = sum(pages)
+    kc, vc = _cache(total, H, ps, D, [D, ps])
+    perm = np.random.default_rng(1).permutation(total)
+    indptr = np.concatenate([[0], np.cumsum(pages)])
+    kv = vx.PagedKV(torch.from_numpy(kc).cuda(), torch.from_numpy(vc).cuda(), block_size=block)
+    batch = vx.BatchSpec(_gpu(indptr), _gpu(perm), _gpu(lens), max(bound, max(pages)))
+    x = _mx.unpack(kc, "k")
+    begin = [2, 0, 1, 7, 0] if first else [0] * 5
+    want = {n: np.full((total * r, H, D), -7.0) for n in ("mean", "max", "min")}
+    for i, n in enumerate(lens):
+        for j in range(begin[i], -(-n // bs)):
+            p, b = perm[indptr[i] + j // r], j % r
+            rows = x[p, :, b * bs: b * bs + min(bs, n - j * bs)]
+            want["mean"][p * r + b], want["max"][p * r + b], want["min"][p * r + b] = rows.mean(1), rows.max(1), rows.min(1)
+    new = lambda dt: torch.full((total * r, H, D), -7.0, dtype=dt, device="cuda")  # noqa: E731
+    for names in (("mean",), ("max", "min"), ("mean", "max", "min", "mean_bf16")):
+        out = {n: new(torch.float32 if n == "mean" else torch.bfloat16) for n in names}
+        vx.page_summarize(kv, batch, _gpu(begin) if first else None, **out)
+        torch.cuda.synchronize()
+        for n in names:
+            got = out[n].cpu()
+            if n == "mean":      # bs fp32 additions and a division, each within 2^-24 of at most bs max|x| / bs
+                assert np.abs(got.double().numpy() - want["mean"]).max() <= (bs + 1) * 2.0 ** -24 * np.abs(x).max()
+            elif n == "mean_bf16":
+                assert torch.equal(got, out["mean"].cpu().to(torch.bfloat16))
+            else:                # the cache's values are bf16 values
+                assert np.array_equal(got.double().numpy(), want[n])
+
+
+def test_a_nan_group_marks_its_summaries():
+    kc, vc = _cache(2, 1, 16, 64, 3)
+    _, _, sc = _mx.places(16, 64, "k")
+    kc.reshape(2, -1)[1, sc[4, 32]] = 255
+    kv = vx.PagedKV(torch.from_numpy(kc).cuda(), torch.from_numpy(vc).cuda())
+    mean = torch.zeros((2, 1, 64), device="cuda")
+    vx.page_summarize(kv, vx.BatchSpec(_gpu([0, 2]), _gpu([0, 1]), _gpu([32]), 2), mean=mean)
+    torch.cuda.synchronize()
+    assert torch.isnan(mean[1, 0, 32:]).all() and torch.isfinite(mean[1, 0, :32]).all() and torch.isfinite(mean[0]).all()
+
+
+@pytest.mark.parametrize("H,D,ps,block", [(8, 128, 16, 0), (4, 64, 64, 0), (1, 64, 32, 16), (16, 128, 64, 32)])
+@pytest.mark.parametrize("fused", [None, "wave", "bucket", "two_pass", "late"])
+def test_append_equals_a_write_and_a_pass(H, D, ps, block, fused):
+    """vx_kv_append_summarize, and vx_append_score_topk by every selection that carries the append."""
+    bs = block or ps
+    r = ps // bs
+    L = {None: 40, "wave": 40, "bucket": 600 * bs // 16, "two_pass": 40, "late": 40}[fused]
+    lens = np.array([L * 3 + 1, 1, ps, ps + 1, L * 16, 5 * ps - 3])
+    pages = -(-lens // ps)
+    total, bound = int(pages.sum()), int(pages.max())
+    kc, vc = _cache(total, H, ps, D, [D, ps, H])
+    rng = np.random.default_rng(2)
+    indptr, perm = np.concatenate([[0], np.cumsum(pages)]), rng.permutation(total)
+    batch = vx.BatchSpec(_gpu(indptr), _gpu(perm), _gpu(lens), bound)
+    rows = torch.from_numpy(rng.normal(size=(2, len(lens), H, D))).to(torch.bfloat16)
+    rows[0, 0, 0, :32] = 0
+    rows[1, 2, H - 1, 40] = float("inf")
+    rows[0, 3, 0, 7] = 3e38
+    rows = rows.cuda()
+
+    def state():
+        kv = vx.PagedKV(torch.from_numpy(kc).cuda(), torch.from_numpy(vc).cuda(), block_size=block)
+        s = {"mean": torch.full((total * r, H, D), 3.0, device="cuda")}
+        for n in ("mean_bf16", "max", "min"):
+            s[n] = torch.full((total * r, H, D), 3.0, dtype=torch.bfloat16, device="cuda")
+        vx.page_summarize(kv, batch, **s)
+        return kv, s
+
+    want_kv, want = state()
+    last = perm[indptr[:-1] + pages - 1].astype(np.int64) * ps + (lens - 1) % ps
+    vx.kv_write(want_kv, rows[0], rows[1], torch.from_numpy(last).cuda())
+    vx.page_summarize(want_kv, batch, _gpu((lens - 1) // bs), **want)
+    got_kv, got = state()
+    if fused is None:
+        vx.kv_append_summarize(got_kv, batch, rows[0], rows[1], **got)
+    else:
+        kind = {"wave": vx.MEAN_DOT, "bucket": vx.MEAN_DOT, "two_pass": vx.QUEST, "late": vx.NSA}[fused]
+        q = torch.from_numpy(rng.normal(size=(len(lens), 2 * H, D))).to(torch.bfloat16).cuda()
+        sel, cnt = torch.zeros((len(lens), H, 6), dtype=torch.int32, device="cuda"), torch.zeros(len(lens), dtype=torch.int32, device="cuda")
+        ws = torch.zeros(vx.workspace_size(vx.STAGE_SCORE_TOPK, got_kv, batch, 2 * H, 6), dtype=torch.uint8, device="cuda")
+        bud = _gpu([6] * len(lens))
+        args = (q, kind, bud, 1, 2, 6)
+        two = fused == "two_pass"
+        vx.append_score_topk(got_kv, batch, rows[0], rows[1], got["mean"], got["max"], got["min"], *args, sel, cnt, ws,
+                             mean_bf16=got["mean_bf16"])
+        sel2, cnt2 = torch.zeros_like(sel), torch.zeros_like(cnt)
+        vx.page_score_topk(q, want_kv, batch, kind, want["mean"], want["max"], want["min"], *args[2:], sel2, cnt2, ws,
+                           mean_bf16=want["mean_bf16"] if not two else None)
+        torch.cuda.synchronize()
+        assert torch.equal(cnt, cnt2) and torch.equal(sel, sel2)
+    torch.cuda.synchronize()
+    assert torch.equal(got_kv.k, want_kv.k) and torch.equal(got_kv.v, want_kv.v)
+    for n in got:
+        view = torch.int32 if n == "mean" else torch.int16
+        assert torch.equal(got[n].view(view), want[n].view(view)), n
+
+
+@pytest.mark.parametrize("block,kind", [(0, vx.MEAN_DOT), (16, vx.QUEST)])
+def test_a_batch_that_grows_and_ends(block, kind):
+    """Prompts in chunks, decode steps through SparseDecoder, requests that end and others that take their
+    pages: pages, slots, cache, summaries, selection and attention together, against fp64."""
+    H, g, D, ps, bs = 2, 4, 128, 32, block or 32
+    B, stride, P = 4, 12, 40
+    rng = np.random.default_rng(11)
+    pool = vx.PagePool.empty(P, B, stride, ps, block)
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32, device="cuda")  # noqa: E731
+    batch = vx.BatchSpec(i32(B + 1), i32(P), i32(B), stride)
+    k, v = vx.mxfp4_cache(P, H, ps, D), vx.mxfp4_cache(P, H, ps, D)
+    kv = vx.PagedKV(k, v, block_size=block)
+    dec = SparseDecoder(kv, batch, H * g, kind, 1, 2, 6, D ** -0.5)
+    rows_of, tokens, granted, first = _gpu(rng.permutation(B)), i32(B + 1), i32(B), i32(B)
+    slots, ws = torch.zeros(400, dtype=torch.int64, device="cuda"), i32(vx.page_workspace_size(B) // 4)
+    kept = [np.zeros((2, 0, H, D)) for _ in range(B)]             # the rows of each request as the cache holds them
+    budget = _gpu([6] * B)
+
+    def extend(new, k_new=None):
+        vx.page_extend(pool, rows_of, _gpu(new), batch, tokens, slots, granted, ws, first)
+
+    def rows(n):
+        return torch.from_numpy(rng.normal(size=(2, n, H, D))).to(torch.bfloat16)
+
+    def note(new, r):
+        at = 0
+        for i, n in enumerate(new):
+            x = r[:, at:at + n].double().numpy()
+            kept[i] = np.concatenate([kept[i], _mx.values(*_mx.quantize(x))], 1)
+            at += n
+
+    for new in ([70, 33, 1, 0], [100, 0, 64, 90]):                 # two chunks of prompts
+        extend(new)
+        n = sum(new)
+        r = rows(n)
+        vx.kv_write(kv, r[0].cuda(), r[1].cuda(), slots[:n].clone())
+        vx.page_summarize(kv, batch, first, dec.mean, dec.max, dec.min, mean_bf16=dec.mean_bf16)
+        assert granted.tolist() == new
+        note(new, r)
+    for step in range(40):
+        if step == 20:                                             # requests 1 and 2 end, another takes their place
+            vx.page_release(pool, rows_of, _gpu([kept[0].shape[1], 0, 0, kept[3].shape[1]]), ws)
+            kept[1], kept[2] = kept[1][:, :0], kept[2][:, :0]
+            new = [0, 150, 17, 0]
+            extend(new)
+            r = rows(167)
+            vx.kv_write(kv, r[0].cuda(), r[1].cuda(), slots[:167].clone())
+            vx.page_summarize(kv, batch, first, dec.mean, dec.max, dec.min, mean_bf16=dec.mean_bf16)
+            note(new, r)
+        extend([1] * B)
+        r = rows(B)
+        q = torch.from_numpy(rng.normal(size=(B, H * g, D))).to(torch.bfloat16)
+        out = dec.step(q.cuda(), budget, None, kv_new=(r[0].cuda(), r[1].cuda()))
+        note([1] * B, r)
+        torch.cuda.synchronize()
+        assert granted.tolist() == [1] * B and batch.seq_lens.tolist() == [x.shape[1] for x in kept]
+        if step % 7:
+            continue
+        got, sel, cnt = out.double().cpu().numpy(), dec.sel_pages.cpu().numpy(), dec.sel_count.cpu().numpy()
+        for i in range(B):
+            L = kept[i].shape[1]
+            blocks = -(-L // bs)
+            assert cnt[i] == min(6, blocks)
+            for h in range(H):
+                js = sel[i, h, : cnt[i]]
+                assert set(js) >= {0, max(0, blocks - 2), blocks - 1} and (np.diff(js) > 0).all()
+                heads = slice(h * g, (h + 1) * g)
+                qq = q[i, heads].double().numpy()
+                if blocks > 6 and kind == vx.MEAN_DOT:             # the selected blocks are the best ones
+                    score = np.array([(qq.mean(0) * kept[i][0, b * bs:(b + 1) * bs, h].mean(0)).sum() for b in range(blocks)])
+                    free = [b for b in range(1, blocks - 2)]
+                    worst = min(score[b] for b in js if b in free)
+                    assert all(score[b] <= worst + 1e-5 for b in free if b not in js)
+                pos = np.concatenate([np.arange(j * bs, min((j + 1) * bs, L)) for j in js])
+                ref, absv, qk = _mx.attend(qq, kept[i][0, pos, h], kept[i][1, pos, h], D ** -0.5)
+                tol = _mx.attend_tolerance(ref, absv, qk, D ** -0.5, D, len(pos))
+                assert (np.abs(got[i, heads] - ref) <= tol).all()
+    vx.page_release(pool, rows_of, None, ws)
+    torch.cuda.synchronize()
+    assert int(pool.free_count) == P and sorted(pool.free_pages.tolist()) == list(range(P))

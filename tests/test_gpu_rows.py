@@ -1,0 +1,161 @@
+"""Rows into and out of the cache by slot (vx_kv_write, vx_kv_read) against 64-bit references: every
+cache type, head layouts, strided rows, padded and foreign slots, values where rounding can go wrong."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2606_06453_amd import vx
+from tests import _mx
+
+pytestmark = pytest.mark.gpu
+FP8 = {"fp8_e4m3": (torch.float8_e4m3fn, 448.0), "fp8_e5m2": (torch.float8_e5m2, 57344.0)}
+TORCH = {"bf16": torch.bfloat16, "fp8_e4m3": torch.float8_e4m3fn, "fp8_e5m2": torch.float8_e5m2}
+
+
+def _cache(kv, P, H, ps, D, fill=0):
+    if kv == "mxfp4":
+        return torch.full((P, H, ps, D * 17 // 32), fill, dtype=torch.uint8, device="cuda")
+    t = torch.full((P * H * ps * D * (2 if kv == "bf16" else 1),), fill, dtype=torch.uint8, device="cuda")
+    return t.view(TORCH[kv]).view(P, H, ps, D)
+
+
+def _expected(kv, x, scale):
+    """fp64 value that a bf16 row is read back as."""
+    if kv == "bf16":
+        return x
+    if kv == "mxfp4":
+        return _mx.values(*_mx.quantize(x))
+    dtype, top = FP8[kv]
+    codes = torch.arange(256, dtype=torch.uint8).view(dtype).double().numpy()[:128]
+    grid = codes[np.isfinite(codes)]
+    q = np.minimum(np.abs((x.astype(np.float32) / np.float32(scale)).astype(np.float64)), top)
+    hi = np.clip(np.searchsorted(grid, np.nan_to_num(q)), 1, len(grid) - 1)
+    lo = hi - 1
+    pick = np.where(q - grid[lo] < grid[hi] - q, lo, np.where(q - grid[lo] > grid[hi] - q, hi, np.where(hi % 2 == 0, hi, lo)))
+    v = (np.copysign(grid[pick], x)).astype(np.float32) * np.float32(scale)
+    v = torch.from_numpy(v).to(torch.bfloat16).double().numpy()
+    return np.where(np.isnan(x), np.nan, v)
+
+
+def _special(x, rng):
+    """Zero groups, tiny and huge groups, groups with an infinity or NaN, ties."""
+    n, H, D = x.shape
+    x[rng.integers(n), :, :32] = 0.0
+    x[rng.integers(n), 0, 32:64] *= 2.0 ** -130
+    x[rng.integers(n), 0, :32] *= 2.0 ** 120
+    x[rng.integers(n), H - 1, 3] = np.inf
+    x[rng.integers(n), H - 1, D - 1] = -np.inf
+    x[rng.integers(n), 0, D - 40] = np.nan
+    x[rng.integers(n), 0, :64] = np.tile([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, -5.0], 8)
+    return x
+
+
+@pytest.mark.parametrize("kv", ["mxfp4", "bf16", "fp8_e4m3", "fp8_e5m2"])
+@pytest.mark.parametrize("H,D,ps", [(8, 128, 16), (1, 64, 16), (2, 64, 64), (16, 128, 32), (1, 576, 64)])
+@pytest.mark.parametrize("n", [1, 3, 37, 260])
+def test_write_then_read(kv, H, D, ps, n):
+    if kv == "mxfp4" and D == 576:
+        pytest.skip("mxfp4 caches have the GQA geometry")
+    rng = np.random.default_rng([n, H, D, ps])
+    P = n // ps + 3
+    scale_k, scale_v = (0.0137, 0.25) if kv in FP8 else (1.0, 1.0)
+    k, v = _cache(kv, P, H, ps, D, 0x11), None if D == 576 else _cache(kv, P, H, ps, D, 0x22)
+    cache = vx.PagedKV(k, v, 512 if D == 576 else D, scale_k, scale_v)
+    before = {"k": k.clone(), "v": None if v is None else v.clone()}
+    # the projection's output, heads of a token side by side, with room between the parts
+    qkv = torch.from_numpy(_special(rng.normal(size=(n, 3 * H + 1, D)), rng)).to(torch.bfloat16)
+    kr, vr = qkv[:, 1:H + 1], qkv[:, 2 * H + 1:]
+    gpu = qkv.cuda()
+    perm = rng.permutation(P * ps)
+    slots = perm[:n].copy()
+    if n > 2:
+        slots[n // 2], slots[n // 3] = -1, P * ps + 5              # padded; past the cache
+    vx.kv_write(cache, gpu[:, 1:H + 1], None if v is None else gpu[:, 2 * H + 1:], torch.from_numpy(slots).cuda())
+    inside = (slots >= 0) & (slots < P * ps)
+    ask = np.concatenate([slots, slots[inside][:2], [-7, P * ps]])
+    out = [torch.full((len(ask), H, D), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    vx.kv_read(cache, torch.from_numpy(ask).cuda(), out[0], None if v is None else out[1])
+    torch.cuda.synchronize()
+    src = np.concatenate([np.arange(n), np.flatnonzero(inside)[:2], [0, 0]])
+    good = (ask >= 0) & (ask < P * ps)
+    for got, rows, scale in ((out[0], kr, scale_k), (out[1], vr, scale_v))[: 1 if v is None else 2]:
+        want = _expected(kv, rows.double().numpy()[src], scale)
+        if kv in FP8:                                              # infinities saturate
+            assert np.isfinite(want[~np.isnan(want)]).all()
+        got = got.double().cpu().numpy()
+        assert np.array_equal(got[good], want[good], equal_nan=True)
+        assert (got[~good] == 0).all()
+    # nothing else changed
+    rest = torch.from_numpy(np.setdiff1d(np.arange(P * ps), slots[inside])).cuda()
+    for name, t in (("k", k), ("v", v)):
+        if t is None:
+            continue
+        if kv == "mxfp4":
+            # K and V slices have their own orders: compare the bytes that no written row owns
+            for h in range(H):
+                at, _, sc = _mx.places(ps, D, name)
+                mine = np.zeros((P, ps * D * 17 // 32), bool)
+                for s in slots[inside]:
+                    mine[s // ps, at[s % ps]] = True
+                    mine[s // ps, sc[s % ps]] = True
+                now = t[:, h].reshape(P, -1).cpu().numpy()
+                assert (now[~mine] == (0x11 if name == "k" else 0x22)).all()
+        else:
+            rows_of = lambda c: c.view(torch.uint8).view(P, H, ps, -1).transpose(1, 2).reshape(P * ps, H, -1)[rest]  # noqa: E731
+            assert torch.equal(rows_of(t), rows_of(before[name]))
+
+
+
+@pytest.mark.parametrize("D,ps", [(128, 16), (64, 32)])
+def test_the_slices_hold_the_documented_bytes(D, ps):
+    rng = np.random.default_rng(D)
+    P, H = 5, 2
+    x = {w: _special(rng.normal(size=(P * ps, H, D)), rng) for w in "kv"}
+    x = {w: torch.from_numpy(a).to(torch.bfloat16) for w, a in x.items()}
+    cache = {w: vx.mxfp4_cache(P, H, ps, D) for w in "kv"}
+    vx.kv_write(vx.PagedKV(cache["k"], cache["v"]), x["k"].cuda(), x["v"].cuda(), torch.arange(P * ps, device="cuda"))
+    torch.cuda.synchronize()
+    for w in "kv":
+        rows = x[w].double().numpy().reshape(P, ps, H, D).transpose(0, 2, 1, 3)
+        assert np.array_equal(cache[w].cpu().numpy(), _mx.pack(rows, w))
+
+
+def test_strides_of_any_order():
+    """Head-major rows, reversed rows (through a negative stride at the C entry), one head of many."""
+    H, D, ps, n = 4, 128, 16, 21
+    gen = torch.Generator().manual_seed(3)
+    x = torch.randn((H, n, D), generator=gen).to(torch.bfloat16).cuda()
+    k, v = vx.mxfp4_cache(4, H, ps, D), vx.mxfp4_cache(4, H, ps, D)
+    kv, slots = vx.PagedKV(k, v), torch.randperm(4 * ps, generator=gen)[:n].cuda()
+    vx.kv_write(kv, x.transpose(0, 1), x.transpose(0, 1), slots)
+    out = torch.zeros((2, H, n, D), dtype=torch.bfloat16, device="cuda")
+    vx.kv_read(kv, slots, out[0].transpose(0, 1), out[1].transpose(0, 1))
+    plain = torch.zeros((2, n, H, D), dtype=torch.bfloat16, device="cuda")
+    vx.kv_read(kv, slots, plain[0], plain[1])
+    back = torch.zeros_like(plain)
+    s = torch.cuda.current_stream().cuda_stream
+    rc = vx.lib().vx_kv_read(kv.ref(), back[0, n - 1].data_ptr(), -H * D, D, back[1, n - 1].data_ptr(), -H * D, D,
+                             slots.data_ptr(), n, s)
+    torch.cuda.synchronize()
+    want = torch.from_numpy(_mx.values(*_mx.quantize(x.double().cpu().numpy()))).to(torch.bfloat16)
+    assert rc == 0
+    for i in range(2):
+        assert torch.equal(out[i].cpu(), want) and torch.equal(plain[i].transpose(0, 1).cpu(), want)
+        assert torch.equal(back[i].flip(0).transpose(0, 1).cpu(), want)
+
+
+def test_slots_past_two_gigabytes():
+    """Slices whose byte offsets pass 31 and 32 bits."""
+    H, D, ps = 8, 128, 64
+    P = (1 << 32) // (H * ps * D * 17 // 32) + 100
+    k, v = vx.mxfp4_cache(P, H, ps, D), vx.mxfp4_cache(P, H, ps, D)
+    kv = vx.PagedKV(k, v)
+    slots = torch.tensor([P * ps - 1, P * ps - 64, P // 2 * ps + 3, P // 2 * ps + 100, 5], device="cuda")
+    x = torch.randn((5, H, D), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
+    vx.kv_write(kv, x.cuda(), -x.cuda(), slots)
+    out = torch.zeros((2, 5, H, D), dtype=torch.bfloat16, device="cuda")
+    vx.kv_read(kv, slots, out[0], out[1])
+    torch.cuda.synchronize()
+    want = torch.from_numpy(_mx.values(*_mx.quantize(x.double().numpy()))).to(torch.bfloat16)
+    assert torch.equal(out[0].cpu(), want) and torch.equal(out[1].cpu(), -want)
+    assert int(k.view(-1).view(torch.int64).ne(0).sum()) <= 5 * H * (D // 16 + 4)      # and nothing wrapped to other pages
