@@ -1,0 +1,393 @@
+// Sparse paged attention over an mxfp4 cache (GQA geometry): the split kernel of decode.hip's work
+// plan for slices of E2M1 codes and E8M0 scales.
+//
+// A (page of 16, KV head) is 1088 bytes of K and of V at D = 128, a quarter of bf16, so the time per
+// byte is a quarter and the vector instructions per token decide.  A wave takes two 16-token tiles
+// per round, 32 tokens:
+//   S^T = K Q^T   MFMA 16x16x32 per tile: a lane's K codes are D/4 consecutive channels of one token
+//                 (one load), widened with their scale by the E2M1 conversion (a code times a power
+//                 of two is a bf16 value, so nothing is rounded)
+//   softmax       log2 domain.  The running maximum of a head moves only when a score passes it by
+//                 more than 2^8: below that the probabilities stay under 256, which fp32 sums and the
+//                 two bf16 parts carry as exactly as values below 1, and a round needs no exchange
+//                 between lanes
+//   O^T += V^T P^T  MFMA 16x16x32 over the 32 tokens: a lane's V codes are one piece (D/16 channels) of
+//                 four tokens side by side, widened and paired by tokens (v_perm).  P's layout is that
+//                 of S^T, 4 tokens of each tile per lane, and V^T's rows follow it.
+// P is the sum of two bf16 parts, hi = p cut to 8 bits and lo = (p - hi) cut to 8, 2^-15 of p.  With at
+// most 8 query heads per KV head the 16 columns hold every head twice, the hi parts in columns 0 to 7
+// and the lo parts in 8 to 15, so one MFMA per operand does both; else two.
+#include "decode_common.h"
+#include "mxfp4.h"
+
+namespace vx {
+using namespace dec;
+namespace {
+
+constexpr float kRescaleLog2 = 8.f;
+constexpr float kNoMax = -1e30f;          // running maximum before the first token
+
+template <int D>
+struct MxTile {
+  uint32_t k[D / 32], v[D / 32];          // codes: token col, channels D/4 * grp ..; tokens 4 grp .., piece col
+  uint32_t ke, ve;                        // scale bytes: k's; v's four tokens
+};
+
+// Lane constants of a tile's loads, bytes from the tile's codes and scales.
+struct MxLane {
+  uint32_t kc, vc, ks, vs;
+};
+
+template <int D>
+__device__ __forceinline__ MxLane mx_lane(int col, int grp) {
+  return MxLane{(uint32_t)(col * (D / 2) + grp * (D / 8)), (uint32_t)(grp * (2 * D) + col * (D / 8)),
+                (uint32_t)(col * (D / 32) + grp * D / 128), (uint32_t)(grp * (D / 8) + col / (512 / D) * 4)};
+}
+
+template <int D>
+__device__ __forceinline__ void mx_load(const uint8_t* __restrict__ k, const uint8_t* __restrict__ v, int64_t slice,
+                                        int t0, int ps, const MxLane& l, MxTile<D>& t) {
+  const uint8_t* kc = k + slice + t0 * (D / 2);            // uniform bases, lane offsets
+  const uint8_t* vc = v + slice + t0 * (D / 2);
+  const uint8_t* ks = k + slice + ps * (D / 2) + t0 * (D / 32);
+  const uint8_t* vs = v + slice + ps * (D / 2) + t0 * (D / 32);
+  if constexpr (D == 128) {
+    const uint4 a = load_stream_u4(kc + l.kc), b = load_stream_u4(vc + l.vc);
+    t.k[0] = a.x; t.k[1] = a.y; t.k[2] = a.z; t.k[3] = a.w;
+    t.v[0] = b.x; t.v[1] = b.y; t.v[2] = b.z; t.v[3] = b.w;
+  } else {
+    const uint2 a = load_stream_u2(kc + l.kc), b = load_stream_u2(vc + l.vc);
+    t.k[0] = a.x; t.k[1] = a.y;
+    t.v[0] = b.x; t.v[1] = b.y;
+  }
+  t.ke = __builtin_nontemporal_load(ks + l.ks);
+  t.ve = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(vs + l.vs));
+}
+
+// S^T of a tile: lane (grp, col) holds tokens 4 grp + i of query column col.
+template <int D>
+__device__ __forceinline__ f32x4_t mx_scores(const MxTile<D>& t, const bf16x8_t (&qv)[D / 32]) {
+  const float s = mx::scale_operand(t.ke);
+  f32x4_t st = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int kk = 0; kk < D / 32; kk++) {
+    const u32x4_t w = {mx::pair_bf16<0>(t.k[kk], s), mx::pair_bf16<1>(t.k[kk], s), mx::pair_bf16<2>(t.k[kk], s),
+                       mx::pair_bf16<3>(t.k[kk], s)};
+    st = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, w), qv[kk], st, 0, 0, 0);
+  }
+  return st;
+}
+
+// V of a tile as channel pairs: word x of token row r.
+template <int D>
+__device__ __forceinline__ void mx_widen_v(const MxTile<D>& t, uint32_t (&w)[4][D / 32]) {
+  // the conversion takes the exponent field alone: the byte of each row shifted there will do
+  const float s[4] = {__uint_as_float(t.ve << 23), __uint_as_float(t.ve << 15), __uint_as_float(t.ve << 7),
+                      __uint_as_float(t.ve >> 1)};
+#pragma unroll
+  for (int r = 0; r < 4; r++) {
+    if constexpr (D == 128) {
+      w[r][0] = mx::pair_bf16<0>(t.v[r], s[r]);
+      w[r][1] = mx::pair_bf16<1>(t.v[r], s[r]);
+      w[r][2] = mx::pair_bf16<2>(t.v[r], s[r]);
+      w[r][3] = mx::pair_bf16<3>(t.v[r], s[r]);
+    } else {
+      const uint32_t c = t.v[r >> 1];
+      w[r][0] = (r & 1) ? mx::pair_bf16<2>(c, s[r]) : mx::pair_bf16<0>(c, s[r]);
+      w[r][1] = (r & 1) ? mx::pair_bf16<3>(c, s[r]) : mx::pair_bf16<1>(c, s[r]);
+    }
+  }
+}
+
+// Rows at and past `valid` (of 16) drop out: their scores to -inf, their V to code 0 at scale 1, so that
+// no garbage or NaN meets their zero weight.
+template <int D>
+__device__ __forceinline__ void mx_mask(int valid, int grp, f32x4_t& st, MxTile<D>& t) {
+#pragma unroll
+  for (int r = 0; r < 4; r++) {
+    if (4 * grp + r >= valid) {
+      st[r] = -INFINITY;
+      t.ve = (t.ve & ~(0xffu << (8 * r))) | (127u << (8 * r));
+      if constexpr (D == 128) t.v[r] = 0u;
+      else t.v[r >> 1] &= (r & 1) ? 0x0000ffffu : 0xffff0000u;
+    }
+  }
+}
+
+__device__ __forceinline__ uint32_t high_halves(float lo, float hi) {
+  return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+}
+
+// Round of two tiles.  G8: at most 8 query heads, lo_mask 0 in the columns of the hi parts and the upper
+// half's bits in those of the lo parts.
+template <int D, bool G8>
+__device__ __forceinline__ void mx_round(MxTile<D>& ta, MxTile<D>& tb, int va, int vb, const bf16x8_t (&qv)[D / 32],
+                                         int grp, float scale_log2, uint32_t lo_mask, float& m, float& lsum,
+                                         f32x4_t (&acc)[D / 16]) {
+  f32x4_t sa = mx_scores<D>(ta, qv), sb = mx_scores<D>(tb, qv);
+  if (va < 16) mx_mask<D>(va, grp, sa, ta);                 // uniform
+  if (vb < 16) mx_mask<D>(vb, grp, sb, tb);
+  const float top = fmaxf(fmaxf(fmaxf(sa[0], sa[1]), fmaxf(sa[2], sa[3])),
+                          fmaxf(fmaxf(sb[0], sb[1]), fmaxf(sb[2], sb[3])));
+  if (__builtin_amdgcn_ballot_w64(top * scale_log2 > m + kRescaleLog2) != 0) {
+    float mt = top;
+    mt = fmaxf(mt, xor_shfl(mt, 16));
+    mt = fmaxf(mt, xor_shfl(mt, 32));
+    const float m_new = fmaxf(m, mt * scale_log2);
+    const float alpha = __builtin_amdgcn_exp2f(m - m_new);
+    m = m_new;
+    lsum *= alpha;
+#pragma unroll
+    for (int j = 0; j < D / 16; j++) {
+      acc[j][0] *= alpha;
+      acc[j][1] *= alpha;
+      acc[j][2] *= alpha;
+      acc[j][3] *= alpha;
+    }
+  }
+  float p[8];
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sa[i], scale_log2, -m));
+    p[4 + i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sb[i], scale_log2, -m));
+  }
+  lsum += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+  auto cut = [&](uint32_t mask) {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) x[i] = p[i] - __uint_as_float(__float_as_uint(p[i]) & mask);
+    return __builtin_bit_cast(bf16x8_t, (u32x4_t{high_halves(x[0], x[1]), high_halves(x[2], x[3]),
+                                                  high_halves(x[4], x[5]), high_halves(x[6], x[7])}));
+  };
+  const bf16x8_t p0 = cut(G8 ? lo_mask : 0u);
+  bf16x8_t p1{};
+  if constexpr (!G8) p1 = cut(0xffff0000u);
+  uint32_t wa[4][D / 32], wb[4][D / 32];
+  mx_widen_v<D>(ta, wa);
+  mx_widen_v<D>(tb, wb);
+#pragma unroll
+  for (int x = 0; x < D / 32; x++) {
+#pragma unroll
+    for (int odd = 0; odd < 2; odd++) {
+      // channel 2 x + odd of the piece: the tokens' halves side by side
+      const uint32_t sel = odd ? 0x07060302u : 0x05040100u;
+      const u32x4_t w = {__builtin_amdgcn_perm(wa[1][x], wa[0][x], sel), __builtin_amdgcn_perm(wa[3][x], wa[2][x], sel),
+                         __builtin_amdgcn_perm(wb[1][x], wb[0][x], sel), __builtin_amdgcn_perm(wb[3][x], wb[2][x], sel)};
+      const bf16x8_t a = __builtin_bit_cast(bf16x8_t, w);
+      f32x4_t& o = acc[2 * x + odd];
+      o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p0, o, 0, 0, 0);
+      if constexpr (!G8) o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p1, o, 0, 0, 0);
+    }
+  }
+}
+
+// One wave's share of a split, as gqa_wave_slots of decode.hip: the slots lo + w, lo + w + U, .. below
+// min(hi_fixed, cnt).
+template <int D, bool G8>
+__device__ __forceinline__ void mx_wave_slots(const DecodeArgs& a, int i, int h, int lo, int hi_fixed, int w, int U,
+                                              int lane, float& m, float& lsum, f32x4_t (&acc)[D / 16], int& cnt_all) {
+  const uint8_t* kbase = static_cast<const uint8_t*>(a.k);
+  const uint8_t* vbase = static_cast<const uint8_t*>(a.v);
+  constexpr int KS = D / 32;
+  const int col = lane & 15, grp = lane >> 4;
+  const int head = G8 ? (col & 7) : col;
+  const uint32_t lo_mask = G8 && col >= 8 ? 0xffff0000u : 0u;
+#pragma unroll
+  for (int j = 0; j < D / 16; j++) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  m = kNoMax;
+  lsum = 0.f;
+  const int32_t* sel = a.sel_pages + ((int64_t)i * a.H + h) * a.max_sel;
+  const int cnt_raw = a.sel_count[i];
+  const int L = a.seq_lens[i];
+  const int base = a.indptr[i];
+  const int list_len = a.indptr[i + 1] - base;
+  const int slot0 = lo + w + U * lane;
+  const int j_first = slot0 < hi_fixed ? sel[slot0] : -1;
+  bf16x8_t qv[KS];
+  {
+    const bool hv = head < a.g;
+    const uint16_t* qp = a.q + ((int64_t)i * a.Hq + h * a.g + (hv ? head : 0)) * D + KS * 8 * grp;
+#pragma unroll
+    for (int kk = 0; kk < KS; kk++) {
+      qv[kk] = *reinterpret_cast<const bf16x8_t*>(qp + 8 * kk);
+      if (!hv) qv[kk] = bf16x8_t{};
+    }
+  }
+  cnt_all = min(max(cnt_raw, 0), a.max_sel);
+  const int cnt = min(cnt_all, hi_fixed);
+  const int P = num_pages(L, a.bs, list_len * a.r, INT_MAX);
+  const int tps = a.bs >> 4;                               // tiles per slot
+  const int64_t slice_bytes = mx::slice_bytes(a.ps, D);
+  const MxLane ln = mx_lane<D>(col, grp);
+
+  for (int w0 = 0; lo + w + U * w0 < cnt; w0 += kWave) {
+    const int slot = slot0 + U * w0;
+    const int j = w0 == 0 ? j_first : (slot < hi_fixed ? sel[slot] : -1);
+    // lane: physical page of its slot's block, and (tile offset of the block in the page) << 16 |
+    // valid tokens (0: an id outside the request, whose tiles weigh nothing)
+    int my_p = 0, my_n = 0;
+    if (slot < cnt && j >= 0 && j < P) {
+      const int jp = j / a.r, blk = j - jp * a.r;
+      my_p = (int)clamp_page(a.indices[base + jp], a.num_phys);
+      my_n = min(a.bs, L - j * a.bs) | ((blk * tps) << 16);
+    }
+    const int nb = min(kWave, (cnt - lo - w - U * w0 + U - 1) / U);
+    int ls = 0, ltt = 0;                                   // cursor over (slot, tile)
+    // Loads the cursor's tile and moves on; past the last one it loads nothing and gives 0.
+    auto fetch = [&](MxTile<D>& t) -> int {
+      while (ls < nb) {
+        const int n = __builtin_amdgcn_readlane(my_n, ls);
+        const int left = (n & 0xffff) - 16 * ltt;
+        if (left <= 0) {
+          ls++;
+          ltt = 0;
+          continue;
+        }
+        const int64_t p = __builtin_amdgcn_readlane(my_p, ls);
+        mx_load<D>(kbase, vbase, (p * a.H + h) * slice_bytes, 16 * ((n >> 16) + ltt), a.ps, ln, t);
+        ltt++;
+        return min(16, left);
+      }
+      return 0;
+    };
+    MxTile<D> t0{}, t1{}, u0{}, u1{};
+    int a0 = fetch(t0), a1 = fetch(t1);
+    while (a0) {
+      const int b0 = fetch(u0), b1 = fetch(u1);
+      mx_round<D, G8>(t0, t1, a0, a1, qv, grp, a.scale_log2, lo_mask, m, lsum, acc);
+      if (!b0) break;
+      a0 = fetch(t0);
+      a1 = fetch(t1);
+      mx_round<D, G8>(u0, u1, b0, b1, qv, grp, a.scale_log2, lo_mask, m, lsum, acc);
+    }
+  }
+}
+
+template <int D, int NW, bool G8, bool BAL>
+__global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(3))) void decode_mx_kernel(
+    const DecodeArgs a) {
+  constexpr int DPL = D / 16;
+  extern __shared__ __attribute__((aligned(16))) float mx_lds[];
+  load_args(a);
+  const int lane = lane_id(), wv = (int)threadIdx.x >> 6;
+  const int col = lane & 15, grp = lane >> 4;
+  __shared__ int last;
+  const int pairs = (int)gridDim.x / a.S;
+  const int split = (int)blockIdx.x / pairs;
+  int ui = ((int)blockIdx.x - split * pairs) / a.H;
+  const int uh = (int)blockIdx.x - split * pairs - ui * a.H;
+  if constexpr (BAL) ui = balanced_request(a, ui, pairs / a.H);
+  const int T = a.T, pair = ui * a.H + uh, lo = split * T;
+
+  f32x4_t acc[DPL];
+  float m, lsum;
+  int cnt;
+  mx_wave_slots<D, G8>(a, ui, uh, lo, min(lo + T, a.max_sel), wv, NW, lane, m, lsum, acc, cnt);
+  const int Sp = splits_of(cnt, T);                        // uniform: every wave loaded the count
+  if (split >= Sp) return;
+  float lt = lsum + xor_shfl(lsum, 16);
+  lt += xor_shfl(lt, 32);
+  if constexpr (G8) {                                      // hi and lo parts' columns, 8 lanes apart
+#pragma unroll
+    for (int j = 0; j < DPL; j++) {
+#pragma unroll
+      for (int r = 0; r < 4; r++) acc[j][r] += dpp_f32<0x128>(acc[j][r]);
+    }
+  }
+
+  // the waves' states meet in LDS
+  const int g = a.g;
+  float* obuf = mx_lds;                                    // [wave][g][D]
+  float* mbuf = obuf + NW * g * D;                         // [wave][g]
+  float* lbuf = mbuf + NW * g;                             // [wave][g]
+  if (col < g) {
+    // lane (grp, col) holds channels (4*grp + r)*DPL + j of query head col
+    float* dst = obuf + (wv * g + col) * D + 4 * grp * DPL;
+#pragma unroll
+    for (int r = 0; r < 4; r++) {
+#pragma unroll
+      for (int j = 0; j < DPL; j += 4)
+        *reinterpret_cast<float4*>(dst + r * DPL + j) = make_float4(acc[j][r], acc[j + 1][r], acc[j + 2][r], acc[j + 3][r]);
+    }
+    if (grp == 0) {
+      mbuf[wv * g + col] = m;
+      lbuf[wv * g + col] = lt;
+    }
+  }
+  __syncthreads();
+  const uint32_t pair_rows = (uint32_t)(a.S * g);
+  const __amdgpu_buffer_rsrc_t o_rs = coherent_rsrc(a.part_o + (int64_t)pair * pair_rows * D, pair_rows * D * 4u);
+  const __amdgpu_buffer_rsrc_t l_rs = coherent_rsrc(a.part_lse + (int64_t)pair * pair_rows, pair_rows * 4u);
+  for (int x = (int)threadIdx.x; x < g * D / 4; x += NW * kWave) {
+    const int c = (4 * x) / D, d = 4 * x - c * D;
+    float M = kNoMax;
+#pragma unroll
+    for (int k = 0; k < NW; k++) M = fmaxf(M, mbuf[k * g + c]);
+    float Ls = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < NW; k++) {
+      const float wgt = __builtin_amdgcn_exp2f(mbuf[k * g + c] - M);      // a wave without a token has zeros
+      const float4 v = *reinterpret_cast<const float4*>(obuf + (k * g + c) * D + d);
+      Ls += wgt * lbuf[k * g + c];
+      o.x += wgt * v.x;
+      o.y += wgt * v.y;
+      o.z += wgt * v.z;
+      o.w += wgt * v.w;
+    }
+    const float inv = Ls == 0.f ? 0.f : 1.f / Ls;
+    if (Sp == 1) {
+      uint16_t* dst = a.out + ((int64_t)ui * a.Hq + uh * g + c) * D + d;
+      *reinterpret_cast<uint2*>(dst) = make_uint2(f32_to_bf16_rne(o.x * inv) | (f32_to_bf16_rne(o.y * inv) << 16),
+                                                  f32_to_bf16_rne(o.z * inv) | (f32_to_bf16_rne(o.w * inv) << 16));
+    } else {
+      const uint32_t row = (uint32_t)(split * g + c);
+      coherent_store4(o_rs, (row * D + d) * 4u, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+      if (d == 0) coherent_store1(l_rs, row * 4u, Ls == 0.f ? -INFINITY : M + __log2f(Ls));
+    }
+  }
+  if (Sp > 1) {
+    // split pair: the last split to arrive merges, as in decode.hip
+    wait_vm_all();
+    __syncthreads();
+    if (threadIdx.x == 0)
+      last = __builtin_amdgcn_atomic_inc32(a.ctr + pair, (uint32_t)(Sp - 1), __ATOMIC_RELAXED, "agent") ==
+             (uint32_t)(Sp - 1);
+    __syncthreads();
+    if (last) {
+      for (int x = (int)threadIdx.x; x < g * D / 4; x += NW * kWave)
+        merge_one(Sp, 0, a.H, g, a.Hq, D, a.out, pair, x,
+                  [&](int64_t e) { return coherent_load1(l_rs, (uint32_t)e * 4u); },
+                  [&](int64_t e) { return coherent_load4(o_rs, (uint32_t)e * 4u); });
+    }
+  }
+}
+
+template <int D, int NW>
+void launch(const DecodeArgs& a, unsigned grid, hipStream_t stream) {
+  const size_t lds = sizeof(float) * (size_t)NW * a.g * (D + 2);
+  const dim3 block(NW * kWave);
+#define VX_MX(G8, BAL) hipLaunchKernelGGL((decode_mx_kernel<D, NW, G8, BAL>), dim3(grid), block, lds, stream, a)
+  if (a.g <= 8) {
+    if (a.order_block > 0) VX_MX(true, true);
+    else VX_MX(true, false);
+  } else {
+    if (a.order_block > 0) VX_MX(false, true);
+    else VX_MX(false, false);
+  }
+#undef VX_MX
+}
+
+}  // namespace
+
+void launch_decode_mx(const DecodeArgs& a, int D, int waves, unsigned grid, hipStream_t stream) {
+  if (D == 128) {
+    if (waves == 3) launch<128, 3>(a, grid, stream);
+    else launch<128, 4>(a, grid, stream);
+  } else {
+    if (waves == 3) launch<64, 3>(a, grid, stream);
+    else launch<64, 4>(a, grid, stream);
+  }
+}
+
+}  // namespace vx

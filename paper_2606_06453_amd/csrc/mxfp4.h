@@ -33,10 +33,9 @@ __device__ __forceinline__ int v_code(int t, int c8, int D) {
 __device__ __forceinline__ int k_scale(int t, int grp, int D) { return t * (D / kGroup) + grp; }
 __device__ __forceinline__ int v_scale(int t, int grp, int D) { return ((t >> 2) * (D / kGroup) + grp) * 4 + (t & 3); }
 
-// 2^(E - 127) as fp32, NaN for E = 255 (the shift alone would give infinity).
-__device__ __forceinline__ float scale_value(uint32_t e) {
-  return __uint_as_float((e << 23) | (((e + 1u) >> 8) << 22));
-}
+// The conversions' scale operand of scale byte E.  They take its exponent field alone, 255 as NaN, and
+// neither its sign nor its mantissa.
+__device__ __forceinline__ float scale_operand(uint32_t e) { return __uint_as_float(e << 23); }
 
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 

@@ -146,7 +146,7 @@ __device__ __forceinline__ uint4 read_chunk(const RowArgs& a, bool v, int64_t pa
     const uint8_t* slice = base + (page * a.H + h) * mx::slice_bytes(a.ps, D);
     const uint32_t w = v ? mx::get_v_codes(slice, t, c8, D)
                          : *reinterpret_cast<const uint32_t*>(slice + mx::k_code(t, c8, D));
-    const float s = mx::scale_value(
+    const float s = mx::scale_operand(
         slice[mx::codes_bytes(a.ps, D) + (v ? mx::v_scale(t, c8 >> 2, D) : mx::k_scale(t, c8 >> 2, D))]);
     return make_uint4(mx::pair_bf16<0>(w, s), mx::pair_bf16<1>(w, s), mx::pair_bf16<2>(w, s), mx::pair_bf16<3>(w, s));
   } else {

@@ -79,7 +79,7 @@ struct RowChunk<kKvMxFp4> {
   };
   static constexpr int kBytes = 4;
   __device__ static __forceinline__ void values(const Raw& w, float, float (&x)[8]) {
-    const float s = mx::scale_value(w.e);
+    const float s = mx::scale_operand(w.e);
     const float2_t v[4] = {mx::pair_f32<0>(w.codes, s), mx::pair_f32<1>(w.codes, s), mx::pair_f32<2>(w.codes, s),
                            mx::pair_f32<3>(w.codes, s)};
 #pragma unroll

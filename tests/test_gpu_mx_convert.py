@@ -1,6 +1,6 @@
 """What the mxfp4 cache's kernels take of the E2M1 conversions of gfx950 (tests/probes/mx_probe.hip):
-a code's value times a power of two is exact in bf16 and fp32, a NaN scale gives NaN, and a bf16 value
-divided by a power of two rounds to the nearest code, ties to the even one, saturating at 6."""
+a code's value times a power of two is exact in bf16 and fp32, only the exponent of the scale counts
+and 255 gives NaN, and a bf16 value divided by a power of two rounds to the nearest code, ties to the even one, saturating at 6."""
 import ctypes
 import os
 
@@ -52,10 +52,19 @@ def test_every_code_at_every_scale_is_exact():
     assert np.array_equal(vals, want(byte))
 
 
-def test_a_nan_scale_gives_nan():
+@pytest.mark.parametrize("bits", [0x7F800000, 0x7FC00000, 0x7F812345, 0xFF800000, 0xFFFFFFFF])
+def test_an_exponent_of_255_gives_nan(bits):
     byte = np.arange(256)
-    halves, vals = _widen(byte * 0x01010101, np.full(256, 0x7FC00000))
+    halves, vals = _widen(byte * 0x01010101, np.full(256, bits))
     assert np.isnan(halves).all() and np.isnan(vals).all()
+
+
+@pytest.mark.parametrize("bits", [0x3F800001, 0x3FC00000, 0x3FFFFFFF, 0xBF800000, 0xBFFFFFFF])
+def test_only_the_exponent_of_a_scale_counts(bits):
+    byte = np.arange(256)
+    halves, vals = _widen(byte * 0x01010101, np.full(256, bits))
+    one, one_vals = _widen(byte * 0x01010101, np.full(256, 0x3F800000))
+    assert np.array_equal(halves, one) and np.array_equal(vals, one_vals)
 
 
 def test_codes_round_to_nearest_even_and_saturate():
