@@ -54,6 +54,9 @@ namespace {
 constexpr int kDecodeWaves = 4;           // waves per GQA workgroup (3 for some batch shapes)
 constexpr int kGqaTargetWgs = 512;        // two 4-wave workgroups per CU
 constexpr int kGqaWavesPerCu = 12;        // resident GQA split waves per CU (168 VGPRs each)
+constexpr int kMxWgsPerCu = 3;            // resident mxfp4 workgroups per CU
+constexpr int kMxSplitTokens = 2048;      // least tokens of an mxfp4 split beyond one workgroup per CU
+constexpr int kSplitPairs = 1024;         // most pairs of a batch that splits any
 constexpr int kMlaTargetWgs = 256;        // one workgroup per CU
 constexpr int kMergeThreads = 256;
 
@@ -994,11 +997,12 @@ __global__ __launch_bounds__(kMergeThreads) void merge_kernel(int S, int H, int 
 
 }  // namespace
 
-DecodeLayout decode_layout(int batch, int num_kv_heads, int group, int head_dim_v, int max_sel, bool mla) {
+DecodeLayout decode_layout(int batch, int num_kv_heads, int group, int head_dim_v, int max_sel,
+                           int block_size, bool mla, bool mx) {
   DecodeLayout L;
   const long long pairs = (long long)batch * num_kv_heads;
   const long long ms = max_sel > 0 ? max_sel : 1;
-  const long long cus = device_cus();
+  const long long cus = std::min(device_cus(), kSplitPairs / kMxWgsPerCu);   // the counters' places
   if (mla) {
     // one workgroup per CU: S splits per request over fixed slot ranges, merged by merge_kernel
     long long S = pairs > 0 ? (kMlaTargetWgs + pairs - 1) / pairs : 1;
@@ -1006,6 +1010,26 @@ DecodeLayout decode_layout(int batch, int num_kv_heads, int group, int head_dim_
     S = S < 1 ? 1 : S;
     L.splits = (int)S;
     L.waves = 8;
+    L.n_wg = pairs * S;
+  } else if (mx) {
+    // Three 4-wave workgroups (168 VGPRs) are resident on a CU.  Few pairs: one workgroup per CU, down to a
+    // slot per wave.  While not every resident place has a pair of its own, long selections are cut
+    // further, three rounds of workgroups deep, into splits of at least kMxSplitTokens: ragged counts
+    // fill the chip (24 requests of up to 20000 tokens, 64 channels, 8 KV heads: 3 splits 50.7 us, 6
+    // 42.7, 10 40.8; 2048 selected pages of 16 from 100 to 32000 tokens 112 us, in splits of 4096 tokens
+    // 123) and equal ones lose little (24 requests of 32768 tokens 159.5 us, in splits of 4096 154).  A
+    // short selection is not cut for more than a workgroup per CU: 128 pages of 16 for 32 requests of 8 KV
+    // heads, one split 17.2 us, two 19.1; 64 requests 29.4 and 35.9.
+    const long long resident = cus * kMxWgsPerCu;
+    long long S = pairs > 0 ? (cus + pairs - 1) / pairs : 1;
+    S = std::min(S, (ms + kDecodeWaves - 1) / kDecodeWaves);
+    if (pairs > 0 && pairs < resident) S = std::max(S, std::min(3 * resident / pairs, ms * block_size / kMxSplitTokens));
+    S = std::max(S, 1LL);
+    const long long T = (ms + S - 1) / S;
+    S = (ms + T - 1) / T;
+    L.waves = kDecodeWaves;
+    L.splits = (int)S;
+    L.split_slots = (int)T;
     L.n_wg = pairs * S;
   } else {
     // S workgroups per pair so that about kGqaTargetWgs fill the chip when every pair selects
@@ -1027,10 +1051,10 @@ DecodeLayout decode_layout(int batch, int num_kv_heads, int group, int head_dim_
   }
   auto al = [](size_t x) { return (x + 255) & ~(size_t)255; };
   const long long rows = pairs * L.splits;
-  // Only batches of fewer than kGqaTargetWgs pairs split any, and the counters keep their place in
-  // every layout: a buffer that batches of other sizes have used still has them at zero.
+  // Only batches of at most kSplitPairs pairs split any, and the counters keep their place in every
+  // layout: a buffer that batches of other sizes have used still has them at zero.
   L.off_ctr = 0;
-  size_t off = al(sizeof(uint32_t) * kGqaTargetWgs);
+  size_t off = al(sizeof(uint32_t) * kSplitPairs);
   L.off_lse = off;
   off = al(off + sizeof(float) * (size_t)rows * group);
   L.off_o = off;
@@ -1123,7 +1147,7 @@ hipError_t launch_decode(const Geometry& g, const uint16_t* q, int Hq, const int
     else
       hipLaunchKernelGGL(decode_mla_kernel<kKvBf16>, grid, dim3(mla::kThreads), 0, stream, a);
   } else if (g.kv_dtype == kKvMxFp4) {
-    launch_decode_mx(a, g.Dqk, lay.waves, grid.x, stream);
+    launch_decode_mx(a, g.Dqk, grid.x, stream);
   } else {
     const size_t lds = gqa_merge_lds_bytes(group, g.Dqk, lay.waves);
     const dim3 block(lay.waves * kWave);

@@ -184,7 +184,7 @@ __device__ __forceinline__ int splits_of(int cnt, int T) { return cnt > 0 ? (cnt
 
 }  // namespace dec
 
-// The mxfp4 split kernel (decode_mx.hip); waves and grid from the layout.
-void launch_decode_mx(const dec::DecodeArgs& a, int D, int waves, unsigned grid, hipStream_t stream);
+// The mxfp4 split kernel (decode_mx.hip), workgroups of four waves.
+void launch_decode_mx(const dec::DecodeArgs& a, int D, unsigned grid, hipStream_t stream);
 
 }  // namespace vx

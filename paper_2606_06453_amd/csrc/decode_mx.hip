@@ -17,6 +17,8 @@
 // P is the sum of two bf16 parts, hi = p cut to 8 bits and lo = (p - hi) cut to 8, 2^-15 of p.  With at
 // most 8 query heads per KV head the 16 columns hold every head twice, the hi parts in columns 0 to 7
 // and the lo parts in 8 to 15, so one MFMA per operand does both; else two.
+#include <algorithm>
+
 #include "decode_common.h"
 #include "mxfp4.h"
 
@@ -24,6 +26,7 @@ namespace vx {
 using namespace dec;
 namespace {
 
+constexpr int kMxWaves = 4;               // per workgroup
 constexpr float kRescaleLog2 = 8.f;
 constexpr float kNoMax = -1e30f;          // running maximum before the first token
 
@@ -78,24 +81,17 @@ __device__ __forceinline__ f32x4_t mx_scores(const MxTile<D>& t, const bf16x8_t 
   return st;
 }
 
-// V of a tile as channel pairs: word x of token row r.
+// Channels 2 x and 2 x + 1 of token row r of a tile's V.
 template <int D>
-__device__ __forceinline__ void mx_widen_v(const MxTile<D>& t, uint32_t (&w)[4][D / 32]) {
+__device__ __forceinline__ uint32_t mx_widen_v(const MxTile<D>& t, int r, int x) {
   // the conversion takes the exponent field alone: the byte of each row shifted there will do
-  const float s[4] = {__uint_as_float(t.ve << 23), __uint_as_float(t.ve << 15), __uint_as_float(t.ve << 7),
-                      __uint_as_float(t.ve >> 1)};
-#pragma unroll
-  for (int r = 0; r < 4; r++) {
-    if constexpr (D == 128) {
-      w[r][0] = mx::pair_bf16<0>(t.v[r], s[r]);
-      w[r][1] = mx::pair_bf16<1>(t.v[r], s[r]);
-      w[r][2] = mx::pair_bf16<2>(t.v[r], s[r]);
-      w[r][3] = mx::pair_bf16<3>(t.v[r], s[r]);
-    } else {
-      const uint32_t c = t.v[r >> 1];
-      w[r][0] = (r & 1) ? mx::pair_bf16<2>(c, s[r]) : mx::pair_bf16<0>(c, s[r]);
-      w[r][1] = (r & 1) ? mx::pair_bf16<3>(c, s[r]) : mx::pair_bf16<1>(c, s[r]);
-    }
+  const float s = __uint_as_float(r == 0 ? t.ve << 23 : r == 1 ? t.ve << 15 : r == 2 ? t.ve << 7 : t.ve >> 1);
+  const uint32_t c = D == 128 ? t.v[r] : t.v[r >> 1];
+  switch (D == 128 ? x : 2 * (r & 1) + x) {                 // known once unrolled
+    case 0: return mx::pair_bf16<0>(c, s);
+    case 1: return mx::pair_bf16<1>(c, s);
+    case 2: return mx::pair_bf16<2>(c, s);
+    default: return mx::pair_bf16<3>(c, s);
   }
 }
 
@@ -118,15 +114,15 @@ __device__ __forceinline__ uint32_t high_halves(float lo, float hi) {
   return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
 }
 
-// Round of two tiles.  G8: at most 8 query heads, lo_mask 0 in the columns of the hi parts and the upper
-// half's bits in those of the lo parts.
+// Round of two tiles with va and vb valid tokens.  G8: at most 8 query heads, lo_mask 0 in the columns of
+// the hi parts and the upper half's bits in those of the lo parts.
 template <int D, bool G8>
-__device__ __forceinline__ void mx_round(MxTile<D>& ta, MxTile<D>& tb, int va, int vb, const bf16x8_t (&qv)[D / 32],
-                                         int grp, float scale_log2, uint32_t lo_mask, float& m, float& lsum,
+__device__ __forceinline__ void mx_round(MxTile<D> (&t)[2], int va, int vb, const bf16x8_t (&qv)[D / 32], int grp,
+                                         float scale_log2, uint32_t lo_mask, float& m, float& lsum,
                                          f32x4_t (&acc)[D / 16]) {
-  f32x4_t sa = mx_scores<D>(ta, qv), sb = mx_scores<D>(tb, qv);
-  if (va < 16) mx_mask<D>(va, grp, sa, ta);                 // uniform
-  if (vb < 16) mx_mask<D>(vb, grp, sb, tb);
+  f32x4_t sa = mx_scores<D>(t[0], qv), sb = mx_scores<D>(t[1], qv);
+  if (va < 16) mx_mask<D>(va, grp, sa, t[0]);               // uniform
+  if (vb < 16) mx_mask<D>(vb, grp, sb, t[1]);
   const float top = fmaxf(fmaxf(fmaxf(sa[0], sa[1]), fmaxf(sa[2], sa[3])),
                           fmaxf(fmaxf(sb[0], sb[1]), fmaxf(sb[2], sb[3])));
   if (__builtin_amdgcn_ballot_w64(top * scale_log2 > m + kRescaleLog2) != 0) {
@@ -162,17 +158,20 @@ __device__ __forceinline__ void mx_round(MxTile<D>& ta, MxTile<D>& tb, int va, i
   const bf16x8_t p0 = cut(G8 ? lo_mask : 0u);
   bf16x8_t p1{};
   if constexpr (!G8) p1 = cut(0xffff0000u);
-  uint32_t wa[4][D / 32], wb[4][D / 32];
-  mx_widen_v<D>(ta, wa);
-  mx_widen_v<D>(tb, wb);
 #pragma unroll
-  for (int x = 0; x < D / 32; x++) {
+  for (int x = 0; x < D / 32; x++) {                        // channel pair x of every piece
+    uint32_t wa[4], wb[4];
+#pragma unroll
+    for (int r = 0; r < 4; r++) {
+      wa[r] = mx_widen_v<D>(t[0], r, x);
+      wb[r] = mx_widen_v<D>(t[1], r, x);
+    }
 #pragma unroll
     for (int odd = 0; odd < 2; odd++) {
-      // channel 2 x + odd of the piece: the tokens' halves side by side
+      // channel 2 x + odd: the tokens' halves side by side
       const uint32_t sel = odd ? 0x07060302u : 0x05040100u;
-      const u32x4_t w = {__builtin_amdgcn_perm(wa[1][x], wa[0][x], sel), __builtin_amdgcn_perm(wa[3][x], wa[2][x], sel),
-                         __builtin_amdgcn_perm(wb[1][x], wb[0][x], sel), __builtin_amdgcn_perm(wb[3][x], wb[2][x], sel)};
+      const u32x4_t w = {__builtin_amdgcn_perm(wa[1], wa[0], sel), __builtin_amdgcn_perm(wa[3], wa[2], sel),
+                         __builtin_amdgcn_perm(wb[1], wb[0], sel), __builtin_amdgcn_perm(wb[3], wb[2], sel)};
       const bf16x8_t a = __builtin_bit_cast(bf16x8_t, w);
       f32x4_t& o = acc[2 * x + odd];
       o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p0, o, 0, 0, 0);
@@ -216,60 +215,149 @@ __device__ __forceinline__ void mx_wave_slots(const DecodeArgs& a, int i, int h,
   cnt_all = min(max(cnt_raw, 0), a.max_sel);
   const int cnt = min(cnt_all, hi_fixed);
   const int P = num_pages(L, a.bs, list_len * a.r, INT_MAX);
-  const int tps = a.bs >> 4;                               // tiles per slot
+  const int tsh = __builtin_ctz((unsigned)a.bs) - 4;       // log2 of the tiles per slot
   const int64_t slice_bytes = mx::slice_bytes(a.ps, D);
   const MxLane ln = mx_lane<D>(col, grp);
 
   for (int w0 = 0; lo + w + U * w0 < cnt; w0 += kWave) {
     const int slot = slot0 + U * w0;
     const int j = w0 == 0 ? j_first : (slot < hi_fixed ? sel[slot] : -1);
-    // lane: physical page of its slot's block, and (tile offset of the block in the page) << 16 |
-    // valid tokens (0: an id outside the request, whose tiles weigh nothing)
-    int my_p = 0, my_n = 0;
+    // lane: slice of its slot's block, and (first tile of the block in the page) << 16 | valid tokens
+    // (0: an id outside the request, whose tiles weigh nothing)
+    int64_t my_s = 0;
+    int my_n = 0;
     if (slot < cnt && j >= 0 && j < P) {
       const int jp = j / a.r, blk = j - jp * a.r;
-      my_p = (int)clamp_page(a.indices[base + jp], a.num_phys);
-      my_n = min(a.bs, L - j * a.bs) | ((blk * tps) << 16);
+      my_s = (clamp_page(a.indices[base + jp], a.num_phys) * a.H + h) * slice_bytes;
+      my_n = min(a.bs, L - j * a.bs) | ((blk << tsh) << 16);
     }
-    const int nb = min(kWave, (cnt - lo - w - U * w0 + U - 1) / U);
-    int ls = 0, ltt = 0;                                   // cursor over (slot, tile)
-    // Loads the cursor's tile and moves on; past the last one it loads nothing and gives 0.
-    auto fetch = [&](MxTile<D>& t) -> int {
-      while (ls < nb) {
-        const int n = __builtin_amdgcn_readlane(my_n, ls);
-        const int left = (n & 0xffff) - 16 * ltt;
-        if (left <= 0) {
-          ls++;
-          ltt = 0;
-          continue;
-        }
-        const int64_t p = __builtin_amdgcn_readlane(my_p, ls);
-        mx_load<D>(kbase, vbase, (p * a.H + h) * slice_bytes, 16 * ((n >> 16) + ltt), a.ps, ln, t);
-        ltt++;
-        return min(16, left);
-      }
-      return 0;
+    const int tiles = min(kWave, (cnt - lo - w - U * w0 + U - 1) / U) << tsh;
+    // Tile u of the window into t, the last one again past the end.
+    auto load = [&](int u, MxTile<D>& t) {
+      u = min(u, tiles - 1);
+      const int ls = u >> tsh, tt = u - (ls << tsh);
+      const uint32_t s_lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)my_s, ls);
+      const uint32_t s_hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)my_s >> 32), ls);
+      const int t0 = 16 * ((__builtin_amdgcn_readlane(my_n, ls) >> 16) + tt);
+      mx_load<D>(kbase, vbase, (int64_t)(((uint64_t)s_hi << 32) | s_lo), t0, a.ps, ln, t);
     };
-    MxTile<D> t0{}, t1{}, u0{}, u1{};
-    int a0 = fetch(t0), a1 = fetch(t1);
-    while (a0) {
-      const int b0 = fetch(u0), b1 = fetch(u1);
-      mx_round<D, G8>(t0, t1, a0, a1, qv, grp, a.scale_log2, lo_mask, m, lsum, acc);
-      if (!b0) break;
-      a0 = fetch(t0);
-      a1 = fetch(t1);
-      mx_round<D, G8>(u0, u1, b0, b1, qv, grp, a.scale_log2, lo_mask, m, lsum, acc);
+    auto valid = [&](int u) {
+      if (u >= tiles) return 0;
+      const int ls = u >> tsh, tt = u - (ls << tsh);
+      return min(16, (__builtin_amdgcn_readlane(my_n, ls) & 0xffff) - 16 * tt);
+    };
+    // Two rounds' tiles in registers: one loads while the other computes.  The loads are unconditional
+    // (past the end the last tile once more, a cache hit), so that no branch makes the compiler wait
+    // for all of them.
+    MxTile<D> t[2], n[2];
+    load(0, t[0]);
+    load(1, t[1]);
+    for (int u = 0;; u += 4) {
+      load(u + 2, n[0]);
+      load(u + 3, n[1]);
+      mx_round<D, G8>(t, valid(u), valid(u + 1), qv, grp, a.scale_log2, lo_mask, m, lsum, acc);
+      if (u + 2 >= tiles) break;
+      load(u + 4, t[0]);
+      load(u + 5, t[1]);
+      mx_round<D, G8>(n, valid(u + 2), valid(u + 3), qv, grp, a.scale_log2, lo_mask, m, lsum, acc);
+      if (u + 4 >= tiles) break;
     }
   }
 }
 
-template <int D, int NW, bool G8, bool BAL>
-__global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(3))) void decode_mx_kernel(
+__device__ __forceinline__ void put_merged(uint16_t* dst, float W, const float4& o) {
+  const float inv = W == 0.f ? 0.f : 1.f / W;
+  *reinterpret_cast<uint2*>(dst) = make_uint2(f32_to_bf16_rne(o.x * inv) | (f32_to_bf16_rne(o.y * inv) << 16),
+                                              f32_to_bf16_rne(o.z * inv) | (f32_to_bf16_rne(o.w * inv) << 16));
+}
+
+// LSE-weighted merge of a split pair's S partials by the workgroup.  A slot is 4 channels of one head;
+// with fewer slots than threads, G threads share one and take every G-th partial, kMergeBatch loads in
+// flight each, and meet in LDS ([G][slots] of 6 floats): a pair cut into many splits (few requests)
+// is merged in one or two round trips.
+template <int D, int NT>
+__device__ __forceinline__ void merge_pair(int S, int g, __amdgpu_buffer_rsrc_t o_rs, __amdgpu_buffer_rsrc_t l_rs,
+                                           float* lds, uint16_t* out) {
+  const int slots = g * D / 4;
+  const int G = max(1, min(NT / slots, S));
+  for (int y = (int)threadIdx.x; y < slots * G; y += NT) {   // one turn, unless there are more slots than threads
+    const int k = y / slots, x = y - k * slots;
+    const int c = (4 * x) / D, d = 4 * x - c * D;
+    float M = -INFINITY, W = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s0 = k; s0 < S; s0 += G * kMergeBatch) {
+      float l[kMergeBatch];
+      float4 p[kMergeBatch];
+#pragma unroll
+      for (int b = 0; b < kMergeBatch; b++) {
+        const uint32_t row = (uint32_t)(min(s0 + G * b, S - 1) * g + c);
+        l[b] = coherent_load1(l_rs, row * 4u);
+        p[b] = coherent_load4(o_rs, (row * D + d) * 4u);
+      }
+      float m_new = M;
+#pragma unroll
+      for (int b = 0; b < kMergeBatch; b++) {
+        if (s0 + G * b >= S) l[b] = -INFINITY;
+        m_new = fmaxf(m_new, l[b]);
+      }
+      // without a token so far every weight is 0 (or NaN, which stays)
+      const float ref = m_new == -INFINITY ? 0.f : m_new;
+      const float keep = __builtin_amdgcn_exp2f(M - ref);
+      W *= keep;
+      o.x *= keep;
+      o.y *= keep;
+      o.z *= keep;
+      o.w *= keep;
+#pragma unroll
+      for (int b = 0; b < kMergeBatch; b++) {
+        const float wgt = __builtin_amdgcn_exp2f(l[b] - ref);
+        W += wgt;
+        o.x += wgt * p[b].x;
+        o.y += wgt * p[b].y;
+        o.z += wgt * p[b].z;
+        o.w += wgt * p[b].w;
+      }
+      M = m_new;
+    }
+    if (G > 1) {
+      float* q = lds + (size_t)y * 6;
+      q[0] = M;
+      q[1] = W;
+      q[2] = o.x;
+      q[3] = o.y;
+      q[4] = o.z;
+      q[5] = o.w;
+    } else {
+      put_merged(out + c * D + d, W, o);
+    }
+  }
+  if (G == 1) return;                                        // uniform
+  __syncthreads();
+  if ((int)threadIdx.x >= slots) return;
+  const int x = (int)threadIdx.x, c = (4 * x) / D, d = 4 * x - c * D;
+  float M = -INFINITY, W = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int k = 0; k < G; k++) M = fmaxf(M, lds[(size_t)(k * slots + x) * 6]);
+  const float ref = M == -INFINITY ? 0.f : M;
+  for (int k = 0; k < G; k++) {
+    const float* q = lds + (size_t)(k * slots + x) * 6;
+    const float wgt = __builtin_amdgcn_exp2f(q[0] - ref);
+    W += wgt * q[1];
+    o.x += wgt * q[2];
+    o.y += wgt * q[3];
+    o.z += wgt * q[4];
+    o.w += wgt * q[5];
+  }
+  put_merged(out + c * D + d, W, o);
+}
+
+template <int D, bool G8, bool BAL>
+__global__ __launch_bounds__(kMxWaves * kWave) __attribute__((amdgpu_waves_per_eu(3))) void decode_mx_kernel(
     const DecodeArgs a) {
-  constexpr int DPL = D / 16;
+  constexpr int DPL = D / 16, NW = kMxWaves;
   extern __shared__ __attribute__((aligned(16))) float mx_lds[];
   load_args(a);
-  const int lane = lane_id(), wv = (int)threadIdx.x >> 6;
+  const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int col = lane & 15, grp = lane >> 4;
   __shared__ int last;
   const int pairs = (int)gridDim.x / a.S;
@@ -354,20 +442,16 @@ __global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(3)))
       last = __builtin_amdgcn_atomic_inc32(a.ctr + pair, (uint32_t)(Sp - 1), __ATOMIC_RELAXED, "agent") ==
              (uint32_t)(Sp - 1);
     __syncthreads();
-    if (last) {
-      for (int x = (int)threadIdx.x; x < g * D / 4; x += NW * kWave)
-        merge_one(Sp, 0, a.H, g, a.Hq, D, a.out, pair, x,
-                  [&](int64_t e) { return coherent_load1(l_rs, (uint32_t)e * 4u); },
-                  [&](int64_t e) { return coherent_load4(o_rs, (uint32_t)e * 4u); });
-    }
+    if (last) merge_pair<D, NW * kWave>(Sp, g, o_rs, l_rs, mx_lds, a.out + ((int64_t)ui * a.Hq + uh * g) * D);
   }
 }
 
-template <int D, int NW>
+template <int D>
 void launch(const DecodeArgs& a, unsigned grid, hipStream_t stream) {
-  const size_t lds = sizeof(float) * (size_t)NW * a.g * (D + 2);
-  const dim3 block(NW * kWave);
-#define VX_MX(G8, BAL) hipLaunchKernelGGL((decode_mx_kernel<D, NW, G8, BAL>), dim3(grid), block, lds, stream, a)
+  // the waves' states, then merge_pair's
+  const size_t lds = sizeof(float) * (size_t)kMxWaves * std::max(a.g * (D + 2), kWave * 6);
+  const dim3 block(kMxWaves * kWave);
+#define VX_MX(G8, BAL) hipLaunchKernelGGL((decode_mx_kernel<D, G8, BAL>), dim3(grid), block, lds, stream, a)
   if (a.g <= 8) {
     if (a.order_block > 0) VX_MX(true, true);
     else VX_MX(true, false);
@@ -380,14 +464,9 @@ void launch(const DecodeArgs& a, unsigned grid, hipStream_t stream) {
 
 }  // namespace
 
-void launch_decode_mx(const DecodeArgs& a, int D, int waves, unsigned grid, hipStream_t stream) {
-  if (D == 128) {
-    if (waves == 3) launch<128, 3>(a, grid, stream);
-    else launch<128, 4>(a, grid, stream);
-  } else {
-    if (waves == 3) launch<64, 3>(a, grid, stream);
-    else launch<64, 4>(a, grid, stream);
-  }
+void launch_decode_mx(const DecodeArgs& a, int D, unsigned grid, hipStream_t stream) {
+  if (D == 128) launch<128>(a, grid, stream);
+  else launch<64>(a, grid, stream);
 }
 
 }  // namespace vx

@@ -133,6 +133,9 @@ vx_status check_kind(const vx_paged_cache* kv, vx_score_kind kind, const float* 
   return VX_OK;
 }
 
+// Tokens of a block (checked caches only).
+int block_tokens(const vx_paged_cache* kv) { return kv->block_size > 0 ? kv->block_size : kv->page_size; }
+
 // Blocks per request bound: max_pages_per_seq times the blocks per page (checked caches only).
 int max_blocks(const vx_paged_cache* kv, const vx_batch* b) {
   const int r = kv->block_size > 0 ? kv->page_size / kv->block_size : 1;
@@ -183,7 +186,7 @@ vx_status vx_workspace_size(vx_stage stage, const vx_paged_cache* kv, const vx_b
     *bytes = vx::score_workspace_bytes(b->batch, kv->num_kv_heads, num_q_heads, max_blocks(kv, b));
   } else if (stage == VX_STAGE_DECODE) {
     *bytes = vx::decode_layout(b->batch, kv->num_kv_heads, num_q_heads / kv->num_kv_heads, kv->head_dim_v,
-                               max_sel, is_mla(kv))
+                               max_sel, block_tokens(kv), is_mla(kv), kv->kv_dtype == VX_KV_MXFP4)
                  .total;
   } else {
     return fail(VX_ERR_INVALID_ARG, "unknown stage %d", (int)stage);
@@ -391,7 +394,8 @@ vx_status vx_sparse_paged_decode(const void* q, int32_t num_q_heads, const vx_pa
   vx_status s = check_decode(q, num_q_heads, kv, b, sel_pages, sel_count, max_sel, sm_scale, out);
   if (s != VX_OK) return s;
   const vx::DecodeLayout lay = vx::decode_layout(b->batch, kv->num_kv_heads, num_q_heads / kv->num_kv_heads,
-                                                 kv->head_dim_v, max_sel, is_mla(kv));
+                                                 kv->head_dim_v, max_sel,
+                                                 block_tokens(kv), is_mla(kv), kv->kv_dtype == VX_KV_MXFP4);
   if (!workspace || workspace_bytes < lay.total)
     return fail(VX_ERR_WORKSPACE, "decode workspace needs %zu bytes (got %zu)", lay.total, workspace_bytes);
   return hip_status(vx::launch_decode(geometry(kv, b), static_cast<const uint16_t*>(q), num_q_heads, sel_pages,
@@ -406,7 +410,8 @@ vx_status vx_sparse_paged_decode_noalloc(const void* q, int32_t num_q_heads, con
   vx_status s = check_decode(q, num_q_heads, kv, b, sel_pages, sel_count, max_sel, sm_scale, out);
   if (s != VX_OK) return s;
   const vx::DecodeLayout lay = vx::decode_layout(b->batch, kv->num_kv_heads, num_q_heads / kv->num_kv_heads,
-                                                 kv->head_dim_v, max_sel, is_mla(kv));
+                                                 kv->head_dim_v, max_sel,
+                                                 block_tokens(kv), is_mla(kv), kv->kv_dtype == VX_KV_MXFP4);
   void* scratch = nullptr;
   size_t scratch_bytes = 0;
   if ((s = hip_status(vx::noalloc_scratch(&scratch, &scratch_bytes), "vx_sparse_paged_decode_noalloc")) != VX_OK)

@@ -7,13 +7,13 @@
 namespace vx {
 
 // ---- work plan and workspace of the decode stage -----------------------------------
-// GQA: `splits` workgroups of `waves` waves per (request, KV head) pair, split-major; split s
+// GQA (mxfp4 too): `splits` workgroups of `waves` waves per (request, KV head) pair, split-major; split s
 // covers the selection slots [s*split_slots, (s+1)*split_slots) cut at the pair's count, and
 // splits past the count exit at once.  A pair with one split is written directly; the splits
 // of a split pair merge in the split kernel through the pair's counter.
 // MLA: `splits` workgroups per request over fixed slot ranges, merged by a merge launch.
 // Partials: fp32 output and log2-sum-exp per query head, `splits` rows per pair.
-// Workspace: 512 uint32 split counters (GQA; zero before the first call, every call leaves them
+// Workspace: 1024 uint32 split counters (GQA; zero before the first call, every call leaves them
 // zero), then the partials.
 struct DecodeLayout {
   int32_t splits;             // workgroups (partial rows) per pair
@@ -27,7 +27,7 @@ struct DecodeLayout {
 int device_cus();
 
 DecodeLayout decode_layout(int batch, int num_kv_heads, int group, int head_dim_v, int max_sel,
-                           bool mla);
+                           int block_size, bool mla, bool mx);
 
 // fp32 planes [H][B][stride] of the score stage: max(2 H, Hq + H) of them.  Plane 0 holds the
 // scores (or lower bounds), plane 1 the upper bounds; the NSA and smoothing flows put their
