@@ -441,7 +441,8 @@ typedef struct {
   int32_t block_size;
 } vx_page_pool;
 
-/* Host-only: workspace bytes of vx_page_extend and vx_page_release for a batch. */
+/* Host-only: workspace bytes of vx_page_extend and vx_page_release for a batch.  The buffer holds a
+ * counter: zero-fill it once after allocating it; every call leaves it zero again. */
 vx_status vx_page_workspace_size(int32_t batch, size_t* bytes);
 
 /* A step's tokens get their pages and slots (Sec. 4.1, C = (b, p, I)).  Request i is row rows[i]

@@ -478,9 +478,10 @@ vx_status check_pool(const vx_page_pool* p) {
 }
 
 vx::PagePool pool_of(const vx_page_pool* p) {
+  const int ps_shift = __builtin_ctz((unsigned)p->page_size);
   return vx::PagePool{p->free_pages,     p->free_count, p->table,        p->lens,
-                      p->num_phys_pages, p->table_rows, p->table_stride, p->page_size,
-                      p->block_size > 0 ? p->block_size : p->page_size};
+                      p->num_phys_pages, p->table_rows, p->table_stride, ps_shift,
+                      p->block_size > 0 ? __builtin_ctz((unsigned)p->block_size) : ps_shift};
 }
 
 vx_status check_plan(const vx_page_pool* pool, int32_t batch, const int32_t* rows, const void* ws, size_t ws_bytes) {

@@ -113,8 +113,8 @@ struct PagePool {
   int32_t* free_count;
   int32_t* table;
   int32_t* lens;
-  int num_phys, table_rows, table_stride, ps;
-  int bs;                 // block size (tokens)
+  int num_phys, table_rows, table_stride;
+  int ps_shift, bs_shift; // log2 of the page and block size in tokens
 };
 size_t plan_workspace_bytes(int batch);
 hipError_t launch_page_extend(const PagePool& pool, int batch, const int32_t* rows, const int32_t* new_lens,

@@ -30,11 +30,14 @@ KV_BF16, KV_FP8_E4M3, KV_FP8_E5M2, KV_MXFP4 = 0, 1, 2, 3
 def kv_dtype_code(t: torch.Tensor) -> int:
     """vx_kv_dtype of a cache tensor: bfloat16, float8_e4m3fn (OCP E4M3), float8_e5m2, or uint8 for
     the slices of an mxfp4 cache (mxfp4_cache)."""
-    codes = {torch.bfloat16: KV_BF16, torch.float8_e4m3fn: KV_FP8_E4M3, torch.float8_e5m2: KV_FP8_E5M2,
-             torch.uint8: KV_MXFP4}
-    if t.dtype not in codes:
+    code = _KV_CODES.get(t.dtype)
+    if code is None:
         raise TypeError(f"KV cache dtype {t.dtype} is not bfloat16, float8_e4m3fn, float8_e5m2 or uint8 (mxfp4)")
-    return codes[t.dtype]
+    return code
+
+
+_KV_CODES = {torch.bfloat16: KV_BF16, torch.float8_e4m3fn: KV_FP8_E4M3, torch.float8_e5m2: KV_FP8_E5M2,
+             torch.uint8: KV_MXFP4}
 
 
 def mxfp4_cache(num_pages: int, num_kv_heads: int, page_size: int, head_dim: int, device="cuda") -> torch.Tensor:
@@ -134,9 +137,14 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return t.data_ptr()
 
 
+# The handle of the current stream, without the Stream object (2.7 us of a call's 10).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        stream = torch.cuda.current_stream()
+        return _raw_stream(torch.cuda.current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -228,7 +236,9 @@ class PagePool:
 
     def struct(self) -> _Pool:
         for n in ("free_pages", "free_count", "table", "lens"):
-            _int32(getattr(self, n), n)
+            t = getattr(self, n)
+            if t.dtype != torch.int32 or t.device != self.table.device:
+                raise TypeError(f"{n} must be int32 on {self.table.device} (got {t.dtype} on {t.device})")
         rows, stride = self.table.shape
         if self.lens.numel() != rows:
             raise ValueError(f"lens has {self.lens.numel()} entries for {rows} table rows")
@@ -243,17 +253,24 @@ class PagePool:
         return self._ref
 
 
-def _on_gpu(*tensors) -> None:
-    """The kernels take device addresses of the current GPU: anything else would fault it."""
-    for t in tensors:
-        if t is not None and (t.device.type != "cuda" or t.device.index != torch.cuda.current_device()):
-            raise ValueError(f"tensors must be on the current GPU (got one on {t.device})")
+def _gpu_of(t: torch.Tensor) -> int:
+    """The current GPU, which t has to be on: the kernels take addresses, and another device's or the
+    host's would fault it."""
+    d = t.get_device()
+    if d < 0 or d != torch.cuda.current_device():
+        raise ValueError(f"tensors must be on the current GPU (got one on {t.device})")
+    return d
 
 
-def _int32(t: torch.Tensor, name: str) -> torch.Tensor:
-    if t.dtype != torch.int32:
-        raise TypeError(f"{name} must be int32 (got {t.dtype})")
-    return t
+def _refuse(t: torch.Tensor, dtype: torch.dtype, n: Optional[int], name: str) -> None:
+    """Says what is wrong with an argument that a call's own checks have found unfit."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
+    if n is not None and t.numel() != n:
+        raise ValueError(f"{name} has {t.numel()} entries, {n} are needed")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    raise ValueError(f"tensors must be on the current GPU (got {name} on {t.device})")
 
 
 def page_workspace_size(batch: int) -> int:
@@ -267,54 +284,67 @@ def page_extend(pool: PagePool, rows: torch.Tensor, new_lens: torch.Tensor, batc
                 first_block: Optional[torch.Tensor] = None, stream=None) -> None:
     """Gives request i (row rows[i] of the pool) its new_lens[i] tokens: batch's page_indptr,
     page_indices and seq_lens are written for the lengths with them, and token_indptr, slots
-    (int64), granted and first_block as include/vx.h says."""
-    B = rows.numel()
+    (int64), granted and first_block as include/vx.h says.  workspace: page_workspace_size bytes,
+    zero-filled once."""
+    B, i32, d = rows.numel(), torch.int32, _gpu_of(pool.table)
     for t, n, name in ((rows, B, "rows"), (new_lens, B, "new_lens"), (batch.seq_lens, B, "seq_lens"),
                        (batch.page_indptr, B + 1, "page_indptr"), (token_indptr, B + 1, "token_indptr"),
-                       (granted, B, "granted"), (first_block, B, "first_block")):
-        if t is not None and _int32(t, name).numel() != n:
-            raise ValueError(f"{name} has {t.numel()} entries, {n} are needed")
-    _int32(batch.page_indices, "page_indices")
-    if slots.dtype != torch.int64:
-        raise TypeError(f"slots must be int64 (got {slots.dtype})")
-    _on_gpu(pool.table, pool.free_pages, pool.free_count, pool.lens, rows, new_lens, batch.seq_lens, batch.page_indptr,
-            batch.page_indices, token_indptr, slots, granted, first_block, workspace)
-    _check(lib().vx_page_extend(pool.ref(), B, _ptr(rows), _ptr(new_lens), _ptr(batch.seq_lens), _ptr(batch.page_indptr),
-                                _ptr(batch.page_indices), batch.page_indices.numel(), _ptr(token_indptr), _ptr(slots),
-                                slots.numel(), _ptr(granted), _ptr(first_block), _ptr(workspace),
+                       (granted, B, "granted")):
+        if t.dtype is not i32 or t.numel() != n or t.get_device() != d or not t.is_contiguous():
+            _refuse(t, i32, n, name)
+    first = None
+    if first_block is not None:
+        if first_block.dtype is not i32 or first_block.numel() != B or first_block.get_device() != d:
+            _refuse(first_block, i32, B, "first_block")
+        first = _ptr(first_block)
+    pages = batch.page_indices
+    if pages.dtype is not i32 or pages.get_device() != d:
+        _refuse(pages, i32, None, "page_indices")
+    if slots.dtype is not torch.int64 or slots.get_device() != d:
+        _refuse(slots, torch.int64, None, "slots")
+    if workspace.get_device() != d:
+        _refuse(workspace, workspace.dtype, None, "workspace")
+    _check(lib().vx_page_extend(pool.ref(), B, rows.data_ptr(), new_lens.data_ptr(), batch.seq_lens.data_ptr(),
+                                batch.page_indptr.data_ptr(), _ptr(pages), pages.numel(), token_indptr.data_ptr(),
+                                _ptr(slots), slots.numel(), granted.data_ptr(), first, _ptr(workspace),
                                 workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
 def page_release(pool: PagePool, rows: torch.Tensor, keep_lens: Optional[torch.Tensor], workspace: torch.Tensor,
                  stream=None) -> None:
     """Row rows[i] keeps its first keep_lens[i] tokens (None: none) and gives its other pages back."""
-    B = _int32(rows, "rows").numel()
-    if keep_lens is not None and _int32(keep_lens, "keep_lens").numel() != B:
-        raise ValueError(f"keep_lens has {keep_lens.numel()} entries, {B} are needed")
-    _on_gpu(pool.table, pool.free_pages, pool.free_count, pool.lens, rows, keep_lens, workspace)
+    B, i32, d = rows.numel(), torch.int32, _gpu_of(pool.table)
+    if rows.dtype is not i32 or rows.get_device() != d:
+        _refuse(rows, i32, B, "rows")
+    if keep_lens is not None and (keep_lens.dtype is not i32 or keep_lens.numel() != B or keep_lens.get_device() != d):
+        _refuse(keep_lens, i32, B, "keep_lens")
+    if workspace.get_device() != d:
+        _refuse(workspace, workspace.dtype, None, "workspace")
     _check(lib().vx_page_release(pool.ref(), B, _ptr(rows), _ptr(keep_lens), _ptr(workspace),
                                  workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
-def _row_args(kv: PagedKV, t: Optional[torch.Tensor], n: int, dim: int, name: str):
-    """Address and strides of rows [n][H][dim], bf16, channels side by side."""
+def _row_args(t: Optional[torch.Tensor], n: int, heads: int, dim: int, d: int, name: str):
+    """Address and strides of rows [n][heads][dim], bf16, channels side by side."""
     if t is None:
         return None, 0, 0
-    if t.dtype != torch.bfloat16:
-        raise TypeError(f"{name} must be bfloat16 (got {t.dtype})")
-    if tuple(t.shape) != (n, kv.k.shape[1], dim) or (t.numel() > 0 and t.stride(2) != 1):
-        raise ValueError(f"{name} must be [{n}][{kv.k.shape[1]}][{dim}] with contiguous channels (got {tuple(t.shape)}, "
-                         f"strides {tuple(t.stride())})")
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    if t.dtype is not torch.bfloat16 or t.get_device() != d:
+        _refuse(t, torch.bfloat16, None, name)
+    stride = t.stride()
+    if t.shape != (n, heads, dim) or (n > 0 and stride[2] != 1):
+        raise ValueError(f"{name} must be [{n}][{heads}][{dim}] with contiguous channels (got {tuple(t.shape)}, "
+                         f"strides {stride})")
+    return t.data_ptr(), stride[0], stride[1]
 
 
 def _kv_rows(fn, kv: PagedKV, slots: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor], names, stream) -> None:
-    if slots.dtype != torch.int64:
-        raise TypeError(f"slots must be int64 (got {slots.dtype})")
-    n, c = slots.numel(), kv.ref()
-    rows = (*_row_args(kv, k, n, kv._st.head_dim_qk, names[0]), *_row_args(kv, v, n, kv._st.head_dim_v, names[1]))
-    _on_gpu(kv.k, kv.v, slots, k, v)
-    _check(fn(c, *rows, _ptr(slots), n, _stream(stream)))
+    d, c = _gpu_of(kv.k), kv.ref()
+    if slots.dtype is not torch.int64 or slots.get_device() != d:
+        _refuse(slots, torch.int64, None, "slots")
+    n, st = slots.numel(), kv._st
+    k_args = _row_args(k, n, st.num_kv_heads, st.head_dim_qk, d, names[0])
+    v_args = _row_args(v, n, st.num_kv_heads, st.head_dim_v, d, names[1])
+    _check(fn(c, *k_args, *v_args, _ptr(slots), n, _stream(stream)))
 
 
 def kv_write(kv: PagedKV, k_new: torch.Tensor, v_new: Optional[torch.Tensor], slots: torch.Tensor, stream=None) -> None:

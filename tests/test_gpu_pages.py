@@ -33,7 +33,7 @@ class Rig:
         new = lambda n, t=torch.int32: torch.full((n,), -77, dtype=t, device="cuda")  # noqa: E731
         self.batch = vx.BatchSpec(new(B + 1), new(self.page_cap), new(B), stride)
         self.tokens, self.slots, self.granted, self.first = new(B + 1), new(slot_cap, torch.int64), new(B), new(B)
-        self.ws = new(vx.page_workspace_size(B) // 4)
+        self.ws = torch.zeros(vx.page_workspace_size(B), dtype=torch.uint8, device="cuda")
         self.gpu_rows = gpu(self.rows)
 
     def extend(self, new):
@@ -200,3 +200,16 @@ def test_on_a_stream_of_its_own():
     with torch.cuda.stream(torch.cuda.Stream()):
         rig.extend(np.full(20, 3))
         rig.release(np.zeros(20, np.int64))
+
+
+def test_the_largest_batch():
+    """65535 requests (256 a workgroup), with and without a shortage."""
+    rng = np.random.default_rng(6)
+    B, lens = 65535, rng.integers(0, 40, size=65535)
+    held = int((-(-lens // 16)).sum())
+    rig = Rig(B, held + 30000, 4, 16, rng, lens, slot_cap=200000)
+    rig.extend(rng.integers(0, 5, size=B))
+    rig.extend(rng.integers(0, 30, size=B) * (rng.random(B) < 0.2))
+    rig.extend(np.full(B, 3))                      # the pool runs short on the way
+    assert 0 < int((rig.granted == 0).sum()) < B
+    rig.release(lens)
