@@ -12,10 +12,10 @@
 // stack, page.  Every workgroup sums all the requests itself (12 bytes each, from L2), places a range
 // of at most kPlanRange of them and moves their pages.  The lengths and the free count, which every
 // workgroup reads, change only after the last one has read them: a counter in the workspace tells,
-// and that last workgroup writes them.  Extend and release, 64 requests of 8192 to 32768 tokens: 8.4 and
-// 5.7 us (with the sums in a launch of one workgroup before the move 9.0 and 4.2 us, and two more
+// and that last workgroup writes them.  Extend and release, 64 requests of 8192 to 32768 tokens: 6.8 and
+// 5.2 us (with the sums in a launch of one workgroup before the move 9.0 and 4.2 us, and two more
 // launches of 2.4 us each for the host); 4096 requests, 2 million page entries and 1.2 million slots:
-// 28 and 16 us (74 and 21 us; with four times the workgroups 70 and 21, since each sums all requests).
+// 27 and 15 us (74 and 21 us; with four times the workgroups 70 and 21, since each sums all requests).
 #include <algorithm>
 #include <climits>
 
@@ -30,6 +30,7 @@ constexpr int kPlanWaves = kPlanThreads / kWave;
 constexpr int kPlanRanges = 256;      // ranges of requests (one per CU)
 constexpr int kPlanRange = 256;       // most requests of a range: a batch has at most 65535
 constexpr int kPlanWgs = 256;        // most workgroups
+constexpr int kLaneAsks = kPlanRange / kWave;
 constexpr int kLanePages = 4;         // pages (or tokens) a lane moves per turn
 constexpr int kTurn = kWave * kLanePages;
 
@@ -121,12 +122,6 @@ __device__ __forceinline__ Back back_with(const PagePool& P, int row, int len, i
   q.first = min((int)pages_of(q.keep, P.ps_shift), q.last);
   return q;
 }
-__device__ __forceinline__ Back back_of(const ReleaseArgs& a, int j) {
-  const int row = row_of(a.rows, a.batch, a.pool, j);
-  const int keep = a.keep_lens ? a.keep_lens[min(j, a.batch - 1)] : 0;
-  return back_with(a.pool, row, a.pool.lens[max(row, 0)], keep);
-}
-
 template <class F>
 __device__ __forceinline__ void each_back(const ReleaseArgs& a, F f) {
   for (int j0 = (int)threadIdx.x; j0 < a.batch; j0 += kAsks * kPlanThreads) {
@@ -144,76 +139,75 @@ __device__ __forceinline__ void each_back(const ReleaseArgs& a, F f) {
   }
 }
 
-template <int N>
-using GroupLds = int64_t[N][kPlanWaves];
+// Inclusive sums over the wave's lanes (DPP row shifts, then the rows' ends to the rows above).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t dpp_add(int64_t x) {
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, ROWS, 0xf, false);
+  const int hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)((uint64_t)x >> 32), CTRL, ROWS, 0xf, false);
+  return x + (int64_t)(((uint64_t)(uint32_t)hi << 32) | (uint32_t)lo);
+}
+__device__ __forceinline__ int64_t wave_scan(int64_t x) {
+  x = dpp_add<0x111, 0xf>(x);         // row_shr 1, 2, 4, 8
+  x = dpp_add<0x112, 0xf>(x);
+  x = dpp_add<0x114, 0xf>(x);
+  x = dpp_add<0x118, 0xf>(x);
+  x = dpp_add<0x142, 0xa>(x);         // row_bcast 15 into rows 1 and 3
+  return dpp_add<0x143, 0xc>(x);      // row_bcast 31 into rows 2 and 3
+}
 
-// Sums over the workgroup, in every thread.
+// The waves' sums of N values, in LDS; a barrier, then group_total.
 template <int N>
-__device__ __forceinline__ void group_sum(int64_t (&x)[N], GroupLds<N>& lds) {
+using WaveSums = int64_t[N][kPlanWaves];
+template <int N>
+__device__ __forceinline__ void put_wave_sums(const int64_t (&x)[N], WaveSums<N>& lds) {
 #pragma unroll
   for (int v = 0; v < N; v++) {
-#pragma unroll
-    for (int d = kWave / 2; d > 0; d >>= 1) x[v] += __shfl_xor(x[v], d, kWave);
-    if (lane_id() == 0) lds[v][threadIdx.x >> 6] = x[v];
+    const int64_t y = wave_scan(x[v]);
+    if (lane_id() == kWave - 1) lds[v][threadIdx.x >> 6] = y;
   }
-  __syncthreads();
+}
+template <int N>
+__device__ __forceinline__ void group_total(int64_t (&x)[N], const WaveSums<N>& lds) {
 #pragma unroll
   for (int v = 0; v < N; v++) {
     x[v] = 0;
 #pragma unroll
     for (int k = 0; k < kPlanWaves; k++) x[v] += lds[v][k];
   }
-  __syncthreads();
-}
-
-// Inclusive sums over the threads before and with this one; total: over all.
-template <int N>
-__device__ __forceinline__ void group_scan(int64_t (&x)[N], int64_t (&total)[N], GroupLds<N>& lds) {
-  const int w = (int)threadIdx.x >> 6;
-#pragma unroll
-  for (int v = 0; v < N; v++) {
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-      const int64_t y = __shfl_up(x[v], d, kWave);
-      if (lane_id() >= d) x[v] += y;
-    }
-    if (lane_id() == kWave - 1) lds[v][w] = x[v];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int v = 0; v < N; v++) {
-    total[v] = 0;
-#pragma unroll
-    for (int k = 0; k < kPlanWaves; k++) {
-      if (k < w) x[v] += lds[v][k];
-      total[v] += lds[v][k];
-    }
-  }
-  __syncthreads();
 }
 
 // The needs in order, when they sum to more than the c free pages: the largest sum <= c, and the sum
-// before request r0.  COMMIT writes the granted lengths on the way.
+// before request r0.  COMMIT writes the granted lengths on the way.  Every thread of the workgroup.
+struct ShortLds {
+  WaveSums<1> sums;
+  int64_t taken, before;
+};
 template <bool COMMIT>
-__device__ __forceinline__ void short_pool(const ExtendArgs& a, int64_t c, int r0, GroupLds<1>& lds, int64_t& taken_lds,
-                                           int64_t& taken, int64_t& before_r0) {
+__device__ __forceinline__ void short_pool(const ExtendArgs& a, int64_t c, int r0, ShortLds& lds, int64_t& taken,
+                                           int64_t& before_r0) {
   int64_t carry = 0;
-  if (threadIdx.x == 0) taken_lds = 0;
+  if (threadIdx.x == 0) lds.taken = 0;
   for (int j0 = 0; j0 < a.batch; j0 += kPlanThreads) {
-    const int j = j0 + (int)threadIdx.x;
+    const int j = j0 + (int)threadIdx.x, w = (int)threadIdx.x >> 6;
     const Ask q = ask_of(a, j);
-    int64_t x[1] = {q.need}, total[1];
-    group_scan<1>(x, total, lds);
-    const int64_t cum = carry + x[0];
+    const int64_t mine = wave_scan(q.need);
+    __syncthreads();
+    if (lane_id() == kWave - 1) lds.sums[0][w] = mine;
+    __syncthreads();
+    int64_t cum = carry + mine;
+    for (int k = 0; k < kPlanWaves; k++) {
+      if (k < w) cum += lds.sums[0][k];
+      carry += lds.sums[0][k];
+    }
     const uint64_t below = __ballot(cum <= c);             // the wave's first lanes: the sums never fall
     if (below != 0 && lane_id() == 63 - __clzll(below))
-      atomicMax(reinterpret_cast<unsigned long long*>(&taken_lds), (unsigned long long)cum);
+      atomicMax(reinterpret_cast<unsigned long long*>(&lds.taken), (unsigned long long)cum);
     if (COMMIT && q.fits && (q.need == 0 || cum <= c)) a.pool.lens[q.row] = q.L + q.n;
-    if (r0 >= j0 && r0 < j0 + kPlanThreads && j == r0) before_r0 = cum - q.need;
-    carry += total[0];
+    if (j == r0) lds.before = cum - q.need;
   }
   __syncthreads();
-  taken = taken_lds;
+  taken = lds.taken;
+  before_r0 = lds.before;
   __syncthreads();
 }
 
@@ -223,24 +217,22 @@ struct Placed {
   int64_t start, token;               // its page list's and its tokens' first entries
 };
 
-// Whether this workgroup is the last of the launch to get here (thread 0 alone knows); the counter wraps
-// back to zero.  What any of its threads has read before is in registers: each waits for its loads
-// ahead of the barrier.
+// A thread's loads have arrived: ahead of the barrier behind which arrive() says so.
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+
+// Whether this workgroup is the last of the launch to get here; the counter wraps back to zero.  One
+// thread, behind a barrier that every thread has reached with its loads (wait_loads).
 __device__ __forceinline__ uint32_t arrive(uint32_t* ctr) {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-  __syncthreads();
-  if (threadIdx.x != 0) return 0;
   const uint32_t wgs = gridDim.x * gridDim.y;
   return __builtin_amdgcn_atomic_inc32(ctr, wgs - 1, __ATOMIC_RELAXED, "agent") == wgs - 1;
 }
 
 // Grid (pieces, ranges): the pieces of a range share out its pages and tokens.
 __global__ __launch_bounds__(kPlanThreads) void extend_kernel(const ExtendArgs a) {
-  __shared__ GroupLds<5> sums;
-  __shared__ GroupLds<1> scan1;
-  __shared__ GroupLds<3> scan3;
+  __shared__ WaveSums<5> sums;
+  __shared__ ShortLds short_lds;
+  __shared__ Ask asks[kPlanRange];
   __shared__ Placed placed[kPlanRange];
-  __shared__ int64_t taken_lds, before_lds;
   __shared__ uint32_t last;
   const PagePool& P = a.pool;
   const int tid = (int)threadIdx.x;
@@ -256,42 +248,57 @@ __global__ __launch_bounds__(kPlanThreads) void extend_kernel(const ExtendArgs a
       s[2] += q.need;
       s[3] += q.held;
       s[4] += q.n;
+    } else if (j < r0 + nr) {
+      asks[j - r0] = q;
     }
   });
-  const Ask q = ask_of(a, tid < nr ? r0 + tid : a.batch);
-  group_sum<5>(s, sums);
+  put_wave_sums<5>(s, sums);
+  wait_loads();
+  __syncthreads();
+  group_total<5>(s, sums);
   const bool shortage = s[0] > c;     // uniform
   int64_t taken = s[0], before_r0 = s[2];
-  if (shortage) {
-    short_pool<false>(a, c, r0, scan1, taken_lds, taken, before_r0);
-    if (tid == r0 % kPlanThreads) before_lds = before_r0;
-    __syncthreads();
-    before_r0 = before_lds;
-  }
-  const uint32_t am_last = arrive(a.ctr);   // no more reads of the lengths or the free count from here
-  if (tid == 0) last = am_last;
+  if (shortage) short_pool<false>(a, c, r0, short_lds, taken, before_r0);
+  // no more reads of the lengths or the free count from here
+  if (tid == 0) last = arrive(a.ctr);
 
-  {
-    int64_t x[3] = {q.need, q.held, q.n}, total[3];
-    group_scan<3>(x, total, scan3);
-    const int64_t cum = before_r0 + x[0], before = cum - q.need;
-    const bool ok = q.fits && (q.need == 0 || cum <= c);
+  // the first wave places the range, kLaneAsks consecutive requests a lane
+  if (tid < kWave) {
+    Ask q[kLaneAsks];
+    int64_t need = 0, held = 0, n = 0;
+#pragma unroll
+    for (int b = 0; b < kLaneAsks; b++) {
+      const int k = tid * kLaneAsks + b;
+      if (k < nr) q[b] = asks[k];
+      else q[b] = Ask{-1, 0, 0, 0, 0, false};
+      need += q[b].need;
+      held += q[b].held;
+      n += q[b].n;
+    }
+    int64_t cum = before_r0 + wave_scan(need) - need;
+    int64_t lists = s[3] + wave_scan(held) - held, token = s[4] + wave_scan(n) - n;
     auto granted_before = [&](int64_t sum) { return sum <= c ? sum : taken; };
-    if (tid < nr) {
-      const int i = r0 + tid, got = ok ? q.n : 0;
-      const Placed p{q.row, q.L, q.n, q.L + got, ok ? (int)before : -1, s[3] + x[1] - q.held + granted_before(before),
-                     s[4] + x[2] - q.n};
-      placed[tid] = p;
-      if (piece == 0) {
-        a.page_indptr[i] = (int)min(p.start, (int64_t)a.page_cap);
-        a.token_indptr[i] = (int)min(p.token, (int64_t)INT_MAX);
-        a.seq_lens[i] = p.now;
-        a.granted[i] = got;
-        if (a.first_block) a.first_block[i] = q.L >> P.bs_shift;
-        if (i == a.batch - 1) {
-          a.page_indptr[a.batch] = (int)min(s[3] + x[1] + granted_before(cum), (int64_t)a.page_cap);
-          a.token_indptr[a.batch] = (int)min(s[4] + x[2], (int64_t)INT_MAX);
-        }
+#pragma unroll
+    for (int b = 0; b < kLaneAsks; b++) {
+      const int k = tid * kLaneAsks + b, i = r0 + k;
+      if (k >= nr) break;
+      const int64_t before = cum;
+      cum += q[b].need;
+      const bool ok = q[b].fits && (q[b].need == 0 || cum <= c);
+      const int got = ok ? q[b].n : 0;
+      const Placed p{q[b].row, q[b].L, q[b].n, q[b].L + got, ok ? (int)before : -1, lists + granted_before(before), token};
+      placed[k] = p;
+      lists += q[b].held;
+      token += q[b].n;
+      if (piece != 0) continue;
+      a.page_indptr[i] = (int)min(p.start, (int64_t)a.page_cap);
+      a.token_indptr[i] = (int)min(p.token, (int64_t)INT_MAX);
+      a.seq_lens[i] = p.now;
+      a.granted[i] = got;
+      if (a.first_block) a.first_block[i] = q[b].L >> P.bs_shift;
+      if (i == a.batch - 1) {
+        a.page_indptr[a.batch] = (int)min(lists + granted_before(cum), (int64_t)a.page_cap);
+        a.token_indptr[a.batch] = (int)min(token, (int64_t)INT_MAX);
       }
     }
   }
@@ -346,7 +353,7 @@ __global__ __launch_bounds__(kPlanThreads) void extend_kernel(const ExtendArgs a
   if (!last) return;
   if (shortage) {
     int64_t ignored;
-    short_pool<true>(a, c, -1, scan1, taken_lds, taken, ignored);
+    short_pool<true>(a, c, 0, short_lds, taken, ignored);
   } else {
     each_ask(a, [&](int, const Ask& w) {
       if (w.fits) P.lens[w.row] = w.L + w.n;
@@ -356,8 +363,7 @@ __global__ __launch_bounds__(kPlanThreads) void extend_kernel(const ExtendArgs a
 }
 
 __global__ __launch_bounds__(kPlanThreads) void release_kernel(const ReleaseArgs a) {
-  __shared__ GroupLds<2> sums;
-  __shared__ GroupLds<1> scan1;
+  __shared__ WaveSums<2> sums;
   __shared__ Back back[kPlanRange];
   __shared__ int64_t base[kPlanRange];
   __shared__ uint32_t last;
@@ -370,16 +376,28 @@ __global__ __launch_bounds__(kPlanThreads) void release_kernel(const ReleaseArgs
   each_back(a, [&](int j, const Back& q) {
     s[0] += q.last - q.first;
     if (j < r0) s[1] += q.last - q.first;
+    else if (j < r0 + nr) back[j - r0] = q;
   });
-  const Back q = back_of(a, tid < nr ? r0 + tid : a.batch);
-  group_sum<2>(s, sums);
-  const uint32_t am_last = arrive(a.ctr);
-  if (tid == 0) last = am_last;
-  int64_t x[1] = {q.last - q.first}, total[1];
-  group_scan<1>(x, total, scan1);
-  if (tid < nr) {
-    back[tid] = q;
-    base[tid] = s[1] + x[0] - (q.last - q.first);
+  put_wave_sums<2>(s, sums);
+  wait_loads();
+  __syncthreads();
+  group_total<2>(s, sums);
+  if (tid == 0) last = arrive(a.ctr);
+  if (tid < kWave) {
+    int64_t sum = 0;
+#pragma unroll
+    for (int b = 0; b < kLaneAsks; b++) {
+      const int k = tid * kLaneAsks + b;
+      sum += k < nr ? back[k].last - back[k].first : 0;
+    }
+    int64_t at = s[1] + wave_scan(sum) - sum;
+#pragma unroll
+    for (int b = 0; b < kLaneAsks; b++) {
+      const int k = tid * kLaneAsks + b;
+      if (k >= nr) break;
+      base[k] = at;
+      at += back[k].last - back[k].first;
+    }
   }
   __syncthreads();
   // a stack that is full (pages given back twice) drops the pages that do not fit

@@ -12,6 +12,11 @@
 // 16k to 32k tokens on pages of 16, Mean and its bf16 copy (969 MB), 205 -> 189 us; 16 prompts of 131072
 // tokens on pages of 32, Max and Min (4.6 GB), 967 -> 820 us.  (Of the first 16 us: wider batches and
 // non-temporal loads 10, stores 6; with four rounds of tasks per workgroup 193 us, with sixteen 212.)
+// mxfp4 caches: a task loads 4 bytes of codes and its group's scale byte per token, and the values are
+// exact.  16 prompts of 16384 to 32768 tokens, 8 KV heads of 128, pages of 16, Mean with its bf16 copy:
+// 80 us, 4.5 TB/s, the rate of a large copy (4.7).  16 channels a task (121 us: its stores of a Mean
+// leave lines half written), and tiles copied to LDS in 16-byte loads (77 to 91 us, the envelope 83
+// instead of 70) were no better.
 // fp8 caches: each code is converted exactly to fp32 and multiplied by the K scale (one fp32
 // rounding), which is the cache value the summaries are taken over.
 //
@@ -129,6 +134,7 @@ hipError_t launch_summarize(const Geometry& g, const int32_t* first_page, float*
     // 173.0, envelope 184.2 / 182.9, Mean 189.6 / 193.0; 128 (16 of 4k to 64k, lognormal) E4M3 Mean 120.7 /
     // 107.5, bf16 Max 153.9 / 149.3, Mean 162.4 / 164.6; 32 (32 of 1k to 8k, lognormal) E4M3 Mean 38.9 / 39.7,
     // bf16 Max 48.0 / 49.5; 16 (64 of 256 to 2048) 30.6 / 34.7, 35.0 / 39.2.  Blocks of 64, E4M3 89.0 / 93.9.
+    // mxfp4, 64 workgroups per CU: Mean with its bf16 copy 83.0 / 80.2, envelope 75.7 / 69.7.
     const int ppb1 = tasks_per_page >= kThreads ? 1 : kThreads / tasks_per_page;
     const long long wgs = ((long long)g.max_pages + ppb1 - 1) / ppb1 * g.batch;
     const bool two = g.bs <= 16 && (g.kv_dtype != kKvBf16 || (!mean && !mean_bf)) && wgs >= 48LL * device_cus();
