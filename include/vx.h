@@ -312,8 +312,8 @@ vx_status vx_page_score_topk(const void* q, int32_t num_q_heads,
  * score launch reads that block's summary from before the append, and only that block's
  * (unused) score depends on it.  The append's workgroups are their own, ahead of the selection's
  * in the launch.  With n_local == 0, NSA or MEAN_DOT_SMOOTH (whose flows couple the blocks), an
- * approximate selection (opt) or more than 16384 blocks per request, the call appends first and
- * then selects, in three launches.
+ * approximate selection (opt), more than 16384 blocks per request or an mxfp4 cache, the call
+ * appends first and then selects, in three launches.
  * Arguments and requirements are those of the two calls (mean, mean_bf16, max and min are
  * written by the append and read by the selection; seq_lens counts the new token, so every
  * request has L_i >= 1; a request with L_i = 0, or whose token L_i - 1 lies past its page

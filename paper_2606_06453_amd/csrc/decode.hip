@@ -40,6 +40,7 @@
 //                only when S > 1.
 #include <algorithm>
 #include <climits>
+#include <cmath>
 #include <mutex>
 #include <type_traits>
 
@@ -1024,6 +1025,12 @@ DecodeLayout decode_layout(int batch, int num_kv_heads, int group, int head_dim_
     long long S = pairs > 0 ? (cus + pairs - 1) / pairs : 1;
     S = std::min(S, (ms + kDecodeWaves - 1) / kDecodeWaves);
     if (pairs > 0 && pairs < resident) S = std::max(S, std::min(3 * resident / pairs, ms * block_size / kMxSplitTokens));
+    // Every split adds to the merge of its pair (group * channels / 4 threads of a workgroup take 8 of
+    // them a round trip) and takes from the stream of each: the sum is least at the square root.  One
+    // request of 8 KV heads, 4 query heads each, 2048 tokens: 8 to 16 splits 7.7 us, 32 9.9; 32768 tokens: 16
+    // 18.7, 32 15.3, 64 17.0; one KV head, 8 query heads, 131072 tokens: 32 30.6, 64 21.6, 128 21.0, 256 27.9;
+    // one query head of 64 channels, 32000 tokens: 32 10.8, 64 8.8, 128 8.3, 256 10.3.
+    S = std::min(S, (long long)std::sqrt((double)ms * block_size * 32 / (group * head_dim_v)));
     S = std::max(S, 1LL);
     const long long T = (ms + S - 1) / S;
     S = (ms + T - 1) / T;

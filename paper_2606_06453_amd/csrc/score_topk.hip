@@ -2763,7 +2763,8 @@ hipError_t launch_score_topk(const Geometry& g, const uint16_t* q, int Hq, int k
   const bool wave = !approx && !mean_two_pass && !env_two_pass && g.max_pages <= kWaveMaxPages;
   // The step's append: workgroups of its own inside the selection launch, or a launch ahead of
   // everything when the selection reads every block's score (the flows couple the pages; the
-  // radix path is not fused).
+  // radix path is not fused).  An mxfp4 append, which quantises its rows, is a launch ahead too: inside,
+  // it takes every selection kernel of the bins from 75 registers to 80 and spills for all cache types.
   AppendStep ap{};
   if (sa.k_new) {
     if (approx || g.max_pages > kTwoPassMaxPages || flow || g.kv_dtype == kKvMxFp4) {

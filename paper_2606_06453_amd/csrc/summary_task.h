@@ -145,7 +145,7 @@ __device__ __forceinline__ void task(const void* __restrict__ kv, float k_scale,
     static_assert(!APPEND || TS == 4, "a group's tasks are 4 lanes apart");
     const int64_t in = (((int64_t)i * H + h) * D + c8 * 8) * 2;
     const uint4 k16 = *reinterpret_cast<const uint4*>(static_cast<const char*>(app.knew) + in);
-    const uint4 v16 = *reinterpret_cast<const uint4*>(static_cast<const char*>(app.vnew) + in);
+    const uint4 v16 = app.vnew ? *reinterpret_cast<const uint4*>(static_cast<const char*>(app.vnew) + in) : uint4{};
     new_row.e = mx::group_scale(group_max(mx::amax_bits(k16)));
     new_row.codes = mx::encode8(k16, new_row.e);
     new_v.e = mx::group_scale(group_max(mx::amax_bits(v16)));
@@ -204,10 +204,10 @@ __device__ __forceinline__ void task(const void* __restrict__ kv, float k_scale,
         uint8_t* ks = static_cast<uint8_t*>(app.kw) + mxs;
         uint8_t* vs = static_cast<uint8_t*>(app.vw) + mxs;
         *reinterpret_cast<uint32_t*>(ks + mx::k_code(t, c8, D)) = new_row.codes;
-        mx::put_v_codes(vs, t, c8, D, new_v.codes);
-        if ((c8 & 3) == 0) {
-          ks[sc + mx::k_scale(t, c8 >> 2, D)] = (uint8_t)new_row.e;
-          vs[sc + mx::v_scale(t, c8 >> 2, D)] = (uint8_t)new_v.e;
+        if ((c8 & 3) == 0) ks[sc + mx::k_scale(t, c8 >> 2, D)] = (uint8_t)new_row.e;
+        if (app.vnew) {
+          mx::put_v_codes(vs, t, c8, D, new_v.codes);
+          if ((c8 & 3) == 0) vs[sc + mx::v_scale(t, c8 >> 2, D)] = (uint8_t)new_v.e;
         }
       }
     } else if (writer) {

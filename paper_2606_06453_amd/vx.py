@@ -167,7 +167,8 @@ class PagedKV:
         if self.v is not None and kv_dtype_code(self.v) != dt:
             raise TypeError("K and V caches must have the same dtype")
         if dt == KV_MXFP4:
-            Dqk, Dv = self._mx_dim(Dqk), self._mx_dim(Dv) if self.v is not None else Dv
+            Dqk = self._mx_dim(Dqk)
+            Dv = self._mx_dim(Dv) if self.v is not None else (self.head_dim_v or Dqk)
         return _Cache(_ptr(self.k), _ptr(self.v), P, H, ps, Dqk, Dv, dt, float(self.k_scale), float(self.v_scale),
                       int(self.block_size))
 

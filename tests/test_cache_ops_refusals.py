@@ -128,3 +128,8 @@ def test_the_binding_checks_types_and_places():
             vx.kv_write(kv, k, rows, s)
         with pytest.raises((TypeError, ValueError)):
             vx.kv_read(kv, s, k, rows)
+
+
+def test_keys_alone():
+    kv = vx.PagedKV(vx.mxfp4_cache(3, 2, 16, 64, "cpu"), None)
+    assert (kv.struct().head_dim_qk, kv.struct().head_dim_v) == (64, 64)

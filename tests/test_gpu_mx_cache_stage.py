@@ -206,3 +206,74 @@ def test_a_batch_that_grows_and_ends(block, kind):
     vx.page_release(pool, rows_of, None, ws)
     torch.cuda.synchronize()
     assert int(pool.free_count) == P and sorted(pool.free_pages.tolist()) == list(range(P))
+
+
+@pytest.mark.parametrize("D,ps", [(128, 16), (64, 64)])
+def test_an_append_to_keys_alone(D, ps):
+    """A cache of keys without values (the selection's side alone) takes k_new and no v_new."""
+    H, lens = 2, [ps + 3, 1]
+    kc, _ = _cache(3, H, ps, D, 9)
+    batch = vx.BatchSpec(_gpu([0, 2, 3]), _gpu([2, 0, 1]), _gpu(lens), 2)
+    row = torch.randn((2, H, D), generator=torch.Generator().manual_seed(2)).to(torch.bfloat16)
+    k = torch.from_numpy(kc).cuda()
+    mean = torch.zeros((3, H, D), device="cuda")
+    vx.kv_append_summarize(vx.PagedKV(k, None), batch, row.cuda(), None, mean=mean)
+    torch.cuda.synchronize()
+    want = _mx.unpack(kc, "k")
+    for i, (page, t) in enumerate(((0, 2), (1, 0))):
+        want[page, :, t] = _mx.values(*_mx.quantize(row[i].double().numpy()))
+    got = _mx.unpack(k.cpu().numpy(), "k")
+    assert np.array_equal(got, want)
+    bound = 4 * 2.0 ** -24 * np.abs(want).max()                    # at most three additions and a division
+    assert np.abs(mean[0].cpu().double().numpy() - want[0, :, :3].mean(1)).max() <= bound
+
+
+def test_a_captured_step_of_a_growing_batch():
+    """A serving step, pages for the new tokens, append, selection and attention, captured once and replayed
+    over more than one page of growth, against the same steps launched one by one."""
+    H, g, D, ps, B, stride, P = 4, 4, 128, 16, 6, 30, 150
+    rng = np.random.default_rng(21)
+    lens = rng.integers(100, 300, size=B)
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32, device="cuda")  # noqa: E731
+    prompt = torch.from_numpy(rng.normal(size=(2, int(lens.sum()), H, D))).to(torch.bfloat16).cuda()
+
+    def rig():
+        r = type("Rig", (), {})()
+        r.pool, r.batch = vx.PagePool.empty(P, B, stride, ps), vx.BatchSpec(i32(B + 1), i32(P), i32(B), stride)
+        r.kv = vx.PagedKV(vx.mxfp4_cache(P, H, ps, D), vx.mxfp4_cache(P, H, ps, D))
+        r.dec = SparseDecoder(r.kv, r.batch, H * g, vx.MEAN_DOT, 1, 2, 8, D ** -0.5)
+        r.dec.mean.zero_()                                         # rows of free pages, which nothing writes
+        r.rows, r.tokens, r.granted = _gpu(np.arange(B)), i32(B + 1), i32(B)
+        r.slots, r.ws = torch.zeros(int(lens.sum()), dtype=torch.int64, device="cuda"), i32(vx.page_workspace_size(B) // 4)
+        r.one, r.budget = _gpu([1] * B), _gpu([8] * B)
+        r.q, r.new = (torch.zeros((*n, D), dtype=torch.bfloat16, device="cuda") for n in ((B, H * g), (2, B, H)))
+        vx.page_extend(r.pool, r.rows, _gpu(lens), r.batch, r.tokens, r.slots, r.granted, r.ws)
+        vx.kv_write(r.kv, prompt[0], prompt[1], r.slots)
+        r.dec.summarize()
+
+        def step():
+            vx.page_extend(r.pool, r.rows, r.one, r.batch, r.tokens, r.slots, r.granted, r.ws)
+            return r.dec.step(r.q, r.budget, None, kv_new=(r.new[0], r.new[1]))
+        r.step = step
+        return r
+
+    eager, graphed = rig(), rig()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        graphed.step()
+    torch.cuda.synchronize()
+    for n in range(20):
+        q = torch.from_numpy(rng.normal(size=(B, H * g, D))).to(torch.bfloat16).cuda()
+        new = torch.from_numpy(rng.normal(size=(2, B, H, D))).to(torch.bfloat16).cuda()
+        for r in (eager, graphed):
+            r.q.copy_(q)
+            r.new.copy_(new)
+        want = eager.step().clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(graphed.dec.out.view(torch.int16), want.view(torch.int16)), n
+        for a, b in ((eager.kv.k, graphed.kv.k), (eager.kv.v, graphed.kv.v), (eager.batch.seq_lens, graphed.batch.seq_lens),
+                     (eager.pool.table, graphed.pool.table), (eager.slots, graphed.slots), (eager.dec.mean, graphed.dec.mean)):
+            assert torch.equal(a, b), n
+    assert eager.batch.seq_lens.tolist() == (lens + 20).tolist()

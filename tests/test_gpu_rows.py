@@ -159,3 +159,21 @@ def test_slots_past_two_gigabytes():
     want = torch.from_numpy(_mx.values(*_mx.quantize(x.double().numpy()))).to(torch.bfloat16)
     assert torch.equal(out[0].cpu(), want) and torch.equal(out[1].cpu(), -want)
     assert int(k.view(-1).view(torch.int64).ne(0).sum()) <= 5 * H * (D // 16 + 4)      # and nothing wrapped to other pages
+
+
+def test_rows_that_do_not_fit_are_refused():
+    kv = vx.PagedKV(vx.mxfp4_cache(3, 2, 16, 64), vx.mxfp4_cache(3, 2, 16, 64))
+    rows, slots = torch.zeros((5, 2, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros(5, dtype=torch.int64, device="cuda")
+    odd = torch.zeros((5, 2, 72), dtype=torch.bfloat16, device="cuda")[..., 1:65]                # not 16-byte aligned
+    for k, s, error in ((rows.float(), slots, TypeError), (rows[:4], slots, ValueError), (rows[..., :32], slots, ValueError),
+                        (rows, slots.int(), TypeError), (rows.cpu(), slots, ValueError), (rows, slots.cpu(), ValueError),
+                        (rows.transpose(1, 2).contiguous().transpose(1, 2), slots, ValueError), (odd, slots, vx.VxError)):
+        with pytest.raises(error):
+            vx.kv_write(kv, k, rows, s)
+        with pytest.raises(error):
+            vx.kv_read(kv, s, rows, k)
+    vx.kv_write(kv, rows[:0], rows[:0], slots[:0])                                               # nothing to do
+    wide = vx.PagedKV(torch.zeros((3, 1, 64, 576), dtype=torch.bfloat16, device="cuda"), None, 512)
+    latent = torch.zeros((5, 1, 576), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(vx.VxError):                                                              # an aliased V has no rows
+        vx.kv_write(wide, latent, torch.zeros((5, 1, 512), dtype=torch.bfloat16, device="cuda"), slots)
