@@ -47,24 +47,36 @@ __device__ __forceinline__ MxLane mx_lane(int col, int grp) {
                 (uint32_t)(col * (D / 32) + grp * D / 128), (uint32_t)(grp * (D / 8) + col / (512 / D) * 4)};
 }
 
+// The tile at token t0 of a slice.  Buffer loads: the slice's address is uniform and goes into the
+// resource, the lane's part is the same for every tile, so a load costs no vector instruction and no
+// access can leave the slice.
+constexpr int kStreamLoad = 2;             // cache policy bits: nt
 template <int D>
 __device__ __forceinline__ void mx_load(const uint8_t* __restrict__ k, const uint8_t* __restrict__ v, int64_t slice,
-                                        int t0, int ps, const MxLane& l, MxTile<D>& t) {
-  const uint8_t* kc = k + slice + t0 * (D / 2);            // uniform bases, lane offsets
-  const uint8_t* vc = v + slice + t0 * (D / 2);
-  const uint8_t* ks = k + slice + ps * (D / 2) + t0 * (D / 32);
-  const uint8_t* vs = v + slice + ps * (D / 2) + t0 * (D / 32);
+                                        int slice_bytes, int t0, int ps, const MxLane& l, MxTile<D>& t) {
+  const __amdgpu_buffer_rsrc_t kr = coherent_rsrc(k + slice, (uint32_t)slice_bytes);
+  const __amdgpu_buffer_rsrc_t vr = coherent_rsrc(v + slice, (uint32_t)slice_bytes);
+  const int codes = t0 * (D / 2), scales = ps * (D / 2) + t0 * (D / 32);
   if constexpr (D == 128) {
-    const uint4 a = load_stream_u4(kc + l.kc), b = load_stream_u4(vc + l.vc);
-    t.k[0] = a.x; t.k[1] = a.y; t.k[2] = a.z; t.k[3] = a.w;
-    t.v[0] = b.x; t.v[1] = b.y; t.v[2] = b.z; t.v[3] = b.w;
+    const u32x4v_t a = __builtin_amdgcn_raw_buffer_load_b128(kr, (int)l.kc, codes, kStreamLoad);
+    const u32x4v_t b = __builtin_amdgcn_raw_buffer_load_b128(vr, (int)l.vc, codes, kStreamLoad);
+#pragma unroll
+    for (int x = 0; x < 4; x++) {
+      t.k[x] = a[x];
+      t.v[x] = b[x];
+    }
   } else {
-    const uint2 a = load_stream_u2(kc + l.kc), b = load_stream_u2(vc + l.vc);
-    t.k[0] = a.x; t.k[1] = a.y;
-    t.v[0] = b.x; t.v[1] = b.y;
+    typedef unsigned int u32x2v_t __attribute__((ext_vector_type(2)));
+    const u32x2v_t a = __builtin_amdgcn_raw_buffer_load_b64(kr, (int)l.kc, codes, kStreamLoad);
+    const u32x2v_t b = __builtin_amdgcn_raw_buffer_load_b64(vr, (int)l.vc, codes, kStreamLoad);
+#pragma unroll
+    for (int x = 0; x < 2; x++) {
+      t.k[x] = a[x];
+      t.v[x] = b[x];
+    }
   }
-  t.ke = __builtin_nontemporal_load(ks + l.ks);
-  t.ve = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(vs + l.vs));
+  t.ke = __builtin_amdgcn_raw_buffer_load_b8(kr, (int)l.ks, scales, kStreamLoad);
+  t.ve = __builtin_amdgcn_raw_buffer_load_b32(vr, (int)l.vs, scales, kStreamLoad);
 }
 
 // S^T of a tile: lane (grp, col) holds tokens 4 grp + i of query column col.
@@ -239,7 +251,7 @@ __device__ __forceinline__ void mx_wave_slots(const DecodeArgs& a, int i, int h,
       const uint32_t s_lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)my_s, ls);
       const uint32_t s_hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)my_s >> 32), ls);
       const int t0 = 16 * ((__builtin_amdgcn_readlane(my_n, ls) >> 16) + tt);
-      mx_load<D>(kbase, vbase, (int64_t)(((uint64_t)s_hi << 32) | s_lo), t0, a.ps, ln, t);
+      mx_load<D>(kbase, vbase, (int64_t)(((uint64_t)s_hi << 32) | s_lo), (int)slice_bytes, t0, a.ps, ln, t);
     };
     auto valid = [&](int u) {
       if (u >= tiles) return 0;

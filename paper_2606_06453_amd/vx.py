@@ -142,9 +142,9 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
-def _stream(stream) -> Optional[int]:
+def _stream(stream, device: Optional[int] = None) -> Optional[int]:
     if stream is None:
-        return _raw_stream(torch.cuda.current_device())
+        return _raw_stream(torch.cuda.current_device() if device is None else device)
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -308,7 +308,7 @@ def page_extend(pool: PagePool, rows: torch.Tensor, new_lens: torch.Tensor, batc
     _check(lib().vx_page_extend(pool.ref(), B, rows.data_ptr(), new_lens.data_ptr(), batch.seq_lens.data_ptr(),
                                 batch.page_indptr.data_ptr(), _ptr(pages), pages.numel(), token_indptr.data_ptr(),
                                 _ptr(slots), slots.numel(), granted.data_ptr(), first, _ptr(workspace),
-                                workspace.numel() * workspace.element_size(), _stream(stream)))
+                                workspace.numel() * workspace.element_size(), _stream(stream, d)))
 
 
 def page_release(pool: PagePool, rows: torch.Tensor, keep_lens: Optional[torch.Tensor], workspace: torch.Tensor,
@@ -322,7 +322,7 @@ def page_release(pool: PagePool, rows: torch.Tensor, keep_lens: Optional[torch.T
     if workspace.get_device() != d:
         _refuse(workspace, workspace.dtype, None, "workspace")
     _check(lib().vx_page_release(pool.ref(), B, _ptr(rows), _ptr(keep_lens), _ptr(workspace),
-                                 workspace.numel() * workspace.element_size(), _stream(stream)))
+                                 workspace.numel() * workspace.element_size(), _stream(stream, d)))
 
 
 def _row_args(t: Optional[torch.Tensor], n: int, heads: int, dim: int, d: int, name: str):
@@ -345,7 +345,7 @@ def _kv_rows(fn, kv: PagedKV, slots: torch.Tensor, k: torch.Tensor, v: Optional[
     n, st = slots.numel(), kv._st
     k_args = _row_args(k, n, st.num_kv_heads, st.head_dim_qk, d, names[0])
     v_args = _row_args(v, n, st.num_kv_heads, st.head_dim_v, d, names[1])
-    _check(fn(c, *k_args, *v_args, _ptr(slots), n, _stream(stream)))
+    _check(fn(c, *k_args, *v_args, _ptr(slots), n, _stream(stream, d)))
 
 
 def kv_write(kv: PagedKV, k_new: torch.Tensor, v_new: Optional[torch.Tensor], slots: torch.Tensor, stream=None) -> None:
