@@ -1063,7 +1063,7 @@ DecodeLayout decode_layout(int batch, int num_kv_heads, int group, int head_dim_
   L.off_ctr = 0;
   size_t off = al(sizeof(uint32_t) * kSplitPairs);
   L.off_lse = off;
-  off = al(off + sizeof(float) * (size_t)rows * group);
+  off = al(off + sizeof(float) * (size_t)rows * group * (mx ? 2 : 1));   // mxfp4: maximum and sum apart
   L.off_o = off;
   off = al(off + sizeof(float) * (size_t)rows * group * head_dim_v);
   L.total = L.splits > 1 ? off : 256;      // no partials when no pair can be split

@@ -28,7 +28,7 @@ namespace {
 
 constexpr int kMxWaves = 4;               // per workgroup
 constexpr float kRescaleLog2 = 8.f;
-constexpr float kNoMax = -1e30f;          // running maximum before the first token
+constexpr float kNoMax = -3.4028234e38f;  // running maximum before the first token: no score is below it
 
 template <int D>
 struct MxTile {
@@ -66,9 +66,9 @@ __device__ __forceinline__ void mx_load(const uint8_t* __restrict__ k, const uin
       t.v[x] = b[x];
     }
   } else {
-    typedef unsigned int u32x2v_t __attribute__((ext_vector_type(2)));
-    const u32x2v_t a = __builtin_amdgcn_raw_buffer_load_b64(kr, (int)l.kc, codes, kStreamLoad);
-    const u32x2v_t b = __builtin_amdgcn_raw_buffer_load_b64(vr, (int)l.vc, codes, kStreamLoad);
+    typedef unsigned int u32x2_load __attribute__((ext_vector_type(2)));
+    const u32x2_load a = __builtin_amdgcn_raw_buffer_load_b64(kr, (int)l.kc, codes, kStreamLoad);
+    const u32x2_load b = __builtin_amdgcn_raw_buffer_load_b64(vr, (int)l.vc, codes, kStreamLoad);
 #pragma unroll
     for (int x = 0; x < 2; x++) {
       t.k[x] = a[x];
@@ -126,7 +126,7 @@ __device__ __forceinline__ uint32_t high_halves(float lo, float hi) {
   return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
 }
 
-// Round of two tiles with va and vb valid tokens.  G8: at most 8 query heads, lo_mask 0 in the columns of
+// A round of two tiles with va and vb valid tokens.  G8: at most 8 query heads, lo_mask 0 in the columns of
 // the hi parts and the upper half's bits in those of the lo parts.
 template <int D, bool G8>
 __device__ __forceinline__ void mx_round(MxTile<D> (&t)[2], int va, int vb, const bf16x8_t (&qv)[D / 32], int grp,
@@ -135,13 +135,20 @@ __device__ __forceinline__ void mx_round(MxTile<D> (&t)[2], int va, int vb, cons
   f32x4_t sa = mx_scores<D>(t[0], qv), sb = mx_scores<D>(t[1], qv);
   if (va < 16) mx_mask<D>(va, grp, sa, t[0]);               // uniform
   if (vb < 16) mx_mask<D>(vb, grp, sb, t[1]);
-  const float top = fmaxf(fmaxf(fmaxf(sa[0], sa[1]), fmaxf(sa[2], sa[3])),
-                          fmaxf(fmaxf(sb[0], sb[1]), fmaxf(sb[2], sb[3])));
-  if (__builtin_amdgcn_ballot_w64(top * scale_log2 > m + kRescaleLog2) != 0) {
-    float mt = top;
+  // Scaled and rounded before the maximum is taken off (a fused form would leave the product's rounding
+  // error in the exponent, which overflows for scores past 2^30).
+  float z[8];
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+#pragma clang fp contract(off)
+    z[i] = sa[i] * scale_log2;
+    z[4 + i] = sb[i] * scale_log2;
+  }
+  float mt = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
+  if (__builtin_amdgcn_ballot_w64(mt > m + kRescaleLog2) != 0) {
     mt = fmaxf(mt, xor_shfl(mt, 16));
     mt = fmaxf(mt, xor_shfl(mt, 32));
-    const float m_new = fmaxf(m, mt * scale_log2);
+    const float m_new = fmaxf(m, mt);
     const float alpha = __builtin_amdgcn_exp2f(m - m_new);
     m = m_new;
     lsum *= alpha;
@@ -155,9 +162,9 @@ __device__ __forceinline__ void mx_round(MxTile<D> (&t)[2], int va, int vb, cons
   }
   float p[8];
 #pragma unroll
-  for (int i = 0; i < 4; i++) {
-    p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sa[i], scale_log2, -m));
-    p[4 + i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sb[i], scale_log2, -m));
+  for (int i = 0; i < 8; i++) {
+#pragma clang fp contract(off)
+    p[i] = __builtin_amdgcn_exp2f(z[i] - m);
   }
   lsum += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
   auto cut = [&](uint32_t mask) {
@@ -283,7 +290,19 @@ __device__ __forceinline__ void put_merged(uint16_t* dst, float W, const float4&
                                               f32_to_bf16_rne(o.z * inv) | (f32_to_bf16_rne(o.w * inv) << 16));
 }
 
-// LSE-weighted merge of a split pair's S partials by the workgroup.  A slot is 4 channels of one head;
+// A partial's running maximum and sum.  Their log-sum-exp in one float would round at the maximum's
+// magnitude: at scores of 2^24 a split's weight would be off by half.
+typedef unsigned int u32x2v_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void put_state(__amdgpu_buffer_rsrc_t r, uint32_t row, float m, float l) {
+  __builtin_amdgcn_raw_buffer_store_b64((u32x2v_t{__float_as_uint(m), __float_as_uint(l)}), r, (int)(row * 8u), 0,
+                                        kAgentCoherent);
+}
+__device__ __forceinline__ float2_t get_state(__amdgpu_buffer_rsrc_t r, uint32_t row) {
+  const u32x2v_t w = __builtin_amdgcn_raw_buffer_load_b64(r, (int)(row * 8u), 0, kAgentCoherent);
+  return float2_t{__uint_as_float(w.x), __uint_as_float(w.y)};
+}
+
+// Merge of a split pair's S partials by the workgroup, each weighing its sum.  A slot is 4 channels of one head;
 // with fewer slots than threads, G threads share one and take every G-th partial, kMergeBatch loads in
 // flight each, and meet in LDS ([G][slots] of 6 floats): a pair cut into many splits (few requests)
 // is merged in one or two round trips.
@@ -295,26 +314,24 @@ __device__ __forceinline__ void merge_pair(int S, int g, __amdgpu_buffer_rsrc_t 
   for (int y = (int)threadIdx.x; y < slots * G; y += NT) {   // one turn, unless there are more slots than threads
     const int k = y / slots, x = y - k * slots;
     const int c = (4 * x) / D, d = 4 * x - c * D;
-    float M = -INFINITY, W = 0.f;
+    float M = kNoMax, W = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int s0 = k; s0 < S; s0 += G * kMergeBatch) {
-      float l[kMergeBatch];
+      float2_t l[kMergeBatch];
       float4 p[kMergeBatch];
 #pragma unroll
       for (int b = 0; b < kMergeBatch; b++) {
         const uint32_t row = (uint32_t)(min(s0 + G * b, S - 1) * g + c);
-        l[b] = coherent_load1(l_rs, row * 4u);
+        l[b] = get_state(l_rs, row);
         p[b] = coherent_load4(o_rs, (row * D + d) * 4u);
       }
       float m_new = M;
 #pragma unroll
       for (int b = 0; b < kMergeBatch; b++) {
-        if (s0 + G * b >= S) l[b] = -INFINITY;
-        m_new = fmaxf(m_new, l[b]);
+        if (s0 + G * b >= S) l[b] = float2_t{kNoMax, 0.f};
+        m_new = fmaxf(m_new, l[b][0]);
       }
-      // without a token so far every weight is 0 (or NaN, which stays)
-      const float ref = m_new == -INFINITY ? 0.f : m_new;
-      const float keep = __builtin_amdgcn_exp2f(M - ref);
+      const float keep = __builtin_amdgcn_exp2f(M - m_new);
       W *= keep;
       o.x *= keep;
       o.y *= keep;
@@ -322,7 +339,7 @@ __device__ __forceinline__ void merge_pair(int S, int g, __amdgpu_buffer_rsrc_t 
       o.w *= keep;
 #pragma unroll
       for (int b = 0; b < kMergeBatch; b++) {
-        const float wgt = __builtin_amdgcn_exp2f(l[b] - ref);
+        const float wgt = __builtin_amdgcn_exp2f(l[b][0] - m_new) * l[b][1];
         W += wgt;
         o.x += wgt * p[b].x;
         o.y += wgt * p[b].y;
@@ -347,13 +364,12 @@ __device__ __forceinline__ void merge_pair(int S, int g, __amdgpu_buffer_rsrc_t 
   __syncthreads();
   if ((int)threadIdx.x >= slots) return;
   const int x = (int)threadIdx.x, c = (4 * x) / D, d = 4 * x - c * D;
-  float M = -INFINITY, W = 0.f;
+  float M = kNoMax, W = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int k = 0; k < G; k++) M = fmaxf(M, lds[(size_t)(k * slots + x) * 6]);
-  const float ref = M == -INFINITY ? 0.f : M;
   for (int k = 0; k < G; k++) {
     const float* q = lds + (size_t)(k * slots + x) * 6;
-    const float wgt = __builtin_amdgcn_exp2f(q[0] - ref);
+    const float wgt = __builtin_amdgcn_exp2f(q[0] - M);
     W += wgt * q[1];
     o.x += wgt * q[2];
     o.y += wgt * q[3];
@@ -417,7 +433,7 @@ __global__ __launch_bounds__(kMxWaves * kWave) __attribute__((amdgpu_waves_per_e
   __syncthreads();
   const uint32_t pair_rows = (uint32_t)(a.S * g);
   const __amdgpu_buffer_rsrc_t o_rs = coherent_rsrc(a.part_o + (int64_t)pair * pair_rows * D, pair_rows * D * 4u);
-  const __amdgpu_buffer_rsrc_t l_rs = coherent_rsrc(a.part_lse + (int64_t)pair * pair_rows, pair_rows * 4u);
+  const __amdgpu_buffer_rsrc_t l_rs = coherent_rsrc(a.part_lse + (int64_t)pair * pair_rows * 2, pair_rows * 8u);
   for (int x = (int)threadIdx.x; x < g * D / 4; x += NW * kWave) {
     const int c = (4 * x) / D, d = 4 * x - c * D;
     float M = kNoMax;
@@ -443,7 +459,7 @@ __global__ __launch_bounds__(kMxWaves * kWave) __attribute__((amdgpu_waves_per_e
     } else {
       const uint32_t row = (uint32_t)(split * g + c);
       coherent_store4(o_rs, (row * D + d) * 4u, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-      if (d == 0) coherent_store1(l_rs, row * 4u, Ls == 0.f ? -INFINITY : M + __log2f(Ls));
+      if (d == 0) put_state(l_rs, row, M, Ls);
     }
   }
   if (Sp > 1) {

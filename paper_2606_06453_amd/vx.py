@@ -339,13 +339,13 @@ def _row_args(t: Optional[torch.Tensor], n: int, heads: int, dim: int, d: int, n
 
 
 def _kv_rows(fn, kv: PagedKV, slots: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor], names, stream) -> None:
-    d, c = _gpu_of(kv.k), kv.ref()
+    d, st = _gpu_of(kv.k), kv.struct()
     if slots.dtype is not torch.int64 or slots.get_device() != d:
         _refuse(slots, torch.int64, None, "slots")
-    n, st = slots.numel(), kv._st
+    n = slots.numel()
     k_args = _row_args(k, n, st.num_kv_heads, st.head_dim_qk, d, names[0])
     v_args = _row_args(v, n, st.num_kv_heads, st.head_dim_v, d, names[1])
-    _check(fn(c, *k_args, *v_args, _ptr(slots), n, _stream(stream, d)))
+    _check(fn(ctypes.byref(st), *k_args, *v_args, _ptr(slots), n, _stream(stream, d)))
 
 
 def kv_write(kv: PagedKV, k_new: torch.Tensor, v_new: Optional[torch.Tensor], slots: torch.Tensor, stream=None) -> None:

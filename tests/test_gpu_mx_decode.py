@@ -176,3 +176,16 @@ def test_caches_past_four_gigabytes():
     vx.sparse_paged_decode(p["q"].cuda(), kv, batch, gpu(p["sel"]), gpu(p["count"]), p["M"], p["scale"], out, ws)
     torch.cuda.synchronize()
     assert np.array_equal(out.double().cpu().numpy(), small)
+
+
+def test_scores_far_below_zero():
+    """Every score -1e34: the weights are equal, and the output is the mean of V."""
+    p = _problem(1, 1, 4, 128, 16, 16, [75], 9, 6)
+    p["q"][:] = 1.0
+    p["kc"] = _mx.pack(np.full(p["kc"].shape[:3] + (128,), -(2.0 ** 106)), "k")
+    got = _launch(p)
+    v = _mx.unpack(p["vc"], "v")[p["perm"]].reshape(-1, 128)[:75]
+    want = v.mean(0)
+    # equal scores leave weights of exactly 1; 75 additions in fp32, a division, bf16
+    tol = 2.0 ** -8 * np.abs(want) + 80 * 2.0 ** -23 * np.abs(v).mean(0)
+    assert (np.abs(got[0] - want) <= tol).all()
