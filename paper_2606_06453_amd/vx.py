@@ -196,6 +196,17 @@ class PagedKV:
         return self._ref
 
 
+    def current(self):
+        """ref(), built again where the caches, their shape or scales have been replaced since."""
+        now = (self.k.data_ptr(), None if self.v is None else self.v.data_ptr(), self.k.shape, self.k_scale, self.v_scale)
+        if getattr(self, "_seen", None) != now:
+            if self.v is not None and self.v.device != self.k.device:
+                raise ValueError(f"K and V caches must be on one device (got {self.k.device} and {self.v.device})")
+            self._ref = None
+            self._seen = now
+        return self.ref()
+
+
 @dataclass
 class BatchSpec:
     """Ragged batch over the paged cache: int32 device tensors plus a host bound on P_i."""
@@ -339,13 +350,13 @@ def _row_args(t: Optional[torch.Tensor], n: int, heads: int, dim: int, d: int, n
 
 
 def _kv_rows(fn, kv: PagedKV, slots: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor], names, stream) -> None:
-    d, st = _gpu_of(kv.k), kv.struct()
+    d, c = _gpu_of(kv.k), kv.current()
     if slots.dtype is not torch.int64 or slots.get_device() != d:
         _refuse(slots, torch.int64, None, "slots")
-    n = slots.numel()
+    n, st = slots.numel(), kv._st
     k_args = _row_args(k, n, st.num_kv_heads, st.head_dim_qk, d, names[0])
     v_args = _row_args(v, n, st.num_kv_heads, st.head_dim_v, d, names[1])
-    _check(fn(ctypes.byref(st), *k_args, *v_args, _ptr(slots), n, _stream(stream, d)))
+    _check(fn(c, *k_args, *v_args, _ptr(slots), n, _stream(stream, d)))
 
 
 def kv_write(kv: PagedKV, k_new: torch.Tensor, v_new: Optional[torch.Tensor], slots: torch.Tensor, stream=None) -> None:

@@ -133,3 +133,15 @@ def test_the_binding_checks_types_and_places():
 def test_keys_alone():
     kv = vx.PagedKV(vx.mxfp4_cache(3, 2, 16, 64, "cpu"), None)
     assert (kv.struct().head_dim_qk, kv.struct().head_dim_v) == (64, 64)
+
+
+def test_a_replaced_cache_is_described_anew():
+    new = lambda P: torch.zeros((P, 2, 16, 64), dtype=torch.float8_e4m3fn)  # noqa: E731
+    kv = vx.PagedKV(new(3), new(3), k_scale=0.5)
+    kv.current()
+    assert (kv._st.num_phys_pages, kv._st.k_scale, kv._st.k) == (3, 0.5, kv.k.data_ptr())
+    kept = kv.current()
+    assert kv.current() is kept
+    kv.k, kv.v, kv.k_scale = new(4), new(4), 0.25
+    kv.current()
+    assert (kv._st.num_phys_pages, kv._st.k_scale, kv._st.k, kv._st.v) == (4, 0.25, kv.k.data_ptr(), kv.v.data_ptr())

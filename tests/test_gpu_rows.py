@@ -177,3 +177,10 @@ def test_rows_that_do_not_fit_are_refused():
     latent = torch.zeros((5, 1, 576), dtype=torch.bfloat16, device="cuda")
     with pytest.raises(vx.VxError):                                                              # an aliased V has no rows
         vx.kv_write(wide, latent, torch.zeros((5, 1, 512), dtype=torch.bfloat16, device="cuda"), slots)
+
+
+def test_caches_on_two_devices_are_refused():
+    kv = vx.PagedKV(vx.mxfp4_cache(3, 2, 16, 64), vx.mxfp4_cache(3, 2, 16, 64, "cpu"))
+    rows, slots = torch.zeros((5, 2, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros(5, dtype=torch.int64, device="cuda")
+    with pytest.raises(ValueError, match="one device"):
+        vx.kv_write(kv, rows, rows, slots)
