@@ -195,14 +195,17 @@ class PagedKV:
             self._ref = ctypes.byref(self._st)
         return self._ref
 
-
     def current(self):
-        """ref(), built again where the caches, their shape or scales have been replaced since."""
-        now = (self.k.data_ptr(), None if self.v is None else self.v.data_ptr(), self.k.shape, self.k_scale, self.v_scale)
+        """ref(), built again where anything that struct() reads has changed since."""
+        k, v = self.k, self.v
+        now = (k.data_ptr(), k.dtype, k.shape, k.is_contiguous(), k.get_device(), self.head_dim_v, self.k_scale,
+               self.v_scale, self.block_size,
+               None if v is None else (v.data_ptr(), v.dtype, v.shape, v.is_contiguous(), v.get_device()))
         if getattr(self, "_seen", None) != now:
-            if self.v is not None and self.v.device != self.k.device:
-                raise ValueError(f"K and V caches must be on one device (got {self.k.device} and {self.v.device})")
-            self._ref = None
+            if v is not None and v.device != k.device:
+                raise ValueError(f"K and V caches must be on one device (got {k.device} and {v.device})")
+            self._ref = self._seen = None
+            self.ref()
             self._seen = now
         return self.ref()
 

@@ -1,0 +1,65 @@
+"""The descriptions of caches and pools that the binding hands to the library follow the tensors they
+describe (no GPU needed)."""
+import pytest
+import torch
+
+from paper_2606_06453_amd import vx
+
+BF16, E4M3, E5M2 = torch.bfloat16, torch.float8_e4m3fn, torch.float8_e5m2
+
+
+def _kv(P=3, H=2, ps=16, D=64, dtype=BF16, room=1 << 18):
+    """K and V at the starts of two buffers that other caches can take over."""
+    bufs = [torch.zeros(room, dtype=torch.uint8) for _ in range(2)]
+    kv = vx.PagedKV(*(_on(b, P, H, ps, D, dtype) for b in bufs), k_scale=0.5, v_scale=0.5)
+    return kv, bufs
+
+
+def _on(buf, P, H, ps, D, dtype):
+    n = P * H * ps * D * torch.empty(0, dtype=dtype).element_size()
+    return buf[:n].view(dtype).view(P, H, ps, D)
+
+
+def _told(kv):
+    kv.current()
+    return {n: getattr(kv._st, n) for n, _ in vx._Cache._fields_}
+
+
+def _fresh(kv):
+    st = kv.struct()
+    return {n: getattr(st, n) for n, _ in vx._Cache._fields_}
+
+
+@pytest.mark.parametrize("first,second", [(BF16, E4M3), (E4M3, E5M2), (E5M2, BF16)])
+def test_another_type_on_the_same_address_and_shape(first, second):
+    kv, bufs = _kv(dtype=first)
+    _told(kv)
+    kv.k, kv.v = (_on(b, 3, 2, 16, 64, second) for b in bufs)
+    assert _told(kv)["kv_dtype"] == vx.kv_dtype_code(kv.k) and _told(kv) == _fresh(kv)
+
+
+def test_each_field_that_a_description_holds():
+    kv, bufs = _kv(ps=32)
+    _told(kv)
+    for name, value in (("block_size", 16), ("k_scale", 0.25), ("v_scale", 0.125)):
+        setattr(kv, name, value)
+        assert _told(kv)[name] == value and _told(kv) == _fresh(kv)
+    kv.v = _on(bufs[1][64:], 3, 2, 32, 64, BF16)                       # V alone
+    assert _told(kv)["v"] == kv.v.data_ptr()
+    latent = vx.PagedKV(torch.zeros((2, 1, 16, 576), dtype=BF16), None, 512)
+    _told(latent)
+    latent.head_dim_v = 576
+    assert _told(latent)["head_dim_v"] == 576
+
+
+def test_a_cache_turned_into_a_view_is_refused():
+    kv, bufs = _kv(H=16, ps=16)
+    _told(kv)
+    kv.k = kv.k.transpose(1, 2)                                        # same address, same shape
+    with pytest.raises(AssertionError):
+        kv.current()
+
+
+def test_an_unchanged_cache_keeps_its_description():
+    kv, _ = _kv()
+    assert kv.current() is kv.current()
