@@ -164,8 +164,14 @@ class PagedKV:
         P, H, ps, Dqk = self.k.shape
         Dv = self.v.shape[3] if self.v is not None else (self.head_dim_v or Dqk)
         dt = kv_dtype_code(self.k)
-        if self.v is not None and kv_dtype_code(self.v) != dt:
-            raise TypeError("K and V caches must have the same dtype")
+        if self.v is not None:
+            if kv_dtype_code(self.v) != dt:
+                raise TypeError("K and V caches must have the same dtype")
+            if self.v.device != self.k.device:
+                raise ValueError(f"K and V caches must be on one device (got {self.k.device} and {self.v.device})")
+            if self.v.shape[1] != H or self.v.shape[2] != ps or self.v.shape[0] < P:
+                raise ValueError(f"the V cache must have K's pages, KV heads and page size (got {tuple(self.v.shape)} "
+                                 f"beside {tuple(self.k.shape)})")
         if dt == KV_MXFP4:
             Dqk = self._mx_dim(Dqk)
             Dv = self._mx_dim(Dv) if self.v is not None else (self.head_dim_v or Dqk)
@@ -202,8 +208,6 @@ class PagedKV:
                self.v_scale, self.block_size,
                None if v is None else (v.data_ptr(), v.dtype, v.shape, v.is_contiguous(), v.get_device()))
         if getattr(self, "_seen", None) != now:
-            if v is not None and v.device != k.device:
-                raise ValueError(f"K and V caches must be on one device (got {k.device} and {v.device})")
             self._ref = self._seen = None
             self.ref()
             self._seen = now

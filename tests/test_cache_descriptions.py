@@ -63,3 +63,23 @@ def test_a_cache_turned_into_a_view_is_refused():
 def test_an_unchanged_cache_keeps_its_description():
     kv, _ = _kv()
     assert kv.current() is kv.current()
+
+
+def test_v_must_have_the_pages_of_k():
+    """Slots and page ids are bounded by K's pages: a V cache with fewer would be written past its end."""
+    for dtype in (BF16, torch.uint8):
+        D = 68 if dtype == torch.uint8 else 128
+        new = lambda P, H, ps: torch.zeros((P, H, ps, D), dtype=dtype)  # noqa: E731
+        for shape in ((8, 2, 16), (9, 1, 16), (9, 2, 8), (9, 4, 16)):
+            kv = vx.PagedKV(new(9, 2, 16), new(*shape))
+            for describe in (kv.struct, kv.ref, kv.current):
+                with pytest.raises(ValueError, match="V cache"):
+                    describe()
+        assert vx.PagedKV(new(9, 2, 16), new(11, 2, 16)).struct().num_phys_pages == 9     # more pages do no harm
+
+
+def test_k_and_v_on_two_devices():
+    kv = vx.PagedKV(torch.zeros((3, 2, 16, 64), dtype=BF16), torch.zeros((3, 2, 16, 64), dtype=BF16, device="meta"))
+    for describe in (kv.struct, kv.current):
+        with pytest.raises(ValueError, match="one device"):
+            describe()
