@@ -254,22 +254,21 @@ class PagePool:
                    torch.zeros((table_rows, table_stride), **i32), torch.zeros(table_rows, **i32), page_size, block_size)
 
     def struct(self) -> _Pool:
-        for n in ("free_pages", "free_count", "table", "lens"):
-            t = getattr(self, n)
-            if t.dtype != torch.int32 or t.device != self.table.device:
-                raise TypeError(f"{n} must be int32 on {self.table.device} (got {t.dtype} on {t.device})")
-        rows, stride = self.table.shape
-        if self.lens.numel() != rows:
-            raise ValueError(f"lens has {self.lens.numel()} entries for {rows} table rows")
-        return _Pool(_ptr(self.free_pages), _ptr(self.free_count), _ptr(self.table), _ptr(self.lens),
-                     self.free_pages.numel(), rows, stride, int(self.page_size), int(self.block_size))
-
-    def ref(self):
-        """A by-reference argument holding this pool, built once (see PagedKV.ref)."""
-        if getattr(self, "_ref", None) is None:
-            self._st = self.struct()
-            self._ref = ctypes.byref(self._st)
-        return self._ref
+        """The pool as it is now: every call describes it anew, so its tensors may be replaced."""
+        free, count, table, lens = self.free_pages, self.free_count, self.table, self.lens
+        i32, d = torch.int32, table.get_device()
+        if not (free.dtype is i32 and count.dtype is i32 and table.dtype is i32 and lens.dtype is i32
+                and free.get_device() == d and count.get_device() == d and lens.get_device() == d):
+            for t, n in ((free, "free_pages"), (count, "free_count"), (table, "table"), (lens, "lens")):
+                if t.dtype is not i32 or t.get_device() != d:
+                    raise TypeError(f"{n} must be int32 on {table.device} (got {t.dtype} on {t.device})")
+        rows, stride = table.shape
+        if lens.numel() != rows:
+            raise ValueError(f"lens has {lens.numel()} entries for {rows} table rows")
+        if count.numel() < 1:
+            raise ValueError("free_count must have an entry")
+        return _Pool(_ptr(free), count.data_ptr(), _ptr(table), _ptr(lens), free.numel(), rows, stride,
+                     int(self.page_size), int(self.block_size))
 
 
 def _gpu_of(t: torch.Tensor) -> int:
@@ -323,9 +322,9 @@ def page_extend(pool: PagePool, rows: torch.Tensor, new_lens: torch.Tensor, batc
         _refuse(slots, torch.int64, None, "slots")
     if workspace.get_device() != d:
         _refuse(workspace, workspace.dtype, None, "workspace")
-    _check(lib().vx_page_extend(pool.ref(), B, rows.data_ptr(), new_lens.data_ptr(), batch.seq_lens.data_ptr(),
-                                batch.page_indptr.data_ptr(), _ptr(pages), pages.numel(), token_indptr.data_ptr(),
-                                _ptr(slots), slots.numel(), granted.data_ptr(), first, _ptr(workspace),
+    _check(lib().vx_page_extend(ctypes.byref(pool.struct()), B, rows.data_ptr(), new_lens.data_ptr(),
+                                batch.seq_lens.data_ptr(), batch.page_indptr.data_ptr(), _ptr(pages), pages.numel(),
+                                token_indptr.data_ptr(), _ptr(slots), slots.numel(), granted.data_ptr(), first, _ptr(workspace),
                                 workspace.numel() * workspace.element_size(), _stream(stream, d)))
 
 
@@ -339,7 +338,7 @@ def page_release(pool: PagePool, rows: torch.Tensor, keep_lens: Optional[torch.T
         _refuse(keep_lens, i32, B, "keep_lens")
     if workspace.get_device() != d:
         _refuse(workspace, workspace.dtype, None, "workspace")
-    _check(lib().vx_page_release(pool.ref(), B, _ptr(rows), _ptr(keep_lens), _ptr(workspace),
+    _check(lib().vx_page_release(ctypes.byref(pool.struct()), B, _ptr(rows), _ptr(keep_lens), _ptr(workspace),
                                  workspace.numel() * workspace.element_size(), _stream(stream, d)))
 
 

@@ -83,3 +83,51 @@ def test_k_and_v_on_two_devices():
     for describe in (kv.struct, kv.current):
         with pytest.raises(ValueError, match="one device"):
             describe()
+
+
+def _pool_told(monkeypatch, pool):
+    """The pool that page_extend and page_release describe to the library, from a call that gets no further."""
+    told = []
+
+    class Lib:
+        @staticmethod
+        def vx_page_extend(p, *a):
+            told.append({n: getattr(p._obj, n) for n, _ in vx._Pool._fields_})
+            return 0
+
+        vx_page_release = vx_page_extend
+
+    monkeypatch.setattr(vx, "lib", lambda: Lib)
+    monkeypatch.setattr(vx, "_gpu_of", lambda t: t.get_device())
+    monkeypatch.setattr(vx, "_stream", lambda *a: None)
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    vx.page_extend(pool, i32(2), i32(2), vx.BatchSpec(i32(3), i32(6), i32(2), 4), i32(3),
+                   torch.zeros(9, dtype=torch.int64), i32(2), i32(64))
+    vx.page_release(pool, i32(2), None, i32(64))
+    return told
+
+
+def test_a_pool_is_described_as_it_is_now(monkeypatch):
+    pool = vx.PagePool.empty(6, 3, 4, 16, device="cpu")
+    first = _pool_told(monkeypatch, pool)
+    assert first[0] == first[1] and (first[0]["table"], first[0]["table_stride"]) == (pool.table.data_ptr(), 4)
+    pool.table, pool.lens = torch.zeros((5, 8), dtype=torch.int32), torch.zeros(5, dtype=torch.int32)      # it has grown
+    pool.free_pages, pool.block_size, pool.page_size = torch.zeros(9, dtype=torch.int32), 16, 32
+    for told in _pool_told(monkeypatch, pool):
+        assert told == dict(free_pages=pool.free_pages.data_ptr(), free_count=pool.free_count.data_ptr(),
+                            table=pool.table.data_ptr(), lens=pool.lens.data_ptr(), num_phys_pages=9, table_rows=5,
+                            table_stride=8, page_size=32, block_size=16)
+
+
+def test_pools_that_do_not_fit_are_refused(monkeypatch):
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    pool = vx.PagePool.empty(6, 3, 4, 16, device="cpu")
+    _pool_told(monkeypatch, pool)
+    for name, bad in (("lens", i32(2)), ("free_count", i32(0)), ("table", i32((4, 3)).t()), ("lens", i32(6)[::2]),
+                      ("free_pages", torch.zeros(6)), ("free_pages", i32(12)[::2])):
+        was = getattr(pool, name)
+        setattr(pool, name, bad)
+        with pytest.raises((TypeError, ValueError, AssertionError)):
+            _pool_told(monkeypatch, pool)
+        setattr(pool, name, was)
+    _pool_told(monkeypatch, pool)
