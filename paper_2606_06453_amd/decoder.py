@@ -55,9 +55,42 @@ class SparseDecoder:
         self.ws_decode = torch.zeros((ws_d,), dtype=torch.uint8, device=dev)
 
         self._bound = {}
+        self._geometry = self._now()
+        self._describe()
+
+    def _now(self):
+        """What the buffers above are sized and typed for."""
+        kv, b = self.kv, self.batch
+        return (kv.k.shape, kv.k.dtype, kv.k.device, None if kv.v is None else kv.v.shape, kv.head_dim_v, kv.block_size,
+                b.seq_lens.numel(), b.max_pages_per_seq)
+
+    def _describe(self):
+        """Describes the cache and the batch as they are, for calls that are bound from here on."""
+        kv, b = self.kv, self.batch
+        self._bound.clear()
+        kv.current()
+        b.current()
+        # the tensors themselves are held, so that another one is never taken for one of them
+        self._held = (kv.k, kv.k.data_ptr(), kv.v, None if kv.v is None else kv.v.data_ptr(), kv.k_scale, kv.v_scale,
+                      kv.block_size, kv.head_dim_v, b.page_indptr, b.page_indices, b.seq_lens, b.max_pages_per_seq)
+
+    def _follow(self):
+        """Replaced tensors of the cache and the batch, and new scales, are taken up by the next call (the
+        summaries are still those of the cache before); other sizes or types do not fit the buffers."""
+        kv, b, h = self.kv, self.batch, self._held
+        if (kv.k is h[0] and h[1] == kv.k.data_ptr() and kv.v is h[2] and (h[2] is None or h[3] == kv.v.data_ptr())
+                and kv.k_scale == h[4] and kv.v_scale == h[5] and kv.block_size == h[6] and kv.head_dim_v == h[7]
+                and b.page_indptr is h[8] and b.page_indices is h[9] and b.seq_lens is h[10]
+                and b.max_pages_per_seq == h[11]):
+            return
+        if self._now() != self._geometry:
+            raise ValueError(f"the cache or the batch has another geometry than this SparseDecoder's buffers (now "
+                             f"{self._now()}, then {self._geometry}): make a new SparseDecoder")
+        self._describe()
 
     def _bound_call(self, key, make):
         """The step's calls with their arguments marshalled once, keyed by the tensors that vary."""
+        self._follow()
         c = self._bound.get(key)
         if c is None:
             if len(self._bound) >= 32:
@@ -68,6 +101,7 @@ class SparseDecoder:
 
     def summarize(self, first_page: Optional[torch.Tensor] = None, stream=None):
         if first_page is None:           # prefill: every page (not a per-step call)
+            self._follow()
             vx.page_summarize(self.kv, self.batch, None, self.mean, self.max, self.min, stream,
                               mean_bf16=self.mean_bf16)
             return

@@ -194,8 +194,8 @@ class PagedKV:
         return torch.bfloat16 if kv_dtype_code(self.k) == KV_MXFP4 else self.k.dtype
 
     def ref(self):
-        """A by-reference argument holding this geometry, built once (the tensors must not be
-        replaced afterwards)."""
+        """A by-reference argument holding this geometry, built once; current() follows tensors that
+        are replaced afterwards."""
         if getattr(self, "_ref", None) is None:
             self._st = self.struct()
             self._ref = ctypes.byref(self._st)
@@ -232,6 +232,11 @@ class BatchSpec:
             self._st = self.struct()
             self._ref = ctypes.byref(self._st)
         return self._ref
+
+    def current(self):
+        """ref(), built again for the tensors and the bound as they are now."""
+        self._ref = None
+        return self.ref()
 
 
 @dataclass

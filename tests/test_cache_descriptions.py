@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from paper_2606_06453_amd import vx
+from paper_2606_06453_amd.decoder import SparseDecoder
 
 BF16, E4M3, E5M2 = torch.bfloat16, torch.float8_e4m3fn, torch.float8_e5m2
 
@@ -131,3 +132,102 @@ def test_pools_that_do_not_fit_are_refused(monkeypatch):
             _pool_told(monkeypatch, pool)
         setattr(pool, name, was)
     _pool_told(monkeypatch, pool)
+
+
+class _Recorder:
+    """The library's calls, recorded instead of made: the cache and the batch that each is given."""
+
+    def __init__(self):
+        self.told, self.real = [], vx.lib()
+
+    def __getattr__(self, name):
+        if name == "vx_workspace_size":
+            return self.real.vx_workspace_size
+
+        def call(*args):
+            given = [a._obj for a in args if hasattr(a, "_obj")]
+            cache = next(g for g in given if isinstance(g, vx._Cache))
+            batch = next(g for g in given if isinstance(g, vx._Batch))
+            self.told.append((name, cache.k, cache.v, cache.k_scale, batch.page_indptr, batch.page_indices, batch.seq_lens))
+            return 0
+        return call
+
+
+def _decoder(monkeypatch, dtype=BF16):
+    rec = _Recorder()
+    monkeypatch.setattr(vx, "lib", lambda: rec)
+    monkeypatch.setattr(vx, "_stream", lambda *a: None)
+    D = 68 if dtype == torch.uint8 else 128
+    cache = lambda P=6: torch.zeros((P, 2, 16, D), dtype=dtype)  # noqa: E731
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    kv, batch = vx.PagedKV(cache(), cache(), k_scale=0.5), vx.BatchSpec(i32(3), i32(6), i32(2), 3)
+    dec = SparseDecoder(kv, batch, 4, vx.MEAN_DOT, 1, 1, 3, 0.1)
+    row = lambda t: torch.zeros((2, 2, 128), dtype=t)  # noqa: E731
+    q, new, budget = torch.zeros((2, 4, 128), dtype=BF16), (row(kv.row_dtype), row(kv.row_dtype)), i32(2)
+
+    def every_call():
+        rec.told.clear()
+        dec.summarize()
+        dec.summarize(i32(2))
+        dec.append(*new)
+        dec.select(q, budget)
+        dec.append_select(*new, q, budget)
+        dec.step(q, budget, None, kv_new=new)
+        assert len(rec.told) == 7
+        return {t[1:] for t in rec.told}
+    return dec, cache, i32, every_call
+
+
+def _now(dec):
+    kv, b = dec.kv, dec.batch
+    return {(kv.k.data_ptr(), kv.v.data_ptr(), kv.k_scale, b.page_indptr.data_ptr(), b.page_indices.data_ptr(),
+             b.seq_lens.data_ptr())}
+
+
+def test_a_decoder_follows_replaced_tensors(monkeypatch):
+    dec, cache, i32, every_call = _decoder(monkeypatch)
+    assert every_call() == _now(dec)
+    keep = [dec.kv.k, dec.kv.v, dec.batch.seq_lens]                     # so that no address is used again
+    dec.kv.k, dec.kv.v = cache(), cache()
+    assert every_call() == _now(dec)
+    dec.kv.k_scale = 0.25
+    assert every_call() == _now(dec)
+    dec.batch.seq_lens, dec.batch.page_indices, dec.batch.page_indptr = i32(2), i32(9), i32(3)
+    assert every_call() == _now(dec)
+    keep.append(dec.kv.k.data)
+    dec.kv.k.data = cache()                                             # the same tensor, other memory
+    assert every_call() == _now(dec)
+    assert len({t.data_ptr() for t in keep}) == 4
+
+
+@pytest.mark.parametrize("change", ["pages", "type", "batch", "bound", "keys", "page_size"])
+def test_a_decoder_refuses_what_its_buffers_do_not_fit(monkeypatch, change):
+    dec, cache, i32, every_call = _decoder(monkeypatch)
+    every_call()
+    if change == "pages":
+        dec.kv.k, dec.kv.v = cache(7), cache(7)
+    elif change == "type":
+        dec.kv.k, dec.kv.v = cache().to(E4M3), cache().to(E4M3)
+    elif change == "batch":
+        dec.batch.seq_lens, dec.batch.page_indptr = i32(3), i32(4)
+    elif change == "bound":
+        dec.batch.max_pages_per_seq = 5
+    elif change == "keys":
+        dec.kv.v = None
+    else:
+        dec.kv.k, dec.kv.v = (torch.zeros((3, 2, 32, 128), dtype=BF16) for _ in range(2))
+    for call in (dec.summarize, lambda: dec.summarize(i32(2)), lambda: dec.decode(torch.zeros((2, 4, 128), dtype=BF16))):
+        with pytest.raises(ValueError, match="SparseDecoder"):
+            call()
+
+
+def test_a_new_decoder_describes_the_cache_as_it_is(monkeypatch):
+    dec, cache, i32, every_call = _decoder(monkeypatch)
+    every_call()
+    old = dec.kv.k
+    dec.kv.k = cache()
+    other = SparseDecoder(dec.kv, dec.batch, 4, vx.MEAN_DOT, 1, 1, 3, 0.1)
+    rec = vx.lib()
+    rec.told.clear()
+    other.select(torch.zeros((2, 4, 128), dtype=BF16), i32(2))
+    assert rec.told[0][1] == dec.kv.k.data_ptr() != old.data_ptr()
