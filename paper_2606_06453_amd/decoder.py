@@ -110,9 +110,20 @@ class SparseDecoder:
             (self.kv.ref(), self.batch.ref(), first_page.data_ptr(), vx._ptr(self.mean), vx._ptr(self.mean_bf16),
              vx._ptr(self.max), vx._ptr(self.min), None), 7))(stream)
 
+    def _check_rows(self, k_new: torch.Tensor, v_new: Optional[torch.Tensor]):
+        """New rows are bf16 for an mxfp4 cache, which quantises them, else elements of the cache's type
+        (or their bits in another type of its size)."""
+        want = self.kv.row_dtype
+        for t in (k_new, v_new):
+            if t is None or t.dtype is want:
+                continue
+            if want is not self.kv.k.dtype or t.element_size() != self.kv.k.element_size():
+                raise TypeError(f"new rows must be {want} (got {t.dtype})")
+
     def append(self, k_new: torch.Tensor, v_new: Optional[torch.Tensor], stream=None):
         """The step's cache stage in one launch: new K/V rows at token seq_lens[i]-1, then that
         page's summaries."""
+        self._check_rows(k_new, v_new)
         assert k_new.is_contiguous() and (v_new is None or v_new.is_contiguous())
         self._bound_call(("append", k_new.data_ptr(), None if v_new is None else v_new.data_ptr()),
                          lambda: vx.BoundCall(
@@ -132,8 +143,9 @@ class SparseDecoder:
 
     def append_select(self, k_new: torch.Tensor, v_new: Optional[torch.Tensor], q: torch.Tensor,
                       pages_budget: torch.Tensor, stream=None):
-        """append() then select(), with the append inside the top-K launch when that is exact
-        (vx_append_score_topk)."""
+        """append() then select(), with the append inside the top-K launch where vx_append_score_topk
+        puts it there (never for an mxfp4 cache, whose append is a launch of its own)."""
+        self._check_rows(k_new, v_new)
         assert k_new.is_contiguous() and (v_new is None or v_new.is_contiguous())
         assert q.is_contiguous() and pages_budget.is_contiguous()
         key = ("append_select", k_new.data_ptr(), None if v_new is None else v_new.data_ptr(), q.data_ptr(),
@@ -161,7 +173,7 @@ class SparseDecoder:
     def step(self, q: torch.Tensor, pages_budget: torch.Tensor, first_page: Optional[torch.Tensor],
              stream=None, kv_new=None) -> torch.Tensor:
         """One decode step: refresh the newest page's summary (with kv_new = (k_new, v_new): append
-        the new rows and refresh them inside the selection's launches), select, attend."""
+        the new rows and refresh it, as append_select does), select, attend."""
         if kv_new is not None:
             self.append_select(kv_new[0], kv_new[1], q, pages_budget, stream)
         else:

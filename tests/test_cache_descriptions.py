@@ -231,3 +231,23 @@ def test_a_new_decoder_describes_the_cache_as_it_is(monkeypatch):
     rec.told.clear()
     other.select(torch.zeros((2, 4, 128), dtype=BF16), i32(2))
     assert rec.told[0][1] == dec.kv.k.data_ptr() != old.data_ptr()
+
+
+@pytest.mark.parametrize("dtype,good,bad", [
+    (torch.uint8, (BF16,), (torch.uint8, torch.float16, torch.float32)),      # mxfp4: rows are quantised by the append
+    (BF16, (BF16, torch.int16), (torch.float32, E4M3, torch.uint8)),
+    (E4M3, (E4M3, torch.uint8), (BF16, torch.float32)),                       # codes, or their bytes
+])
+def test_a_decoder_checks_the_type_of_new_rows(monkeypatch, dtype, good, bad):
+    dec, _, i32, _ = _decoder(monkeypatch, dtype)
+    q, budget = torch.zeros((2, 4, 128), dtype=BF16), i32(2)
+    row = lambda t: torch.zeros((2, 2, 128), dtype=t)  # noqa: E731
+    for t in good:
+        dec.append(row(t), row(t))
+        dec.append_select(row(t), row(t), q, budget)
+    for t in bad:
+        for rows in ((row(t), row(good[0])), (row(good[0]), row(t))):
+            for call in (lambda: dec.append(*rows), lambda: dec.append_select(*rows, q, budget),
+                         lambda: dec.step(q, budget, None, kv_new=rows)):
+                with pytest.raises(TypeError, match="new rows"):
+                    call()
