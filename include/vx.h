@@ -465,7 +465,9 @@ vx_status vx_page_workspace_size(int32_t batch, size_t* bytes);
  *   first_block [batch] or NULL   L_i / block_size: the first block whose summary changes
  *                                 (first_page of vx_page_summarize)
  * rows must differ from each other; a row outside the table is refused and has no pages.  An empty
- * batch writes nothing.  seq_lens must not be pool->lens. */
+ * batch writes nothing.  No array that the call writes (the outputs, the workspace and the pool's
+ * free_count, table and lens) may overlap another of its arrays: granted cannot be new_lens, nor
+ * seq_lens the pool's lens. */
 vx_status vx_page_extend(const vx_page_pool* pool, int32_t batch, const int32_t* rows, const int32_t* new_lens,
                          int32_t* seq_lens, int32_t* page_indptr, int32_t* page_indices, int32_t page_indices_cap,
                          int32_t* token_indptr, int64_t* slots, int32_t slots_cap, int32_t* granted,
@@ -475,7 +477,8 @@ vx_status vx_page_extend(const vx_page_pool* pool, int32_t batch, const int32_t*
  * ended); its pages past them go back to the stack, the first one listed (in the order of the batch
  * and of each row) on top, so that a release to the former lengths takes a vx_page_extend of the same
  * rows back exactly.  rows must differ from each other; rows outside the table are skipped.  A page
- * that other rows or requests still use must not be released here. */
+ * that other rows or requests still use must not be released here.  The workspace and the
+ * pool's free_pages, free_count and lens must not overlap another of the call's arrays. */
 vx_status vx_page_release(const vx_page_pool* pool, int32_t batch, const int32_t* rows, const int32_t* keep_lens,
                           void* workspace, size_t workspace_bytes, hipStream_t stream);
 

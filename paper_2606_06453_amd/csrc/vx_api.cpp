@@ -495,6 +495,28 @@ vx_status check_plan(const vx_page_pool* pool, int32_t batch, const int32_t* row
   return VX_OK;
 }
 
+// An array of a page plan.
+struct Span {
+  const char* name;
+  const void* p;
+  size_t bytes;
+  bool written;
+};
+
+// The workgroups of a plan read its inputs and the pool while others write the outputs: no array that a
+// call writes may share a byte with another one.
+vx_status check_apart(const Span* s, int n) {
+  for (int i = 0; i < n; i++) {
+    for (int j = i + 1; j < n; j++) {
+      if (!(s[i].written || s[j].written) || s[i].bytes == 0 || s[j].bytes == 0) continue;
+      const uintptr_t a = reinterpret_cast<uintptr_t>(s[i].p), b = reinterpret_cast<uintptr_t>(s[j].p);
+      if (a < b + s[j].bytes && b < a + s[i].bytes)
+        return fail(VX_ERR_INVALID_ARG, "%s and %s overlap", s[i].name, s[j].name);
+    }
+  }
+  return VX_OK;
+}
+
 }  // namespace
 
 vx_status vx_kv_write(const vx_paged_cache* kv, const void* k_new, int64_t k_row_stride, int64_t k_head_stride,
@@ -530,6 +552,25 @@ vx_status vx_page_extend(const vx_page_pool* pool, int32_t batch, const int32_t*
                     (page_indices_cap > 0 && !page_indices) || (slots_cap > 0 && !slots)))
     return fail(VX_ERR_INVALID_ARG, "new_lens, seq_lens, page_indptr, page_indices, token_indptr, slots and granted "
                                     "must be non-NULL");
+  const size_t n = batch > 0 ? (size_t)batch : 0, w = sizeof(int32_t);
+  const Span spans[] = {
+      {"rows", rows, n * w, false},
+      {"new_lens", new_lens, n * w, false},
+      {"free_pages", pool->free_pages, (size_t)pool->num_phys_pages * w, false},
+      {"free_count", pool->free_count, w, true},
+      {"table", pool->table, (size_t)pool->table_rows * pool->table_stride * w, true},
+      {"lens", pool->lens, (size_t)pool->table_rows * w, true},
+      {"seq_lens", seq_lens, n * w, true},
+      {"page_indptr", page_indptr, (n + 1) * w, true},
+      {"page_indices", page_indices, (size_t)page_indices_cap * w, true},
+      {"token_indptr", token_indptr, (n + 1) * w, true},
+      {"slots", slots, (size_t)slots_cap * sizeof(int64_t), true},
+      {"granted", granted, n * w, true},
+      {"first_block", first_block, first_block ? n * w : 0, true},
+      {"workspace", workspace, vx::plan_workspace_bytes(batch), true},
+  };
+  vx_status apart;
+  if (batch > 0 && (apart = check_apart(spans, (int)(sizeof spans / sizeof spans[0]))) != VX_OK) return apart;
   return hip_status(vx::launch_page_extend(pool_of(pool), batch, rows, new_lens, seq_lens, page_indptr, page_indices,
                                            page_indices_cap, token_indptr, slots, slots_cap, granted, first_block,
                                            workspace, stream),
@@ -540,6 +581,18 @@ vx_status vx_page_release(const vx_page_pool* pool, int32_t batch, const int32_t
                           void* workspace, size_t workspace_bytes, hipStream_t stream) {
   const vx_status s = check_plan(pool, batch, rows, workspace, workspace_bytes);
   if (s != VX_OK) return s;
+  const size_t n = batch > 0 ? (size_t)batch : 0, w = sizeof(int32_t);
+  const Span spans[] = {
+      {"rows", rows, n * w, false},
+      {"keep_lens", keep_lens, keep_lens ? n * w : 0, false},
+      {"table", pool->table, (size_t)pool->table_rows * pool->table_stride * w, false},
+      {"free_pages", pool->free_pages, (size_t)pool->num_phys_pages * w, true},
+      {"free_count", pool->free_count, w, true},
+      {"lens", pool->lens, (size_t)pool->table_rows * w, true},
+      {"workspace", workspace, vx::plan_workspace_bytes(batch), true},
+  };
+  vx_status apart;
+  if (batch > 0 && (apart = check_apart(spans, (int)(sizeof spans / sizeof spans[0]))) != VX_OK) return apart;
   return hip_status(vx::launch_page_release(pool_of(pool), batch, rows, keep_lens, workspace, stream),
                     "vx_page_release");
 }

@@ -1,0 +1,60 @@
+"""Arrays of the cache's own operators that overlap are refused before any launch
+(no GPU needed: every call here is refused)."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2606_06453_amd import vx
+
+B, ROWS, STRIDE, PHYS = 4, 6, 8, 40
+SLAB = torch.zeros(1 << 16, dtype=torch.uint8)
+
+
+def _place(sizes):
+    """An address for every array, apart from each other."""
+    at, places = SLAB.data_ptr() + (-SLAB.data_ptr()) % 256, {}
+    for name, n in sizes.items():
+        places[name] = at
+        at += (n + 255) // 256 * 256 + 512
+    assert at < SLAB.data_ptr() + SLAB.numel()
+    return places
+
+
+POOL = dict(free_pages=4 * PHYS, free_count=4, table=4 * ROWS * STRIDE, lens=4 * ROWS)
+EXTEND = dict(POOL, rows=4 * B, new_lens=4 * B, seq_lens=4 * B, page_indptr=4 * (B + 1), page_indices=4 * 9,
+              token_indptr=4 * (B + 1), slots=8 * 11, granted=4 * B, first_block=4 * B, workspace=256)
+RELEASE = dict(POOL, rows=4 * B, keep_lens=4 * B, workspace=256)
+READ = {"extend": {"free_pages", "rows", "new_lens"}, "release": {"table", "rows", "keep_lens"}}
+
+
+def _call(op, at):
+    pool = vx._Pool(at["free_pages"], at["free_count"], at["table"], at["lens"], PHYS, ROWS, STRIDE, 16, 0)
+    if op == "release":
+        return vx.lib().vx_page_release(ctypes.byref(pool), B, at["rows"], at["keep_lens"], at["workspace"], 256, None)
+    return vx.lib().vx_page_extend(ctypes.byref(pool), B, at["rows"], at["new_lens"], at["seq_lens"], at["page_indptr"],
+                                   at["page_indices"], 9, at["token_indptr"], at["slots"], 11, at["granted"],
+                                   at["first_block"], at["workspace"], 256, None)
+
+
+def _msg():
+    return vx.lib().vx_last_error().decode()
+
+
+@pytest.mark.parametrize("op", ["extend", "release"])
+def test_arrays_that_overlap(op):
+    """Every pair of which the call writes one: the same address, and the last bytes of one the first of the other."""
+    sizes = EXTEND if op == "extend" else RELEASE
+    names, seen = list(sizes), 0
+    for a in names:
+        for b in names:
+            if a == b or {a, b} <= READ[op]:
+                continue
+            step = 8 if "slots" in (a, b) else 4
+            for shift in {0, sizes[a] - step} if sizes[a] > step else {0}:
+                at = _place(sizes)
+                at[b] = at[a] + shift
+                assert _call(op, at) == 1, (a, b, shift)
+                assert a in _msg() and b in _msg() and "overlap" in _msg(), (a, b, _msg())
+                seen += 1
+    assert seen > 2 * len(names)
