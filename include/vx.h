@@ -442,7 +442,8 @@ typedef struct {
 } vx_page_pool;
 
 /* Host-only: workspace bytes of vx_page_extend and vx_page_release for a batch.  The buffer holds a
- * counter: zero-fill it once after allocating it; every call leaves it zero again. */
+ * counter: zero-fill it once after allocating it; every call leaves it zero again.  It is 4-byte
+ * aligned, as every int32 array of these calls; slots are 8-byte aligned. */
 vx_status vx_page_workspace_size(int32_t batch, size_t* bytes);
 
 /* A step's tokens get their pages and slots (Sec. 4.1, C = (b, p, I)).  Request i is row rows[i]

@@ -446,6 +446,8 @@ vx_status kv_rows(const vx_paged_cache* kv, const void* k, int64_t k_row, int64_
   if ((reinterpret_cast<uintptr_t>(kv->k) & 15) != 0 || (reinterpret_cast<uintptr_t>(kv->v) & 15) != 0)
     return fail(VX_ERR_INVALID_ARG, "the caches must be 16-byte aligned");
   if (!slots) return fail(VX_ERR_INVALID_ARG, "slots must be non-NULL");
+  if (reinterpret_cast<uintptr_t>(slots) % sizeof(int64_t) != 0)
+    return fail(VX_ERR_INVALID_ARG, "slots must be %zu-byte aligned", sizeof(int64_t));
   if ((s = check_rows(write ? "k_new" : "k_out", k, k_row, k_head)) != VX_OK)
     return s;
   if (!kv->v && v) return fail(VX_ERR_INVALID_ARG, "V rows given but V is aliased to K (kv->v is NULL)");
@@ -501,11 +503,17 @@ struct Span {
   const void* p;
   size_t bytes;
   bool written;
+  size_t align = sizeof(int32_t);
 };
 
 // The workgroups of a plan read its inputs and the pool while others write the outputs: no array that a
-// call writes may share a byte with another one.
-vx_status check_apart(const Span* s, int n) {
+// call writes may share a byte with another one.  Each lies at its elements' alignment (the workspace's
+// counter is one of 32 bits).
+vx_status check_spans(const Span* s, int n) {
+  for (int i = 0; i < n; i++) {
+    if (reinterpret_cast<uintptr_t>(s[i].p) % s[i].align != 0)
+      return fail(VX_ERR_INVALID_ARG, "%s must be %zu-byte aligned", s[i].name, s[i].align);
+  }
   for (int i = 0; i < n; i++) {
     for (int j = i + 1; j < n; j++) {
       if (!(s[i].written || s[j].written) || s[i].bytes == 0 || s[j].bytes == 0) continue;
@@ -564,13 +572,13 @@ vx_status vx_page_extend(const vx_page_pool* pool, int32_t batch, const int32_t*
       {"page_indptr", page_indptr, (n + 1) * w, true},
       {"page_indices", page_indices, (size_t)page_indices_cap * w, true},
       {"token_indptr", token_indptr, (n + 1) * w, true},
-      {"slots", slots, (size_t)slots_cap * sizeof(int64_t), true},
+      {"slots", slots, (size_t)slots_cap * sizeof(int64_t), true, sizeof(int64_t)},
       {"granted", granted, n * w, true},
       {"first_block", first_block, first_block ? n * w : 0, true},
       {"workspace", workspace, vx::plan_workspace_bytes(batch), true},
   };
-  vx_status apart;
-  if (batch > 0 && (apart = check_apart(spans, (int)(sizeof spans / sizeof spans[0]))) != VX_OK) return apart;
+  vx_status bad;
+  if (batch > 0 && (bad = check_spans(spans, (int)(sizeof spans / sizeof spans[0]))) != VX_OK) return bad;
   return hip_status(vx::launch_page_extend(pool_of(pool), batch, rows, new_lens, seq_lens, page_indptr, page_indices,
                                            page_indices_cap, token_indptr, slots, slots_cap, granted, first_block,
                                            workspace, stream),
@@ -591,8 +599,8 @@ vx_status vx_page_release(const vx_page_pool* pool, int32_t batch, const int32_t
       {"lens", pool->lens, (size_t)pool->table_rows * w, true},
       {"workspace", workspace, vx::plan_workspace_bytes(batch), true},
   };
-  vx_status apart;
-  if (batch > 0 && (apart = check_apart(spans, (int)(sizeof spans / sizeof spans[0]))) != VX_OK) return apart;
+  vx_status bad;
+  if (batch > 0 && (bad = check_spans(spans, (int)(sizeof spans / sizeof spans[0]))) != VX_OK) return bad;
   return hip_status(vx::launch_page_release(pool_of(pool), batch, rows, keep_lens, workspace, stream),
                     "vx_page_release");
 }

@@ -1,4 +1,4 @@
-"""Arrays of the cache's own operators that overlap are refused before any launch
+"""Arrays of the cache's own operators that overlap or lie at odd addresses are refused before any launch
 (no GPU needed: every call here is refused)."""
 import ctypes
 
@@ -58,3 +58,19 @@ def test_arrays_that_overlap(op):
                 assert a in _msg() and b in _msg() and "overlap" in _msg(), (a, b, _msg())
                 seen += 1
     assert seen > 2 * len(names)
+@pytest.mark.parametrize("op", ["extend", "release"])
+def test_odd_addresses(op):
+    sizes = EXTEND if op == "extend" else RELEASE
+    for name in sizes:
+        for off in (1, 2) + ((4,) if name == "slots" else ()):
+            at = _place(sizes)
+            at[name] += off
+            assert _call(op, at) == 1 and name in _msg() and "aligned" in _msg(), (name, off, _msg())
+
+
+def test_odd_slots_of_rows():
+    at = _place(dict(k=8192, v=8192, rows=8192, slots=80))
+    kv = vx._Cache(at["k"], at["v"], 2, 2, 16, 64, 64, vx.KV_BF16, 1.0, 1.0, 0)
+    for fn in (vx.lib().vx_kv_write, vx.lib().vx_kv_read):
+        assert fn(ctypes.byref(kv), at["rows"], 128, 64, at["rows"] + 4096, 128, 64, at["slots"] + 4, 3, None) == 1
+        assert "slots" in _msg() and "aligned" in _msg()
