@@ -511,16 +511,16 @@ struct Span {
 // counter is one of 32 bits).
 vx_status check_spans(const Span* s, int n) {
   for (int i = 0; i < n; i++) {
-    if (reinterpret_cast<uintptr_t>(s[i].p) % s[i].align != 0)
-      return fail(VX_ERR_INVALID_ARG, "%s must be %zu-byte aligned", s[i].name, s[i].align);
-  }
-  for (int i = 0; i < n; i++) {
     for (int j = i + 1; j < n; j++) {
       if (!(s[i].written || s[j].written) || s[i].bytes == 0 || s[j].bytes == 0) continue;
       const uintptr_t a = reinterpret_cast<uintptr_t>(s[i].p), b = reinterpret_cast<uintptr_t>(s[j].p);
       if (a < b + s[j].bytes && b < a + s[i].bytes)
         return fail(VX_ERR_INVALID_ARG, "%s and %s overlap", s[i].name, s[j].name);
     }
+  }
+  for (int i = 0; i < n; i++) {
+    if (reinterpret_cast<uintptr_t>(s[i].p) % s[i].align != 0)
+      return fail(VX_ERR_INVALID_ARG, "%s must be %zu-byte aligned", s[i].name, s[i].align);
   }
   return VX_OK;
 }
