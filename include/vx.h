@@ -412,7 +412,8 @@ vx_status vx_sparse_paged_decode(const void* q, int32_t num_q_heads,
  * outputs, with no workspace argument.  Its split counters and partials live in a static
  * 12 MiB device buffer of the library, one per GPU, held until the process ends; the call
  * itself allocates nothing.  A batch whose decode workspace (vx_workspace_size with
- * VX_STAGE_DECODE) exceeds 12 MiB returns VX_ERR_WORKSPACE.  Every call on a GPU shares that
+ * VX_STAGE_DECODE) exceeds 12 MiB returns VX_ERR_WORKSPACE; on an mxfp4 cache it is cut into fewer
+ * splits instead, whose partials fit (its sums are then in another order).  Every call on a GPU shares that
  * GPU's buffer: calls that overlap on one GPU (different streams, or other host threads) race
  * and give wrong results; serialise them.  The buffer is zero when the library loads, and every
  * call leaves its split counters zero again. */

@@ -999,8 +999,10 @@ __global__ __launch_bounds__(kMergeThreads) void merge_kernel(int S, int H, int 
 }  // namespace
 
 DecodeLayout decode_layout(int batch, int num_kv_heads, int group, int head_dim_v, int max_sel,
-                           int block_size, bool mla, bool mx) {
+                           int block_size, bool mla, bool mx, size_t scratch) {
   DecodeLayout L;
+  auto al = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  const size_t counters = al(sizeof(uint32_t) * kSplitPairs);
   const long long pairs = (long long)batch * num_kv_heads;
   const long long ms = max_sel > 0 ? max_sel : 1;
   const long long cus = std::min(device_cus(), kSplitPairs / kMxWgsPerCu);   // the counters' places
@@ -1031,6 +1033,11 @@ DecodeLayout decode_layout(int batch, int num_kv_heads, int group, int head_dim_
     // 18.7, 32 15.3, 64 17.0; one KV head, 8 query heads, 131072 tokens: 32 30.6, 64 21.6, 128 21.0, 256 27.9;
     // one query head of 64 channels, 32000 tokens: 32 10.8, 64 8.8, 128 8.3, 256 10.3.
     S = std::min(S, (long long)std::sqrt((double)ms * block_size * 32 / (group * head_dim_v)));
+    // No more partials than the scratch holds (rows of an output, a maximum and a sum; 512 bytes for the
+    // two alignments).  From 12 heads of 128 channels a KV head the rounds above can pass 12 MiB: 32 requests
+    // of 32768 tokens, 8 KV heads of 16, 9 splits 228 us, the 5 that fit 218; of 12, 9 splits 222, 7 221.
+    const size_t row = sizeof(float) * (size_t)group * (head_dim_v + 2);
+    if (S > 1 && scratch > counters + 512) S = std::min(S, (long long)((scratch - counters - 512) / row) / pairs);
     S = std::max(S, 1LL);
     const long long T = (ms + S - 1) / S;
     S = (ms + T - 1) / T;
@@ -1056,12 +1063,11 @@ DecodeLayout decode_layout(int batch, int num_kv_heads, int group, int head_dim_
     L.split_slots = (int)T;
     L.n_wg = pairs * S;
   }
-  auto al = [](size_t x) { return (x + 255) & ~(size_t)255; };
   const long long rows = pairs * L.splits;
   // Only batches of at most kSplitPairs pairs split any, and the counters keep their place in every
   // layout: a buffer that batches of other sizes have used still has them at zero.
   L.off_ctr = 0;
-  size_t off = al(sizeof(uint32_t) * kSplitPairs);
+  size_t off = counters;
   L.off_lse = off;
   off = al(off + sizeof(float) * (size_t)rows * group * (mx ? 2 : 1));   // mxfp4: maximum and sum apart
   L.off_o = off;

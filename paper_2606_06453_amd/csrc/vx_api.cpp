@@ -409,13 +409,13 @@ vx_status vx_sparse_paged_decode_noalloc(const void* q, int32_t num_q_heads, con
                                          int32_t max_sel, float sm_scale, void* out, hipStream_t stream) {
   vx_status s = check_decode(q, num_q_heads, kv, b, sel_pages, sel_count, max_sel, sm_scale, out);
   if (s != VX_OK) return s;
-  const vx::DecodeLayout lay = vx::decode_layout(b->batch, kv->num_kv_heads, num_q_heads / kv->num_kv_heads,
-                                                 kv->head_dim_v, max_sel,
-                                                 block_tokens(kv), is_mla(kv), kv->kv_dtype == VX_KV_MXFP4);
   void* scratch = nullptr;
   size_t scratch_bytes = 0;
   if ((s = hip_status(vx::noalloc_scratch(&scratch, &scratch_bytes), "vx_sparse_paged_decode_noalloc")) != VX_OK)
     return s;
+  const vx::DecodeLayout lay = vx::decode_layout(b->batch, kv->num_kv_heads, num_q_heads / kv->num_kv_heads,
+                                                 kv->head_dim_v, max_sel, block_tokens(kv), is_mla(kv),
+                                                 kv->kv_dtype == VX_KV_MXFP4, scratch_bytes);
   if (lay.total > scratch_bytes)
     return fail(VX_ERR_WORKSPACE,
                 "vx_sparse_paged_decode_noalloc: this batch needs %zu bytes of scratch, more than the %zu-byte "

@@ -26,8 +26,10 @@ struct DecodeLayout {
 // Compute units of the current device (256 when the query fails).
 int device_cus();
 
+// scratch: the bytes that an mxfp4 layout has to fit (with no splits it always does); the others do not
+// depend on it.
 DecodeLayout decode_layout(int batch, int num_kv_heads, int group, int head_dim_v, int max_sel,
-                           int block_size, bool mla, bool mx);
+                           int block_size, bool mla, bool mx, size_t scratch = SIZE_MAX);
 
 // fp32 planes [H][B][stride] of the score stage: max(2 H, Hq + H) of them.  Plane 0 holds the
 // scores (or lower bounds), plane 1 the upper bounds; the NSA and smoothing flows put their
