@@ -14,9 +14,10 @@
 //   O^T += V^T P^T  MFMA 16x16x32 over the 32 tokens: a lane's V codes are one piece (D/16 channels) of
 //                 four tokens side by side, widened and paired by tokens (v_perm).  P's layout is that
 //                 of S^T, 4 tokens of each tile per lane, and V^T's rows follow it.
-// P is the sum of two bf16 parts, hi = p cut to 8 bits and lo = (p - hi) cut to 8, 2^-15 of p.  With at
-// most 8 query heads per KV head the 16 columns hold every head twice, the hi parts in columns 0 to 7
-// and the lo parts in 8 to 15, so one MFMA per operand does both; else two.
+// P is the sum of two bf16 parts, hi = p and lo = p - hi, each to the nearest: 2^-17 of p, unbiased as the
+// weights' sum needs (parts cut to 8 bits are up to 0.5% faster, but 2^-15 too small: 0.6% of the
+// outputs were not the nearest bf16, now 0.2%).  With at most 8 query heads per KV head the 16 columns hold every head twice, the hi parts in columns 0 to 7 and the
+// lo parts in 8 to 15, so one MFMA per operand does both; else two.
 //
 // D = 128, 8 KV heads: 64 requests of 128 selected pages of 16 and 32 query heads take 29.2 us (4.9 TB/s
 // of the cache; the launches' start and the merge are the rest), 128 requests of 256 blocks of 32 and 48
@@ -126,15 +127,21 @@ __device__ __forceinline__ void mx_mask(int valid, int grp, f32x4_t& st, MxTile<
   }
 }
 
-__device__ __forceinline__ uint32_t high_halves(float lo, float hi) {
-  return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+// Two floats as packed bf16, to the nearest even (one instruction).
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((float2_t{lo, hi}), mx::bf16x2_t));
 }
 
-// A round of two tiles with va and vb valid tokens.  G8: at most 8 query heads, lo_mask 0 in the columns of
-// the hi parts and the upper half's bits in those of the lo parts.
+// Which halves of a packed pair a lane takes off as floats: both in the columns of the lo parts (a v_perm
+// selector and a mask), none in those of the hi parts.
+struct LoPart {
+  uint32_t low, high;
+};
+
+// A round of two tiles with va and vb valid tokens.  G8: at most 8 query heads, lo by the lane's column.
 template <int D, bool G8>
 __device__ __forceinline__ void mx_round(MxTile<D> (&t)[2], int va, int vb, const bf16x8_t (&qv)[D / 32], int grp,
-                                         float scale_log2, uint32_t lo_mask, float& m, float& lsum,
+                                         float scale_log2, const LoPart& lo, float& m, float& lsum,
                                          f32x4_t (&acc)[D / 16]) {
   f32x4_t sa = mx_scores<D>(t[0], qv), sb = mx_scores<D>(t[1], qv);
   if (va < 16) mx_mask<D>(va, grp, sa, t[0]);               // uniform
@@ -171,16 +178,18 @@ __device__ __forceinline__ void mx_round(MxTile<D> (&t)[2], int va, int vb, cons
     p[i] = __builtin_amdgcn_exp2f(z[i] - m);
   }
   lsum += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-  auto cut = [&](uint32_t mask) {
-    float x[8];
+  // the hi parts, and what is left of each p (G8: in the columns of the lo parts; p itself in the others)
+  const u32x4_t hi = {pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])};
+  float x[8];
 #pragma unroll
-    for (int i = 0; i < 8; i++) x[i] = p[i] - __uint_as_float(__float_as_uint(p[i]) & mask);
-    return __builtin_bit_cast(bf16x8_t, (u32x4_t{high_halves(x[0], x[1]), high_halves(x[2], x[3]),
-                                                  high_halves(x[4], x[5]), high_halves(x[6], x[7])}));
-  };
-  const bf16x8_t p0 = cut(G8 ? lo_mask : 0u);
-  bf16x8_t p1{};
-  if constexpr (!G8) p1 = cut(0xffff0000u);
+  for (int i = 0; i < 8; i += 2) {
+    const uint32_t h = hi[i >> 1];
+    x[i] = p[i] - __uint_as_float(G8 ? __builtin_amdgcn_perm(0u, h, lo.low) : h << 16);
+    x[i + 1] = p[i + 1] - __uint_as_float(h & (G8 ? lo.high : 0xffff0000u));
+  }
+  const bf16x8_t left = __builtin_bit_cast(
+      bf16x8_t, (u32x4_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])}));
+  const bf16x8_t p0 = G8 ? left : __builtin_bit_cast(bf16x8_t, hi), p1 = left;
 #pragma unroll
   for (int x = 0; x < D / 32; x++) {                        // channel pair x of every piece
     uint32_t wa[4], wb[4];
@@ -213,7 +222,7 @@ __device__ __forceinline__ void mx_wave_slots(const DecodeArgs& a, int i, int h,
   constexpr int KS = D / 32;
   const int col = lane & 15, grp = lane >> 4;
   const int head = G8 ? (col & 7) : col;
-  const uint32_t lo_mask = G8 && col >= 8 ? 0xffff0000u : 0u;
+  const LoPart part = G8 && col >= 8 ? LoPart{0x01000c0cu, 0xffff0000u} : LoPart{0x0c0c0c0cu, 0u};
 #pragma unroll
   for (int j = 0; j < D / 16; j++) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   m = kNoMax;
@@ -278,11 +287,11 @@ __device__ __forceinline__ void mx_wave_slots(const DecodeArgs& a, int i, int h,
     for (int u = 0;; u += 4) {
       load(u + 2, n[0]);
       load(u + 3, n[1]);
-      mx_round<D, G8>(t, valid(u), valid(u + 1), qv, grp, a.scale_log2, lo_mask, m, lsum, acc);
+      mx_round<D, G8>(t, valid(u), valid(u + 1), qv, grp, a.scale_log2, part, m, lsum, acc);
       if (u + 2 >= tiles) break;
       load(u + 4, t[0]);
       load(u + 5, t[1]);
-      mx_round<D, G8>(n, valid(u + 2), valid(u + 3), qv, grp, a.scale_log2, lo_mask, m, lsum, acc);
+      mx_round<D, G8>(n, valid(u + 2), valid(u + 3), qv, grp, a.scale_log2, part, m, lsum, acc);
       if (u + 4 >= tiles) break;
     }
   }
