@@ -161,21 +161,27 @@ class PagedKV:
     block_size: int = 0      # 0: one block per page; else 16 or 32 dividing the page size
 
     def struct(self) -> _Cache:
-        P, H, ps, Dqk = self.k.shape
-        Dv = self.v.shape[3] if self.v is not None else (self.head_dim_v or Dqk)
-        dt = kv_dtype_code(self.k)
-        if self.v is not None:
-            if kv_dtype_code(self.v) != dt:
+        k, v = self.k, self.v
+        P, H, ps, Dqk = k.shape
+        dt = kv_dtype_code(k)
+        if v is None:
+            Dv = self.head_dim_v or (self._mx_dim(Dqk) if dt == KV_MXFP4 else Dqk)
+        else:
+            Pv, Hv, psv, Dv = v.shape
+            if v.dtype is not k.dtype:
+                kv_dtype_code(v)
                 raise TypeError("K and V caches must have the same dtype")
-            if self.v.device != self.k.device:
-                raise ValueError(f"K and V caches must be on one device (got {self.k.device} and {self.v.device})")
-            if self.v.shape[1] != H or self.v.shape[2] != ps or self.v.shape[0] < P:
-                raise ValueError(f"the V cache must have K's pages, KV heads and page size (got {tuple(self.v.shape)} "
-                                 f"beside {tuple(self.k.shape)})")
+            d = k.get_device()
+            if v.get_device() != d or (d < 0 and v.device != k.device):
+                raise ValueError(f"K and V caches must be on one device (got {k.device} and {v.device})")
+            if Hv != H or psv != ps or Pv < P:
+                raise ValueError(f"the V cache must have K's pages, KV heads and page size (got {tuple(v.shape)} "
+                                 f"beside {tuple(k.shape)})")
         if dt == KV_MXFP4:
-            Dqk = self._mx_dim(Dqk)
-            Dv = self._mx_dim(Dv) if self.v is not None else (self.head_dim_v or Dqk)
-        return _Cache(_ptr(self.k), _ptr(self.v), P, H, ps, Dqk, Dv, dt, float(self.k_scale), float(self.v_scale),
+            row, Dqk = Dqk, self._mx_dim(Dqk)
+            if v is not None:
+                Dv = Dqk if Dv == row else self._mx_dim(Dv)
+        return _Cache(_ptr(k), _ptr(v), P, H, ps, Dqk, Dv, dt, float(self.k_scale), float(self.v_scale),
                       int(self.block_size))
 
     @staticmethod
@@ -259,21 +265,31 @@ class PagePool:
                    torch.zeros((table_rows, table_stride), **i32), torch.zeros(table_rows, **i32), page_size, block_size)
 
     def struct(self) -> _Pool:
-        """The pool as it is now: every call describes it anew, so its tensors may be replaced."""
-        free, count, table, lens = self.free_pages, self.free_count, self.table, self.lens
-        i32, d = torch.int32, table.get_device()
-        if not (free.dtype is i32 and count.dtype is i32 and table.dtype is i32 and lens.dtype is i32
-                and free.get_device() == d and count.get_device() == d and lens.get_device() == d):
-            for t, n in ((free, "free_pages"), (count, "free_count"), (table, "table"), (lens, "lens")):
-                if t.dtype is not i32 or t.get_device() != d:
-                    raise TypeError(f"{n} must be int32 on {table.device} (got {t.dtype} on {t.device})")
-        rows, stride = table.shape
-        if lens.numel() != rows:
-            raise ValueError(f"lens has {lens.numel()} entries for {rows} table rows")
-        if count.numel() < 1:
+        for n in ("free_pages", "free_count", "table", "lens"):
+            t = getattr(self, n)
+            if t.dtype != torch.int32 or t.device != self.table.device:
+                raise TypeError(f"{n} must be int32 on {self.table.device} (got {t.dtype} on {t.device})")
+        rows, stride = self.table.shape
+        if self.lens.numel() != rows:
+            raise ValueError(f"lens has {self.lens.numel()} entries for {rows} table rows")
+        if self.free_count.numel() < 1:
             raise ValueError("free_count must have an entry")
-        return _Pool(_ptr(free), count.data_ptr(), _ptr(table), _ptr(lens), free.numel(), rows, stride,
-                     int(self.page_size), int(self.block_size))
+        return _Pool(_ptr(self.free_pages), _ptr(self.free_count), _ptr(self.table), _ptr(self.lens),
+                     self.free_pages.numel(), rows, stride, int(self.page_size), int(self.block_size))
+
+    def __setattr__(self, name, value):
+        self.__dict__[name] = value
+        self.__dict__["_ref"] = None
+
+    def current(self):
+        """A by-reference argument holding this pool as it is now: built again where a field has been
+        assigned, or a tensor has other memory, since."""
+        at = (self.free_pages.data_ptr(), self.free_count.data_ptr(), self.table.data_ptr(), self.lens.data_ptr())
+        kept = self.__dict__["_ref"]
+        if kept is None or kept[0] != at:
+            st = self.struct()
+            kept = self.__dict__["_ref"] = (at, ctypes.byref(st))
+        return kept[1]
 
 
 def _gpu_of(t: torch.Tensor) -> int:
@@ -310,11 +326,12 @@ def page_extend(pool: PagePool, rows: torch.Tensor, new_lens: torch.Tensor, batc
     (int64), granted and first_block as include/vx.h says.  workspace: page_workspace_size bytes,
     zero-filled once."""
     B, i32, d = rows.numel(), torch.int32, _gpu_of(pool.table)
-    for t, n, name in ((rows, B, "rows"), (new_lens, B, "new_lens"), (batch.seq_lens, B, "seq_lens"),
-                       (batch.page_indptr, B + 1, "page_indptr"), (token_indptr, B + 1, "token_indptr"),
-                       (granted, B, "granted")):
+    seq_lens, page_indptr = batch.seq_lens, batch.page_indptr
+    for t, n in ((rows, B), (new_lens, B), (seq_lens, B), (page_indptr, B + 1), (token_indptr, B + 1), (granted, B)):
         if t.dtype is not i32 or t.numel() != n or t.get_device() != d or not t.is_contiguous():
-            _refuse(t, i32, n, name)
+            names = {id(rows): "rows", id(new_lens): "new_lens", id(seq_lens): "seq_lens", id(page_indptr): "page_indptr",
+                     id(token_indptr): "token_indptr", id(granted): "granted"}
+            _refuse(t, i32, n, names[id(t)])
     first = None
     if first_block is not None:
         if first_block.dtype is not i32 or first_block.numel() != B or first_block.get_device() != d:
@@ -327,7 +344,7 @@ def page_extend(pool: PagePool, rows: torch.Tensor, new_lens: torch.Tensor, batc
         _refuse(slots, torch.int64, None, "slots")
     if workspace.get_device() != d:
         _refuse(workspace, workspace.dtype, None, "workspace")
-    _check(lib().vx_page_extend(ctypes.byref(pool.struct()), B, rows.data_ptr(), new_lens.data_ptr(),
+    _check(lib().vx_page_extend(pool.current(), B, rows.data_ptr(), new_lens.data_ptr(),
                                 batch.seq_lens.data_ptr(), batch.page_indptr.data_ptr(), _ptr(pages), pages.numel(),
                                 token_indptr.data_ptr(), _ptr(slots), slots.numel(), granted.data_ptr(), first, _ptr(workspace),
                                 workspace.numel() * workspace.element_size(), _stream(stream, d)))
@@ -343,7 +360,7 @@ def page_release(pool: PagePool, rows: torch.Tensor, keep_lens: Optional[torch.T
         _refuse(keep_lens, i32, B, "keep_lens")
     if workspace.get_device() != d:
         _refuse(workspace, workspace.dtype, None, "workspace")
-    _check(lib().vx_page_release(ctypes.byref(pool.struct()), B, _ptr(rows), _ptr(keep_lens), _ptr(workspace),
+    _check(lib().vx_page_release(pool.current(), B, _ptr(rows), _ptr(keep_lens), _ptr(workspace),
                                  workspace.numel() * workspace.element_size(), _stream(stream, d)))
 
 
