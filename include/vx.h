@@ -487,7 +487,8 @@ vx_status vx_page_release(const vx_page_pool* pool, int32_t batch, const int32_t
 /* Rows into the cache by slot: row n of k_new and v_new, bf16, goes to token slots[n] % page_size of
  * page slots[n] / page_size, for every KV head.
  *   k_new[n * k_row_stride + h * k_head_stride + c], v_new alike (strides in elements, any sign,
- *   multiples of 8; rows 16-byte aligned); v_new NULL when V is aliased.
+ *   multiples of 8; rows 16-byte aligned; the stride of a dimension of one entry is not looked at); v_new
+ *   NULL when V is aliased.
  *   bf16   the value itself
  *   fp8    the code nearest to the fp32 quotient value / scale, ties to the even code; larger
  *          magnitudes, infinities too, become the largest finite one; NaN stays NaN

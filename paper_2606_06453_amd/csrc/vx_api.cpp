@@ -429,10 +429,12 @@ vx_status vx_sparse_paged_decode_noalloc(const void* q, int32_t num_q_heads, con
 
 namespace {
 
-// Rows of vx_kv_write and vx_kv_read: 16-byte accesses of 8 channels.
-vx_status check_rows(const char* name, const void* rows, int64_t row_stride, int64_t head_stride) {
+// Rows [n][heads][D] of vx_kv_write and vx_kv_read: 16-byte accesses of 8 channels.  The stride of a
+// dimension of one entry is not looked at.
+vx_status check_rows(const char* name, const void* rows, int n, int heads, int64_t row_stride, int64_t head_stride) {
   if (!rows) return fail(VX_ERR_INVALID_ARG, "%s must be non-NULL", name);
-  if ((reinterpret_cast<uintptr_t>(rows) & 15) != 0 || row_stride % 8 != 0 || head_stride % 8 != 0)
+  if ((reinterpret_cast<uintptr_t>(rows) & 15) != 0 || (n > 1 && row_stride % 8 != 0) ||
+      (heads > 1 && head_stride % 8 != 0))
     return fail(VX_ERR_INVALID_ARG, "%s must be 16-byte aligned with strides of whole 8 elements", name);
   return VX_OK;
 }
@@ -448,12 +450,10 @@ vx_status kv_rows(const vx_paged_cache* kv, const void* k, int64_t k_row, int64_
   if (!slots) return fail(VX_ERR_INVALID_ARG, "slots must be non-NULL");
   if (reinterpret_cast<uintptr_t>(slots) % sizeof(int64_t) != 0)
     return fail(VX_ERR_INVALID_ARG, "slots must be %zu-byte aligned", sizeof(int64_t));
-  if ((s = check_rows(write ? "k_new" : "k_out", k, k_row, k_head)) != VX_OK)
-    return s;
+  const int H = kv->num_kv_heads;
+  if ((s = check_rows(write ? "k_new" : "k_out", k, n, H, k_row, k_head)) != VX_OK) return s;
   if (!kv->v && v) return fail(VX_ERR_INVALID_ARG, "V rows given but V is aliased to K (kv->v is NULL)");
-  if (kv->v &&
-      (s = check_rows(write ? "v_new" : "v_out", v, v_row, v_head)) != VX_OK)
-    return s;
+  if (kv->v && (s = check_rows(write ? "v_new" : "v_out", v, n, H, v_row, v_head)) != VX_OK) return s;
   vx_batch none{};
   const vx::RowView kr{k, k_row, k_head}, vr{v, v_row, v_head};
   const vx::Geometry g = geometry(kv, &none);

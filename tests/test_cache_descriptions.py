@@ -251,3 +251,11 @@ def test_a_decoder_checks_the_type_of_new_rows(monkeypatch, dtype, good, bad):
                          lambda: dec.step(q, budget, None, kv_new=rows)):
                 with pytest.raises(TypeError, match="new rows"):
                     call()
+
+
+def test_a_pool_whose_tensor_takes_other_memory(monkeypatch):
+    pool = vx.PagePool.empty(6, 3, 4, 16, device="cpu")
+    old = [_pool_told(monkeypatch, pool), pool.table.data]
+    pool.table.data = torch.zeros((3, 9), dtype=torch.int32)
+    for told in _pool_told(monkeypatch, pool):
+        assert (told["table"], told["table_stride"]) == (pool.table.data_ptr(), 9) and told != old[0][0]
