@@ -199,24 +199,27 @@ class PagedKV:
         """Element type of new rows at a decode step: the cache's own, bf16 for an mxfp4 cache."""
         return torch.bfloat16 if kv_dtype_code(self.k) == KV_MXFP4 else self.k.dtype
 
+    def __setattr__(self, name, value):
+        self.__dict__[name] = value
+        self.__dict__["_ref"] = None
+
     def ref(self):
-        """A by-reference argument holding this geometry, built once; current() follows tensors that
-        are replaced afterwards."""
-        if getattr(self, "_ref", None) is None:
-            self._st = self.struct()
-            self._ref = ctypes.byref(self._st)
+        """A by-reference argument holding this geometry, built once for the fields' present values."""
+        if self._ref is None:
+            self.__dict__["_st"] = self.struct()
+            self.__dict__["_ref"] = ctypes.byref(self._st)
+            self.__dict__["_seen"] = self._tensors()
         return self._ref
 
-    def current(self):
-        """ref(), built again where anything that struct() reads has changed since."""
+    def _tensors(self):
         k, v = self.k, self.v
-        now = (k.data_ptr(), k.dtype, k.shape, k.is_contiguous(), k.get_device(), self.head_dim_v, self.k_scale,
-               self.v_scale, self.block_size,
-               None if v is None else (v.data_ptr(), v.dtype, v.shape, v.is_contiguous(), v.get_device()))
-        if getattr(self, "_seen", None) != now:
-            self._ref = self._seen = None
-            self.ref()
-            self._seen = now
+        return (k.data_ptr(), k.shape, k.is_contiguous(),
+                None if v is None else (v.data_ptr(), v.shape, v.is_contiguous()))
+
+    def current(self):
+        """ref(), built again where a tensor has taken other memory or another shape in place."""
+        if self._ref is not None and self._seen != self._tensors():
+            self.__dict__["_ref"] = None
         return self.ref()
 
 
