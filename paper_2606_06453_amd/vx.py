@@ -213,11 +213,11 @@ class PagedKV:
 
     def _tensors(self):
         k, v = self.k, self.v
-        return (k.data_ptr(), k.shape, k.is_contiguous(),
-                None if v is None else (v.data_ptr(), v.shape, v.is_contiguous()))
+        return (k.data_ptr(), k.dtype, k.shape, k.is_contiguous(),
+                None if v is None else (v.data_ptr(), v.dtype, v.shape, v.is_contiguous()))
 
     def current(self):
-        """ref(), built again where a tensor has taken other memory or another shape in place."""
+        """ref(), built again where a tensor has taken other memory, another type or shape in place."""
         if self._ref is not None and self._seen != self._tensors():
             self.__dict__["_ref"] = None
         return self.ref()

@@ -61,6 +61,15 @@ def test_a_cache_turned_into_a_view_is_refused():
         kv.current()
 
 
+def test_a_tensor_that_changes_in_place():
+    kv, bufs = _kv(dtype=E4M3)
+    _told(kv)
+    kv.k.data, kv.v.data = (_on(b, 3, 2, 16, 64, E5M2) for b in bufs)
+    assert _told(kv)["kv_dtype"] == vx.KV_FP8_E5M2 and _told(kv) == _fresh(kv)
+    kv.k.data, kv.v.data = (_on(b, 2, 2, 16, 64, E5M2) for b in bufs)
+    assert _told(kv)["num_phys_pages"] == 2 and _told(kv) == _fresh(kv)
+
+
 def test_an_unchanged_cache_keeps_its_description():
     kv, _ = _kv()
     assert kv.current() is kv.current()
