@@ -504,7 +504,8 @@ vx_status vx_kv_write(const vx_paged_cache* kv, const void* k_new, int64_t k_row
 
 /* Rows out of the cache by slot: the values of token slots[n], rounded to bf16 (exact for bf16 and
  * mxfp4 caches), to k_out and v_out laid out as the rows of vx_kv_write; zeros for a slot below 0
- * or past the cache.  Slots may repeat. */
+ * or past the cache.  Slots may repeat.  No two of the rows written, of k_out or of v_out, may share an
+ * element (strides that make rows of one of them overlap are refused). */
 vx_status vx_kv_read(const vx_paged_cache* kv, void* k_out, int64_t k_row_stride, int64_t k_head_stride, void* v_out,
                      int64_t v_row_stride, int64_t v_head_stride, const int64_t* slots, int32_t num_rows,
                      hipStream_t stream);

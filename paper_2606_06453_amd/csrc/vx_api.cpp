@@ -439,6 +439,24 @@ vx_status check_rows(const char* name, const void* rows, int n, int heads, int64
   return VX_OK;
 }
 
+// Whether two of the rows [n][heads][D] share an element: rows r and heads h apart do if |r row + h head| < D.
+// For each h the nearest r are looked at.
+bool rows_overlap(int n, int heads, int D, int64_t row, int64_t head) {
+  if (n > 1 && row < D && row > -D) return true;
+  constexpr int64_t kFar = INT64_MAX / 64;               // past it a stride brings no two rows together
+  const bool apart = n == 1 || row > kFar || row < -kFar;
+  if (head > kFar || head < -kFar) return false;
+  for (int h = 1; h < heads; h++) {
+    const int64_t at = h * head, near = apart ? 0 : -at / row;
+    for (int64_t r = near - 1; r <= near + 1; r++) {
+      if (r <= -n || r >= n || (apart && r != 0)) continue;
+      const int64_t d = apart ? at : r * row + at;
+      if (d < D && d > -D) return true;
+    }
+  }
+  return false;
+}
+
 vx_status kv_rows(const vx_paged_cache* kv, const void* k, int64_t k_row, int64_t k_head, const void* v, int64_t v_row,
                   int64_t v_head, const int64_t* slots, int32_t n, bool write, hipStream_t stream, const char* name) {
   vx_status s;
@@ -454,6 +472,11 @@ vx_status kv_rows(const vx_paged_cache* kv, const void* k, int64_t k_row, int64_
   if ((s = check_rows(write ? "k_new" : "k_out", k, n, H, k_row, k_head)) != VX_OK) return s;
   if (!kv->v && v) return fail(VX_ERR_INVALID_ARG, "V rows given but V is aliased to K (kv->v is NULL)");
   if (kv->v && (s = check_rows(write ? "v_new" : "v_out", v, n, H, v_row, v_head)) != VX_OK) return s;
+  if (!write) {                            // stored at the same time; rows that are only read may overlap
+    if (rows_overlap(n, H, kv->head_dim_qk, k_row, k_head)) return fail(VX_ERR_INVALID_ARG, "rows of k_out overlap");
+    if (kv->v && rows_overlap(n, H, kv->head_dim_v, v_row, v_head))
+      return fail(VX_ERR_INVALID_ARG, "rows of v_out overlap");
+  }
   vx_batch none{};
   const vx::RowView kr{k, k_row, k_head}, vr{v, v_row, v_head};
   const vx::Geometry g = geometry(kv, &none);

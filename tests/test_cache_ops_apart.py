@@ -74,3 +74,30 @@ def test_odd_slots_of_rows():
     for fn in (vx.lib().vx_kv_write, vx.lib().vx_kv_read):
         assert fn(ctypes.byref(kv), at["rows"], 128, 64, at["rows"] + 4096, 128, 64, at["slots"] + 4, 3, None) == 1
         assert "slots" in _msg() and "aligned" in _msg()
+
+
+def _first_overlap(n, heads, row, head, dim):
+    """Whether two of the rows at r * row + h * head, `dim` long, share an element: by looking at all of them."""
+    at = sorted(r * row + h * head for r in range(n) for h in range(heads))
+    return any(b - a < dim for a, b in zip(at, at[1:]))
+
+
+def test_rows_read_into_one_another():
+    """vx_kv_read stores every row at the same time; rows of k_out or v_out that overlap are refused."""
+    at = _place(dict(k=8192, v=8192, rows=16384, slots=800))
+    L, D, seen = vx.lib(), 64, {False: 0, True: 0}
+    strides = [0, 8, 56, 64, 72, 128, 136, 192, 256, 264, 320, 512, 1024, -64, -128, -192, -1024]
+    for heads in (1, 2, 4):
+        kv = vx._Cache(at["k"], at["v"], 2, heads, 16, D, D, vx.KV_BF16, 1.0, 1.0, 0)
+        for n in (1, 2, 3, 7):
+            for row in strides:
+                for head in strides:
+                    bad = _first_overlap(n, heads, row, head, D)
+                    seen[bad] += 1
+                    if not bad:
+                        continue                                     # a call that would be made
+                    good = (heads * D, D)
+                    for a, b, name in (((row, head), good, "k_out"), (good, (row, head), "v_out")):
+                        assert L.vx_kv_read(ctypes.byref(kv), at["rows"], *a, at["rows"] + 8192, *b, at["slots"], n, None) == 1
+                        assert name in _msg() and "overlap" in _msg(), (heads, n, row, head, _msg())
+    assert min(seen.values()) > 100

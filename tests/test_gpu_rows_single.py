@@ -45,3 +45,28 @@ def test_the_stride_of_a_single_entry(mx, n, H, strides):
         vx.kv_read(kv, slots, ko, vo)
         torch.cuda.synchronize()
         assert torch.equal(ko.cpu(), want[0]) and torch.equal(vo.cpu(), want[1])
+
+
+@pytest.mark.parametrize("row,head", [(192, 128), (-192, 128), (64, 640), (136, 1224)])
+def test_rows_between_rows(row, head):
+    """Layouts whose rows and heads lie between each other without meeting are read into."""
+    H, n, D, ps = 2, 9, 64, 16
+    kv = vx.PagedKV(vx.mxfp4_cache(2, H, ps, D), vx.mxfp4_cache(2, H, ps, D))
+    x = torch.randn((2, n, H, D), generator=torch.Generator().manual_seed(row + head)).to(torch.bfloat16).cuda()
+    slots = torch.randperm(2 * ps, generator=torch.Generator().manual_seed(2))[:n].cuda()
+    vx.kv_write(kv, x[0], x[1], slots)
+    want = torch.zeros_like(x)
+    vx.kv_read(kv, slots, want[0], want[1])
+    buf = torch.full((2, 4096), 7.0, dtype=torch.bfloat16, device="cuda")
+    first = 8 * -row if row < 0 else 0
+    s = torch.cuda.current_stream().cuda_stream
+    assert vx.lib().vx_kv_read(kv.ref(), buf[0, first:].data_ptr(), row, head, buf[1, first:].data_ptr(), row, head,
+                               slots.data_ptr(), n, s) == 0
+    torch.cuda.synchronize()
+    taken = torch.zeros(4096, dtype=torch.bool)
+    for r in range(n):
+        for h in range(H):
+            at = first + r * row + h * head
+            taken[at:at + D] = True
+            assert torch.equal(buf[:, at:at + D], want[:, r, h])
+    assert (buf.cpu()[:, ~taken] == 7.0).all()
