@@ -295,6 +295,9 @@ class PagePool:
         return kept[1]
 
 
+_MOST = 2 ** 31 - 1      # what the calls' 32-bit counts hold
+
+
 def _gpu_of(t: torch.Tensor) -> int:
     """The current GPU, which t has to be on: the kernels take addresses, and another device's or the
     host's would fault it."""
@@ -347,9 +350,9 @@ def page_extend(pool: PagePool, rows: torch.Tensor, new_lens: torch.Tensor, batc
         _refuse(slots, torch.int64, None, "slots")
     if workspace.get_device() != d:
         _refuse(workspace, workspace.dtype, None, "workspace")
-    _check(lib().vx_page_extend(pool.current(), B, rows.data_ptr(), new_lens.data_ptr(),
-                                batch.seq_lens.data_ptr(), batch.page_indptr.data_ptr(), _ptr(pages), pages.numel(),
-                                token_indptr.data_ptr(), _ptr(slots), slots.numel(), granted.data_ptr(), first, _ptr(workspace),
+    _check(lib().vx_page_extend(pool.current(), B, rows.data_ptr(), new_lens.data_ptr(), seq_lens.data_ptr(),
+                                page_indptr.data_ptr(), _ptr(pages), min(pages.numel(), _MOST), token_indptr.data_ptr(),
+                                _ptr(slots), min(slots.numel(), _MOST), granted.data_ptr(), first, _ptr(workspace),
                                 workspace.numel() * workspace.element_size(), _stream(stream, d)))
 
 
@@ -385,6 +388,8 @@ def _kv_rows(fn, kv: PagedKV, slots: torch.Tensor, k: torch.Tensor, v: Optional[
     if slots.dtype is not torch.int64 or slots.get_device() != d:
         _refuse(slots, torch.int64, None, "slots")
     n, st = slots.numel(), kv._st
+    if n > _MOST:
+        raise ValueError(f"at most {_MOST} rows a call (got {n})")
     k_args = _row_args(k, n, st.num_kv_heads, st.head_dim_qk, d, names[0])
     v_args = _row_args(v, n, st.num_kv_heads, st.head_dim_v, d, names[1])
     _check(fn(c, *k_args, *v_args, _ptr(slots), n, _stream(stream, d)))

@@ -268,3 +268,37 @@ def test_a_pool_whose_tensor_takes_other_memory(monkeypatch):
     pool.table.data = torch.zeros((3, 9), dtype=torch.int32)
     for told in _pool_told(monkeypatch, pool):
         assert (told["table"], told["table_stride"]) == (pool.table.data_ptr(), 9) and told != old[0][0]
+
+
+def test_counts_past_31_bits(monkeypatch):
+    """Entries past what a call's 32-bit count holds: a capacity is the largest count, rows are refused."""
+    told = {}
+
+    class Lib:
+        @staticmethod
+        def vx_page_extend(*a):
+            told["caps"] = a[7], a[10]
+            return 0
+
+        @staticmethod
+        def vx_kv_write(*a):
+            raise AssertionError("called with a cut count")
+
+        vx_kv_read = vx_kv_write
+
+    monkeypatch.setattr(vx, "lib", lambda: Lib)
+    monkeypatch.setattr(vx, "_gpu_of", lambda t: t.get_device())
+    monkeypatch.setattr(vx, "_stream", lambda *a: None)
+    monkeypatch.setattr(vx, "_ptr", lambda t: None if t is None else t.data_ptr())
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    wide = lambda n, t: torch.zeros(1, dtype=t).expand(n)  # noqa: E731
+    big = 2 ** 32 + 5
+    vx.page_extend(vx.PagePool.empty(6, 3, 4, 16, device="cpu"), i32(2), i32(2),
+                   vx.BatchSpec(i32(3), wide(big, torch.int32), i32(2), 4), i32(3), wide(big, torch.int64), i32(2), i32(64))
+    assert told["caps"] == (2 ** 31 - 1, 2 ** 31 - 1)
+    kv = vx.PagedKV(torch.zeros((1, 1, 16, 576), dtype=BF16), None, 512)
+    rows = torch.zeros((1, 1, 576), dtype=BF16).expand(big, 1, 576)
+    with pytest.raises(ValueError, match="rows"):
+        vx.kv_write(kv, rows, None, wide(big, torch.int64))
+    with pytest.raises(ValueError, match="rows"):
+        vx.kv_read(kv, wide(big, torch.int64), rows, None)
