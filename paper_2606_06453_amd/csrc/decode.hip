@@ -1033,7 +1033,7 @@ DecodeLayout decode_layout(int batch, int num_kv_heads, int group, int head_dim_
     // 18.7, 32 15.3, 64 17.0; one KV head, 8 query heads, 131072 tokens: 32 30.6, 64 21.6, 128 21.0, 256 27.9;
     // one query head of 64 channels, 32000 tokens: 32 10.8, 64 8.8, 128 8.3, 256 10.3.
     S = std::min(S, (long long)std::sqrt((double)ms * block_size * 32 / (group * head_dim_v)));
-    // No more partials than the scratch holds (rows of an output, a maximum and a sum; 512 bytes for the
+    // No more partials than the scratch holds (rows of an output, a bound and a sum; 512 bytes for the
     // two alignments).  From 12 heads of 128 channels a KV head the rounds above can pass 12 MiB: 32 requests
     // of 32768 tokens, 8 KV heads of 16, 9 splits 228 us, the 5 that fit 218; of 12, 9 splits 222, 7 221.
     const size_t row = sizeof(float) * (size_t)group * (head_dim_v + 2);
@@ -1069,7 +1069,7 @@ DecodeLayout decode_layout(int batch, int num_kv_heads, int group, int head_dim_
   L.off_ctr = 0;
   size_t off = counters;
   L.off_lse = off;
-  off = al(off + sizeof(float) * (size_t)rows * group * (mx ? 2 : 1));   // mxfp4: maximum and sum apart
+  off = al(off + sizeof(float) * (size_t)rows * group * (mx ? 2 : 1));   // mxfp4: bound and sum apart
   L.off_o = off;
   off = al(off + sizeof(float) * (size_t)rows * group * head_dim_v);
   L.total = L.splits > 1 ? off : 256;      // no partials when no pair can be split

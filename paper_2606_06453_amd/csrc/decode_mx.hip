@@ -7,17 +7,18 @@
 //   S^T = K Q^T   MFMA 16x16x32 per tile: a lane's K codes are D/4 consecutive channels of one token
 //                 (one load), widened with their scale by the E2M1 conversion (a code times a power
 //                 of two is a bf16 value, so nothing is rounded)
-//   softmax       log2 domain.  The running maximum of a head moves only when a score passes it by
-//                 more than 2^8: below that the probabilities stay under 256, which fp32 sums and the
-//                 two bf16 parts carry as exactly as values below 1, and a round needs no exchange
-//                 between lanes
+//   softmax       log2 domain, against a running bound of a head's scores instead of their maximum.  A score
+//                 that passes it moves it 2^8 past that score; until the next one does, a round needs no
+//                 exchange between lanes.  Weights are at most 1, as against the maximum (2^-8 for the score
+//                 that moved the bound: fp32 sums and the two bf16 parts carry those as exactly)
 //   O^T += V^T P^T  MFMA 16x16x32 over the 32 tokens: a lane's V codes are one piece (D/16 channels) of
 //                 four tokens side by side, widened and paired by tokens (v_perm).  P's layout is that
 //                 of S^T, 4 tokens of each tile per lane, and V^T's rows follow it.
 // P is the sum of two bf16 parts, hi = p and lo = p - hi, each to the nearest: 2^-17 of p, unbiased as the
-// weights' sum needs (parts cut to 8 bits are up to 0.5% faster, but 2^-15 too small: 0.6% of the
-// outputs were not the nearest bf16, now 0.2%).  With at most 8 query heads per KV head the 16 columns hold every head twice, the hi parts in columns 0 to 7 and the
-// lo parts in 8 to 15, so one MFMA per operand does both; else two.
+// weights' sum needs (parts cut to 8 bits are up to 0.5% faster, but 2^-15 too small: 0.6% of the outputs
+// were not the nearest bf16, now 0.2%).  With at most 8 query heads per KV head the 16 columns hold every
+// head twice, the hi parts in columns 0 to 7 and the lo parts in 8 to 15, so one MFMA per operand does
+// both; else two.
 //
 // D = 128, 8 KV heads: 64 requests of 128 selected pages of 16 and 32 query heads take 29.2 us (4.9 TB/s
 // of the cache; the launches' start and the merge are the rest), 128 requests of 256 blocks of 32 and 48
@@ -32,8 +33,8 @@ using namespace dec;
 namespace {
 
 constexpr int kMxWaves = 4;               // per workgroup
-constexpr float kRescaleLog2 = 8.f;
-constexpr float kNoMax = -3.4028234e38f;  // running maximum before the first token: no score is below it
+constexpr float kRoomLog2 = 8.f;
+constexpr float kNoMax = -3.4028234e38f;  // running bound before the first token: no score is below it
 
 template <int D>
 struct MxTile {
@@ -146,7 +147,7 @@ __device__ __forceinline__ void mx_round(MxTile<D> (&t)[2], int va, int vb, cons
   f32x4_t sa = mx_scores<D>(t[0], qv), sb = mx_scores<D>(t[1], qv);
   if (va < 16) mx_mask<D>(va, grp, sa, t[0]);               // uniform
   if (vb < 16) mx_mask<D>(vb, grp, sb, t[1]);
-  // Scaled and rounded before the maximum is taken off (a fused form would leave the product's rounding
+  // Scaled and rounded before the bound is taken off (a fused form would leave the product's rounding
   // error in the exponent, which overflows for scores past 2^30).
   float z[8];
 #pragma unroll
@@ -156,10 +157,10 @@ __device__ __forceinline__ void mx_round(MxTile<D> (&t)[2], int va, int vb, cons
     z[4 + i] = sb[i] * scale_log2;
   }
   float mt = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
-  if (__builtin_amdgcn_ballot_w64(mt > m + kRescaleLog2) != 0) {
+  if (__builtin_amdgcn_ballot_w64(mt > m) != 0) {
     mt = fmaxf(mt, xor_shfl(mt, 16));
     mt = fmaxf(mt, xor_shfl(mt, 32));
-    const float m_new = fmaxf(m, mt);
+    const float m_new = fmaxf(m, mt + kRoomLog2);
     const float alpha = __builtin_amdgcn_exp2f(m - m_new);
     m = m_new;
     lsum *= alpha;
@@ -303,8 +304,8 @@ __device__ __forceinline__ void put_merged(uint16_t* dst, float W, const float4&
                                               f32_to_bf16_rne(o.z * inv) | (f32_to_bf16_rne(o.w * inv) << 16));
 }
 
-// A partial's running maximum and sum.  Their log-sum-exp in one float would round at the maximum's
-// magnitude: at scores of 2^24 a split's weight would be off by half.
+// A partial's running bound (no score is above it) and sum.  Their log-sum-exp in one float would round at
+// the bound's magnitude: at scores of 2^24 a split's weight would be off by half.
 typedef unsigned int u32x2v_t __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ void put_state(__amdgpu_buffer_rsrc_t r, uint32_t row, float m, float l) {
   __builtin_amdgcn_raw_buffer_store_b64((u32x2v_t{__float_as_uint(m), __float_as_uint(l)}), r, (int)(row * 8u), 0,

@@ -12,7 +12,7 @@ namespace vx {
 // splits past the count exit at once.  A pair with one split is written directly; the splits
 // of a split pair merge in the split kernel through the pair's counter.
 // MLA: `splits` workgroups per request over fixed slot ranges, merged by a merge launch.
-// Partials: fp32 output and log2-sum-exp (mxfp4: maximum and sum) per query head, `splits` rows per pair.
+// Partials: fp32 output and log2-sum-exp (mxfp4: running bound and sum) per query head, `splits` rows per pair.
 // Workspace: 1024 uint32 split counters (GQA; zero before the first call, every call leaves them
 // zero), then the partials.
 struct DecodeLayout {

@@ -48,3 +48,25 @@ def test_weights_of_cancelling_rows(D, g):
     assert (got == got[..., :1]).all()
     err = np.abs(got[..., 0] - ref)
     assert (err <= 2.0 ** -8 * np.abs(ref) + 2.0 ** -17 * inexact + 2.0 ** -20 * absv).all(), float((err / inexact).max() * 2 ** 17)
+
+
+@pytest.mark.parametrize("g", [2, 16])
+@pytest.mark.parametrize("top", [4.0, 7.5])
+def test_the_largest_values(g, top):
+    """Values of V at the type's largest, 6 2^125: no weight passes 1, so a dominant row does not leave fp32, also
+    when its score lies above an earlier one by less than the running maximum's step of 2^8."""
+    D, n = 128, 64
+    p = _problem(3, 2, g, D, 64, 64, [n] * 3, 1, [g, int(top)], poison=False)
+    k, v = np.zeros((len(p["kc"]), 2, 64, D)), np.zeros((len(p["kc"]), 2, 64, D))
+    k[:, :, :, 0] = -6.0                                            # rows without weight: score -6 * 32
+    k[:, :, 3, 0], k[:, :, 3, 1] = 0.0, 0.0                         # one early row, score 0
+    k[:, :, 40, 0], k[:, :, 40, 1] = 0.0, 1.0                       # one later row, score top * ln 2
+    v[:] = np.where(np.arange(D) % 2, -6.0, 6.0) * 2.0 ** 125
+    p["kc"], p["vc"], p["scale"] = _mx.pack(k, "k"), _mx.pack(v, "v"), 1.0
+    q = np.zeros((3, 2 * g, D))
+    q[..., 0], q[..., 1] = 32.0, top * np.log(2)
+    p["q"] = torch.from_numpy(q).to(torch.bfloat16)
+    got = _launch(p)
+    want = v[0, 0, 0]
+    # every row has the same values: the weights' errors (2^-17), sums and division are far below bf16's 2^-8
+    assert (np.abs(got - want) <= 2.0 ** -8 * np.abs(want)).all(), got[0, 0, :4]
