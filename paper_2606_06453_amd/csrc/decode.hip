@@ -1018,20 +1018,20 @@ DecodeLayout decode_layout(int batch, int num_kv_heads, int group, int head_dim_
     // Three 4-wave workgroups (168 VGPRs) are resident on a CU.  Few pairs: one workgroup per CU, down to a
     // slot per wave.  While not every resident place has a pair of its own, long selections are cut
     // further, three rounds of workgroups deep, into splits of at least kMxSplitTokens: ragged counts
-    // fill the chip (24 requests of up to 20000 tokens, 64 channels, 8 KV heads: 3 splits 50.7 us, 6
-    // 42.7, 10 40.8; 2048 selected pages of 16 from 100 to 32000 tokens 112 us, in splits of 4096 tokens
-    // 123) and equal ones lose little (24 requests of 32768 tokens 159.5 us, in splits of 4096 154).  A
-    // short selection is not cut for more than a workgroup per CU: 128 pages of 16 for 32 requests of 8 KV
-    // heads, one split 17.2 us, two 19.1; 64 requests 29.4 and 35.9.
+    // fill the chip (24 requests of up to 20000 tokens, 64 channels, 8 KV heads: 3 splits 49.8 us, 6 40.7,
+    // 10 39.1; 32 requests of 100 to 32000 tokens, 2048 pages of 16: 2 splits 153, 4 126, 8 122) and equal
+    // ones lose little (24 requests of 32768 tokens: 4 splits 155, 8 151, 16 158).  A short selection is
+    // not cut for more than a workgroup per CU: 128 pages of 16 for 32 requests of 8 KV heads, one split
+    // 17.8 us, two 19.8; 64 requests 30.4 and 37.8.
     const long long resident = cus * kMxWgsPerCu;
     long long S = pairs > 0 ? (cus + pairs - 1) / pairs : 1;
     S = std::min(S, (ms + kDecodeWaves - 1) / kDecodeWaves);
     if (pairs > 0 && pairs < resident) S = std::max(S, std::min(3 * resident / pairs, ms * block_size / kMxSplitTokens));
     // Every split adds to the merge of its pair (group * channels / 4 threads of a workgroup take 8 of
     // them a round trip) and takes from the stream of each: the sum is least at the square root.  One
-    // request of 8 KV heads, 4 query heads each, 2048 tokens: 8 to 16 splits 7.7 us, 32 9.9; 32768 tokens: 16
-    // 18.7, 32 15.3, 64 17.0; one KV head, 8 query heads, 131072 tokens: 32 30.6, 64 21.6, 128 21.0, 256 27.9;
-    // one query head of 64 channels, 32000 tokens: 32 10.8, 64 8.8, 128 8.3, 256 10.3.
+    // request of 8 KV heads, 4 query heads each, 2048 tokens: 8 to 16 splits 7.9 us, 32 10.2; 32768 tokens: 16
+    // 18.0, 32 15.2, 64 17.5; one KV head, 8 query heads, 131072 tokens: 32 29.9, 64 21.7, 128 21.8, 256 29.9;
+    // one query head of 64 channels, 32000 tokens: 32 10.9, 64 8.9, 128 8.5, 256 10.5.
     S = std::min(S, (long long)std::sqrt((double)ms * block_size * 32 / (group * head_dim_v)));
     // No more partials than the scratch holds (rows of an output, a bound and a sum; 512 bytes for the
     // two alignments).  From 12 heads of 128 channels a KV head the rounds above can pass 12 MiB: 32 requests

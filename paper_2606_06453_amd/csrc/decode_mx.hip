@@ -22,7 +22,10 @@
 //
 // D = 128, 8 KV heads: 64 requests of 128 selected pages of 16 and 32 query heads take 29.2 us (4.9 TB/s
 // of the cache; the launches' start and the merge are the rest), 128 requests of 256 blocks of 32 and 48
-// query heads 181 us (6.0 TB/s, a long read's rate being 6.3), one request 8.3 us.
+// query heads 180 us (6.0 TB/s, a long read's rate being 6.3), one request 8.4 us.  Vector instructions take
+// 55% and 65% of the CU cycles of the first two.  With 16 query heads per KV head, two MFMAs per operand,
+// 64 requests take 31.8 us instead of 30.1; 32 requests of 32768 tokens 197 us at 1 head, 205 at 4, 213 at 8, 228
+// at 16 (floor 181).
 #include <algorithm>
 
 #include "decode_common.h"

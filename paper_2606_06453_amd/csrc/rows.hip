@@ -8,6 +8,8 @@
 // 100003 rows of 4 heads of 128 channels written and 50001 read, in random order: E4M3 86 us (5.3 TB/s),
 // bf16 112 us (5.5), mxfp4 96 us (4.1: a lone V row touches four times its bytes).  Two or four tasks a
 // thread are no faster there, and 64 rows take 3.2 and 4.1 us instead of 2.7.
+// The MLA latent (576 channels, K alone), 100003 rows in random order: bf16 written 44.8 us (5.2 TB/s) and read
+// 41.8 (5.5), E4M3 38.7 (4.5) and 34.4 (5.0); 64 rows 2.1 to 2.3 us.
 #include "mxfp4.h"
 #include "vx_device.h"
 #include "vx_internal.h"

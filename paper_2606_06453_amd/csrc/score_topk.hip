@@ -2765,6 +2765,9 @@ hipError_t launch_score_topk(const Geometry& g, const uint16_t* q, int Hq, int k
   // everything when the selection reads every block's score (the flows couple the pages; the
   // radix path is not fused).  An mxfp4 append, which quantises its rows, is a launch ahead too: inside,
   // it takes every selection kernel of the bins from 75 registers to 80 and spills for all cache types.
+  // The launch costs a step 4 to 5 us: append and selection of 64 requests of 8k to 32k tokens, block mean, 51.6 us
+  // (E4M3 47.9, bf16 47.6), of 4 requests 18.1 (13.2, 13.3); with the attention, 81.6 (101.6, 140.9) and 27.5
+  // (25.8, 27.2).
   AppendStep ap{};
   if (sa.k_new) {
     if (approx || g.max_pages > kTwoPassMaxPages || flow || g.kv_dtype == kKvMxFp4) {

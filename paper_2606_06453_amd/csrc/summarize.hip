@@ -24,7 +24,9 @@
 // value rows are written at token L_i - 1, and the page holding it is summarised in the same
 // pass.  The new key row is taken from the step's input, not read back, and enters the
 // running sums last, exactly where a separate summarize pass over the page would add it, so
-// the summaries are bit-identical to an append followed by vx_page_summarize.
+// the summaries are bit-identical to an append followed by vx_page_summarize.  An mxfp4 append quantises its
+// rows on the way: 64 requests of 8 KV heads of 128 channels, pages of 16, Mean with its bf16 copy, 5.5 us (E4M3 and
+// bf16 4.5), 4 requests 4.8 (4.3 and 4.1); all of them the latency of their dependent reads.
 //
 // Blocks below the page size (r = ps / bs blocks per page): the unit is the block.  Logical
 // block j of request i is block j % r of physical page indices[j / r], its summary row is
