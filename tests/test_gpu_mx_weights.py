@@ -70,3 +70,24 @@ def test_the_largest_values(g, top):
     want = v[0, 0, 0]
     # every row has the same values: the weights' errors (2^-17), sums and division are far below bf16's 2^-8
     assert (np.abs(got - want) <= 2.0 ** -8 * np.abs(want)).all(), got[0, 0, :4]
+
+
+@pytest.mark.parametrize("g", [2, 16])
+def test_the_smallest_values(g):
+    """Values of V at the type's smallest scale, 2^-120 to 6 2^-119: the weighted sums below fp32's normal range keep
+    2^-149, 2^-20 of the smallest weight (2^-8) times the smallest value in each of the 40 rows."""
+    D, n = 128, 40
+    p = _problem(3, 2, g, D, 16, 16, [n] * 3, 3, [g, 3], poison=False)
+    rng = np.random.default_rng(g)
+    v = rng.choice([0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], size=(len(p["kc"]), 2, 16, D)) * 2.0 ** -119
+    v[..., ::32] = 2.0 ** -119 * 6.0                                # every group's largest: its scale is 2^-119
+    p["vc"] = _mx.pack(v, "v")
+    assert np.array_equal(_mx.unpack(p["vc"], "v"), v)
+    got, k = _launch(p), _mx.unpack(p["kc"], "k")
+    q = p["q"].double().numpy()
+    for i in range(3):
+        pg, pos = p["perm"][p["indptr"][i] + np.arange(n) // 16], np.arange(n) % 16
+        for h in range(2):
+            ref, absv, qk = _mx.attend(q[i, h * g:(h + 1) * g], k[pg, h, pos], v[pg, h, pos], p["scale"])
+            tol = _mx.attend_tolerance(ref * 2.0 ** 119, absv * 2.0 ** 119, qk, p["scale"], D, n) * 2.0 ** -119
+            assert (np.abs(got[i, h * g:(h + 1) * g] - ref) <= tol + n * 2.0 ** -20 * absv).all()
