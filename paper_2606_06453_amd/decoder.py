@@ -71,17 +71,20 @@ class SparseDecoder:
         kv.current()
         b.current()
         # the tensors themselves are held, so that another one is never taken for one of them
-        self._held = (kv.k, kv.k.data_ptr(), kv.v, None if kv.v is None else kv.v.data_ptr(), kv.k_scale, kv.v_scale,
-                      kv.block_size, kv.head_dim_v, b.page_indptr, b.page_indices, b.seq_lens, b.max_pages_per_seq)
+        self._held = (kv.k, kv.v, b.page_indptr, b.page_indices, b.seq_lens, self._places())
+
+    def _places(self):
+        kv, b = self.kv, self.batch
+        return (kv.k.data_ptr(), None if kv.v is None else kv.v.data_ptr(), b.page_indptr.data_ptr(),
+                b.page_indices.data_ptr(), b.seq_lens.data_ptr(), kv.k_scale, kv.v_scale, kv.block_size, kv.head_dim_v,
+                b.max_pages_per_seq)
 
     def _follow(self):
         """Replaced tensors of the cache and the batch, and new scales, are taken up by the next call (the
         summaries are still those of the cache before); other sizes or types do not fit the buffers."""
         kv, b, h = self.kv, self.batch, self._held
-        if (kv.k is h[0] and h[1] == kv.k.data_ptr() and kv.v is h[2] and (h[2] is None or h[3] == kv.v.data_ptr())
-                and kv.k_scale == h[4] and kv.v_scale == h[5] and kv.block_size == h[6] and kv.head_dim_v == h[7]
-                and b.page_indptr is h[8] and b.page_indices is h[9] and b.seq_lens is h[10]
-                and b.max_pages_per_seq == h[11]):
+        if (kv.k is h[0] and kv.v is h[1] and b.page_indptr is h[2] and b.page_indices is h[3] and b.seq_lens is h[4]
+                and self._places() == h[5]):
             return
         if self._now() != self._geometry:
             raise ValueError(f"the cache or the batch has another geometry than this SparseDecoder's buffers (now "

@@ -209,6 +209,15 @@ def test_a_decoder_follows_replaced_tensors(monkeypatch):
     assert len({t.data_ptr() for t in keep}) == 4
 
 
+def test_a_decoder_follows_the_batch_in_place(monkeypatch):
+    dec, _, i32, every_call = _decoder(monkeypatch)
+    every_call()
+    b = dec.batch
+    keep = [t.data for t in (b.page_indptr, b.page_indices, b.seq_lens)]
+    b.page_indptr.data, b.page_indices.data, b.seq_lens.data = i32(3), i32(6), i32(2)
+    assert every_call() == _now(dec) and b.seq_lens.data_ptr() != keep[2].data_ptr()
+
+
 @pytest.mark.parametrize("change", ["pages", "type", "batch", "bound", "keys", "page_size"])
 def test_a_decoder_refuses_what_its_buffers_do_not_fit(monkeypatch, change):
     dec, cache, i32, every_call = _decoder(monkeypatch)
