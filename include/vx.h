@@ -394,7 +394,7 @@ vx_status vx_topk_select(const float* scores, int32_t score_stride, int32_t num_
  * with online softmax; and an LSE-weighted merge of a split pair's partials (for GQA inside
  * the split kernel, by the pair's last split; for MLA by a merge launch).  Logical ids
  * outside [0, P_i) are skipped.  max_sel above 2^24 returns VX_ERR_UNSUPPORTED.
- * workspace: device buffer of at least vx_workspace_size(VX_STAGE_DECODE) bytes.  It starts
+ * workspace: device buffer of at least vx_workspace_size(VX_STAGE_DECODE) bytes, 4-byte aligned.  It starts
  * with the 32-bit split counters of the (request, KV head) pairs, which must be zero before the
  * first call: zero-fill the buffer once after allocating it.  Every call leaves the counters
  * zero again; the rest of the buffer is scratch.  Batches of any size and geometry may take turns

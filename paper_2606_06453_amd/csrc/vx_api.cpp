@@ -398,6 +398,8 @@ vx_status vx_sparse_paged_decode(const void* q, int32_t num_q_heads, const vx_pa
                                                  block_tokens(kv), is_mla(kv), kv->kv_dtype == VX_KV_MXFP4);
   if (!workspace || workspace_bytes < lay.total)
     return fail(VX_ERR_WORKSPACE, "decode workspace needs %zu bytes (got %zu)", lay.total, workspace_bytes);
+  if (reinterpret_cast<uintptr_t>(workspace) % sizeof(uint32_t) != 0)    // its split counters are atomics
+    return fail(VX_ERR_INVALID_ARG, "the decode workspace must be %zu-byte aligned", sizeof(uint32_t));
   return hip_status(vx::launch_decode(geometry(kv, b), static_cast<const uint16_t*>(q), num_q_heads, sel_pages,
                                       sel_count, max_sel, sm_scale, static_cast<uint16_t*>(out), workspace, lay,
                                       stream),

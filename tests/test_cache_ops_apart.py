@@ -101,3 +101,15 @@ def test_rows_read_into_one_another():
                         assert L.vx_kv_read(ctypes.byref(kv), at["rows"], *a, at["rows"] + 8192, *b, at["slots"], n, None) == 1
                         assert name in _msg() and "overlap" in _msg(), (heads, n, row, head, _msg())
     assert min(seen.values()) > 100
+
+
+@pytest.mark.parametrize("dtype", [vx.KV_BF16, vx.KV_FP8_E4M3, vx.KV_MXFP4])
+def test_an_odd_decode_workspace(dtype):
+    """The split counters at its start are 32-bit atomics."""
+    at = _place(dict(k=8192, v=8192, q=1024, ints=256, out=1024, ws=4096))
+    kv = vx._Cache(at["k"], at["v"], 2, 2, 16, 64, 64, dtype, 1.0, 1.0, 0)
+    b = vx._Batch(1, 4, at["ints"], at["ints"], at["ints"])
+    for off in (1, 2, 3):
+        assert vx.lib().vx_sparse_paged_decode(at["q"], 4, ctypes.byref(kv), ctypes.byref(b), at["ints"], at["ints"], 4, 0.1,
+                                               at["out"], at["ws"] + off, 1 << 24, None) == 1
+        assert "workspace" in _msg() and "aligned" in _msg()
