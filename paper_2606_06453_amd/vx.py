@@ -206,9 +206,11 @@ class PagedKV:
     def ref(self):
         """A by-reference argument holding this geometry, built once for the fields' present values."""
         if self._ref is None:
-            self.__dict__["_st"] = self.struct()
-            self.__dict__["_ref"] = ctypes.byref(self._st)
-            self.__dict__["_seen"] = self._tensors()
+            d = self.__dict__
+            st = d["_st"] = self.struct()
+            d["_dims"] = st.num_kv_heads, st.head_dim_qk, st.head_dim_v
+            d["_seen"] = self._tensors()
+            d["_ref"] = ctypes.byref(st)
         return self._ref
 
     def _tensors(self):
@@ -333,11 +335,19 @@ def page_extend(pool: PagePool, rows: torch.Tensor, new_lens: torch.Tensor, batc
     zero-filled once."""
     B, i32, d = rows.numel(), torch.int32, _gpu_of(pool.table)
     seq_lens, page_indptr = batch.seq_lens, batch.page_indptr
-    for t, n in ((rows, B), (new_lens, B), (seq_lens, B), (page_indptr, B + 1), (token_indptr, B + 1), (granted, B)):
-        if t.dtype is not i32 or t.numel() != n or t.get_device() != d or not t.is_contiguous():
-            names = {id(rows): "rows", id(new_lens): "new_lens", id(seq_lens): "seq_lens", id(page_indptr): "page_indptr",
-                     id(token_indptr): "token_indptr", id(granted): "granted"}
-            _refuse(t, i32, n, names[id(t)])
+    if not (rows.dtype is i32 and new_lens.dtype is i32 and seq_lens.dtype is i32 and page_indptr.dtype is i32
+            and token_indptr.dtype is i32 and granted.dtype is i32
+            and new_lens.numel() == B and seq_lens.numel() == B and page_indptr.numel() == B + 1
+            and token_indptr.numel() == B + 1 and granted.numel() == B
+            and rows.get_device() == d and new_lens.get_device() == d and seq_lens.get_device() == d
+            and page_indptr.get_device() == d and token_indptr.get_device() == d and granted.get_device() == d
+            and rows.is_contiguous() and new_lens.is_contiguous() and seq_lens.is_contiguous()
+            and page_indptr.is_contiguous() and token_indptr.is_contiguous() and granted.is_contiguous()):
+        for t, n, name in ((rows, B, "rows"), (new_lens, B, "new_lens"), (seq_lens, B, "seq_lens"),
+                           (page_indptr, B + 1, "page_indptr"), (token_indptr, B + 1, "token_indptr"),
+                           (granted, B, "granted")):
+            if t.dtype is not i32 or t.numel() != n or t.get_device() != d or not t.is_contiguous():
+                _refuse(t, i32, n, name)
     first = None
     if first_block is not None:
         if first_block.dtype is not i32 or first_block.numel() != B or first_block.get_device() != d:
@@ -387,11 +397,11 @@ def _kv_rows(fn, kv: PagedKV, slots: torch.Tensor, k: torch.Tensor, v: Optional[
     d, c = _gpu_of(kv.k), kv.current()
     if slots.dtype is not torch.int64 or slots.get_device() != d:
         _refuse(slots, torch.int64, None, "slots")
-    n, st = slots.numel(), kv._st
+    n, (heads, dim_qk, dim_v) = slots.numel(), kv._dims
     if n > _MOST:
         raise ValueError(f"at most {_MOST} rows a call (got {n})")
-    k_args = _row_args(k, n, st.num_kv_heads, st.head_dim_qk, d, names[0])
-    v_args = _row_args(v, n, st.num_kv_heads, st.head_dim_v, d, names[1])
+    k_args = _row_args(k, n, heads, dim_qk, d, names[0])
+    v_args = _row_args(v, n, heads, dim_v, d, names[1])
     _check(fn(c, *k_args, *v_args, _ptr(slots), n, _stream(stream, d)))
 
 
