@@ -16,6 +16,10 @@
  * Around the step, the cache's own operators: vx_page_extend gives a step's tokens their pages,
  * page list and slots and vx_page_release takes pages back; vx_kv_write puts whole prompts' rows
  * into the cache by slot and vx_kv_read gives rows back as bf16.
+ * For a chunk of new tokens (a prompt, a part of one, drafted tokens): vx_rope_kv_write rotates the
+ * projection's rows by their positions on the way into the cache, vx_chunk_attention attends
+ * everything before each token, and vx_chunk_score_topk with vx_sparse_chunk_attention selects and
+ * attends blocks of its own for each token.
  *
  * Conventions shared by every call
  * ---------------------------------
@@ -509,6 +513,103 @@ vx_status vx_kv_write(const vx_paged_cache* kv, const void* k_new, int64_t k_row
 vx_status vx_kv_read(const vx_paged_cache* kv, void* k_out, int64_t k_row_stride, int64_t k_head_stride, void* v_out,
                      int64_t v_row_stride, int64_t v_head_stride, const int64_t* slots, int32_t num_rows,
                      hipStream_t stream);
+
+/* ---- chunks of new tokens over the paged cache ------------------------------------------------
+ * The rotation of rows by their tokens' positions.  Channels first .. first + dim - 1 of a row are
+ * dim / 2 pairs (a, b): channels c and c + dim / 2 (interleaved 0) or 2c and 2c + 1 (interleaved 1)
+ * of them, c = 0 .. dim / 2 - 1.  Pair c turns by the angle t = positions[axis[c]] * inv_freq[c]:
+ *   a' = scale (a cos t - b sin t)     b' = scale (b cos t + a sin t)
+ * The angle, its sine and cosine and the products are computed in fp64; each result is rounded to fp32
+ * and then to the type it is stored in.  The other channels pass unchanged.  Several axes are those
+ * of images and video (time, height, width): each pair turns by the position along its own axis. */
+typedef struct {
+  const float* inv_freq;     /* [dim / 2] device */
+  const int32_t* axis;       /* [dim / 2] device, each in 0 .. num_axes - 1; NULL: axis 0 for every pair */
+  int32_t num_axes;          /* >= 1 */
+  int32_t first;             /* first rotated channel, a multiple of 8 */
+  int32_t dim;               /* rotated channels, a multiple of 16, first + dim <= head_dim_qk */
+  int32_t interleaved;       /* 0: halves, 1: neighbours */
+  float scale;               /* finite; 1 for a plain rotation */
+} vx_rope;
+
+/* The rows of a step or a chunk, from the projection into the cache: row n's keys are rotated, rounded to
+ * the cache's type as vx_kv_write rounds its rows (here from fp32 values), and stored at slots[n] with the
+ * row's values; row n's queries are rotated into q_out.
+ *   positions[a * positions_stride + n]   position of row n along axis a, int64, within 0 .. 2^53
+ *   q [n][num_q_heads][head_dim_qk], q_out alike, k_new, v_new: bf16 at element strides, as the rows of
+ *   vx_kv_write.  q and q_out both NULL: no queries (num_q_heads is then not looked at).  q_out may be q
+ *   itself (same address and strides); it must not overlap q otherwise, nor another input, and no two of
+ *   its rows may share an element.
+ * Rows whose slot is below 0 or past the cache store nothing; their queries are rotated all the same.  The
+ * other slots must differ from each other.  The summaries are the caller's to refresh. */
+vx_status vx_rope_kv_write(const vx_paged_cache* kv, const vx_rope* rope, const void* q, int64_t q_row_stride,
+                           int64_t q_head_stride, int32_t num_q_heads, void* q_out, int64_t q_out_row_stride,
+                           int64_t q_out_head_stride, const void* k_new, int64_t k_row_stride, int64_t k_head_stride,
+                           const void* v_new, int64_t v_row_stride, int64_t v_head_stride, const int64_t* positions,
+                           int64_t positions_stride, const int64_t* slots, int32_t num_rows, hipStream_t stream);
+
+/* The queries of a chunk.  Request i of the batch has seq_lens[i] = L_i tokens, the chunk's included, of
+ * which the chunk holds the last n_i; their queries are rows q_indptr[i] .. q_indptr[i] + n_i - 1 of q, in
+ * order, so that token t of them is at position L_i - n_i + t.  n_i = q_lens[i], at most
+ * q_indptr[i+1] - q_indptr[i], or that difference where q_lens is NULL.  With token_indptr and granted of
+ * vx_page_extend as q_indptr and q_lens the rows of refused requests belong to no token.  L_i = 0 is
+ * allowed here.  A row before its request's first token (n_i > L_i) attends and selects nothing.  Rows
+ * that belong to no token are neither read nor written. */
+typedef struct {
+  const int32_t* q_indptr;   /* [batch+1] device, from 0, non-decreasing, at most num_rows */
+  const int32_t* q_lens;     /* [batch] device, or NULL */
+  int32_t num_rows;          /* rows of q and of the outputs */
+} vx_chunk;
+
+typedef enum {
+  VX_CHUNK_ATTENTION = 0,
+  VX_CHUNK_SCORE_TOPK = 1,
+  VX_CHUNK_SPARSE = 2
+} vx_chunk_stage;
+
+/* Host-only: workspace bytes of a chunk call for num_rows rows of queries (max_sel: of the two calls with
+ * selections, else not looked at).  The buffer needs no filling and is 16-byte aligned. */
+vx_status vx_chunk_workspace_size(vx_chunk_stage stage, const vx_paged_cache* kv, const vx_batch* b, int32_t num_rows,
+                                  int32_t num_q_heads, int32_t max_sel, size_t* bytes);
+
+/* Attention of a chunk's tokens over the paged cache, in which their own keys and values already are.  For
+ * the row of the token at position p of request i and query head r (KV head h = r / g):
+ *   out = softmax_t(sm_scale * q_r . k_t) V_t   over tokens t with p - window < t (window 0: all) and
+ *                                               t <= p (causal 1) or t < L_i (causal 0)
+ *   lse = log sum_t exp(sm_scale * q_r . k_t)   (natural logarithm; -inf where there is no token)
+ * q [num_rows][num_q_heads][head_dim_qk] bf16 at element strides (multiples of 8, 16-byte aligned; the
+ * stride of a dimension of one entry is not looked at); out [num_rows][num_q_heads][head_dim_v] bf16,
+ * contiguous, rounded to nearest even from fp32 sums of weights that are rounded to bf16; lse fp32
+ * [num_rows][num_q_heads] or NULL.  A row with no token gives zeros.  Tokens that a row does not attend do
+ * not reach it, whatever their values (infinities and NaN too).  sm_scale > 0.  out and lse overlap no
+ * other array of the call. */
+vx_status vx_chunk_attention(const void* q, int64_t q_row_stride, int64_t q_head_stride, int32_t num_q_heads,
+                             const vx_paged_cache* kv, const vx_batch* b, const vx_chunk* chunk, int32_t window,
+                             int32_t causal, float sm_scale, void* out, float* lse, void* workspace,
+                             size_t workspace_bytes, hipStream_t stream);
+
+/* The blocks that each token of a chunk attends (the indexer stage of vx_page_score_topk, for every token
+ * by itself, GQA geometry).  The token at position p has PB = p / block_size + 1 blocks, scored with its own
+ * queries; F, K_total, ties and the lists are those of vx_page_score_topk with P_i = PB:
+ *   sel_pages [num_rows][num_kv_heads][max_sel], sel_count [num_rows]
+ * kind: VX_SCORE_MEAN_DOT (s_j = mean over the group of q_r . Mean_j, fp64, rounded to fp32).  n_local >= 1,
+ * so that the token's own block, whose summary may hold later tokens, is kept and not scored.  mean_bf16 (may
+ * be NULL) is vx_page_summarize's copy and serves a bounded first pass; the selection is the same with and
+ * without it.  At most 16384 blocks a request.  q as for vx_chunk_attention. */
+vx_status vx_chunk_score_topk(const void* q, int64_t q_row_stride, int64_t q_head_stride, int32_t num_q_heads,
+                              const vx_paged_cache* kv, const vx_batch* b, const vx_chunk* chunk, vx_score_kind kind,
+                              const float* mean, const void* mean_bf16, const int32_t* pages_budget, int32_t n_sink,
+                              int32_t n_local, int32_t max_sel, int32_t* sel_pages, int32_t* sel_count,
+                              void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* vx_chunk_attention (causal, no window, GQA geometry) over the tokens of the blocks that are listed for
+ * each row and KV head: sel_pages[row][h][0 .. sel_count[row] - 1], in any order; a block listed twice
+ * counts once, ids outside [0, p / block_size] are skipped.  At most 16384 blocks a request. */
+vx_status vx_sparse_chunk_attention(const void* q, int64_t q_row_stride, int64_t q_head_stride, int32_t num_q_heads,
+                                    const vx_paged_cache* kv, const vx_batch* b, const vx_chunk* chunk,
+                                    const int32_t* sel_pages, const int32_t* sel_count, int32_t max_sel,
+                                    float sm_scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                    hipStream_t stream);
 
 /* Measurement utility, not a step of the path: reads `bytes` (a positive multiple of 16) from
  * the 16-byte aligned device buffer `buf` with 16-byte loads carrying the non-temporal hint (the

@@ -1,9 +1,11 @@
 // C ABI of libvx: argument validation, workspace sizing and dispatch to the HIP kernels.
 // The declarations and their contracts are in include/vx.h.
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 
 #include "vx.h"
 #include "vx_internal.h"
@@ -628,6 +630,319 @@ vx_status vx_page_release(const vx_page_pool* pool, int32_t batch, const int32_t
   if (batch > 0 && (bad = check_spans(spans, (int)(sizeof spans / sizeof spans[0]))) != VX_OK) return bad;
   return hip_status(vx::launch_page_release(pool_of(pool), batch, rows, keep_lens, workspace, stream),
                     "vx_page_release");
+}
+
+namespace {
+
+// Rows [n][heads][D] at element strides, as far as they can reach (0 rows: none).
+struct Lattice {
+  const char* name;
+  const void* p;
+  int n, heads, D;
+  int64_t row, head;
+};
+
+// First and one past the last byte of the rows.
+void reach(const Lattice& x, uintptr_t* lo, uintptr_t* hi) {
+  const int64_t r = (int64_t)(x.n - 1) * (x.n > 1 ? x.row : 0), h = (int64_t)(x.heads - 1) * (x.heads > 1 ? x.head : 0);
+  const uintptr_t at = reinterpret_cast<uintptr_t>(x.p);
+  *lo = at + 2 * (std::min<int64_t>(r, 0) + std::min<int64_t>(h, 0));
+  *hi = at + 2 * (std::max<int64_t>(r, 0) + std::max<int64_t>(h, 0) + x.D);
+}
+
+// Whether rows of x may share a byte with rows of y.  Rows that lie between each other are told apart where
+// both have the same row stride and each fits one of its periods (slices of one projection's output).
+bool rows_meet(const Lattice& x, const Lattice& y) {
+  if (!x.p || !y.p || x.n == 0 || y.n == 0) return false;
+  uintptr_t a, b, c, d;
+  reach(x, &a, &b);
+  reach(y, &c, &d);
+  if (b <= c || d <= a) return false;
+  const int64_t R = x.n > 1 ? x.row : y.row;
+  if ((x.n > 1 && x.row != R) || (y.n > 1 && y.row != R) || R <= 0) return true;
+  const int64_t off = ((int64_t)(reinterpret_cast<uintptr_t>(y.p) - reinterpret_cast<uintptr_t>(x.p))) / 2;
+  if (((int64_t)(reinterpret_cast<uintptr_t>(y.p) - reinterpret_cast<uintptr_t>(x.p))) % 2) return true;
+  for (int i = 0; i < x.heads; i++) {
+    for (int j = 0; j < y.heads; j++) {
+      int64_t z = (off + (y.heads > 1 ? j * y.head : 0) - (x.heads > 1 ? i * x.head : 0)) % R;
+      if (z < 0) z += R;
+      if (z < x.D || z > R - y.D) return true;
+    }
+  }
+  return false;
+}
+
+// Whether rows of x may share a byte with [p, p + bytes).
+bool rows_touch(const Lattice& x, const void* p, size_t bytes) {
+  if (!x.p || !p || x.n == 0 || bytes == 0) return false;
+  uintptr_t a, b;
+  reach(x, &a, &b);
+  const uintptr_t c = reinterpret_cast<uintptr_t>(p);
+  return a < c + bytes && c < b;
+}
+
+// Bytes of a cache of head dim D (checked caches only).
+size_t cache_bytes(const vx_paged_cache* kv, int D) {
+  const size_t n = (size_t)kv->num_phys_pages * kv->num_kv_heads * kv->page_size * D;
+  return kv->kv_dtype == VX_KV_MXFP4 ? n / 32 * 17 : kv->kv_dtype == VX_KV_BF16 ? 2 * n : n;
+}
+
+bool odd_address(const void* p, size_t align) { return reinterpret_cast<uintptr_t>(p) % align != 0; }
+
+// Strides at which no offset of the kernels leaves 63 bits.
+vx_status check_strides(const char* name, int64_t row, int64_t head, int n, int heads) {
+  constexpr int64_t kFar = (int64_t)1 << 40;
+  if ((n > 1 && (row > kFar || row < -kFar)) || (heads > 1 && (head > kFar || head < -kFar)))
+    return fail(VX_ERR_INVALID_ARG, "%s has a stride beyond 2^40 elements", name);
+  return VX_OK;
+}
+
+}  // namespace
+
+vx_status vx_rope_kv_write(const vx_paged_cache* kv, const vx_rope* rope, const void* q, int64_t q_row_stride,
+                           int64_t q_head_stride, int32_t num_q_heads, void* q_out, int64_t q_out_row_stride,
+                           int64_t q_out_head_stride, const void* k_new, int64_t k_row_stride, int64_t k_head_stride,
+                           const void* v_new, int64_t v_row_stride, int64_t v_head_stride, const int64_t* positions,
+                           int64_t positions_stride, const int64_t* slots, int32_t num_rows, hipStream_t stream) {
+  vx_status s;
+  if ((s = check_cache(kv, true)) != VX_OK) return s;
+  if (!rope) return fail(VX_ERR_INVALID_ARG, "rope is NULL");
+  if (!rope->inv_freq) return fail(VX_ERR_INVALID_ARG, "inv_freq must be non-NULL");
+  if (odd_address(rope->inv_freq, 4) || odd_address(rope->axis, 4))
+    return fail(VX_ERR_INVALID_ARG, "inv_freq and axis must be 4-byte aligned");
+  if (rope->num_axes < 1) return fail(VX_ERR_INVALID_ARG, "num_axes must be >= 1");
+  if (rope->first < 0 || rope->first % 8 != 0 || rope->dim < 16 || rope->dim % 16 != 0 ||
+      rope->dim > kv->head_dim_qk || rope->first > kv->head_dim_qk - rope->dim)
+    return fail(VX_ERR_UNSUPPORTED, "rotated channels: first (%d) a multiple of 8, dim (%d) of 16, both within %d",
+                rope->first, rope->dim, kv->head_dim_qk);
+  if (rope->interleaved != 0 && rope->interleaved != 1) return fail(VX_ERR_INVALID_ARG, "interleaved must be 0 or 1");
+  if (!std::isfinite(rope->scale)) return fail(VX_ERR_INVALID_ARG, "scale must be finite");
+  if (num_rows < 0) return fail(VX_ERR_INVALID_ARG, "num_rows must be >= 0");
+  if (!q != !q_out) return fail(VX_ERR_INVALID_ARG, "q and q_out must be given together");
+  if (q && (s = check_heads(kv, num_q_heads)) != VX_OK) return s;
+  if (num_rows == 0) return VX_OK;
+  const int n = num_rows, H = kv->num_kv_heads, Hq = q ? num_q_heads : 0, D = kv->head_dim_qk;
+  if (odd_address(kv->k, 16) || odd_address(kv->v, 16))
+    return fail(VX_ERR_INVALID_ARG, "the caches must be 16-byte aligned");
+  if (!positions || !slots) return fail(VX_ERR_INVALID_ARG, "positions and slots must be non-NULL");
+  if (odd_address(positions, 8) || odd_address(slots, 8))
+    return fail(VX_ERR_INVALID_ARG, "positions and slots must be 8-byte aligned");
+  if ((s = check_rows("k_new", k_new, n, H, k_row_stride, k_head_stride)) != VX_OK) return s;
+  if (!kv->v && v_new) return fail(VX_ERR_INVALID_ARG, "V rows given but V is aliased to K (kv->v is NULL)");
+  if (kv->v && (s = check_rows("v_new", v_new, n, H, v_row_stride, v_head_stride)) != VX_OK) return s;
+  const Lattice out{"q_out", q_out, n, Hq, D, q_out_row_stride, q_out_head_stride};
+  const Lattice in[] = {{"q", q, n, Hq, D, q_row_stride, q_head_stride},
+                        {"k_new", k_new, n, H, D, k_row_stride, k_head_stride},
+                        {"v_new", v_new, n, H, kv->head_dim_v, v_row_stride, v_head_stride}};
+  for (const Lattice& x : in)
+    if (x.p && (s = check_strides(x.name, x.row, x.head, n, x.heads)) != VX_OK) return s;
+  if (q) {
+    if ((s = check_rows("q", q, n, Hq, q_row_stride, q_head_stride)) != VX_OK) return s;
+    if ((s = check_rows("q_out", q_out, n, Hq, q_out_row_stride, q_out_head_stride)) != VX_OK) return s;
+    if ((s = check_strides("q_out", out.row, out.head, n, Hq)) != VX_OK) return s;
+    if (rows_overlap(n, Hq, D, q_out_row_stride, q_out_head_stride))
+      return fail(VX_ERR_INVALID_ARG, "rows of q_out overlap");
+    const bool same = q == q_out && (n == 1 || q_row_stride == q_out_row_stride) &&
+                      (Hq == 1 || q_head_stride == q_out_head_stride);
+    for (const Lattice& x : in) {
+      if (x.p == q && same) continue;
+      if (rows_meet(out, x)) return fail(VX_ERR_INVALID_ARG, "q_out and %s overlap", x.name);
+    }
+    if (rows_touch(out, kv->k, cache_bytes(kv, D)) || rows_touch(out, kv->v, kv->v ? cache_bytes(kv, kv->head_dim_v) : 0))
+      return fail(VX_ERR_INVALID_ARG, "q_out and the caches overlap");
+    if (rows_touch(out, slots, (size_t)n * 8) || rows_touch(out, positions, (size_t)n * 8))
+      return fail(VX_ERR_INVALID_ARG, "q_out and positions or slots overlap");
+  }
+  if (rope->num_axes > 1 && (positions_stride > ((int64_t)1 << 40) || positions_stride < -((int64_t)1 << 40)))
+    return fail(VX_ERR_INVALID_ARG, "positions_stride is beyond 2^40");
+  vx_batch none{};
+  const vx::Rotation rot{rope->inv_freq, rope->axis, rope->num_axes, rope->first, rope->dim, rope->interleaved,
+                         rope->scale};
+  return hip_status(vx::launch_rope_kv_write(geometry(kv, &none), rot, {q, q_row_stride, q_head_stride},
+                                             {q_out, q_out_row_stride, q_out_head_stride}, Hq,
+                                             {k_new, k_row_stride, k_head_stride}, {v_new, v_row_stride, v_head_stride},
+                                             positions, positions_stride, slots, n, stream),
+                    "vx_rope_kv_write");
+}
+
+namespace {
+
+// What the chunk calls share.  sel: blocks are listed by 16-bit numbers.
+vx_status check_chunk(const void* q, int64_t row, int64_t head, int32_t Hq, const vx_paged_cache* kv, const vx_batch* b,
+                      const vx_chunk* c, bool need_v, bool sel) {
+  vx_status s;
+  if ((s = check_cache(kv, need_v)) != VX_OK) return s;
+  if ((s = check_batch(b)) != VX_OK) return s;
+  if ((s = check_heads(kv, Hq)) != VX_OK) return s;
+  if (!c) return fail(VX_ERR_INVALID_ARG, "chunk is NULL");
+  if (c->num_rows < 0) return fail(VX_ERR_INVALID_ARG, "num_rows must be >= 0");
+  if (c->num_rows > vx::kMaxChunkRows) return fail(VX_ERR_UNSUPPORTED, "num_rows above %d", vx::kMaxChunkRows);
+  if (sel && is_mla(kv)) return fail(VX_ERR_UNSUPPORTED, "selections for each token need the GQA geometry");
+  if (sel && max_blocks(kv, b) > vx::kMaxChunkBlocks)
+    return fail(VX_ERR_UNSUPPORTED, "more than %d blocks a request", vx::kMaxChunkBlocks);
+  if (c->num_rows == 0 || b->batch == 0) return VX_OK;
+  if (odd_address(kv->k, 16) || odd_address(kv->v, 16))
+    return fail(VX_ERR_INVALID_ARG, "the caches must be 16-byte aligned");
+  if (!c->q_indptr) return fail(VX_ERR_INVALID_ARG, "q_indptr must be non-NULL");
+  for (const void* p : {(const void*)c->q_indptr, (const void*)c->q_lens, (const void*)b->page_indptr,
+                        (const void*)b->page_indices, (const void*)b->seq_lens})
+    if (odd_address(p, 4)) return fail(VX_ERR_INVALID_ARG, "int32 arrays must be 4-byte aligned");
+  if ((s = check_rows("q", q, c->num_rows, Hq, row, head)) != VX_OK) return s;
+  return check_strides("q", row, head, c->num_rows, Hq);
+}
+
+vx::ChunkRows chunk_rows(const void* q, int64_t row, int64_t head, int32_t Hq, const vx_chunk* c) {
+  return {static_cast<const uint16_t*>(q), row, head, c->q_indptr, c->q_lens, c->num_rows, Hq};
+}
+
+// Results of a chunk call: none of them, nor the workspace, shares a byte with another array of the call.
+vx_status check_results(const Span* written, int n, const Lattice& q, const vx_paged_cache* kv, const vx_batch* b,
+                        const vx_chunk* c, std::initializer_list<Span> read) {
+  const size_t w = sizeof(int32_t);
+  const Span in[] = {{"q_indptr", c->q_indptr, (b->batch + (size_t)1) * w, false},
+                     {"q_lens", c->q_lens, c->q_lens ? b->batch * w : 0, false},
+                     {"page_indptr", b->page_indptr, (b->batch + (size_t)1) * w, false},
+                     {"seq_lens", b->seq_lens, b->batch * w, false},
+                     {"the K cache", kv->k, cache_bytes(kv, kv->head_dim_qk), false},
+                     {"the V cache", kv->v, kv->v ? cache_bytes(kv, kv->head_dim_v) : 0, false}};
+  auto meet = [](const Span& x, const Span& y) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(x.p), d = reinterpret_cast<uintptr_t>(y.p);
+    return x.p && y.p && x.bytes && y.bytes && a < d + y.bytes && d < a + x.bytes;
+  };
+  for (int i = 0; i < n; i++) {
+    if (rows_touch(q, written[i].p, written[i].bytes)) return fail(VX_ERR_INVALID_ARG, "%s and q overlap", written[i].name);
+    for (int j = i + 1; j < n; j++)
+      if (meet(written[i], written[j])) return fail(VX_ERR_INVALID_ARG, "%s and %s overlap", written[i].name, written[j].name);
+    for (const Span& x : in)
+      if (meet(written[i], x)) return fail(VX_ERR_INVALID_ARG, "%s and %s overlap", written[i].name, x.name);
+    for (const Span& x : read)
+      if (meet(written[i], x)) return fail(VX_ERR_INVALID_ARG, "%s and %s overlap", written[i].name, x.name);
+  }
+  for (int i = 0; i < n; i++)
+    if (odd_address(written[i].p, written[i].align))
+      return fail(VX_ERR_INVALID_ARG, "%s must be %zu-byte aligned", written[i].name, written[i].align);
+  return VX_OK;
+}
+
+vx_status check_workspace(const char* name, const void* ws, size_t bytes, size_t need) {
+  if (!ws || bytes < need) return fail(VX_ERR_WORKSPACE, "%s needs a workspace of %zu bytes (got %zu)", name, need, ws ? bytes : 0);
+  return VX_OK;
+}
+
+vx_status chunk_attention(const char* name, const void* q, int64_t row, int64_t head, int32_t Hq,
+                          const vx_paged_cache* kv, const vx_batch* b, const vx_chunk* c, const vx::ChunkSelection& sel,
+                          int window, bool causal, float sm_scale, void* out, float* lse, void* ws, size_t ws_bytes,
+                          hipStream_t stream) {
+  if (!(sm_scale > 0.f) || std::isinf(sm_scale)) return fail(VX_ERR_INVALID_ARG, "sm_scale must be positive and finite");
+  if (c->num_rows == 0 || b->batch == 0) return VX_OK;
+  const vx::Geometry g = geometry(kv, b);
+  const size_t need = vx::chunk_attention_workspace(g, c->num_rows, Hq, sel.pages != nullptr, sel.max_sel);
+  vx_status s;
+  if ((s = check_workspace(name, ws, ws_bytes, need)) != VX_OK) return s;
+  if (!out) return fail(VX_ERR_INVALID_ARG, "out must be non-NULL");
+  const size_t heads = (size_t)c->num_rows * Hq;
+  const Span written[] = {{"out", out, heads * kv->head_dim_v * 2, true, 16},
+                          {"lse", lse, lse ? heads * 4 : 0, true, 4},
+                          {"workspace", ws, need, true, 16}};
+  const Span lists[] = {
+      {"sel_pages", sel.pages, sel.pages ? (size_t)c->num_rows * kv->num_kv_heads * sel.max_sel * 4 : 0, false},
+      {"sel_count", sel.count, sel.count ? (size_t)c->num_rows * 4 : 0, false}};
+  if ((s = check_results(written, 3, {"q", q, c->num_rows, Hq, kv->head_dim_qk, row, head}, kv, b, c,
+                         {lists[0], lists[1]})) != VX_OK)
+    return s;
+  return hip_status(vx::launch_chunk_attention(g, chunk_rows(q, row, head, Hq, c), sel, window, causal, sm_scale,
+                                               static_cast<uint16_t*>(out), lse, ws, stream),
+                    name);
+}
+
+}  // namespace
+
+vx_status vx_chunk_workspace_size(vx_chunk_stage stage, const vx_paged_cache* kv, const vx_batch* b, int32_t num_rows,
+                                  int32_t num_q_heads, int32_t max_sel, size_t* bytes) {
+  if (!bytes) return fail(VX_ERR_INVALID_ARG, "bytes is NULL");
+  if (stage != VX_CHUNK_ATTENTION && stage != VX_CHUNK_SCORE_TOPK && stage != VX_CHUNK_SPARSE)
+    return fail(VX_ERR_INVALID_ARG, "unknown chunk stage %d", (int)stage);
+  vx_chunk none{nullptr, nullptr, 0};
+  vx_status s;
+  if ((s = check_chunk(nullptr, 0, 0, num_q_heads, kv, b, &none, false, stage != VX_CHUNK_ATTENTION)) != VX_OK) return s;
+  if (num_rows < 0) return fail(VX_ERR_INVALID_ARG, "num_rows must be >= 0");
+  if (num_rows > vx::kMaxChunkRows) return fail(VX_ERR_UNSUPPORTED, "num_rows above %d", vx::kMaxChunkRows);
+  if (stage != VX_CHUNK_ATTENTION && max_sel < 1) return fail(VX_ERR_INVALID_ARG, "max_sel must be >= 1");
+  const vx::Geometry g = geometry(kv, b);
+  *bytes = stage == VX_CHUNK_SCORE_TOPK
+               ? vx::chunk_select_workspace(g, num_rows, num_q_heads)
+               : vx::chunk_attention_workspace(g, num_rows, num_q_heads, stage == VX_CHUNK_SPARSE, max_sel);
+  return VX_OK;
+}
+
+vx_status vx_chunk_attention(const void* q, int64_t q_row_stride, int64_t q_head_stride, int32_t num_q_heads,
+                             const vx_paged_cache* kv, const vx_batch* b, const vx_chunk* chunk, int32_t window,
+                             int32_t causal, float sm_scale, void* out, float* lse, void* workspace,
+                             size_t workspace_bytes, hipStream_t stream) {
+  vx_status s;
+  if ((s = check_chunk(q, q_row_stride, q_head_stride, num_q_heads, kv, b, chunk, true, false)) != VX_OK) return s;
+  if (window < 0) return fail(VX_ERR_INVALID_ARG, "window must be >= 0");
+  if (causal != 0 && causal != 1) return fail(VX_ERR_INVALID_ARG, "causal must be 0 or 1");
+  return chunk_attention("vx_chunk_attention", q, q_row_stride, q_head_stride, num_q_heads, kv, b, chunk, {}, window,
+                         causal != 0, sm_scale, out, lse, workspace, workspace_bytes, stream);
+}
+
+vx_status vx_chunk_score_topk(const void* q, int64_t q_row_stride, int64_t q_head_stride, int32_t num_q_heads,
+                              const vx_paged_cache* kv, const vx_batch* b, const vx_chunk* chunk, vx_score_kind kind,
+                              const float* mean, const void* mean_bf16, const int32_t* pages_budget, int32_t n_sink,
+                              int32_t n_local, int32_t max_sel, int32_t* sel_pages, int32_t* sel_count,
+                              void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  vx_status s;
+  if ((s = check_chunk(q, q_row_stride, q_head_stride, num_q_heads, kv, b, chunk, false, true)) != VX_OK) return s;
+  if (kind != VX_SCORE_MEAN_DOT) {
+    if ((int)kind < 0 || (int)kind > VX_SCORE_MEAN_DOT_SMOOTH)
+      return fail(VX_ERR_INVALID_ARG, "unknown score kind %d", (int)kind);
+    return fail(VX_ERR_UNSUPPORTED, "score kind %d is not built for chunks (VX_SCORE_MEAN_DOT is)", (int)kind);
+  }
+  if (max_sel < 1) return fail(VX_ERR_INVALID_ARG, "max_sel must be >= 1");
+  if (n_sink < 0 || n_local < 1)
+    return fail(VX_ERR_INVALID_ARG, "n_sink must be >= 0 and n_local >= 1 (a token's own block is always kept)");
+  if ((int64_t)n_sink + n_local > max_sel) return fail(VX_ERR_INVALID_ARG, "n_sink + n_local must be <= max_sel");
+  if (chunk->num_rows == 0 || b->batch == 0) return VX_OK;
+  const vx::Geometry g = geometry(kv, b);
+  const size_t need = vx::chunk_select_workspace(g, chunk->num_rows, num_q_heads);
+  if ((s = check_workspace("vx_chunk_score_topk", workspace, workspace_bytes, need)) != VX_OK) return s;
+  if (!mean || !pages_budget || !sel_pages || !sel_count)
+    return fail(VX_ERR_INVALID_ARG, "mean, pages_budget, sel_pages and sel_count must be non-NULL");
+  if (odd_address(mean, 16) || odd_address(mean_bf16, 16))
+    return fail(VX_ERR_INVALID_ARG, "mean and mean_bf16 must be 16-byte aligned");
+  if (odd_address(pages_budget, 4)) return fail(VX_ERR_INVALID_ARG, "int32 arrays must be 4-byte aligned");
+  const size_t rows = chunk->num_rows, means = (size_t)g.num_phys_pages * g.r * g.H * g.Dqk;
+  const Span written[] = {{"sel_pages", sel_pages, rows * g.H * max_sel * 4, true, 4},
+                          {"sel_count", sel_count, rows * 4, true, 4},
+                          {"workspace", workspace, need, true, 16}};
+  if ((s = check_results(written, 3, {"q", q, chunk->num_rows, num_q_heads, g.Dqk, q_row_stride, q_head_stride}, kv, b,
+                         chunk,
+                         {{"mean", mean, means * 4, false},
+                          {"mean_bf16", mean_bf16, mean_bf16 ? means * 2 : 0, false},
+                          {"pages_budget", pages_budget, (size_t)b->batch * 4, false}})) != VX_OK)
+    return s;
+  return hip_status(vx::launch_chunk_select(g, chunk_rows(q, q_row_stride, q_head_stride, num_q_heads, chunk), mean,
+                                            static_cast<const uint16_t*>(mean_bf16), pages_budget, n_sink, n_local,
+                                            max_sel, sel_pages, sel_count, workspace, stream),
+                    "vx_chunk_score_topk");
+}
+
+vx_status vx_sparse_chunk_attention(const void* q, int64_t q_row_stride, int64_t q_head_stride, int32_t num_q_heads,
+                                    const vx_paged_cache* kv, const vx_batch* b, const vx_chunk* chunk,
+                                    const int32_t* sel_pages, const int32_t* sel_count, int32_t max_sel,
+                                    float sm_scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                    hipStream_t stream) {
+  vx_status s;
+  if ((s = check_chunk(q, q_row_stride, q_head_stride, num_q_heads, kv, b, chunk, true, true)) != VX_OK) return s;
+  if (max_sel < 1) return fail(VX_ERR_INVALID_ARG, "max_sel must be >= 1");
+  if (chunk->num_rows > 0 && b->batch > 0) {
+    if (!sel_pages || !sel_count) return fail(VX_ERR_INVALID_ARG, "sel_pages and sel_count must be non-NULL");
+    if (odd_address(sel_pages, 4) || odd_address(sel_count, 4))
+      return fail(VX_ERR_INVALID_ARG, "int32 arrays must be 4-byte aligned");
+  }
+  return chunk_attention("vx_sparse_chunk_attention", q, q_row_stride, q_head_stride, num_q_heads, kv, b, chunk,
+                         {sel_pages, sel_count, max_sel}, 0, true, sm_scale, out, lse, workspace, workspace_bytes, stream);
 }
 
 vx_status vx_stream_read(const void* buf, size_t bytes, uint32_t* sink, int32_t workgroups, hipStream_t stream) {

@@ -109,6 +109,44 @@ hipError_t launch_kv_write(const Geometry& g, const RowView& k, const RowView& v
 hipError_t launch_kv_read(const Geometry& g, const RowView& k, const RowView& v, const int64_t* slots, int n,
                           hipStream_t stream);
 
+// The rotation of rows by position (vx_rope, checked).
+struct Rotation {
+  const float* inv_freq;
+  const int32_t* axis;
+  int num_axes, first, dim, interleaved;
+  float scale;
+};
+// q.rows == nullptr: no queries.
+hipError_t launch_rope_kv_write(const Geometry& g, const Rotation& rope, const RowView& q, const RowView& q_out, int Hq,
+                                const RowView& k, const RowView& v, const int64_t* positions, int64_t positions_stride,
+                                const int64_t* slots, int n, hipStream_t stream);
+
+// The queries of a chunk (vx_chunk, checked).
+struct ChunkRows {
+  const uint16_t* q;
+  int64_t row_stride, head_stride;
+  const int32_t* indptr;
+  const int32_t* lens;    // or nullptr
+  int n, Hq;
+};
+constexpr int kMaxChunkBlocks = 16384;     // blocks per request of the calls with selections
+constexpr int kMaxChunkRows = 1 << 19;
+
+// sel_pages == nullptr: every token (window, causal); else the listed blocks (causal, no window).
+struct ChunkSelection {
+  const int32_t* pages = nullptr;
+  const int32_t* count = nullptr;
+  int max_sel = 0;
+};
+size_t chunk_attention_workspace(const Geometry& g, int n, int Hq, bool sparse, int max_sel);
+hipError_t launch_chunk_attention(const Geometry& g, const ChunkRows& rows, const ChunkSelection& sel, int window,
+                                  bool causal, float sm_scale, uint16_t* out, float* lse, void* ws, hipStream_t stream);
+
+size_t chunk_select_workspace(const Geometry& g, int n, int Hq);
+hipError_t launch_chunk_select(const Geometry& g, const ChunkRows& rows, const float* mean, const uint16_t* mean_bf,
+                               const int32_t* budget, int n_sink, int n_local, int max_sel, int32_t* sel_pages,
+                               int32_t* sel_count, void* ws, hipStream_t stream);
+
 // The state of a page pool (vx_page_pool, checked).
 struct PagePool {
   int32_t* free_pages;

@@ -74,6 +74,16 @@ class _Pool(ctypes.Structure):
                 ("table_stride", ctypes.c_int32), ("page_size", ctypes.c_int32), ("block_size", ctypes.c_int32)]
 
 
+class _Rope(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("axis", ctypes.c_void_p), ("num_axes", ctypes.c_int32),
+                ("first", ctypes.c_int32), ("dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+class _Chunk(ctypes.Structure):
+    _fields_ = [("q_indptr", ctypes.c_void_p), ("q_lens", ctypes.c_void_p), ("num_rows", ctypes.c_int32)]
+
+
 class _Batch(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32),
                 ("page_indptr", ctypes.c_void_p), ("page_indices", ctypes.c_void_p),
@@ -111,6 +121,14 @@ def lib():
         L.vx_page_release.argtypes = [P, i32, P, P, P, sz, P]
         L.vx_kv_write.argtypes = [P, P, i64, i64, P, i64, i64, P, i32, P]
         L.vx_kv_read.argtypes = [P, P, i64, i64, P, i64, i64, P, i32, P]
+        L.vx_rope_kv_write.argtypes = [P, P, P, i64, i64, i32, P, i64, i64, P, i64, i64, P, i64, i64, P, i64, P, i32, P]
+        L.vx_chunk_workspace_size.argtypes = [i32, P, P, i32, i32, i32, ctypes.POINTER(sz)]
+        L.vx_chunk_attention.argtypes = [P, i64, i64, i32, P, P, P, i32, i32, ctypes.c_float, P, P, P, sz, P]
+        L.vx_chunk_score_topk.argtypes = [P, i64, i64, i32, P, P, P, i32, P, P, P, i32, i32, i32, P, P, P, sz, P]
+        L.vx_sparse_chunk_attention.argtypes = [P, i64, i64, i32, P, P, P, P, P, i32, ctypes.c_float, P, P, P, sz, P]
+        for f in (L.vx_rope_kv_write, L.vx_chunk_workspace_size, L.vx_chunk_attention, L.vx_chunk_score_topk,
+                  L.vx_sparse_chunk_attention):
+            f.restype = ctypes.c_int
         for f in (L.vx_page_workspace_size, L.vx_page_extend, L.vx_page_release, L.vx_kv_write, L.vx_kv_read):
             f.restype = ctypes.c_int
         for f in (L.vx_workspace_size, L.vx_page_summarize, L.vx_page_score_topk, L.vx_sparse_paged_decode,
@@ -415,6 +433,163 @@ def kv_read(kv: PagedKV, slots: torch.Tensor, k_out: torch.Tensor, v_out: Option
     """The cache's values at slots [n] as bf16 rows k_out [n][H][Dqk] and v_out [n][H][Dv] (zeros for a
     negative slot)."""
     _kv_rows(lib().vx_kv_read, kv, slots, k_out, v_out, ("k_out", "v_out"), stream)
+
+
+@dataclass
+class Rope:
+    """The rotation of rows by their tokens' positions (vx_rope): inv_freq float32 [dim / 2] on the GPU
+    turns channels first .. first + dim - 1, in pairs of halves or of neighbours (interleaved).  axis
+    int32 [dim / 2]: the axis of each pair, of num_axes (None: one axis)."""
+    inv_freq: torch.Tensor
+    axis: Optional[torch.Tensor] = None
+    num_axes: int = 1
+    first: int = 0
+    interleaved: bool = False
+    scale: float = 1.0
+
+    def current(self, d: int):
+        """A by-reference argument holding this rotation as it is now, on GPU d."""
+        f, ax = self.inv_freq, self.axis
+        if f.dtype is not torch.float32 or f.get_device() != d or not f.is_contiguous():
+            _refuse(f, torch.float32, None, "inv_freq")
+        if ax is not None and (ax.dtype is not torch.int32 or ax.numel() != f.numel() or ax.get_device() != d
+                               or not ax.is_contiguous()):
+            _refuse(ax, torch.int32, f.numel(), "axis")
+        return ctypes.byref(_Rope(f.data_ptr(), None if ax is None else ax.data_ptr(), int(self.num_axes), int(self.first),
+                                  2 * f.numel(), int(bool(self.interleaved)), float(self.scale)))
+
+
+def rope_kv_write(kv: PagedKV, rope: Rope, q: Optional[torch.Tensor], k_new: torch.Tensor,
+                  v_new: Optional[torch.Tensor], positions: torch.Tensor, slots: torch.Tensor,
+                  q_out: Optional[torch.Tensor], stream=None) -> None:
+    """Rows k_new [n][H][Dqk], rotated by positions [n] or [num_axes][n] (int64), and v_new [n][H][Dv] into
+    the cache at slots [n] (int64; negative: skipped), rounded to its type; queries q [n][Hq][Dqk] rotated
+    into q_out (which may be q).  All rows bf16, strided; q and q_out None: keys and values alone."""
+    d, c = _gpu_of(kv.k), kv.current()
+    if slots.dtype is not torch.int64 or slots.get_device() != d:
+        _refuse(slots, torch.int64, None, "slots")
+    n, (heads, dim_qk, dim_v) = slots.numel(), kv._dims
+    if n > _MOST:
+        raise ValueError(f"at most {_MOST} rows a call (got {n})")
+    axes = int(rope.num_axes)
+    if positions.dtype is not torch.int64 or positions.get_device() != d:
+        _refuse(positions, torch.int64, None, "positions")
+    if positions.shape != (axes, n) and not (axes == 1 and positions.shape == (n,)):
+        raise ValueError(f"positions must be [{axes}][{n}] (got {tuple(positions.shape)})")
+    if n > 1 and positions.stride(-1) != 1:
+        raise ValueError("the positions along an axis must be contiguous")
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out must be given together")
+    q_heads = 0 if q is None else q.shape[1]
+    k_args = _row_args(k_new, n, heads, dim_qk, d, "k_new")
+    v_args = _row_args(v_new, n, heads, dim_v, d, "v_new")
+    q_args = _row_args(q, n, q_heads, dim_qk, d, "q")
+    o_args = _row_args(q_out, n, q_heads, dim_qk, d, "q_out")
+    _check(lib().vx_rope_kv_write(c, rope.current(d), *q_args, q_heads, *o_args, *k_args, *v_args, positions.data_ptr(),
+                                  positions.stride(0) if positions.dim() == 2 else 0, _ptr(slots), n,
+                                  _stream(stream, d)))
+
+
+CHUNK_ATTENTION, CHUNK_SCORE_TOPK, CHUNK_SPARSE = 0, 1, 2
+
+
+def chunk_workspace_size(stage: int, kv: PagedKV, batch: BatchSpec, num_rows: int, num_q_heads: int,
+                         max_sel: int = 1) -> int:
+    """Workspace bytes of chunk_attention, chunk_score_topk or sparse_chunk_attention (stage CHUNK_ATTENTION,
+    CHUNK_SCORE_TOPK, CHUNK_SPARSE) for num_rows rows of queries."""
+    out = ctypes.c_size_t(0)
+    _check(lib().vx_chunk_workspace_size(stage, kv.current(), batch.current(), int(num_rows), int(num_q_heads), int(max_sel),
+                                         ctypes.byref(out)))
+    return int(out.value)
+
+
+def _chunk_args(q: torch.Tensor, kv: PagedKV, batch: BatchSpec, q_indptr: torch.Tensor,
+                q_lens: Optional[torch.Tensor], workspace: torch.Tensor):
+    """What the chunk calls share: the device, the query's arguments, the cache, the batch and the chunk."""
+    d, c, i32 = _gpu_of(kv.k), kv.current(), torch.int32
+    B = batch.seq_lens.numel()
+    for t, n, name in ((batch.seq_lens, B, "seq_lens"), (batch.page_indptr, B + 1, "page_indptr"),
+                       (batch.page_indices, None, "page_indices"), (q_indptr, B + 1, "q_indptr"), (q_lens, B, "q_lens")):
+        if t is not None and (t.dtype is not i32 or t.get_device() != d or not t.is_contiguous()
+                              or (n is not None and t.numel() != n)):
+            _refuse(t, i32, n, name)
+    if workspace.get_device() != d or not workspace.is_contiguous():
+        _refuse(workspace, workspace.dtype, None, "workspace")
+    if q.dim() != 3:
+        raise ValueError(f"q must be [rows][heads][dim] (got {tuple(q.shape)})")
+    n, heads = q.shape[0], q.shape[1]
+    if n > _MOST:
+        raise ValueError(f"at most {_MOST} rows a call (got {n})")
+    q_args = _row_args(q, n, heads, kv._dims[1], d, "q")
+    chunk = _Chunk(q_indptr.data_ptr(), None if q_lens is None else q_lens.data_ptr(), n)
+    return d, q_args + (heads, c, batch.current(), ctypes.byref(chunk))
+
+
+def _result(t: Optional[torch.Tensor], dtype: torch.dtype, shape, d: int, name: str):
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != d or not t.is_contiguous():
+        _refuse(t, dtype, None, name)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)} (got {list(t.shape)})")
+    return t.data_ptr()
+
+
+def _bytes(t: torch.Tensor) -> int:
+    return t.numel() * t.element_size()
+
+
+def chunk_attention(q: torch.Tensor, kv: PagedKV, batch: BatchSpec, q_indptr: torch.Tensor, sm_scale: float,
+                    out: torch.Tensor, workspace: torch.Tensor, q_lens: Optional[torch.Tensor] = None,
+                    window: int = 0, causal: bool = True, lse: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Attention of a chunk's tokens over the paged cache, which already holds their own rows: queries
+    q [n][Hq][Dqk] (bf16, strided), rows q_indptr[i] .. of request i (int32 [batch+1]; q_lens int32 [batch]:
+    how many of them are tokens), out [n][Hq][Dv] bf16, lse [n][Hq] float32 or None.  window: each token
+    attends its last `window` tokens (0: all).  workspace: chunk_workspace_size(CHUNK_ATTENTION, ..) bytes."""
+    d, args = _chunk_args(q, kv, batch, q_indptr, q_lens, workspace)
+    n, heads = q.shape[:2]
+    o = _result(out, torch.bfloat16, (n, heads, kv._dims[2]), d, "out")
+    e = _result(lse, torch.float32, (n, heads), d, "lse")
+    _check(lib().vx_chunk_attention(*args, int(window), int(bool(causal)), float(sm_scale), o, e, workspace.data_ptr(),
+                                    _bytes(workspace), _stream(stream, d)))
+
+
+def chunk_score_topk(q: torch.Tensor, kv: PagedKV, batch: BatchSpec, q_indptr: torch.Tensor, kind: int,
+                     mean: torch.Tensor, pages_budget: torch.Tensor, n_sink: int, n_local: int, max_sel: int,
+                     sel_pages: torch.Tensor, sel_count: torch.Tensor, workspace: torch.Tensor,
+                     q_lens: Optional[torch.Tensor] = None, mean_bf16: Optional[torch.Tensor] = None,
+                     stream=None) -> None:
+    """The blocks that each token of a chunk attends: page_score_topk for every token by itself, into
+    sel_pages [n][H][max_sel] and sel_count [n] (int32).  kind: MEAN_DOT; n_local >= 1."""
+    d, args = _chunk_args(q, kv, batch, q_indptr, q_lens, workspace)
+    n, H, D = q.shape[0], kv._dims[0], kv._dims[1]
+    blocks = kv.k.shape[0] * (kv.k.shape[2] // kv.block_size if kv.block_size else 1)
+    m = _result(mean, torch.float32, (blocks, H, D), d, "mean")
+    mb = _result(mean_bf16, torch.bfloat16, (blocks, H, D), d, "mean_bf16")
+    budget = _result(pages_budget, torch.int32, (batch.seq_lens.numel(),), d, "pages_budget")
+    sp = _result(sel_pages, torch.int32, (n, H, max_sel), d, "sel_pages")
+    sc = _result(sel_count, torch.int32, (n,), d, "sel_count")
+    _check(lib().vx_chunk_score_topk(*args, kind, m, mb, budget, n_sink, n_local, max_sel, sp, sc, workspace.data_ptr(),
+                                     _bytes(workspace), _stream(stream, d)))
+
+
+def sparse_chunk_attention(q: torch.Tensor, kv: PagedKV, batch: BatchSpec, q_indptr: torch.Tensor,
+                           sel_pages: torch.Tensor, sel_count: torch.Tensor, sm_scale: float, out: torch.Tensor,
+                           workspace: torch.Tensor, q_lens: Optional[torch.Tensor] = None,
+                           lse: Optional[torch.Tensor] = None, stream=None) -> None:
+    """chunk_attention over the blocks listed for each row and KV head: sel_pages [n][H][max_sel] and
+    sel_count [n] (int32), as chunk_score_topk writes them."""
+    d, args = _chunk_args(q, kv, batch, q_indptr, q_lens, workspace)
+    n, heads = q.shape[:2]
+    if sel_pages.dim() != 3:
+        raise ValueError(f"sel_pages must be [rows][KV heads][max_sel] (got {tuple(sel_pages.shape)})")
+    max_sel = sel_pages.shape[2]
+    sp = _result(sel_pages, torch.int32, (n, kv._dims[0], max_sel), d, "sel_pages")
+    sc = _result(sel_count, torch.int32, (n,), d, "sel_count")
+    o = _result(out, torch.bfloat16, (n, heads, kv._dims[2]), d, "out")
+    e = _result(lse, torch.float32, (n, heads), d, "lse")
+    _check(lib().vx_sparse_chunk_attention(*args, sp, sc, max_sel, float(sm_scale), o, e, workspace.data_ptr(),
+                                           _bytes(workspace), _stream(stream, d)))
 
 
 def workspace_size(stage: int, kv: PagedKV, batch: BatchSpec, num_q_heads: int, max_sel: int) -> int:
