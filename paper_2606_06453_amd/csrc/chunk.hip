@@ -1,18 +1,29 @@
 // Attention of a chunk's tokens over the paged cache: all of it (vx_chunk_attention), or the blocks listed for
 // each token (vx_sparse_chunk_attention).
 //
-// chunk_rows_kernel takes the rows of a tile one by one, with each token's dot product in one lane.
+// chunk_narrow_kernel  tiles of 16 query rows (token, head of the group) whose waves share out the tokens;
+// chunk_wide_kernel    tiles of 64 or 128 rows whose waves share the rows, and the tokens through LDS;
+// chunk_merge_kernel   joins the parts of a list that several workgroups took.
+// A tile whose sums are not finite is done again row by row (attend_rows).
 #include <algorithm>
+#include <climits>
 #include <cmath>
+#include <type_traits>
 
 #include "chunk_common.h"
+#include "chunk_tile.h"
+#include "chunk_wide.h"
 
 namespace vx {
 using namespace chunk;
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
-constexpr int kTileRows = 16;              // query rows (token, head of the group) of a tile
+constexpr int kTileRows = 16;              // query rows (token, head of the group) of a matrix operand
+constexpr int kTargetWgs = 512;            // two workgroups a CU
+constexpr int kMaxParts = 64;              // a merging wave's lanes
+constexpr int kPartTokens = 512;           // least tokens of a part: four pairs of runs a wave
+constexpr float kLn2 = 0.693147180559945309f;
 
 // The blocks listed for the tile's tokens: masks[id] holds a bit for each token that lists block id, ids the
 // listed ones in ascending order.  Returns their count.  Every thread of the workgroup takes part.
@@ -58,62 +69,456 @@ __device__ __forceinline__ int listed_blocks(const ChunkArgs& a, const Tile& t, 
   return total;
 }
 
-template <int D, int DV, int KT, bool SPARSE>
-__global__ __launch_bounds__(kThreads) void chunk_rows_kernel(const ChunkArgs a) {
-  extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
-  const int h = (int)blockIdx.x % a.H;
-  Tile t;
-  if (!find_tile(a, (int)blockIdx.x / a.H, t)) return;
-  Runs runs;
-  if constexpr (SPARSE) {
-    uint16_t* ids = reinterpret_cast<uint16_t*>(lds + (a.max_blocks + 1) / 2);
-    runs.lo = 0;
-    runs.hi = listed_blocks(a, t, h, lds, ids);
-    runs.ids = ids;
-    runs.masks = reinterpret_cast<const uint16_t*>(lds);
-    runs.shift = a.bs_shift;
-  } else {
-    runs.lo = first_key(a, t.p0) >> 6;
-    runs.hi = (end_key(a, t, t.p0 + t.n - 1) + 63) >> 6;
-    runs.ids = nullptr;
-    runs.masks = nullptr;
-    runs.shift = 6;
-  }
+// Part s of the S parts of [lo, hi).
+__device__ __forceinline__ void part_of(int lo, int hi, int s, int S, int& plo, int& phi) {
+  const int per = (hi - lo + S - 1) / S;
+  plo = min(lo + s * per, hi);
+  phi = min(plo + per, hi);
+}
+
+// The tile's rows one by one: where a sum of the tile kernels is not finite.
+template <int D, int DV, int KT>
+__device__ __forceinline__ void attend_rows(const ChunkArgs& a, const Tile& t, int h, const Runs& runs, int split) {
   for (int x = (int)threadIdx.x >> 6; x < t.n * a.g; x += kWaves) {
     RowState<DV> st;
     attend_row<D, DV, KT>(a, t, h, x % a.g, x / a.g, runs, st);
-    store_row<DV>(a, t.row0 + x / a.g, h * a.g + x % a.g, 0, st);
+    store_row<DV>(a, t.row0 + x / a.g, h * a.g + x % a.g, split, st);
   }
 }
 
-template <int D, int DV, int KT>
-hipError_t launch_kt(const ChunkArgs& a, hipStream_t stream) {
-  const int64_t tiles = (int64_t)a.num_rows / a.tokens + a.batch;
-  const dim3 grid((unsigned)(tiles * a.H));
-  if constexpr (D == DV) {
-    if (a.sel_pages) {
-      const size_t lds = sizeof(uint32_t) * ((a.max_blocks + 1) / 2) + sizeof(uint16_t) * a.max_blocks;
-      hipLaunchKernelGGL((chunk_rows_kernel<D, DV, KT, true>), grid, dim3(kThreads), lds, stream, a);
-      return hipGetLastError();
+// The runs of a workgroup's part; shift16: log2 of the 16-token runs of an entry.
+template <bool SPARSE>
+__device__ __forceinline__ Runs part_runs(const ChunkArgs& a, const Tile& t, int h, int split, uint32_t* lds, int& shift16) {
+  Runs runs;
+  if constexpr (SPARSE) {
+    uint16_t* ids = reinterpret_cast<uint16_t*>(lds + (a.max_blocks + 1) / 2);
+    const int all = __builtin_amdgcn_readfirstlane(listed_blocks(a, t, h, lds, ids));
+    runs.ids = ids;
+    runs.masks = reinterpret_cast<const uint16_t*>(lds);
+    runs.shift = a.bs_shift;
+    shift16 = a.bs_shift - 4;
+    part_of(0, all, split, a.splits, runs.lo, runs.hi);
+  } else {
+    runs.ids = nullptr;
+    runs.masks = nullptr;
+    runs.shift = 4;
+    shift16 = 0;
+    part_of(first_key(a, t.p0) >> 4, (end_key(a, t, t.p0 + t.n - 1) + 15) >> 4, split, a.splits, runs.lo, runs.hi);
+  }
+  return runs;
+}
+
+// Four waves share a tile of 16 query rows; each takes every fourth pair of 16-token runs of the tile's list,
+// straight from the cache into matrix operands, and the waves' states meet in LDS.
+template <int D, int KT, bool SPARSE>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void chunk_narrow_kernel(const ChunkArgs a) {
+  constexpr int KS = D / 32, NJ = D / 16, W = D / 32;
+  extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
+  const int tid = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 15, grp = lane >> 4;
+  const int h = (int)blockIdx.x % a.H, split = (int)blockIdx.y;
+  Tile t;
+  if (!find_tile(a, (int)blockIdx.x / a.H, t)) return;
+  int shift16;
+  const Runs runs = part_runs<SPARSE>(a, t, h, split, lds, shift16);
+  const int rows = t.n * a.g, last = end_key(a, t, t.p0 + t.n - 1);        // past every row's tokens
+  Rows<D, D, 1> w;
+  begin_rows<D, D, KT, 1>(a, t, h, 0, col, grp, w);
+
+  const int n16 = (runs.hi - runs.lo) << shift16, pairs = (n16 + 1) >> 1;
+  // 32 pairs of the wave at a time: lane 2 u + e finds run e of its pair u
+  for (int w0 = wave; w0 < pairs; w0 += 32 * kWaves) {
+    int my_page = 0, my_tok = 0, my_mask = 0;
+    {
+      const int x = 2 * (w0 + (lane >> 1) * kWaves) + (lane & 1), y = min(x, n16 - 1);
+      if (y >= 0) {                                      // past the end: the last run again, for no row
+        const int e = runs.lo + (y >> shift16);
+        int id = e;
+        my_mask = 0xffff;
+        if constexpr (SPARSE) {
+          id = runs.ids[e];
+          my_mask = runs.masks[id];
+        }
+        if (x >= n16) my_mask = 0;
+        my_tok = (id << runs.shift) + 16 * (y & ((1 << shift16) - 1));
+        my_page = (int)clamp_page(t.pages[my_tok >> a.ps_shift], a.num_phys);
+      }
+    }
+    const int count = min(32, (pairs - w0 + kWaves - 1) / kWaves);
+    auto fetch = [&](int u, Raw<D, KT> (&r)[2]) {
+#pragma unroll
+      for (int e = 0; e < 2; e++) {
+        const int page = __builtin_amdgcn_readlane(my_page, 2 * u + e), tok = __builtin_amdgcn_readlane(my_tok, 2 * u + e);
+        load_raw<D, KT>(a, slice_of<D, KT>(a, a.k, page, h), slice_of<D, KT>(a, a.v, page, h), tok & (a.ps - 1), col, grp,
+                        r[e]);
+      }
+    };
+    // EDGE: tokens that some row does not attend, and rows behind every row's tokens, which may hold anything
+    auto compute = [&](auto edge, int tok0, int tok1, int mask0, int mask1, Raw<D, KT> (&r)[2]) {
+      constexpr bool EDGE = decltype(edge)::value;
+      uint32_t p[4];
+      {
+        f32x4_t s[2];
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+          s[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int kk = 0; kk < KS; kk++)
+            s[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand<D, KT>(r[e], kk), w.q[0][kk], s[e], 0, 0, 0);
+        }
+        softmax_step<D, D, 1, EDGE>(a.scale_log2, 0, s, tok0, tok1, mask0, mask1, grp, w, p);
+      }
+      uint32_t v0[4][W], v1[4][W];
+      v_rows<D, KT>(r[0], v0);
+      v_rows<D, KT>(r[1], v1);
+      if constexpr (EDGE) {
+#pragma unroll
+        for (int x = 0; x < 4; x++)
+#pragma unroll
+          for (int y = 0; y < W; y++) {
+            v0[x][y] = tok0 + 4 * grp + x < last ? v0[x][y] : 0u;
+            v1[x][y] = tok1 + 4 * grp + x < last ? v1[x][y] : 0u;
+          }
+      }
+#pragma unroll
+      for (int j = 0; j < NJ; j++)
+        w.acc[0][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_operand<W>(v0, v1, j), p_operand(p), w.acc[0][j], 0, 0, 0);
+    };
+    auto step = [&](int u, Raw<D, KT> (&r)[2]) {
+      const int tok0 = __builtin_amdgcn_readlane(my_tok, 2 * u), tok1 = __builtin_amdgcn_readlane(my_tok, 2 * u + 1);
+      const int mask0 = __builtin_amdgcn_readlane(my_mask, 2 * u), mask1 = __builtin_amdgcn_readlane(my_mask, 2 * u + 1);
+      const bool whole = min(tok0, tok1) >= w.all_from && max(tok0, tok1) + 16 <= w.all_to && (mask0 & mask1) == 0xffff;
+      if (whole) compute(std::false_type{}, tok0, tok1, mask0, mask1, r);
+      else compute(std::true_type{}, tok0, tok1, mask0, mask1, r);
+    };
+    Raw<D, KT> ra[2], rb[2];
+    fetch(0, ra);
+    for (int u = 0; u < count; u += 2) {
+      fetch(min(u + 1, count - 1), rb);
+      step(u, ra);
+      if (u + 1 >= count) break;
+      fetch(min(u + 2, count - 1), ra);
+      step(u + 1, rb);
     }
   }
-  hipLaunchKernelGGL((chunk_rows_kernel<D, DV, KT, false>), grid, dim3(kThreads), 0, stream, a);
+
+  // the waves' states meet: weighted means, references and sums
+  constexpr int kRow = D + 4;                            // a row's floats in LDS
+  float* obuf = reinterpret_cast<float*>(lds);           // the lists have been read
+  float2* mbuf = reinterpret_cast<float2*>(obuf + kWaves * 16 * kRow);
+  constexpr int CPT = 16 * D / kThreads;                 // channels of a thread
+  const int orow = tid / (D / CPT), oc = (tid % (D / CPT)) * CPT;
+  __syncthreads();
+  const float sum = column_sum(w.l[0]);
+  if (grp == 0) mbuf[wave * 16 + col] = make_float2(w.m[0], sum);
+#pragma unroll
+  for (int i = 0; i < 4; i++)
+#pragma unroll
+    for (int j = 0; j < NJ; j += 4)
+      *reinterpret_cast<float4*>(obuf + (wave * 16 + col) * kRow + (4 * grp + i) * NJ + j) =
+          make_float4(w.acc[0][j][i], w.acc[0][j + 1][i], w.acc[0][j + 2][i], w.acc[0][j + 3][i]);
+  __syncthreads();
+  float2 ml[kWaves];
+  float top = kNoScore;
+#pragma unroll
+  for (int x = 0; x < kWaves; x++) {
+    ml[x] = mbuf[x * 16 + orow];
+    top = fmaxf(top, ml[x].x);
+  }
+  float total = 0.f, o[CPT];
+#pragma unroll
+  for (int c = 0; c < CPT; c++) o[c] = 0.f;
+#pragma unroll
+  for (int x = 0; x < kWaves; x++) {
+    const float f = __builtin_amdgcn_exp2f(ml[x].x - top);
+    total = fmaf(ml[x].y, f, total);
+#pragma unroll
+    for (int c = 0; c < CPT; c++) o[c] = fmaf(obuf[(x * 16 + orow) * kRow + oc + c], f, o[c]);
+  }
+  const float inv = total > 0.f ? 1.f / total : 0.f;
+  bool fine = fabsf(total) < INFINITY;
+#pragma unroll
+  for (int c = 0; c < CPT; c++) {
+    fine = fine && fabsf(o[c]) < INFINITY;
+    o[c] *= inv;
+  }
+  if (orow < rows) {
+    const int64_t at = (t.row0 + orow / a.g) * a.Hq + h * a.g + orow % a.g;
+    if (a.splits > 1) {
+      float* dst = a.part_o + (at * a.splits + split) * D + oc;
+#pragma unroll
+      for (int c = 0; c < CPT; c += 4) *reinterpret_cast<float4*>(dst + c) = make_float4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+      if (oc == 0) a.part_ml[at * a.splits + split] = make_float2(total > 0.f ? top : -INFINITY, total);
+    } else {
+#pragma unroll
+      for (int c = 0; c < CPT; c += 4)
+        *reinterpret_cast<uint2*>(a.out + at * D + oc + c) =
+            make_uint2(pack_bf16(o[c] * a.v_scale, o[c + 1] * a.v_scale), pack_bf16(o[c + 2] * a.v_scale, o[c + 3] * a.v_scale));
+      if (oc == 0 && a.lse) a.lse[at] = total > 0.f ? (top + log2f(total)) * kLn2 : -INFINITY;
+    }
+  }
+  if (__syncthreads_or(orow < rows && !fine)) {
+    if constexpr (SPARSE) listed_blocks(a, t, h, lds, const_cast<uint16_t*>(runs.ids));
+    attend_rows<D, D, KT>(a, t, h, runs, split);
+  }
+}
+
+// Four waves of 16 RT rows each share the tokens of their tile through LDS (chunk_wide.h).  A wave passes over
+// runs that none of its rows attends.
+template <int D, int DV, int KT, int RT, bool SPARSE>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(D == DV ? 2 : 1))) void chunk_wide_kernel(const ChunkArgs a) {
+  using G = Wide<D, DV, KT>;
+  constexpr int KS = D / 32, NJ = DV / 16;
+  extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
+  const int tid = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 15, grp = lane >> 4;
+  const int h = (int)blockIdx.x % a.H, split = (int)blockIdx.y;
+  Tile t;
+  // the tiles at a request's end attend most and start first
+  if (!find_tile(a, (int)(gridDim.x - 1 - blockIdx.x) / a.H, t)) return;
+  uint8_t* bufs = reinterpret_cast<uint8_t*>(lds);
+  uint32_t* lists = lds + 2 * G::BUF / sizeof(uint32_t);
+  int shift16;
+  const Runs runs = part_runs<SPARSE>(a, t, h, split, lists, shift16);
+  const int rows = t.n * a.g, last = end_key(a, t, t.p0 + t.n - 1);
+  const int r0 = wave * 16 * RT;
+  Rows<D, DV, RT> w;
+  begin_rows<D, DV, kKvBf16, RT>(a, t, h, r0, col, grp, w);
+  // the tile tokens of this wave's rows, and what they attend between them
+  const int x0 = min(r0 / a.g, t.n), x1 = min((r0 + 16 * RT - 1) / a.g, t.n - 1);
+  const int wave_from = first_key(a, t.p0 + x0), wave_to = r0 < rows ? end_key(a, t, t.p0 + x1) : 0;
+  const int wave_mask = r0 < rows ? (2 << (x1 & 15)) - (1 << (x0 & 15)) : 0;
+
+  const int n16 = (runs.hi - runs.lo) << shift16, steps = (n16 + G::UNITS - 1) / G::UNITS;
+  auto run_at = [&](int x, int& mask) {                  // first token of run x of the part
+    const int e = runs.lo + (x >> shift16);
+    int id = e;
+    mask = 0xffff;
+    if constexpr (SPARSE) {
+      id = runs.ids[e];
+      mask = runs.masks[id];
+    }
+    return (id << runs.shift) + 16 * (x & ((1 << shift16) - 1));
+  };
+  // this wave's runs of the next 64 steps, a lane each: page, and first token
+  const int unit = wave / G::WPU;
+  int my_page = 0, my_tok = 0;
+  auto look_up = [&](int s0) {
+    const int x = min(G::UNITS * (s0 + lane) + unit, n16 - 1);           // past the end: the last run again
+    int mask;
+    if (x >= 0) {
+      my_tok = run_at(x, mask);
+      my_page = (int)clamp_page(t.pages[my_tok >> a.ps_shift], a.num_phys);
+    }
+  };
+  Travel<D, DV, KT> travel;
+  auto send = [&](int s) {
+    if ((s & 63) == 0) look_up(s);
+    const int page = __builtin_amdgcn_readlane(my_page, s & 63), tok = __builtin_amdgcn_readlane(my_tok, s & 63);
+    const uint8_t* ks = slice_of<D, KT>(a, a.k, page, h);
+    send_run<D, DV, KT>(a, ks, G::kAlias ? ks : slice_of<D, KT>(a, a.v, page, h), tok & (a.ps - 1), wave, lane,
+                        bufs + (s & 1) * G::BUF, travel);
+  };
+  int tok_sent = 0;                                      // of the run on its way
+  if (steps > 0) {
+    send(0);
+    tok_sent = __builtin_amdgcn_readlane(my_tok, 0);
+  }
+  for (int s = 0; s < steps; s++) {
+    uint8_t* buf = bufs + (s & 1) * G::BUF;
+    land_run<D, DV, KT>(wave, lane, last - tok_sent, buf, travel);
+    lds_barrier();                                       // every wave's part is there, and the other buffer is free
+    if (s + 1 < steps) {
+      send(s + 1);
+      tok_sent = __builtin_amdgcn_readlane(my_tok, (s + 1) & 63);
+    }
+    const uint8_t* vt = G::kAlias ? buf : buf + G::TILE;
+#pragma unroll 1
+    for (int y = 0; y < G::UNITS; y += 2) {
+      const int x = G::UNITS * s + y;
+      if (x >= n16) break;
+      int mask0, mask1;
+      const int tok0 = __builtin_amdgcn_readfirstlane(run_at(x, mask0));
+      const int tok1 = __builtin_amdgcn_readfirstlane(run_at(min(x + 1, n16 - 1), mask1));
+      mask0 = __builtin_amdgcn_readfirstlane(mask0);
+      mask1 = x + 1 < n16 ? __builtin_amdgcn_readfirstlane(mask1) : 0;
+      if (((mask0 | mask1) & wave_mask) == 0 || min(tok0, tok1) >= wave_to || max(tok0, tok1) + 16 <= wave_from) continue;
+      const bool whole = min(tok0, tok1) >= w.all_from && max(tok0, tok1) + 16 <= w.all_to && (mask0 & mask1) == 0xffff;
+      f32x4_t sc[RT][2];
+#pragma unroll
+      for (int rt = 0; rt < RT; rt++) sc[rt][0] = sc[rt][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kk = 0; kk < KS; kk++) {
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+          const bf16x8_t k = k_from_lds<D>(buf, 16 * (y + e), kk, col, grp);
+#pragma unroll
+          for (int rt = 0; rt < RT; rt++) sc[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, w.q[rt][kk], sc[rt][e], 0, 0, 0);
+        }
+      }
+      uint32_t p[RT][4];
+#pragma unroll
+      for (int rt = 0; rt < RT; rt++) {
+        if (whole) softmax_step<D, DV, RT, false>(a.scale_log2, rt, sc[rt], tok0, tok1, mask0, mask1, grp, w, p[rt]);
+        else softmax_step<D, DV, RT, true>(a.scale_log2, rt, sc[rt], tok0, tok1, mask0, mask1, grp, w, p[rt]);
+      }
+#pragma unroll
+      for (int j = 0; j < NJ; j++) {
+        const bf16x8_t v = v_from_lds<D>(vt, 16 * y, j, col, grp);
+#pragma unroll
+        for (int rt = 0; rt < RT; rt++)
+          w.acc[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_operand(p[rt]), w.acc[rt][j], 0, 0, 0);
+      }
+    }
+  }
+
+  bool bad = false;
+#pragma unroll
+  for (int rt = 0; rt < RT; rt++) {
+    const float total = column_sum(w.l[rt]);
+    const float inv = total > 0.f ? 1.f / total : 0.f;
+    const int r = r0 + 16 * rt + col;
+    const bool there = r < rows;
+    const int64_t at = (t.row0 + (there ? r / a.g : 0)) * a.Hq + h * a.g + (there ? r % a.g : 0);
+    bool fine = fabsf(total) < INFINITY;
+#pragma unroll
+    for (int j = 0; j < NJ; j++) {
+      float o[4];
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        fine = fine && fabsf(w.acc[rt][j][i]) < INFINITY;
+        o[i] = w.acc[rt][j][i] * inv;
+      }
+      if (!there) continue;
+      if (a.splits > 1)
+        *reinterpret_cast<float4*>(a.part_o + (at * a.splits + split) * DV + 16 * j + 4 * grp) = make_float4(o[0], o[1], o[2], o[3]);
+      else
+        *reinterpret_cast<uint2*>(a.out + at * DV + 16 * j + 4 * grp) =
+            make_uint2(pack_bf16(o[0] * a.v_scale, o[1] * a.v_scale), pack_bf16(o[2] * a.v_scale, o[3] * a.v_scale));
+    }
+    if (there && grp == 0) {
+      if (a.splits > 1) a.part_ml[at * a.splits + split] = make_float2(total > 0.f ? w.m[rt] : -INFINITY, total);
+      else if (a.lse) a.lse[at] = total > 0.f ? (w.m[rt] + log2f(total)) * kLn2 : -INFINITY;
+    }
+    bad = bad || (there && !fine);
+  }
+  if (__syncthreads_or(bad)) attend_rows<D, DV, KT>(a, t, h, runs, split);
+}
+
+// Joins the parts of every row of a tile, a wave a row: each part's weight is its sum at the rows' largest
+// reference.
+template <int DV>
+__global__ __launch_bounds__(kThreads) void chunk_merge_kernel(const ChunkArgs a) {
+  const int lane = lane_id(), h = (int)blockIdx.x % a.H, S = a.splits;
+  Tile t;
+  if (!find_tile(a, (int)blockIdx.x / a.H, t)) return;
+  for (int x = (int)threadIdx.x >> 6; x < t.n * a.g; x += kWaves) {
+    const int64_t at = (t.row0 + x / a.g) * a.Hq + h * a.g + x % a.g;
+    const float2 ml = lane < S ? a.part_ml[at * S + lane] : make_float2(-INFINITY, 0.f);
+    float top = ml.y != 0.f ? ml.x : -INFINITY;
+#pragma unroll
+    for (int s = 1; s < kWave; s <<= 1) top = fmaxf(top, xor_shfl(top, s));
+    float w = ml.y == 0.f ? 0.f : ml.y * __builtin_amdgcn_exp2f(ml.x - top);   // NaN stays NaN
+    float total = w;
+#pragma unroll
+    for (int s = 1; s < kWave; s <<= 1) total += xor_shfl(total, s);
+    w = total != 0.f ? w / total : 0.f;
+    float o[DV / kWave];
+#pragma unroll
+    for (int c = 0; c < DV / kWave; c++) o[c] = 0.f;
+    for (int s = 0; s < S; s++) {
+      const float f = __shfl(w, s, kWave);
+      if (f == 0.f) continue;
+      const float* src = a.part_o + (at * S + s) * DV + lane;
+#pragma unroll
+      for (int c = 0; c < DV / kWave; c++) o[c] = fmaf(src[c * kWave], f, o[c]);
+    }
+#pragma unroll
+    for (int c = 0; c < DV / kWave; c++) a.out[at * DV + c * kWave + lane] = (uint16_t)f32_to_bf16_rne(o[c] * a.v_scale);
+    if (lane == 0 && a.lse) a.lse[at] = total > 0.f ? (top + log2f(total)) * kLn2 : total == 0.f ? -INFINITY : total;
+  }
+}
+
+// Rows of a wave's operand, tokens of a tile and parts of its list.
+struct Plan {
+  int operands;                            // of 16 rows a wave (wide), 0: narrow
+  int tokens, splits;
+  size_t o_bytes, bytes;
+};
+Plan plan_of(const Geometry& g, int n, int Hq, bool sparse, int max_sel) {
+  Plan p{};
+  const int group = Hq / g.H;
+  const bool latent = g.Dqk != g.Dv;
+  const int64_t batch = std::max(g.batch, 1);
+  auto tokens = [&](int rows) { return std::max(1, sparse ? std::min(16, rows / group) : rows / group); };
+  if (!latent && (int64_t)n <= batch * (kTileRows / group)) p.operands = 0;
+  else p.operands = sparse || latent || (int64_t)n * group <= batch * 4 * kTileRows ? 1 : 2;
+  p.tokens = tokens(p.operands == 0 ? kTileRows : 4 * kTileRows * p.operands);
+  const int64_t tiles = std::max<int64_t>(batch, (n + p.tokens - 1) / p.tokens) * g.H;
+  const int64_t list = std::min<int64_t>((int64_t)g.max_pages * g.bs, sparse ? (int64_t)max_sel * p.tokens * g.bs : INT64_MAX);
+  const int64_t most = std::min<int64_t>(kMaxParts, (list + kPartTokens - 1) / kPartTokens);
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, kTargetWgs / tiles));
+  if (p.splits > 1) {
+    p.o_bytes = (size_t)n * Hq * p.splits * g.Dv * sizeof(float);
+    p.bytes = p.o_bytes + (size_t)n * Hq * p.splits * sizeof(float2);
+  }
+  p.bytes = std::max<size_t>(p.bytes, 16);
+  return p;
+}
+
+template <int D, int KT, bool SPARSE>
+void launch_narrow(const ChunkArgs& a, dim3 grid, size_t lists, hipStream_t stream) {
+  const size_t states = sizeof(float) * kWaves * 16 * (D + 4) + sizeof(float2) * kWaves * 16;
+  hipLaunchKernelGGL((chunk_narrow_kernel<D, KT, SPARSE>), grid, dim3(kThreads), std::max(lists, states), stream, a);
+}
+template <int D, int DV, int KT, int RT, bool SPARSE>
+void launch_wide(const ChunkArgs& a, dim3 grid, size_t lists, hipStream_t stream) {
+  const size_t lds = 2 * (size_t)Wide<D, DV, KT>::BUF + lists;
+  hipLaunchKernelGGL((chunk_wide_kernel<D, DV, KT, RT, SPARSE>), grid, dim3(kThreads), lds, stream, a);
+}
+
+template <int D, int DV, int KT>
+hipError_t launch_kt(const ChunkArgs& a, int operands, hipStream_t stream) {
+  const int64_t tiles = (int64_t)a.num_rows / a.tokens + a.batch;
+  const dim3 grid((unsigned)(tiles * a.H), (unsigned)a.splits);
+  if constexpr (D == DV) {
+    const size_t lists = a.sel_pages ? 2 * sizeof(uint32_t) * ((a.max_blocks + 1) / 2) : 0;    // at most 64 KiB
+    if (operands == 0) {
+      if (a.sel_pages) launch_narrow<D, KT, true>(a, grid, lists, stream);
+      else launch_narrow<D, KT, false>(a, grid, 0, stream);
+    } else if (a.sel_pages) {
+      launch_wide<D, DV, KT, 1, true>(a, grid, lists, stream);
+    } else if (operands == 1) {
+      launch_wide<D, DV, KT, 1, false>(a, grid, 0, stream);
+    } else {
+      launch_wide<D, DV, KT, 2, false>(a, grid, 0, stream);
+    }
+  } else {
+    launch_wide<D, DV, KT, 1, false>(a, grid, 0, stream);
+  }
+  if (a.splits > 1) {
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((chunk_merge_kernel<DV>), dim3((unsigned)(tiles * a.H)), dim3(kThreads), 0, stream, a);
+  }
   return hipGetLastError();
 }
 
 template <int D, int DV>
-hipError_t launch_d(const ChunkArgs& a, int kt, hipStream_t stream) {
-  if (kt == kKvFp8E4M3) return launch_kt<D, DV, kKvFp8E4M3>(a, stream);
-  if (kt == kKvFp8E5M2) return launch_kt<D, DV, kKvFp8E5M2>(a, stream);
+hipError_t launch_d(const ChunkArgs& a, int kt, int operands, hipStream_t stream) {
+  if (kt == kKvFp8E4M3) return launch_kt<D, DV, kKvFp8E4M3>(a, operands, stream);
+  if (kt == kKvFp8E5M2) return launch_kt<D, DV, kKvFp8E5M2>(a, operands, stream);
   if constexpr (D == DV) {
-    if (kt == kKvMxFp4) return launch_kt<D, DV, kKvMxFp4>(a, stream);
+    if (kt == kKvMxFp4) return launch_kt<D, DV, kKvMxFp4>(a, operands, stream);
   }
-  return launch_kt<D, DV, kKvBf16>(a, stream);
+  return launch_kt<D, DV, kKvBf16>(a, operands, stream);
 }
 
 }  // namespace
 
-size_t chunk_attention_workspace(const Geometry& g, int n, int Hq, bool sparse, int max_sel) { return 16; }
+size_t chunk_attention_workspace(const Geometry& g, int n, int Hq, bool sparse, int max_sel) {
+  return plan_of(g, n, Hq, sparse, max_sel).bytes;
+}
 
 hipError_t launch_chunk_attention(const Geometry& g, const ChunkRows& rows, const ChunkSelection& sel, int window,
                                   bool causal, float sm_scale, uint16_t* out, float* lse, void* ws, hipStream_t stream) {
@@ -150,11 +555,14 @@ hipError_t launch_chunk_attention(const Geometry& g, const ChunkRows& rows, cons
   a.v_scale = g.v ? g.v_scale : g.k_scale;
   a.out = out;
   a.lse = lse;
-  a.tokens = kTileRows / a.g;
-  a.splits = 1;
-  if (g.Dqk == 128) return launch_d<128, 128>(a, g.kv_dtype, stream);
-  if (g.Dqk == 64) return launch_d<64, 64>(a, g.kv_dtype, stream);
-  return launch_d<576, 512>(a, g.kv_dtype, stream);
+  const Plan p = plan_of(g, rows.n, rows.Hq, sel.pages != nullptr, sel.max_sel);
+  a.tokens = p.tokens;
+  a.splits = p.splits;
+  a.part_o = static_cast<float*>(ws);
+  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + p.o_bytes);
+  if (g.Dqk == 128) return launch_d<128, 128>(a, g.kv_dtype, p.operands, stream);
+  if (g.Dqk == 64) return launch_d<64, 64>(a, g.kv_dtype, p.operands, stream);
+  return launch_d<576, 512>(a, g.kv_dtype, p.operands, stream);
 }
 
 }  // namespace vx

@@ -1,0 +1,248 @@
+// Matrix operands of 16 cache tokens, from any cache type, and the online softmax that the tile kernels
+// share.
+//
+// S^T = K Q^T is a 16x16x32 product: operand A is 16 tokens (row = lane & 15), operand B 16 query rows.  Lane
+// (grp, col) then holds S[token 4 grp + i][row col], which, as bf16, is operand B of O^T = V^T P^T if the
+// contraction's slot (grp, j) is token 4 grp + j of the first 16 tokens (j < 4) or of the second: no value
+// changes lanes between the two products.  Row `col` of V^T operand j is channel col * D / 16 + j, so that a
+// lane's channels are neighbours in a V row.
+#pragma once
+#include "chunk_common.h"
+
+namespace vx {
+namespace chunk {
+
+typedef __bf16 bf16x2v_t __attribute__((ext_vector_type(2)));
+
+template <int KT, bool HI>
+__device__ __forceinline__ uint32_t fp8_pair(uint32_t w) {
+  bf16x2v_t r;
+  if constexpr (KT == kKvFp8E4M3) r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.0f, HI);
+  else r = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8((int)w, 1.0f, HI);
+  return __builtin_bit_cast(uint32_t, r);
+}
+
+// Two floats as a bf16 pair, to nearest even.
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const bf16x2v_t v = {(__bf16)a, (__bf16)b};
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// Channels of a lane's k-step kk of a K row (and of the query): 8 from here.  Types below 16 bits take D / 4
+// consecutive channels a lane, so that they arrive in 16-byte loads.
+template <int D, int KT>
+__device__ __forceinline__ int k_channel(int kk, int grp) {
+  return KT == kKvBf16 ? 32 * kk + 8 * grp : D / 4 * grp + 8 * kk;
+}
+
+// 16 tokens of K and V as loaded.
+template <int D, int KT>
+struct Raw {
+  static constexpr int KW = KT == kKvBf16 ? D / 8 : KT == kKvMxFp4 ? D / 32 : D / 16;    // words of a lane's part of K
+  static constexpr int VW = KT == kKvBf16 ? D / 32 : KT == kKvMxFp4 ? 1 : D / 64;        // words of a V row's
+  uint32_t k[KW];
+  uint32_t v[4 * (KT == kKvMxFp4 ? 1 : VW)];
+  uint32_t ks, vs;                                                                        // mxfp4 scales
+};
+
+template <int N>
+__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {
+  if constexpr (N >= 4) {
+#pragma unroll
+    for (int x = 0; x < N; x += 4) {
+      const uint4 y = *reinterpret_cast<const uint4*>(p + 4 * x);
+      w[x] = y.x;
+      w[x + 1] = y.y;
+      w[x + 2] = y.z;
+      w[x + 3] = y.w;
+    }
+  } else if constexpr (N == 2) {
+    const uint2 y = *reinterpret_cast<const uint2*>(p);
+    w[0] = y.x;
+    w[1] = y.y;
+  } else {
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
+  }
+}
+
+// Tokens t .. t + 15 (t a multiple of 16) of a page's K and V slices.
+template <int D, int KT>
+__device__ __forceinline__ void load_raw(const ChunkArgs& a, const uint8_t* ks, const uint8_t* vs, int t, int col,
+                                         int grp, Raw<D, KT>& r) {
+  if constexpr (KT == kKvMxFp4) {
+    load_words<D / 32>(ks + (t + col) * (D / 2) + D / 8 * grp, r.k);
+    r.ks = ks[mx::codes_bytes(a.ps, D) + mx::k_scale(t + col, D / 4 * grp / 32, D)];
+    const int quad = (t >> 2) + grp;
+    load_words<D / 32>(vs + (quad * 16 + col) * (D / 8), r.v);
+    r.vs = *reinterpret_cast<const uint32_t*>(vs + mx::codes_bytes(a.ps, D) + (quad * (D / 32) + col * (D / 16) / 32) * 4);
+  } else if constexpr (KT == kKvBf16) {
+#pragma unroll
+    for (int kk = 0; kk < D / 32; kk++) load_words<4>(ks + 2 * ((t + col) * D + 32 * kk + 8 * grp), r.k + 4 * kk);
+#pragma unroll
+    for (int x = 0; x < 4; x++) load_words<D / 32>(vs + 2 * ((t + 4 * grp + x) * D + col * (D / 16)), r.v + x * (D / 32));
+  } else {
+    load_words<D / 16>(ks + (t + col) * D + D / 4 * grp, r.k);
+#pragma unroll
+    for (int x = 0; x < 4; x++) load_words<D / 64>(vs + (t + 4 * grp + x) * D + col * (D / 16), r.v + x * (D / 64));
+  }
+}
+
+// Operand A of k-step kk.
+template <int D, int KT>
+__device__ __forceinline__ bf16x8_t k_operand(const Raw<D, KT>& r, int kk) {
+  u32x4_t w;
+  if constexpr (KT == kKvBf16) {
+    w = u32x4_t{r.k[4 * kk], r.k[4 * kk + 1], r.k[4 * kk + 2], r.k[4 * kk + 3]};
+  } else if constexpr (KT == kKvMxFp4) {
+    const float s = mx::scale_operand(r.ks);
+    const uint32_t c = r.k[kk];
+    w = u32x4_t{mx::pair_bf16<0>(c, s), mx::pair_bf16<1>(c, s), mx::pair_bf16<2>(c, s), mx::pair_bf16<3>(c, s)};
+  } else {
+    const uint32_t lo = r.k[2 * kk], hi = r.k[2 * kk + 1];
+    w = u32x4_t{fp8_pair<KT, false>(lo), fp8_pair<KT, true>(lo), fp8_pair<KT, false>(hi), fp8_pair<KT, true>(hi)};
+  }
+  return __builtin_bit_cast(bf16x8_t, w);
+}
+
+// Rows 4 grp + x of V as bf16 words: channels col * D / 16 ..
+template <int D, int KT>
+__device__ __forceinline__ void v_rows(const Raw<D, KT>& r, uint32_t (&v)[4][D / 32]) {
+#pragma unroll
+  for (int x = 0; x < 4; x++) {
+    if constexpr (KT == kKvBf16) {
+#pragma unroll
+      for (int w = 0; w < D / 32; w++) v[x][w] = r.v[x * (D / 32) + w];
+    } else if constexpr (KT == kKvMxFp4) {
+      const float s = mx::scale_operand((r.vs >> (8 * x)) & 255);
+      if constexpr (D == 128) {
+        v[x][0] = mx::pair_bf16<0>(r.v[x], s);
+        v[x][1] = mx::pair_bf16<1>(r.v[x], s);
+        v[x][2] = mx::pair_bf16<2>(r.v[x], s);
+        v[x][3] = mx::pair_bf16<3>(r.v[x], s);
+      } else {
+        const uint32_t c = r.v[x >> 1];
+        v[x][0] = (x & 1) ? mx::pair_bf16<2>(c, s) : mx::pair_bf16<0>(c, s);
+        v[x][1] = (x & 1) ? mx::pair_bf16<3>(c, s) : mx::pair_bf16<1>(c, s);
+      }
+    } else {
+#pragma unroll
+      for (int w = 0; w < D / 64; w++) {
+        v[x][2 * w] = fp8_pair<KT, false>(r.v[x * (D / 64) + w]);
+        v[x][2 * w + 1] = fp8_pair<KT, true>(r.v[x * (D / 64) + w]);
+      }
+    }
+  }
+}
+
+// Operand A of O^T for output channels col * D / 16 + j, from the rows of two runs of 16 tokens.
+template <int W>
+__device__ __forceinline__ bf16x8_t v_operand(const uint32_t (&v0)[4][W], const uint32_t (&v1)[4][W], int j) {
+  const uint32_t sel = (j & 1) ? 0x07060302u : 0x05040100u;
+  const int w = j >> 1;
+  const u32x4_t o = {__builtin_amdgcn_perm(v0[1][w], v0[0][w], sel), __builtin_amdgcn_perm(v0[3][w], v0[2][w], sel),
+                     __builtin_amdgcn_perm(v1[1][w], v1[0][w], sel), __builtin_amdgcn_perm(v1[3][w], v1[2][w], sel)};
+  return __builtin_bit_cast(bf16x8_t, o);
+}
+
+// Largest over the four lanes of a column (lanes 16 and 32 apart), and sum.
+__device__ __forceinline__ float column_max(float x) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float column_sum(float x) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// The weights' reference: 2^kAhead past the score that moved it, so that it moves seldom and no weight
+// passes 1.
+constexpr float kAhead = 8.f;
+constexpr float kNoScore = -3.0e38f;       // the reference before the first score
+
+// The rows of a wave: operand B, what each attends, and the state of their softmax.
+template <int D, int DV, int RT>
+struct Rows {
+  static constexpr int KS = D / 32, NJ = DV / 16;
+  bf16x8_t q[RT][KS];
+  int from[RT], to[RT], bit[RT];
+  int all_from, all_to;                    // tokens that every row attends (uniform)
+  f32x4_t acc[RT][NJ];
+  float m[RT], l[RT];
+};
+
+template <int D, int DV, int KT, int RT>
+__device__ __forceinline__ void begin_rows(const ChunkArgs& a, const Tile& t, int h, int r0, int col, int grp,
+                                           Rows<D, DV, RT>& w) {
+  const int rows = t.n * a.g;
+#pragma unroll
+  for (int rt = 0; rt < RT; rt++) {
+    const int r = r0 + 16 * rt + col, x = r / a.g, head = r - x * a.g;
+    const bool there = r < rows;
+    const uint16_t* src = a.q + (t.row0 + (there ? x : 0)) * a.q_row + (int64_t)(h * a.g + (there ? head : 0)) * a.q_head;
+#pragma unroll
+    for (int kk = 0; kk < D / 32; kk++) {
+      w.q[rt][kk] = *reinterpret_cast<const bf16x8_t*>(src + k_channel<D, KT>(kk, grp));
+      if (!there) w.q[rt][kk] = bf16x8_t{};
+    }
+    w.from[rt] = first_key(a, t.p0 + x);
+    w.to[rt] = there ? end_key(a, t, t.p0 + x) : 0;
+    w.bit[rt] = x & 15;
+    w.m[rt] = kNoScore;
+    w.l[rt] = 0.f;
+#pragma unroll
+    for (int j = 0; j < DV / 16; j++) w.acc[rt][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  w.all_from = first_key(a, t.p0 + t.n - 1);
+  w.all_to = end_key(a, t, t.p0);
+}
+
+// One step of the softmax: the scores s of 32 tokens (16 from tok0, 16 from tok1, of the tile tokens in mask0 and
+// mask1) become weights p, bf16, operand B of O^T = V^T P^T.  The sum takes the weights before their rounding,
+// which is to the nearest (2^-9 of each at most, without a bias) and halves the matrix work that two parts would need.
+template <int D, int DV, int RT, bool MASK>
+__device__ __forceinline__ void softmax_step(float scale_log2, int rt, f32x4_t (&s)[2], int tok0, int tok1, int mask0,
+                                             int mask1, int grp, Rows<D, DV, RT>& w, uint32_t (&p)[4]) {
+  if constexpr (MASK) {
+    const int t0 = tok0 + 4 * grp, t1 = tok1 + 4 * grp;
+    const int to0 = ((mask0 >> w.bit[rt]) & 1) ? w.to[rt] : 0, to1 = ((mask1 >> w.bit[rt]) & 1) ? w.to[rt] : 0;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      s[0][i] = t0 + i < to0 && t0 + i >= w.from[rt] ? s[0][i] : -INFINITY;
+      s[1][i] = t1 + i < to1 && t1 + i >= w.from[rt] ? s[1][i] : -INFINITY;
+    }
+  }
+  const float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                          fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))) *
+                    scale_log2;
+  if (__any(top > w.m[rt])) {
+    const float c = column_max(top), next = c > w.m[rt] ? c + kAhead : w.m[rt];
+    const float alpha = __builtin_amdgcn_exp2f(w.m[rt] - next);
+    w.m[rt] = next;
+    w.l[rt] *= alpha;
+#pragma unroll
+    for (int j = 0; j < DV / 16; j++)
+#pragma unroll
+      for (int i = 0; i < 4; i++) w.acc[rt][j][i] *= alpha;
+  }
+  float x[8], sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    x[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], scale_log2, -w.m[rt]));
+    sum += x[i];
+  }
+  w.l[rt] += sum;
+#pragma unroll
+  for (int i = 0; i < 4; i++) p[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+}
+
+__device__ __forceinline__ bf16x8_t p_operand(const uint32_t (&p)[4]) {
+  const u32x4_t w = {p[0], p[1], p[2], p[3]};
+  return __builtin_bit_cast(bf16x8_t, w);
+}
+
+}  // namespace chunk
+}  // namespace vx
