@@ -360,8 +360,7 @@ def _run_own(s):
         return {"out": s["out"], "lse": s["lse_out"]}
     if s["op"] == "select":
         vx.chunk_score_topk(s["q"], h["kv"], h["batch"], s["q_indptr"], vx.MEAN_DOT, s["mean"], s["pages_budget"],
-                            s["sink"], s["local"], s["max_sel"], s["sel_pages"], s["sel_count"], h["ws"],
-                            mean_bf16=s["mean_bf16"])
+                            s["sink"], s["local"], s["max_sel"], s["sel_pages"], s["sel_count"], h["ws"])
         return {"pages": s["sel_pages"], "count": s["sel_count"]}
     vx.sparse_chunk_attention(s["q"], h["kv"], h["batch"], s["q_indptr"], s["sel_pages"], s["sel_count"], s["sm_scale"],
                               s["out"], h["ws"], lse=s["lse_out"])
