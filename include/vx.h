@@ -593,14 +593,13 @@ vx_status vx_chunk_attention(const void* q, int64_t q_row_stride, int64_t q_head
  * queries; F, K_total, ties and the lists are those of vx_page_score_topk with P_i = PB:
  *   sel_pages [num_rows][num_kv_heads][max_sel], sel_count [num_rows]
  * kind: VX_SCORE_MEAN_DOT (s_j = mean over the group of q_r . Mean_j, fp64, rounded to fp32).  n_local >= 1,
- * so that the token's own block, whose summary may hold later tokens, is kept and not scored.  mean_bf16 (may
- * be NULL) is vx_page_summarize's copy and serves a bounded first pass; the selection is the same with and
- * without it.  At most 16384 blocks a request.  q as for vx_chunk_attention. */
+ * so that the token's own block, whose summary may hold later tokens, is kept and not scored.  At most 16384
+ * blocks a request.  mean is 16-byte aligned, q as for vx_chunk_attention. */
 vx_status vx_chunk_score_topk(const void* q, int64_t q_row_stride, int64_t q_head_stride, int32_t num_q_heads,
                               const vx_paged_cache* kv, const vx_batch* b, const vx_chunk* chunk, vx_score_kind kind,
-                              const float* mean, const void* mean_bf16, const int32_t* pages_budget, int32_t n_sink,
-                              int32_t n_local, int32_t max_sel, int32_t* sel_pages, int32_t* sel_count,
-                              void* workspace, size_t workspace_bytes, hipStream_t stream);
+                              const float* mean, const int32_t* pages_budget, int32_t n_sink, int32_t n_local,
+                              int32_t max_sel, int32_t* sel_pages, int32_t* sel_count, void* workspace,
+                              size_t workspace_bytes, hipStream_t stream);
 
 /* vx_chunk_attention (causal, no window, GQA geometry) over the tokens of the blocks that are listed for
  * each row and KV head: sel_pages[row][h][0 .. sel_count[row] - 1], in any order; a block listed twice

@@ -889,9 +889,9 @@ vx_status vx_chunk_attention(const void* q, int64_t q_row_stride, int64_t q_head
 
 vx_status vx_chunk_score_topk(const void* q, int64_t q_row_stride, int64_t q_head_stride, int32_t num_q_heads,
                               const vx_paged_cache* kv, const vx_batch* b, const vx_chunk* chunk, vx_score_kind kind,
-                              const float* mean, const void* mean_bf16, const int32_t* pages_budget, int32_t n_sink,
-                              int32_t n_local, int32_t max_sel, int32_t* sel_pages, int32_t* sel_count,
-                              void* workspace, size_t workspace_bytes, hipStream_t stream) {
+                              const float* mean, const int32_t* pages_budget, int32_t n_sink, int32_t n_local, int32_t max_sel,
+                              int32_t* sel_pages, int32_t* sel_count, void* workspace, size_t workspace_bytes,
+                              hipStream_t stream) {
   vx_status s;
   if ((s = check_chunk(q, q_row_stride, q_head_stride, num_q_heads, kv, b, chunk, false, true)) != VX_OK) return s;
   if (kind != VX_SCORE_MEAN_DOT) {
@@ -909,8 +909,7 @@ vx_status vx_chunk_score_topk(const void* q, int64_t q_row_stride, int64_t q_hea
   if ((s = check_workspace("vx_chunk_score_topk", workspace, workspace_bytes, need)) != VX_OK) return s;
   if (!mean || !pages_budget || !sel_pages || !sel_count)
     return fail(VX_ERR_INVALID_ARG, "mean, pages_budget, sel_pages and sel_count must be non-NULL");
-  if (odd_address(mean, 16) || odd_address(mean_bf16, 16))
-    return fail(VX_ERR_INVALID_ARG, "mean and mean_bf16 must be 16-byte aligned");
+  if (odd_address(mean, 16)) return fail(VX_ERR_INVALID_ARG, "mean must be 16-byte aligned");
   if (odd_address(pages_budget, 4)) return fail(VX_ERR_INVALID_ARG, "int32 arrays must be 4-byte aligned");
   const size_t rows = chunk->num_rows, means = (size_t)g.num_phys_pages * g.r * g.H * g.Dqk;
   const Span written[] = {{"sel_pages", sel_pages, rows * g.H * max_sel * 4, true, 4},
@@ -919,12 +918,10 @@ vx_status vx_chunk_score_topk(const void* q, int64_t q_row_stride, int64_t q_hea
   if ((s = check_results(written, 3, {"q", q, chunk->num_rows, num_q_heads, g.Dqk, q_row_stride, q_head_stride}, kv, b,
                          chunk,
                          {{"mean", mean, means * 4, false},
-                          {"mean_bf16", mean_bf16, mean_bf16 ? means * 2 : 0, false},
                           {"pages_budget", pages_budget, (size_t)b->batch * 4, false}})) != VX_OK)
     return s;
   return hip_status(vx::launch_chunk_select(g, chunk_rows(q, q_row_stride, q_head_stride, num_q_heads, chunk), mean,
-                                            static_cast<const uint16_t*>(mean_bf16), pages_budget, n_sink, n_local,
-                                            max_sel, sel_pages, sel_count, workspace, stream),
+                                            pages_budget, n_sink, n_local, max_sel, sel_pages, sel_count, workspace, stream),
                     "vx_chunk_score_topk");
 }
 

@@ -143,9 +143,9 @@ hipError_t launch_chunk_attention(const Geometry& g, const ChunkRows& rows, cons
                                   bool causal, float sm_scale, uint16_t* out, float* lse, void* ws, hipStream_t stream);
 
 size_t chunk_select_workspace(const Geometry& g, int n, int Hq);
-hipError_t launch_chunk_select(const Geometry& g, const ChunkRows& rows, const float* mean, const uint16_t* mean_bf,
-                               const int32_t* budget, int n_sink, int n_local, int max_sel, int32_t* sel_pages,
-                               int32_t* sel_count, void* ws, hipStream_t stream);
+hipError_t launch_chunk_select(const Geometry& g, const ChunkRows& rows, const float* mean, const int32_t* budget,
+                               int n_sink, int n_local, int max_sel, int32_t* sel_pages, int32_t* sel_count, void* ws,
+                               hipStream_t stream);
 
 // The state of a page pool (vx_page_pool, checked).
 struct PagePool {

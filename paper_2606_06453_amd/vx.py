@@ -124,7 +124,7 @@ def lib():
         L.vx_rope_kv_write.argtypes = [P, P, P, i64, i64, i32, P, i64, i64, P, i64, i64, P, i64, i64, P, i64, P, i32, P]
         L.vx_chunk_workspace_size.argtypes = [i32, P, P, i32, i32, i32, ctypes.POINTER(sz)]
         L.vx_chunk_attention.argtypes = [P, i64, i64, i32, P, P, P, i32, i32, ctypes.c_float, P, P, P, sz, P]
-        L.vx_chunk_score_topk.argtypes = [P, i64, i64, i32, P, P, P, i32, P, P, P, i32, i32, i32, P, P, P, sz, P]
+        L.vx_chunk_score_topk.argtypes = [P, i64, i64, i32, P, P, P, i32, P, P, i32, i32, i32, P, P, P, sz, P]
         L.vx_sparse_chunk_attention.argtypes = [P, i64, i64, i32, P, P, P, P, P, i32, ctypes.c_float, P, P, P, sz, P]
         for f in (L.vx_rope_kv_write, L.vx_chunk_workspace_size, L.vx_chunk_attention, L.vx_chunk_score_topk,
                   L.vx_sparse_chunk_attention):
@@ -557,19 +557,17 @@ def chunk_attention(q: torch.Tensor, kv: PagedKV, batch: BatchSpec, q_indptr: to
 def chunk_score_topk(q: torch.Tensor, kv: PagedKV, batch: BatchSpec, q_indptr: torch.Tensor, kind: int,
                      mean: torch.Tensor, pages_budget: torch.Tensor, n_sink: int, n_local: int, max_sel: int,
                      sel_pages: torch.Tensor, sel_count: torch.Tensor, workspace: torch.Tensor,
-                     q_lens: Optional[torch.Tensor] = None, mean_bf16: Optional[torch.Tensor] = None,
-                     stream=None) -> None:
+                     q_lens: Optional[torch.Tensor] = None, stream=None) -> None:
     """The blocks that each token of a chunk attends: page_score_topk for every token by itself, into
     sel_pages [n][H][max_sel] and sel_count [n] (int32).  kind: MEAN_DOT; n_local >= 1."""
     d, args = _chunk_args(q, kv, batch, q_indptr, q_lens, workspace)
     n, H, D = q.shape[0], kv._dims[0], kv._dims[1]
     blocks = kv.k.shape[0] * (kv.k.shape[2] // kv.block_size if kv.block_size else 1)
     m = _result(mean, torch.float32, (blocks, H, D), d, "mean")
-    mb = _result(mean_bf16, torch.bfloat16, (blocks, H, D), d, "mean_bf16")
     budget = _result(pages_budget, torch.int32, (batch.seq_lens.numel(),), d, "pages_budget")
     sp = _result(sel_pages, torch.int32, (n, H, max_sel), d, "sel_pages")
     sc = _result(sel_count, torch.int32, (n,), d, "sel_count")
-    _check(lib().vx_chunk_score_topk(*args, kind, m, mb, budget, n_sink, n_local, max_sel, sp, sc, workspace.data_ptr(),
+    _check(lib().vx_chunk_score_topk(*args, kind, m, budget, n_sink, n_local, max_sel, sp, sc, workspace.data_ptr(),
                                      _bytes(workspace), _stream(stream, d)))
 
 

@@ -142,17 +142,17 @@ def test_sparse_chunk_attention():
 
 
 def test_chunk_score_topk():
-    def call(q=_at(7), qs=(4096, 128), Hq=32, kv=None, b=None, chunk=None, kind=0, mean=_at(10), mb=_at(11), budget=_at(12), sink=1, local=1, M=4, sel=_at(13),
+    def call(q=_at(7), qs=(4096, 128), Hq=32, kv=None, b=None, chunk=None, kind=0, mean=_at(10), budget=_at(12), sink=1, local=1, M=4, sel=_at(13),
              count=_at(14), ws=_at(20), ws_bytes=1 << 30, null=False):
         kv, b = kv or _kv(), b or _batch()
-        return vx.lib().vx_chunk_score_topk(q, *qs, Hq, ctypes.byref(kv), ctypes.byref(b), None if null else chunk or _chunk(), kind, mean, mb, budget, sink,
+        return vx.lib().vx_chunk_score_topk(q, *qs, Hq, ctypes.byref(kv), ctypes.byref(b), None if null else chunk or _chunk(), kind, mean, budget, sink,
                                             local, M, sel, count, ws, ws_bytes, None)
 
     _shared(lambda **kw: call(null="chunk" in kw and kw["chunk"] is None, **kw))
     for kw, st, word in ((dict(kind=1), 2, "kind"), (dict(kind=7), 2, "kind"), (dict(kind=-1), 1, "kind"), (dict(kind=9), 1, "kind"), (dict(mean=None), 1, "mean"),
                          (dict(budget=None), 1, "budget"), (dict(sel=None), 1, "sel_pages"), (dict(count=None), 1, "sel_count"), (dict(local=0), 1, "n_local"),
                          (dict(sink=-1), 1, "n_sink"), (dict(sink=4), 1, "max_sel"), (dict(M=0), 1, "max_sel"), (dict(mean=_at(10) + 4), 1, "aligned"),
-                         (dict(mb=_at(11) + 2), 1, "aligned"), (dict(sel=_at(10)), 1, "overlap"), (dict(count=_at(12)), 1, "overlap"), (dict(sel=_at(14)), 1, "overlap"),
+                         (dict(sel=_at(10)), 1, "overlap"), (dict(count=_at(12)), 1, "overlap"), (dict(sel=_at(14)), 1, "overlap"),
                          (dict(kv=_kv(D=576, Dv=512, H=1, v=None), Hq=16), 2, "GQA"), (dict(b=_batch(pages=20000)), 2, "blocks")):
         assert call(**kw) == st and word in _msg(), (kw, _msg())
 

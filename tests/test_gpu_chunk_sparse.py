@@ -114,15 +114,15 @@ def test_every_block_is_dense_attention():
 
 
 # ---- selection -----------------------------------------------------------------------------------
-def _select(c, mean, budget, n_sink, n_local, M, bf16=True, q=None):
+def _select(c, mean, budget, n_sink, n_local, M, q=None):
     kv, batch, qd, qi, ql = c.on_gpu()
     md = torch.from_numpy(mean).cuda()
     ws = torch.full((vx.chunk_workspace_size(vx.CHUNK_SCORE_TOPK, kv, batch, c.rows, c.Hq, M),), 255, dtype=torch.uint8, device="cuda")
     sel = torch.full((c.rows, c.H, M), -2, dtype=torch.int32, device="cuda")
     count = torch.full((c.rows,), -2, dtype=torch.int32, device="cuda")
-    print(f"[select] H{c.H} g{c.g} D{c.D} ps{c.ps}/{c.block} rows {c.rows} M{M} {bf16}", flush=True)
+    print(f"[select] H{c.H} g{c.g} D{c.D} ps{c.ps}/{c.block} rows {c.rows} M{M}", flush=True)
     vx.chunk_score_topk(qd if q is None else q, kv, batch, qi, vx.MEAN_DOT, md, torch.from_numpy(budget).cuda(), n_sink, n_local, M, sel,
-                        count, ws, q_lens=ql, mean_bf16=md.to(torch.bfloat16) if bf16 else None)
+                        count, ws, q_lens=ql)
     torch.cuda.synchronize()
     return sel.cpu().numpy(), count.cpu().numpy()
 
@@ -135,11 +135,10 @@ def _mean(c, seed, sigma=0.25):
 def _same(c, mean, budget, n_sink, n_local, M):
     budget = np.asarray(budget, np.int32)
     ref = c.select(mean, budget, n_sink, n_local, M)
-    for bf16 in (True, False):
-        got = _select(c, mean, budget, n_sink, n_local, M, bf16)
-        assert np.array_equal(got[1], ref[1])
-        bad = np.argwhere((got[0] != ref[0]).any(-1))
-        assert len(bad) == 0, (bad[:4], [(got[0][tuple(b)], ref[0][tuple(b)]) for b in bad[:2]])
+    got = _select(c, mean, budget, n_sink, n_local, M)
+    assert np.array_equal(got[1], ref[1])
+    bad = np.argwhere((got[0] != ref[0]).any(-1))
+    assert len(bad) == 0, (bad[:4], [(got[0][tuple(b)], ref[0][tuple(b)]) for b in bad[:2]])
 
 
 @pytest.mark.parametrize("D,H,g,ps,block", [(128, 8, 4, 16, 0), (64, 4, 1, 64, 16), (128, 1, 16, 32, 0), (64, 2, 5, 64, 32), (128, 2, 3, 64, 0),
