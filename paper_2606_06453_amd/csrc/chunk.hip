@@ -20,6 +20,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr int kTileRows = 16;              // query rows (token, head of the group) of a matrix operand
+constexpr int kNarrowTiles = 4;            // most narrow tiles of a request, on average
 constexpr int kTargetWgs = 512;            // two workgroups a CU
 constexpr int kMaxParts = 64;              // a merging wave's lanes
 constexpr int kPartTokens = 512;           // least tokens of a part: four pairs of runs a wave
@@ -69,11 +70,24 @@ __device__ __forceinline__ int listed_blocks(const ChunkArgs& a, const Tile& t, 
   return total;
 }
 
-// Part s of the S parts of [lo, hi).
-__device__ __forceinline__ void part_of(int lo, int hi, int s, int S, int& plo, int& phi) {
-  const int per = (hi - lo + S - 1) / S;
+// Part s of [lo, hi), in parts of `per`.
+__device__ __forceinline__ void part_of(int lo, int hi, int s, int per, int& plo, int& phi) {
   plo = min(lo + s * per, hi);
   phi = min(plo + per, hi);
+}
+
+// 16-token runs of a part: the longest list of the batch cut into a.splits, for every request, so that all parts
+// take equally long (four contexts of 24000 to 32768 tokens: cut by their own lengths, the longest's parts end 15%
+// after the mean).
+__device__ __forceinline__ int part_runs16(const ChunkArgs& a) {
+  if (a.splits == 1) return INT_MAX / 2;
+  int most = 0;
+  for (int i = lane_id(); i < a.batch; i += kWave) most = max(most, a.seq_lens[i]);
+#pragma unroll
+  for (int s = 1; s < kWave; s <<= 1) most = max(most, __shfl_xor(most, s, kWave));
+  most = (int)min((int64_t)most, (int64_t)a.max_pages * a.ps);
+  if (a.window > 0) most = (int)min((int64_t)most, (int64_t)a.window + a.tokens + 15 + (a.causal ? 0 : most));
+  return ((most + 15) / 16 + a.splits) / a.splits;       // a window's ends may lie inside runs
 }
 
 // The tile's rows one by one: where a sum of the tile kernels is not finite.
@@ -84,6 +98,14 @@ __device__ __forceinline__ void attend_rows(const ChunkArgs& a, const Tile& t, i
     attend_row<D, DV, KT>(a, t, h, x % a.g, x / a.g, runs, st);
     store_row<DV>(a, t.row0 + x / a.g, h * a.g + x % a.g, split, st);
   }
+}
+
+// A part with no token: its rows' sums are zero, and the join leaves it out.
+__device__ __forceinline__ bool empty_part(const ChunkArgs& a, const Tile& t, int h, int split, const Runs& runs) {
+  if (a.splits == 1 || runs.lo < runs.hi) return false;
+  for (int r = (int)threadIdx.x; r < t.n * a.g; r += kThreads)
+    a.part_ml[((t.row0 + r / a.g) * a.Hq + h * a.g + r % a.g) * a.splits + split] = make_float2(-INFINITY, 0.f);
+  return true;
 }
 
 // The runs of a workgroup's part; shift16: log2 of the 16-token runs of an entry.
@@ -97,13 +119,15 @@ __device__ __forceinline__ Runs part_runs(const ChunkArgs& a, const Tile& t, int
     runs.masks = reinterpret_cast<const uint16_t*>(lds);
     runs.shift = a.bs_shift;
     shift16 = a.bs_shift - 4;
-    part_of(0, all, split, a.splits, runs.lo, runs.hi);
+    part_of(0, all, split, (all + a.splits - 1) / a.splits, runs.lo, runs.hi);
   } else {
     runs.ids = nullptr;
     runs.masks = nullptr;
     runs.shift = 4;
     shift16 = 0;
-    part_of(first_key(a, t.p0) >> 4, (end_key(a, t, t.p0 + t.n - 1) + 15) >> 4, split, a.splits, runs.lo, runs.hi);
+    const int lo = first_key(a, t.p0) >> 4, hi = (end_key(a, t, t.p0 + t.n - 1) + 15) >> 4;
+    part_of(lo, hi, split, __builtin_amdgcn_readfirstlane(part_runs16(a)), runs.lo, runs.hi);
+    if (split == a.splits - 1) runs.hi = hi;             // never less than the whole list
   }
   return runs;
 }
@@ -121,6 +145,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   if (!find_tile(a, (int)blockIdx.x / a.H, t)) return;
   int shift16;
   const Runs runs = part_runs<SPARSE>(a, t, h, split, lds, shift16);
+  if (empty_part(a, t, h, split, runs)) return;
   const int rows = t.n * a.g, last = end_key(a, t, t.p0 + t.n - 1);        // past every row's tokens
   Rows<D, D, 1> w;
   begin_rows<D, D, KT, 1>(a, t, h, 0, col, grp, w);
@@ -145,60 +170,50 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       }
     }
     const int count = min(32, (pairs - w0 + kWaves - 1) / kWaves);
-    auto fetch = [&](int u, Raw<D, KT> (&r)[2]) {
+    // One buffer: a pair's K is sent for when the scores have taken the one before, its V when the sums have, so
+    // that each travels through half a step and the registers leave room for three waves a SIMD.
+    RawK<D, KT> k[2];
+    RawV<D, KT> v[2];
+    auto fetch_k = [&](int u) {
 #pragma unroll
       for (int e = 0; e < 2; e++) {
         const int page = __builtin_amdgcn_readlane(my_page, 2 * u + e), tok = __builtin_amdgcn_readlane(my_tok, 2 * u + e);
-        load_raw<D, KT>(a, slice_of<D, KT>(a, a.k, page, h), slice_of<D, KT>(a, a.v, page, h), tok & (a.ps - 1), col, grp,
-                        r[e]);
+        load_k<D, KT>(a, slice_of<D, KT>(a, a.k, page, h), tok & (a.ps - 1), min(last - tok, 16), col, grp, k[e]);
       }
     };
-    // EDGE: tokens that some row does not attend, and rows behind every row's tokens, which may hold anything
-    auto compute = [&](auto edge, int tok0, int tok1, int mask0, int mask1, Raw<D, KT> (&r)[2]) {
-      constexpr bool EDGE = decltype(edge)::value;
-      uint32_t p[4];
-      {
-        f32x4_t s[2];
+    auto fetch_v = [&](int u) {
 #pragma unroll
-        for (int e = 0; e < 2; e++) {
-          s[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int kk = 0; kk < KS; kk++)
-            s[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand<D, KT>(r[e], kk), w.q[0][kk], s[e], 0, 0, 0);
-        }
-        softmax_step<D, D, 1, EDGE>(a.scale_log2, 0, s, tok0, tok1, mask0, mask1, grp, w, p);
+      for (int e = 0; e < 2; e++) {
+        const int page = __builtin_amdgcn_readlane(my_page, 2 * u + e), tok = __builtin_amdgcn_readlane(my_tok, 2 * u + e);
+        load_v<D, KT>(a, slice_of<D, KT>(a, a.v, page, h), tok & (a.ps - 1), min(last - tok, 16), col, grp, v[e]);
       }
-      uint32_t v0[4][W], v1[4][W];
-      v_rows<D, KT>(r[0], v0);
-      v_rows<D, KT>(r[1], v1);
-      if constexpr (EDGE) {
-#pragma unroll
-        for (int x = 0; x < 4; x++)
-#pragma unroll
-          for (int y = 0; y < W; y++) {
-            v0[x][y] = tok0 + 4 * grp + x < last ? v0[x][y] : 0u;
-            v1[x][y] = tok1 + 4 * grp + x < last ? v1[x][y] : 0u;
-          }
-      }
-#pragma unroll
-      for (int j = 0; j < NJ; j++)
-        w.acc[0][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_operand<W>(v0, v1, j), p_operand(p), w.acc[0][j], 0, 0, 0);
     };
-    auto step = [&](int u, Raw<D, KT> (&r)[2]) {
+    fetch_k(0);
+    fetch_v(0);
+    for (int u = 0; u < count; u++) {
       const int tok0 = __builtin_amdgcn_readlane(my_tok, 2 * u), tok1 = __builtin_amdgcn_readlane(my_tok, 2 * u + 1);
       const int mask0 = __builtin_amdgcn_readlane(my_mask, 2 * u), mask1 = __builtin_amdgcn_readlane(my_mask, 2 * u + 1);
       const bool whole = min(tok0, tok1) >= w.all_from && max(tok0, tok1) + 16 <= w.all_to && (mask0 & mask1) == 0xffff;
-      if (whole) compute(std::false_type{}, tok0, tok1, mask0, mask1, r);
-      else compute(std::true_type{}, tok0, tok1, mask0, mask1, r);
-    };
-    Raw<D, KT> ra[2], rb[2];
-    fetch(0, ra);
-    for (int u = 0; u < count; u += 2) {
-      fetch(min(u + 1, count - 1), rb);
-      step(u, ra);
-      if (u + 1 >= count) break;
-      fetch(min(u + 2, count - 1), ra);
-      step(u + 1, rb);
+      const int next = min(u + 1, count - 1);
+      f32x4_t s[2];
+#pragma unroll
+      for (int e = 0; e < 2; e++) {
+        s[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kk = 0; kk < KS; kk++)
+          s[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand<D, KT>(k[e], kk), w.q[0][kk], s[e], 0, 0, 0);
+      }
+      fetch_k(next);
+      if (!whole) mask_scores<D, D, 1>(0, s, tok0, tok1, mask0, mask1, grp, w);
+      uint32_t p[4];
+      softmax_step<D, D, 1>(a.scale_log2, 0, s, w, p);
+      uint32_t v0[4][W], v1[4][W];
+      v_rows<D, KT>(v[0], v0);
+      v_rows<D, KT>(v[1], v1);
+#pragma unroll
+      for (int j = 0; j < NJ; j++)
+        w.acc[0][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_operand<W>(v0, v1, j), p_operand(p), w.acc[0][j], 0, 0, 0);
+      fetch_v(next);
     }
   }
 
@@ -280,6 +295,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(D == D
   uint32_t* lists = lds + 2 * G::BUF / sizeof(uint32_t);
   int shift16;
   const Runs runs = part_runs<SPARSE>(a, t, h, split, lists, shift16);
+  if (empty_part(a, t, h, split, runs)) return;
   const int rows = t.n * a.g, last = end_key(a, t, t.p0 + t.n - 1);
   const int r0 = wave * 16 * RT;
   Rows<D, DV, RT> w;
@@ -316,7 +332,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(D == D
     if ((s & 63) == 0) look_up(s);
     const int page = __builtin_amdgcn_readlane(my_page, s & 63), tok = __builtin_amdgcn_readlane(my_tok, s & 63);
     const uint8_t* ks = slice_of<D, KT>(a, a.k, page, h);
-    send_run<D, DV, KT>(a, ks, G::kAlias ? ks : slice_of<D, KT>(a, a.v, page, h), tok & (a.ps - 1), wave, lane,
+    send_run<D, DV, KT>(a, ks, G::kAlias ? ks : slice_of<D, KT>(a, a.v, page, h), tok & (a.ps - 1), last - tok, wave, lane,
                         bufs + (s & 1) * G::BUF, travel);
   };
   int tok_sent = 0;                                      // of the run on its way
@@ -359,8 +375,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(D == D
       uint32_t p[RT][4];
 #pragma unroll
       for (int rt = 0; rt < RT; rt++) {
-        if (whole) softmax_step<D, DV, RT, false>(a.scale_log2, rt, sc[rt], tok0, tok1, mask0, mask1, grp, w, p[rt]);
-        else softmax_step<D, DV, RT, true>(a.scale_log2, rt, sc[rt], tok0, tok1, mask0, mask1, grp, w, p[rt]);
+        if (!whole) mask_scores<D, DV, RT>(rt, sc[rt], tok0, tok1, mask0, mask1, grp, w);
+        softmax_step<D, DV, RT>(a.scale_log2, rt, sc[rt], w, p[rt]);
       }
 #pragma unroll
       for (int j = 0; j < NJ; j++) {
@@ -405,15 +421,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(D == D
   if (__syncthreads_or(bad)) attend_rows<D, DV, KT>(a, t, h, runs, split);
 }
 
-// Joins the parts of every row of a tile, a wave a row: each part's weight is its sum at the rows' largest
-// reference.
+// Joins the parts of every row, a wave a row and a token a workgroup (a.tokens is 1): each part's weight is its
+// sum at the row's largest reference.
 template <int DV>
 __global__ __launch_bounds__(kThreads) void chunk_merge_kernel(const ChunkArgs a) {
+  constexpr int N = DV / kWave, kBatch = 8;              // channels of a lane; parts on their way at a time
   const int lane = lane_id(), h = (int)blockIdx.x % a.H, S = a.splits;
   Tile t;
   if (!find_tile(a, (int)blockIdx.x / a.H, t)) return;
-  for (int x = (int)threadIdx.x >> 6; x < t.n * a.g; x += kWaves) {
-    const int64_t at = (t.row0 + x / a.g) * a.Hq + h * a.g + x % a.g;
+  for (int x = (int)threadIdx.x >> 6; x < a.g; x += kWaves) {
+    const int64_t at = t.row0 * a.Hq + h * a.g + x;
     const float2 ml = lane < S ? a.part_ml[at * S + lane] : make_float2(-INFINITY, 0.f);
     float top = ml.y != 0.f ? ml.x : -INFINITY;
 #pragma unroll
@@ -423,18 +440,43 @@ __global__ __launch_bounds__(kThreads) void chunk_merge_kernel(const ChunkArgs a
 #pragma unroll
     for (int s = 1; s < kWave; s <<= 1) total += xor_shfl(total, s);
     w = total != 0.f ? w / total : 0.f;
-    float o[DV / kWave];
+    float o[N];
 #pragma unroll
-    for (int c = 0; c < DV / kWave; c++) o[c] = 0.f;
-    for (int s = 0; s < S; s++) {
-      const float f = __shfl(w, s, kWave);
-      if (f == 0.f) continue;
-      const float* src = a.part_o + (at * S + s) * DV + lane;
+    for (int c = 0; c < N; c++) o[c] = 0.f;
+    const float* src = a.part_o + at * S * DV + N * lane;
+    for (int s0 = 0; s0 < S; s0 += kBatch) {
+      float v[kBatch][N];
 #pragma unroll
-      for (int c = 0; c < DV / kWave; c++) o[c] = fmaf(src[c * kWave], f, o[c]);
+      for (int y = 0; y < kBatch; y++) {
+        const float* p = src + (int64_t)min(s0 + y, S - 1) * DV;
+        if constexpr (N == 1) {
+          v[y][0] = p[0];
+        } else if constexpr (N == 2) {
+          const float2 u = *reinterpret_cast<const float2*>(p);
+          v[y][0] = u.x;
+          v[y][1] = u.y;
+        } else {
+#pragma unroll
+          for (int c = 0; c < N; c += 4) {
+            const float4 u = *reinterpret_cast<const float4*>(p + c);
+            v[y][c] = u.x;
+            v[y][c + 1] = u.y;
+            v[y][c + 2] = u.z;
+            v[y][c + 3] = u.w;
+          }
+        }
+      }
+#pragma unroll
+      for (int y = 0; y < kBatch; y++) {
+        const float f = s0 + y < S ? __shfl(w, min(s0 + y, S - 1), kWave) : 0.f;
+        if (f != 0.f)                                    // a part with no token is not written
+#pragma unroll
+          for (int c = 0; c < N; c++) o[c] = fmaf(v[y][c], f, o[c]);
+      }
     }
+    uint16_t* dst = a.out + at * DV + N * lane;
 #pragma unroll
-    for (int c = 0; c < DV / kWave; c++) a.out[at * DV + c * kWave + lane] = (uint16_t)f32_to_bf16_rne(o[c] * a.v_scale);
+    for (int c = 0; c < N; c++) dst[c] = (uint16_t)f32_to_bf16_rne(o[c] * a.v_scale);
     if (lane == 0 && a.lse) a.lse[at] = total > 0.f ? (top + log2f(total)) * kLn2 : total == 0.f ? -INFINITY : total;
   }
 }
@@ -451,7 +493,7 @@ Plan plan_of(const Geometry& g, int n, int Hq, bool sparse, int max_sel) {
   const bool latent = g.Dqk != g.Dv;
   const int64_t batch = std::max(g.batch, 1);
   auto tokens = [&](int rows) { return std::max(1, sparse ? std::min(16, rows / group) : rows / group); };
-  if (!latent && (int64_t)n <= batch * (kTileRows / group)) p.operands = 0;
+  if (!latent && (int64_t)n <= batch * kNarrowTiles * (kTileRows / group)) p.operands = 0;
   else p.operands = sparse || latent || (int64_t)n * group <= batch * 4 * kTileRows ? 1 : 2;
   p.tokens = tokens(p.operands == 0 ? kTileRows : 4 * kTileRows * p.operands);
   const int64_t tiles = std::max<int64_t>(batch, (n + p.tokens - 1) / p.tokens) * g.H;
@@ -499,7 +541,10 @@ hipError_t launch_kt(const ChunkArgs& a, int operands, hipStream_t stream) {
   if (a.splits > 1) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((chunk_merge_kernel<DV>), dim3((unsigned)(tiles * a.H)), dim3(kThreads), 0, stream, a);
+    ChunkArgs m = a;
+    m.tokens = 1;
+    const int64_t rows = (int64_t)a.num_rows + a.batch;
+    hipLaunchKernelGGL((chunk_merge_kernel<DV>), dim3((unsigned)(rows * a.H)), dim3(kThreads), 0, stream, m);
   }
   return hipGetLastError();
 }

@@ -35,70 +35,102 @@ __device__ __forceinline__ int k_channel(int kk, int grp) {
   return KT == kKvBf16 ? 32 * kk + 8 * grp : D / 4 * grp + 8 * kk;
 }
 
-// 16 tokens of K and V as loaded.
+// 16 tokens of K, and of V, as loaded.
 template <int D, int KT>
-struct Raw {
-  static constexpr int KW = KT == kKvBf16 ? D / 8 : KT == kKvMxFp4 ? D / 32 : D / 16;    // words of a lane's part of K
-  static constexpr int VW = KT == kKvBf16 ? D / 32 : KT == kKvMxFp4 ? 1 : D / 64;        // words of a V row's
-  uint32_t k[KW];
-  uint32_t v[4 * (KT == kKvMxFp4 ? 1 : VW)];
-  uint32_t ks, vs;                                                                        // mxfp4 scales
+struct RawK {
+  static constexpr int W = KT == kKvBf16 ? D / 8 : KT == kKvMxFp4 ? D / 32 : D / 16;     // words of a lane's part
+  uint32_t w[W], scale;                    // scale: mxfp4
+};
+template <int D, int KT>
+struct RawV {
+  static constexpr int W = KT == kKvBf16 ? D / 32 : KT == kKvMxFp4 ? D / 128 : D / 64;   // words of a row's
+  static constexpr int N = KT == kKvMxFp4 ? D / 32 : 4 * W;
+  uint32_t w[N], scale;
 };
 
+// Loads go through buffer resources of the page's slices: a base that all lanes share, lane offsets that stay the same
+// for the whole kernel, and zeros for what lies behind the last token that any row attends, which may hold
+// anything.
+struct Slices {
+  __amdgpu_buffer_rsrc_t k, v, k_scale, v_scale;         // scales: mxfp4
+};
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const uint8_t* base, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, bytes, 0x00020000);
+}
+
+// Tokens t .. t + 15 (t a multiple of 16, the same in all lanes) of a page, the first n of which are looked at.
+template <int D, int KT>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const ChunkArgs& a, const uint8_t* slice, int t, int n) {
+  constexpr int kRow = KT == kKvBf16 ? 2 * D : KT == kKvMxFp4 ? D / 2 : D;
+  // mxfp4: four tokens of V share their codes' bytes; what is not looked at goes by its scale
+  return rsrc(slice + t * kRow, (KT == kKvMxFp4 ? 16 : n) * kRow);
+}
+template <int D>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t scales_of(const ChunkArgs& a, const uint8_t* slice, int t) {
+  return rsrc(slice + mx::codes_bytes(a.ps, D) + t * (D / 32), 16 * (D / 32));
+}
+
 template <int N>
-__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {
+__device__ __forceinline__ void load_words(__amdgpu_buffer_rsrc_t r, int off, uint32_t* w) {
   if constexpr (N >= 4) {
 #pragma unroll
     for (int x = 0; x < N; x += 4) {
-      const uint4 y = *reinterpret_cast<const uint4*>(p + 4 * x);
+      const u32x4_t y = __builtin_amdgcn_raw_buffer_load_b128(r, off + 4 * x, 0, 0);
       w[x] = y.x;
       w[x + 1] = y.y;
       w[x + 2] = y.z;
       w[x + 3] = y.w;
     }
   } else if constexpr (N == 2) {
-    const uint2 y = *reinterpret_cast<const uint2*>(p);
+    const u32x2_t y = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
     w[0] = y.x;
     w[1] = y.y;
   } else {
-    w[0] = *reinterpret_cast<const uint32_t*>(p);
+    w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0);
   }
 }
 
-// Tokens t .. t + 15 (t a multiple of 16) of a page's K and V slices.
+// n: tokens of the run that some row may attend.
 template <int D, int KT>
-__device__ __forceinline__ void load_raw(const ChunkArgs& a, const uint8_t* ks, const uint8_t* vs, int t, int col,
-                                         int grp, Raw<D, KT>& r) {
+__device__ __forceinline__ void load_k(const ChunkArgs& a, const uint8_t* slice, int t, int n, int col, int grp, RawK<D, KT>& r) {
+  const __amdgpu_buffer_rsrc_t k = rows_of<D, KT>(a, slice, t, n);
   if constexpr (KT == kKvMxFp4) {
-    load_words<D / 32>(ks + (t + col) * (D / 2) + D / 8 * grp, r.k);
-    r.ks = ks[mx::codes_bytes(a.ps, D) + mx::k_scale(t + col, D / 4 * grp / 32, D)];
-    const int quad = (t >> 2) + grp;
-    load_words<D / 32>(vs + (quad * 16 + col) * (D / 8), r.v);
-    r.vs = *reinterpret_cast<const uint32_t*>(vs + mx::codes_bytes(a.ps, D) + (quad * (D / 32) + col * (D / 16) / 32) * 4);
+    load_words<D / 32>(k, col * (D / 2) + D / 8 * grp, r.w);
+    r.scale = __builtin_amdgcn_raw_buffer_load_b8(scales_of<D>(a, slice, t), col * (D / 32) + D / 4 * grp / 32, 0, 0);
   } else if constexpr (KT == kKvBf16) {
 #pragma unroll
-    for (int kk = 0; kk < D / 32; kk++) load_words<4>(ks + 2 * ((t + col) * D + 32 * kk + 8 * grp), r.k + 4 * kk);
-#pragma unroll
-    for (int x = 0; x < 4; x++) load_words<D / 32>(vs + 2 * ((t + 4 * grp + x) * D + col * (D / 16)), r.v + x * (D / 32));
+    for (int kk = 0; kk < D / 32; kk++) load_words<4>(k, 2 * (col * D + 8 * grp) + 64 * kk, r.w + 4 * kk);
   } else {
-    load_words<D / 16>(ks + (t + col) * D + D / 4 * grp, r.k);
+    load_words<D / 16>(k, col * D + D / 4 * grp, r.w);
+  }
+}
+template <int D, int KT>
+__device__ __forceinline__ void load_v(const ChunkArgs& a, const uint8_t* slice, int t, int n, int col, int grp, RawV<D, KT>& r) {
+  const __amdgpu_buffer_rsrc_t v = rows_of<D, KT>(a, slice, t, n);
+  if constexpr (KT == kKvMxFp4) {
+    load_words<D / 32>(v, (grp * 16 + col) * (D / 8), r.w);
+    r.scale = __builtin_amdgcn_raw_buffer_load_b32(scales_of<D>(a, slice, t), (grp * (D / 32) + col * (D / 16) / 32) * 4, 0, 0);
+    const int left = n - 4 * grp;                        // byte x: token 4 grp + x; a scale of 0 is 2^-127
+    r.scale &= left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1;
+  } else {
+    constexpr int B = KT == kKvBf16 ? 2 : 1, W = RawV<D, KT>::W;
 #pragma unroll
-    for (int x = 0; x < 4; x++) load_words<D / 64>(vs + (t + 4 * grp + x) * D + col * (D / 16), r.v + x * (D / 64));
+    for (int x = 0; x < 4; x++) load_words<W>(v, B * (4 * grp * D + col * (D / 16)) + B * x * D, r.w + x * W);
   }
 }
 
 // Operand A of k-step kk.
 template <int D, int KT>
-__device__ __forceinline__ bf16x8_t k_operand(const Raw<D, KT>& r, int kk) {
+__device__ __forceinline__ bf16x8_t k_operand(const RawK<D, KT>& r, int kk) {
   u32x4_t w;
   if constexpr (KT == kKvBf16) {
-    w = u32x4_t{r.k[4 * kk], r.k[4 * kk + 1], r.k[4 * kk + 2], r.k[4 * kk + 3]};
+    w = u32x4_t{r.w[4 * kk], r.w[4 * kk + 1], r.w[4 * kk + 2], r.w[4 * kk + 3]};
   } else if constexpr (KT == kKvMxFp4) {
-    const float s = mx::scale_operand(r.ks);
-    const uint32_t c = r.k[kk];
+    const float s = mx::scale_operand(r.scale);
+    const uint32_t c = r.w[kk];
     w = u32x4_t{mx::pair_bf16<0>(c, s), mx::pair_bf16<1>(c, s), mx::pair_bf16<2>(c, s), mx::pair_bf16<3>(c, s)};
   } else {
-    const uint32_t lo = r.k[2 * kk], hi = r.k[2 * kk + 1];
+    const uint32_t lo = r.w[2 * kk], hi = r.w[2 * kk + 1];
     w = u32x4_t{fp8_pair<KT, false>(lo), fp8_pair<KT, true>(lo), fp8_pair<KT, false>(hi), fp8_pair<KT, true>(hi)};
   }
   return __builtin_bit_cast(bf16x8_t, w);
@@ -106,29 +138,29 @@ __device__ __forceinline__ bf16x8_t k_operand(const Raw<D, KT>& r, int kk) {
 
 // Rows 4 grp + x of V as bf16 words: channels col * D / 16 ..
 template <int D, int KT>
-__device__ __forceinline__ void v_rows(const Raw<D, KT>& r, uint32_t (&v)[4][D / 32]) {
+__device__ __forceinline__ void v_rows(const RawV<D, KT>& r, uint32_t (&v)[4][D / 32]) {
 #pragma unroll
   for (int x = 0; x < 4; x++) {
     if constexpr (KT == kKvBf16) {
 #pragma unroll
-      for (int w = 0; w < D / 32; w++) v[x][w] = r.v[x * (D / 32) + w];
+      for (int w = 0; w < D / 32; w++) v[x][w] = r.w[x * (D / 32) + w];
     } else if constexpr (KT == kKvMxFp4) {
-      const float s = mx::scale_operand((r.vs >> (8 * x)) & 255);
+      const float s = mx::scale_operand((r.scale >> (8 * x)) & 255);
       if constexpr (D == 128) {
-        v[x][0] = mx::pair_bf16<0>(r.v[x], s);
-        v[x][1] = mx::pair_bf16<1>(r.v[x], s);
-        v[x][2] = mx::pair_bf16<2>(r.v[x], s);
-        v[x][3] = mx::pair_bf16<3>(r.v[x], s);
+        v[x][0] = mx::pair_bf16<0>(r.w[x], s);
+        v[x][1] = mx::pair_bf16<1>(r.w[x], s);
+        v[x][2] = mx::pair_bf16<2>(r.w[x], s);
+        v[x][3] = mx::pair_bf16<3>(r.w[x], s);
       } else {
-        const uint32_t c = r.v[x >> 1];
+        const uint32_t c = r.w[x >> 1];
         v[x][0] = (x & 1) ? mx::pair_bf16<2>(c, s) : mx::pair_bf16<0>(c, s);
         v[x][1] = (x & 1) ? mx::pair_bf16<3>(c, s) : mx::pair_bf16<1>(c, s);
       }
     } else {
 #pragma unroll
       for (int w = 0; w < D / 64; w++) {
-        v[x][2 * w] = fp8_pair<KT, false>(r.v[x * (D / 64) + w]);
-        v[x][2 * w + 1] = fp8_pair<KT, true>(r.v[x * (D / 64) + w]);
+        v[x][2 * w] = fp8_pair<KT, false>(r.w[x * (D / 64) + w]);
+        v[x][2 * w + 1] = fp8_pair<KT, true>(r.w[x * (D / 64) + w]);
       }
     }
   }
@@ -200,25 +232,49 @@ __device__ __forceinline__ void begin_rows(const ChunkArgs& a, const Tile& t, in
   w.all_to = end_key(a, t, t.p0);
 }
 
-// One step of the softmax: the scores s of 32 tokens (16 from tok0, 16 from tok1, of the tile tokens in mask0 and
-// mask1) become weights p, bf16, operand B of O^T = V^T P^T.  The sum takes the weights before their rounding,
-// which is to the nearest (2^-9 of each at most, without a bias) and halves the matrix work that two parts would need.
-template <int D, int DV, int RT, bool MASK>
-__device__ __forceinline__ void softmax_step(float scale_log2, int rt, f32x4_t (&s)[2], int tok0, int tok1, int mask0,
-                                             int mask1, int grp, Rows<D, DV, RT>& w, uint32_t (&p)[4]) {
-  if constexpr (MASK) {
-    const int t0 = tok0 + 4 * grp, t1 = tok1 + 4 * grp;
-    const int to0 = ((mask0 >> w.bit[rt]) & 1) ? w.to[rt] : 0, to1 = ((mask1 >> w.bit[rt]) & 1) ? w.to[rt] : 0;
+// Scores of tokens that a row does not attend: s holds 16 tokens from tok0 and 16 from tok1, of the tile tokens in
+// mask0 and mask1.
+template <int D, int DV, int RT>
+__device__ __forceinline__ void mask_scores(int rt, f32x4_t (&s)[2], int tok0, int tok1, int mask0, int mask1, int grp,
+                                            const Rows<D, DV, RT>& w) {
+  const int t0 = tok0 + 4 * grp, t1 = tok1 + 4 * grp;
+  const int to0 = ((mask0 >> w.bit[rt]) & 1) ? w.to[rt] : 0, to1 = ((mask1 >> w.bit[rt]) & 1) ? w.to[rt] : 0;
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-      s[0][i] = t0 + i < to0 && t0 + i >= w.from[rt] ? s[0][i] : -INFINITY;
-      s[1][i] = t1 + i < to1 && t1 + i >= w.from[rt] ? s[1][i] : -INFINITY;
-    }
+  for (int i = 0; i < 4; i++) {
+    s[0][i] = t0 + i < to0 && t0 + i >= w.from[rt] ? s[0][i] : -INFINITY;
+    s[1][i] = t1 + i < to1 && t1 + i >= w.from[rt] ? s[1][i] : -INFINITY;
   }
-  const float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
-                          fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))) *
-                    scale_log2;
-  if (__any(top > w.m[rt])) {
+}
+
+typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+
+// Whether one of 8 weights, bf16 and not negative, passes 1 (or is not a number).
+__device__ __forceinline__ bool weights_pass_one(const uint32_t (&p)[4]) {
+  const u16x2_t a = __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, p[0]), __builtin_bit_cast(u16x2_t, p[1]));
+  const u16x2_t b = __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, p[2]), __builtin_bit_cast(u16x2_t, p[3]));
+  const u16x2_t c = __builtin_elementwise_max(a, b);
+  return max((uint32_t)c.x, (uint32_t)c.y) > 0x3f80u;
+}
+
+// One step of the softmax: the scores s of 32 tokens become weights p, bf16, operand B of O^T = V^T P^T.  The
+// weights are taken at the present reference first and seldom pass 1; only then it moves.  The sum takes the weights
+// before their rounding, which is to the nearest (2^-9 of each at most, without a bias) and halves the matrix work
+// that two parts would need.
+template <int D, int DV, int RT>
+__device__ __forceinline__ void softmax_step(float scale_log2, int rt, const f32x4_t (&s)[2], Rows<D, DV, RT>& w,
+                                             uint32_t (&p)[4]) {
+  float x[8];
+  auto weigh = [&] {
+#pragma unroll
+    for (int i = 0; i < 8; i++) x[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], scale_log2, -w.m[rt]));
+#pragma unroll
+    for (int i = 0; i < 4; i++) p[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+  };
+  weigh();
+  if (__builtin_expect(__any(weights_pass_one(p)), 0)) {
+    const float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                            fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))) *
+                      scale_log2;
     const float c = column_max(top), next = c > w.m[rt] ? c + kAhead : w.m[rt];
     const float alpha = __builtin_amdgcn_exp2f(w.m[rt] - next);
     w.m[rt] = next;
@@ -227,16 +283,9 @@ __device__ __forceinline__ void softmax_step(float scale_log2, int rt, f32x4_t (
     for (int j = 0; j < DV / 16; j++)
 #pragma unroll
       for (int i = 0; i < 4; i++) w.acc[rt][j][i] *= alpha;
+    weigh();
   }
-  float x[8], sum = 0.f;
-#pragma unroll
-  for (int i = 0; i < 8; i++) {
-    x[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], scale_log2, -w.m[rt]));
-    sum += x[i];
-  }
-  w.l[rt] += sum;
-#pragma unroll
-  for (int i = 0; i < 4; i++) p[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+  w.l[rt] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
 }
 
 __device__ __forceinline__ bf16x8_t p_operand(const uint32_t (&p)[4]) {

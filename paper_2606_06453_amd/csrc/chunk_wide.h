@@ -64,73 +64,122 @@ __device__ __forceinline__ void piece(int wave, int k, int lane, int& token, int
   c = (slot % G::CH) ^ swizzle<D>(token);
 }
 
-// A wave's pieces of a run on their way through registers (types below 16 bits).
+// A wave's part of a run on its way through registers: fp8, 16 codes a lane and piece; mxfp4, a lane's D / 4 codes of
+// one K row and the codes of D / 16 channels of four V rows, and their scales.
 template <int D, int DV, int KT>
 struct Travel {
-  static constexpr int N = Wide<D, DV, KT>::NI;
-  uint2 k[N], v[Wide<D, DV, KT>::kAlias ? 1 : N];        // mxfp4: codes and scale
+  static constexpr bool kMx = KT == kKvMxFp4;
+  static constexpr int N = kMx ? 1 : (D + 64 * Wide<D, DV, KT>::WPU - 1) / (64 * Wide<D, DV, KT>::WPU);
+  static constexpr int W = kMx ? D / 32 : 4;
+  uint32_t k[N][W], v[Wide<D, DV, KT>::kAlias ? 1 : N][W], k_scale, v_scale;
 };
 
-// Starts a run's way into the buffer (bf16), or into registers.  t: its first token's place in the page.
+// fp8: lane's piece x of a run, token and 16 channels; false past the run.
 template <int D, int DV, int KT>
-__device__ __forceinline__ void send_run(const ChunkArgs& a, const uint8_t* ks, const uint8_t* vs, int t, int wave,
+__device__ __forceinline__ bool codes_piece(int wave, int x, int lane, int& token, int& c16) {
+  using G = Wide<D, DV, KT>;
+  const int slot = 64 * ((wave % G::WPU) * Travel<D, DV, KT>::N + x) + lane;
+  token = slot / (D / 16);
+  c16 = slot % (D / 16);
+  return slot < D;
+}
+
+// Starts a run's way into the buffer (bf16), or into registers.  t: its first token's place in the page; left: its
+// tokens before the last one that any row attends (other types: what lies behind arrives as zeros).
+template <int D, int DV, int KT>
+__device__ __forceinline__ void send_run(const ChunkArgs& a, const uint8_t* ks, const uint8_t* vs, int t, int left, int wave,
                                          int lane, uint8_t* buf, Travel<D, DV, KT>& r) {
   using G = Wide<D, DV, KT>;
-  const int unit = wave / G::WPU;
+  using T = Travel<D, DV, KT>;
+  if constexpr (KT == kKvBf16) {
+    const uint32_t dst = lds_address(buf) + (wave / G::WPU) * 16 * D * 2;
 #pragma unroll
-  for (int k = 0; k < G::NI; k++) {
-    int token, c;
-    piece<D, DV, KT>(wave, k, lane, token, c);
-    if constexpr (KT == kKvBf16) {
-      const uint32_t dst = lds_address(buf) + unit * 16 * D * 2 + 1024 * ((wave % G::WPU) * G::NI + k);
-      const uint32_t at = 2 * (token * D + 8 * c);
-      send16(ks + 2 * t * D, at, dst);
-      if constexpr (!G::kAlias) send16(vs + 2 * t * D, at, dst + G::TILE);
-    } else if constexpr (KT == kKvMxFp4) {
-      const int base = mx::codes_bytes(a.ps, D);
-      r.k[k] = make_uint2(*reinterpret_cast<const uint32_t*>(ks + mx::k_code(t + token, c, D)),
-                          ks[base + mx::k_scale(t + token, c >> 2, D)]);
-      r.v[k] = make_uint2(mx::get_v_codes(vs, t + token, c, D), vs[base + mx::v_scale(t + token, c >> 2, D)]);
-    } else {
-      const int at = (t + token) * D + 8 * c;
-      r.k[k] = *reinterpret_cast<const uint2*>(ks + at);
-      if constexpr (!G::kAlias) r.v[k] = *reinterpret_cast<const uint2*>(vs + at);
-    }
-  }
-}
-
-template <int KT>
-__device__ __forceinline__ uint4 widen_chunk(const uint2& w) {
-  if constexpr (KT == kKvMxFp4) {
-    const float s = mx::scale_operand(w.y);
-    return make_uint4(mx::pair_bf16<0>(w.x, s), mx::pair_bf16<1>(w.x, s), mx::pair_bf16<2>(w.x, s), mx::pair_bf16<3>(w.x, s));
-  } else {
-    return make_uint4(fp8_pair<KT, false>(w.x), fp8_pair<KT, true>(w.x), fp8_pair<KT, false>(w.y), fp8_pair<KT, true>(w.y));
-  }
-}
-
-// Ends it: widened rows into the buffer, and V rows of tokens that lie behind every row's last (from `left` tokens
-// into the run on) set to zero, for they may hold anything.
-template <int D, int DV, int KT>
-__device__ __forceinline__ void land_run(int wave, int lane, int left, uint8_t* buf, const Travel<D, DV, KT>& r) {
-  using G = Wide<D, DV, KT>;
-  const int unit = wave / G::WPU;
-  if constexpr (KT != kKvBf16) {
-#pragma unroll
-    for (int k = 0; k < G::NI; k++) {
-      uint8_t* dst = buf + unit * 16 * D * 2 + 1024 * ((wave % G::WPU) * G::NI + k) + 16 * lane;
-      *reinterpret_cast<uint4*>(dst) = widen_chunk<KT>(r.k[k]);
-      if constexpr (!G::kAlias) *reinterpret_cast<uint4*>(dst + G::TILE) = widen_chunk<KT>(r.v[k]);
-    }
-  } else {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  }
-  if (left < 16) {
     for (int k = 0; k < G::NI; k++) {
       int token, c;
       piece<D, DV, KT>(wave, k, lane, token, c);
-      uint8_t* dst = buf + unit * 16 * D * 2 + 1024 * ((wave % G::WPU) * G::NI + k) + 16 * lane + (G::kAlias ? 0 : G::TILE);
-      if (token >= left) *reinterpret_cast<uint4*>(dst) = make_uint4(0, 0, 0, 0);
+      const uint32_t to = dst + 1024 * ((wave % G::WPU) * G::NI + k), at = 2 * (token * D + 8 * c);
+      send16(ks + 2 * t * D, at, to);
+      if constexpr (!G::kAlias) send16(vs + 2 * t * D, at, to + G::TILE);
+    }
+  } else if constexpr (T::kMx) {
+    const int col = lane & 15, grp = lane >> 4;
+    load_words<T::W>(rows_of<D, KT>(a, ks, t, 16), lane * (D / 8), r.k[0]);
+    r.k_scale = __builtin_amdgcn_raw_buffer_load_b8(scales_of<D>(a, ks, t), (lane >> 2) * (D / 32) + (lane & 3) * D / 128, 0, 0);
+    load_words<T::W>(rows_of<D, KT>(a, vs, t, 16), lane * (D / 8), r.v[0]);
+    r.v_scale = __builtin_amdgcn_raw_buffer_load_b32(scales_of<D>(a, vs, t), (grp * (D / 32) + col * (D / 16) / 32) * 4, 0, 0);
+    const int n = left - 4 * grp;                        // byte x: token 4 grp + x; a scale of 0 is 2^-127
+    r.v_scale &= n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1;
+  } else {
+    const int n = min(left, 16);
+#pragma unroll
+    for (int x = 0; x < T::N; x++) {
+      int token, c16;
+      codes_piece<D, DV, KT>(wave, x, lane, token, c16);
+      const int off = token * D + 16 * c16;              // past the run it is past the resource too
+      load_words<4>(rows_of<D, KT>(a, ks, t, n), off, r.k[x]);
+      if constexpr (!G::kAlias) load_words<4>(rows_of<D, KT>(a, vs, t, n), off, r.v[x]);
+    }
+  }
+}
+
+// Chunk c of token `token` of a run at `run`.
+template <int D>
+__device__ __forceinline__ uint4* chunk_place(uint8_t* run, int token, int c) {
+  return reinterpret_cast<uint4*>(run + token * D * 2 + 16 * (c ^ swizzle<D>(token)));
+}
+template <int KT>
+__device__ __forceinline__ uint4 widen_codes(uint32_t lo, uint32_t hi) {
+  return make_uint4(fp8_pair<KT, false>(lo), fp8_pair<KT, true>(lo), fp8_pair<KT, false>(hi), fp8_pair<KT, true>(hi));
+}
+__device__ __forceinline__ uint4 widen_mx(uint32_t w, float s) {
+  return make_uint4(mx::pair_bf16<0>(w, s), mx::pair_bf16<1>(w, s), mx::pair_bf16<2>(w, s), mx::pair_bf16<3>(w, s));
+}
+
+// Ends it: widened rows into the buffer; of bf16 rows, those of V behind the last token that any row attends (which may
+// hold anything) are set to zero.
+template <int D, int DV, int KT>
+__device__ __forceinline__ void land_run(int wave, int lane, int left, uint8_t* buf, const Travel<D, DV, KT>& r) {
+  using G = Wide<D, DV, KT>;
+  using T = Travel<D, DV, KT>;
+  uint8_t* run = buf + (wave / G::WPU) * 16 * D * 2;
+  if constexpr (KT == kKvBf16) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (left < 16) {
+      for (int k = 0; k < G::NI; k++) {
+        int token, c;
+        piece<D, DV, KT>(wave, k, lane, token, c);
+        uint8_t* dst = run + 1024 * ((wave % G::WPU) * G::NI + k) + 16 * lane + (G::kAlias ? 0 : G::TILE);
+        if (token >= left) *reinterpret_cast<uint4*>(dst) = make_uint4(0, 0, 0, 0);
+      }
+    }
+  } else if constexpr (T::kMx) {
+    // K: lane holds D / 4 channels of token lane / 4
+    const float s = mx::scale_operand(r.k_scale);
+#pragma unroll
+    for (int x = 0; x < D / 32; x++) *chunk_place<D>(run, lane >> 2, (lane & 3) * (D / 32) + x) = widen_mx(r.k[0][x], s);
+    // V: channels col D / 16 .. of tokens 4 grp + x
+    const int col = lane & 15, grp = lane >> 4;
+#pragma unroll
+    for (int x = 0; x < 4; x++) {
+      const float f = mx::scale_operand((r.v_scale >> (8 * x)) & 255);
+      if constexpr (D == 128) {
+        *chunk_place<D>(run + G::TILE, 4 * grp + x, col) = widen_mx(r.v[0][x], f);
+      } else {
+        const uint32_t w = r.v[0][x >> 1];
+        uint2* p = reinterpret_cast<uint2*>(chunk_place<D>(run + G::TILE, 4 * grp + x, col >> 1)) + (col & 1);
+        *p = (x & 1) ? make_uint2(mx::pair_bf16<2>(w, f), mx::pair_bf16<3>(w, f)) : make_uint2(mx::pair_bf16<0>(w, f), mx::pair_bf16<1>(w, f));
+      }
+    }
+  } else {
+#pragma unroll
+    for (int x = 0; x < T::N; x++) {
+      int token, c16;
+      if (!codes_piece<D, DV, KT>(wave, x, lane, token, c16)) continue;
+#pragma unroll
+      for (int e = 0; e < 2; e++) {
+        *chunk_place<D>(run, token, 2 * c16 + e) = widen_codes<KT>(r.k[x][2 * e], r.k[x][2 * e + 1]);
+        if constexpr (!G::kAlias) *chunk_place<D>(run + G::TILE, token, 2 * c16 + e) = widen_codes<KT>(r.v[x][2 * e], r.v[x][2 * e + 1]);
+      }
     }
   }
 }
