@@ -24,6 +24,7 @@ constexpr int kNarrowTiles = 4;            // most narrow tiles of a request, on
 constexpr int kTargetWgs = 512;            // two workgroups a CU
 constexpr int kMaxParts = 64;              // a merging wave's lanes
 constexpr int kPartTokens = 512;           // least tokens of a part: four pairs of runs a wave
+constexpr int kAtOnce = 4;                 // K operands of a run that are sent for together
 constexpr float kLn2 = 0.693147180559945309f;
 
 // The blocks listed for the tile's tokens: masks[id] holds a bit for each token that lists block id, ids the
@@ -195,24 +196,24 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       const int mask0 = __builtin_amdgcn_readlane(my_mask, 2 * u), mask1 = __builtin_amdgcn_readlane(my_mask, 2 * u + 1);
       const bool whole = min(tok0, tok1) >= w.all_from && max(tok0, tok1) + 16 <= w.all_to && (mask0 & mask1) == 0xffff;
       const int next = min(u + 1, count - 1);
-      f32x4_t s[2];
+      f32x4_t s[1][2];
 #pragma unroll
       for (int e = 0; e < 2; e++) {
-        s[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        s[0][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int kk = 0; kk < KS; kk++)
-          s[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand<D, KT>(k[e], kk), w.q[0][kk], s[e], 0, 0, 0);
+          s[0][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand<D, KT>(k[e], kk), w.q[0][kk], s[0][e], 0, 0, 0);
       }
       fetch_k(next);
-      if (!whole) mask_scores<D, D, 1>(0, s, tok0, tok1, mask0, mask1, grp, w);
-      uint32_t p[4];
-      softmax_step<D, D, 1>(a.scale_log2, 0, s, w, p);
+      if (!whole) mask_scores<D, D, 1>(0, s[0], tok0, tok1, mask0, mask1, grp, w);
+      uint32_t p[1][4];
+      softmax_step<D, D, 1>(a.scale_log2, s, w, p);
       uint32_t v0[4][W], v1[4][W];
       v_rows<D, KT>(v[0], v0);
       v_rows<D, KT>(v[1], v1);
 #pragma unroll
       for (int j = 0; j < NJ; j++)
-        w.acc[0][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_operand<W>(v0, v1, j), p_operand(p), w.acc[0][j], 0, 0, 0);
+        w.acc[0][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_operand<W>(v0, v1, j), p_operand(p[0]), w.acc[0][j], 0, 0, 0);
       fetch_v(next);
     }
   }
@@ -349,41 +350,51 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(D == D
       tok_sent = __builtin_amdgcn_readlane(my_tok, (s + 1) & 63);
     }
     const uint8_t* vt = G::kAlias ? buf : buf + G::TILE;
-#pragma unroll 1
+#pragma unroll
     for (int y = 0; y < G::UNITS; y += 2) {
       const int x = G::UNITS * s + y;
-      if (x >= n16) break;
-      int mask0, mask1;
-      const int tok0 = __builtin_amdgcn_readfirstlane(run_at(x, mask0));
-      const int tok1 = __builtin_amdgcn_readfirstlane(run_at(min(x + 1, n16 - 1), mask1));
-      mask0 = __builtin_amdgcn_readfirstlane(mask0);
-      mask1 = x + 1 < n16 ? __builtin_amdgcn_readfirstlane(mask1) : 0;
-      if (((mask0 | mask1) & wave_mask) == 0 || min(tok0, tok1) >= wave_to || max(tok0, tok1) + 16 <= wave_from) continue;
-      const bool whole = min(tok0, tok1) >= w.all_from && max(tok0, tok1) + 16 <= w.all_to && (mask0 & mask1) == 0xffff;
-      f32x4_t sc[RT][2];
+      int mask0 = 0, mask1 = 0, tok0 = 0, tok1 = 0;
+      if (x < n16) {
+        tok0 = __builtin_amdgcn_readfirstlane(run_at(x, mask0));
+        tok1 = __builtin_amdgcn_readfirstlane(run_at(min(x + 1, n16 - 1), mask1));
+        mask0 = __builtin_amdgcn_readfirstlane(mask0);
+        mask1 = x + 1 < n16 ? __builtin_amdgcn_readfirstlane(mask1) : 0;
+      }
+      if (((mask0 | mask1) & wave_mask) != 0 && min(tok0, tok1) < wave_to && max(tok0, tok1) + 16 > wave_from) {
+        const bool whole = min(tok0, tok1) >= w.all_from && max(tok0, tok1) + 16 <= w.all_to && (mask0 & mask1) == 0xffff;
+        f32x4_t sc[RT][2];
 #pragma unroll
-      for (int rt = 0; rt < RT; rt++) sc[rt][0] = sc[rt][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int rt = 0; rt < RT; rt++) sc[rt][0] = sc[rt][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int kk = 0; kk < KS; kk++) {
+        for (int k0 = 0; k0 < KS; k0 += kAtOnce) {       // a few operands at a time, sent for together
+          bf16x8_t k[kAtOnce][2];
 #pragma unroll
-        for (int e = 0; e < 2; e++) {
-          const bf16x8_t k = k_from_lds<D>(buf, 16 * (y + e), kk, col, grp);
+          for (int kk = 0; kk < kAtOnce; kk++)
 #pragma unroll
-          for (int rt = 0; rt < RT; rt++) sc[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, w.q[rt][kk], sc[rt][e], 0, 0, 0);
+            for (int e = 0; e < 2; e++)
+              if (k0 + kk < KS) k[kk][e] = k_from_lds<D>(buf, 16 * (y + e), k0 + kk, col, grp);
+#pragma unroll
+          for (int kk = 0; kk < kAtOnce; kk++)
+#pragma unroll
+            for (int e = 0; e < 2; e++)
+#pragma unroll
+              for (int rt = 0; rt < RT; rt++)
+                if (k0 + kk < KS)
+                  sc[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[kk][e], w.q[rt][k0 + kk], sc[rt][e], 0, 0, 0);
         }
-      }
-      uint32_t p[RT][4];
+        if (!whole) {
 #pragma unroll
-      for (int rt = 0; rt < RT; rt++) {
-        if (!whole) mask_scores<D, DV, RT>(rt, sc[rt], tok0, tok1, mask0, mask1, grp, w);
-        softmax_step<D, DV, RT>(a.scale_log2, rt, sc[rt], w, p[rt]);
-      }
+          for (int rt = 0; rt < RT; rt++) mask_scores<D, DV, RT>(rt, sc[rt], tok0, tok1, mask0, mask1, grp, w);
+        }
+        uint32_t p[RT][4];
+        softmax_step<D, DV, RT>(a.scale_log2, sc, w, p);
 #pragma unroll
-      for (int j = 0; j < NJ; j++) {
-        const bf16x8_t v = v_from_lds<D>(vt, 16 * y, j, col, grp);
+        for (int j = 0; j < NJ; j++) {
+          const bf16x8_t v = v_from_lds<D>(vt, 16 * y, j, col, grp);
 #pragma unroll
-        for (int rt = 0; rt < RT; rt++)
-          w.acc[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_operand(p[rt]), w.acc[rt][j], 0, 0, 0);
+          for (int rt = 0; rt < RT; rt++)
+            w.acc[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_operand(p[rt]), w.acc[rt][j], 0, 0, 0);
+        }
       }
     }
   }

@@ -190,8 +190,8 @@ __device__ __forceinline__ float column_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// The weights' reference: 2^kAhead past the score that moved it, so that it moves seldom and no weight
-// passes 1.
+// The weights' reference: 2^kAhead past the score that moved it, so that it moves seldom and weights stay
+// below 2.
 constexpr float kAhead = 8.f;
 constexpr float kNoScore = -3.0e38f;       // the reference before the first score
 
@@ -246,46 +246,46 @@ __device__ __forceinline__ void mask_scores(int rt, f32x4_t (&s)[2], int tok0, i
   }
 }
 
-typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
-
-// Whether one of 8 weights, bf16 and not negative, passes 1 (or is not a number).
-__device__ __forceinline__ bool weights_pass_one(const uint32_t (&p)[4]) {
-  const u16x2_t a = __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, p[0]), __builtin_bit_cast(u16x2_t, p[1]));
-  const u16x2_t b = __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, p[2]), __builtin_bit_cast(u16x2_t, p[3]));
-  const u16x2_t c = __builtin_elementwise_max(a, b);
-  return max((uint32_t)c.x, (uint32_t)c.y) > 0x3f80u;
-}
-
 // One step of the softmax: the scores s of 32 tokens become weights p, bf16, operand B of O^T = V^T P^T.  The
-// weights are taken at the present reference first and seldom pass 1; only then it moves.  The sum takes the weights
-// before their rounding, which is to the nearest (2^-9 of each at most, without a bias) and halves the matrix work
-// that two parts would need.
+// weights are taken at the present references first and seldom reach 2 (bit 14 of a bf16 number; infinities and
+// NaN have it too); only then the references move.  The sum takes the weights before their rounding, which is to the
+// nearest (2^-9 of each at most, without a bias) and halves the matrix work that two parts would need.
 template <int D, int DV, int RT>
-__device__ __forceinline__ void softmax_step(float scale_log2, int rt, const f32x4_t (&s)[2], Rows<D, DV, RT>& w,
-                                             uint32_t (&p)[4]) {
-  float x[8];
-  auto weigh = [&] {
+__device__ __forceinline__ void softmax_step(float scale_log2, const f32x4_t (&s)[RT][2], Rows<D, DV, RT>& w,
+                                             uint32_t (&p)[RT][4]) {
+  float x[RT][8];
+  auto weigh = [&](int rt) {
 #pragma unroll
-    for (int i = 0; i < 8; i++) x[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], scale_log2, -w.m[rt]));
+    for (int i = 0; i < 8; i++) x[rt][i] = __builtin_amdgcn_exp2f(fmaf(s[rt][i >> 2][i & 3], scale_log2, -w.m[rt]));
 #pragma unroll
-    for (int i = 0; i < 4; i++) p[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+    for (int i = 0; i < 4; i++) p[rt][i] = pack_bf16(x[rt][2 * i], x[rt][2 * i + 1]);
   };
-  weigh();
-  if (__builtin_expect(__any(weights_pass_one(p)), 0)) {
-    const float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
-                            fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))) *
-                      scale_log2;
-    const float c = column_max(top), next = c > w.m[rt] ? c + kAhead : w.m[rt];
-    const float alpha = __builtin_amdgcn_exp2f(w.m[rt] - next);
-    w.m[rt] = next;
-    w.l[rt] *= alpha;
+  uint32_t seen = 0;
 #pragma unroll
-    for (int j = 0; j < DV / 16; j++)
-#pragma unroll
-      for (int i = 0; i < 4; i++) w.acc[rt][j][i] *= alpha;
-    weigh();
+  for (int rt = 0; rt < RT; rt++) {
+    weigh(rt);
+    seen |= (p[rt][0] | p[rt][1]) | (p[rt][2] | p[rt][3]);
   }
-  w.l[rt] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+  if (__builtin_expect(__any((seen & 0x40004000u) != 0), 0)) {
+#pragma unroll
+    for (int rt = 0; rt < RT; rt++) {
+      const float top = fmaxf(fmaxf(fmaxf(s[rt][0][0], s[rt][0][1]), fmaxf(s[rt][0][2], s[rt][0][3])),
+                              fmaxf(fmaxf(s[rt][1][0], s[rt][1][1]), fmaxf(s[rt][1][2], s[rt][1][3]))) *
+                        scale_log2;
+      const float c = column_max(top), next = c > w.m[rt] ? c + kAhead : w.m[rt];
+      const float alpha = __builtin_amdgcn_exp2f(w.m[rt] - next);
+      w.m[rt] = next;
+      w.l[rt] *= alpha;
+#pragma unroll
+      for (int j = 0; j < DV / 16; j++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) w.acc[rt][j][i] *= alpha;
+      weigh(rt);
+    }
+  }
+#pragma unroll
+  for (int rt = 0; rt < RT; rt++)
+    w.l[rt] += ((x[rt][0] + x[rt][1]) + (x[rt][2] + x[rt][3])) + ((x[rt][4] + x[rt][5]) + (x[rt][6] + x[rt][7]));
 }
 
 __device__ __forceinline__ bf16x8_t p_operand(const uint32_t (&p)[4]) {
