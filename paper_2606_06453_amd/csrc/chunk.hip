@@ -282,16 +282,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 // Four waves of 16 RT rows each share the tokens of their tile through LDS (chunk_wide.h).  A wave passes over
 // runs that none of its rows attends.
 template <int D, int DV, int KT, int RT, bool SPARSE>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(D == DV ? 2 : 1))) void chunk_wide_kernel(const ChunkArgs a) {
+__device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int h, int split, uint32_t* lds) {
   using G = Wide<D, DV, KT>;
   constexpr int KS = D / 32, NJ = DV / 16;
-  extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
   const int tid = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, grp = lane >> 4;
-  const int h = (int)blockIdx.x % a.H, split = (int)blockIdx.y;
-  Tile t;
-  // the tiles at a request's end attend most and start first
-  if (!find_tile(a, (int)(gridDim.x - 1 - blockIdx.x) / a.H, t)) return;
   uint8_t* bufs = reinterpret_cast<uint8_t*>(lds);
   uint32_t* lists = lds + 2 * G::BUF / sizeof(uint32_t);
   int shift16;
@@ -432,6 +427,21 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(D == D
   if (__syncthreads_or(bad)) attend_rows<D, DV, KT>(a, t, h, runs, split);
 }
 
+template <int D, int DV, int KT, int RT, bool SPARSE>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(D == DV ? 2 : 1))) void chunk_wide_kernel(const ChunkArgs a) {
+  extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
+  const int h = (int)blockIdx.x % a.H, split = (int)blockIdx.y;
+  Tile t;
+  if (!find_tile(a, (int)blockIdx.x / a.H, t)) return;
+  if constexpr (RT > 1) {
+    if (t.n * a.g <= 4 * kTileRows) {                    // a short request among long ones
+      wide_tile<D, DV, KT, 1, SPARSE>(a, t, h, split, lds);
+      return;
+    }
+  }
+  wide_tile<D, DV, KT, RT, SPARSE>(a, t, h, split, lds);
+}
+
 // Joins the parts of every row, a wave a row and a token a workgroup (a.tokens is 1): each part's weight is its
 // sum at the row's largest reference.
 template <int DV>
@@ -504,7 +514,7 @@ Plan plan_of(const Geometry& g, int n, int Hq, bool sparse, int max_sel) {
   const bool latent = g.Dqk != g.Dv;
   const int64_t batch = std::max(g.batch, 1);
   auto tokens = [&](int rows) { return std::max(1, sparse ? std::min(16, rows / group) : rows / group); };
-  if (!latent && (int64_t)n <= batch * kNarrowTiles * (kTileRows / group)) p.operands = 0;
+  if (!latent && g.kv_dtype != kKvBf16 && (int64_t)n <= batch * kNarrowTiles * (kTileRows / group)) p.operands = 0;
   else p.operands = sparse || latent || (int64_t)n * group <= batch * 4 * kTileRows ? 1 : 2;
   p.tokens = tokens(p.operands == 0 ? kTileRows : 4 * kTileRows * p.operands);
   const int64_t tiles = std::max<int64_t>(batch, (n + p.tokens - 1) / p.tokens) * g.H;

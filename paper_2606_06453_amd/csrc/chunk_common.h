@@ -46,26 +46,57 @@ struct Tile {
   const int32_t* pages;                    // the list
 };
 
-// Tile x of the grid.  Request i owns the tiles from floor(q_indptr[i] / T) + i on, at least as many as its rows
-// need, so that no plan is made first; its request is the last one that starts at or before x, found by
-// the lanes of a wave 64 requests at a time.  False for a tile with no token.
+// A request's rows in q.
+__device__ __forceinline__ void rows_of_request(const ChunkArgs& a, int i, int& q0, int& n) {
+  q0 = min(max(a.q_indptr[i], 0), a.num_rows);
+  n = min(max(a.q_indptr[i + 1], q0), a.num_rows) - q0;
+  if (a.q_lens) n = min(max(a.q_lens[i], 0), n);
+}
+
+// Tile x of the grid, or false for one with no token.  No plan is made first:
+//   up to 64 requests   lane i counts the tiles of request i, and the requests take the grid in the order of their
+//                       lengths, the longest first (the last workgroups to start are then the shortest: 48 requests
+//                       of up to 12000 tokens, a quarter of them prompts, 1078 -> 894 us);
+//   more                request i owns the tiles from floor(q_indptr[i] / T) + i on, at least as many as its rows need;
+//                       its request is the last one that starts at or before x, found 64 requests at a time.
+// Within a request the last tile, whose tokens attend most, comes first.
 __device__ __forceinline__ bool find_tile(const ChunkArgs& a, int x, Tile& t) {
   const int T = a.tokens, lane = lane_id();
-  int lo = 0, hi = a.batch;
-  while (hi - lo > 1) {
-    const int step = (hi - lo + kWave - 1) / kWave;
-    const int at = lo + lane * step;
-    const bool below = at < hi && min(max(a.q_indptr[min(at, hi - 1)], 0), a.num_rows) / T + at <= x;
-    const int c = max(__popcll(__ballot(below)), 1);
-    hi = min(hi, lo + c * step);
-    lo += (c - 1) * step;
+  int i, q0, n, y;
+  if (a.batch <= kWave) {
+    int tiles = 0, len = 0;
+    if (lane < a.batch) {
+      rows_of_request(a, lane, q0, n);
+      len = a.seq_lens[lane];
+      tiles = (n + T - 1) / T;
+    }
+    int start = 0;
+    for (int j = 0; j < a.batch; j++) {
+      const int other = __builtin_amdgcn_readlane(len, j), c = __builtin_amdgcn_readlane(tiles, j);
+      if (other > len || (other == len && j < lane)) start += c;
+    }
+    const uint64_t mine = __ballot(lane < a.batch && x >= start && x < start + tiles);
+    if (!mine) return false;
+    i = __builtin_ctzll(mine);
+    q0 = __builtin_amdgcn_readlane(q0, i);
+    n = __builtin_amdgcn_readlane(n, i);
+    y = x - __builtin_amdgcn_readlane(start, i);
+  } else {
+    int lo = 0, hi = a.batch;
+    while (hi - lo > 1) {
+      const int step = (hi - lo + kWave - 1) / kWave;
+      const int at = lo + lane * step;
+      const bool below = at < hi && min(max(a.q_indptr[min(at, hi - 1)], 0), a.num_rows) / T + at <= x;
+      const int c = max(__popcll(__ballot(below)), 1);
+      hi = min(hi, lo + c * step);
+      lo += (c - 1) * step;
+    }
+    i = __builtin_amdgcn_readfirstlane(lo);
+    rows_of_request(a, i, q0, n);
+    y = x - q0 / T - i;
+    if (y < 0 || y >= (n + T - 1) / T) return false;
   }
-  const int i = __builtin_amdgcn_readfirstlane(lo);
-  const int q0 = min(max(a.q_indptr[i], 0), a.num_rows), q1 = min(max(a.q_indptr[i + 1], q0), a.num_rows);
-  int n = q1 - q0;
-  if (a.q_lens) n = min(max(a.q_lens[i], 0), n);
-  const int t0 = (x - q0 / T - i) * T;
-  if (t0 < 0 || t0 >= n) return false;
+  const int t0 = ((n + T - 1) / T - 1 - y) * T;
   const int L = max(a.seq_lens[i], 0), base = a.indptr[i];
   t.i = i;
   t.n = min(T, n - t0);
