@@ -3,17 +3,21 @@
 //
 // A score is sum_c qbar_c mean_jc in fp64, rounded to fp32 (qbar: the mean of the group's queries), and the
 // selection is by these scores exactly.  Few of them are computed so:
-//   1. A workgroup takes up to 32 tokens and one KV head.  Scores s' come from matrix products of bf16 parts,
-//      qbar = qh + ql and mean = mh + ml (s' = qh mh + ql mh + qh ml in fp32), and stay in LDS as bf16 numbers f.
+//   1. chunk_score_kernel: scores s' from matrix products of bf16 parts, qbar = qh + ql and mean = mh + ml
+//      (s' = qh mh + ql mh + qh ml in fp32), kept as bf16 numbers f in the workspace.  A workgroup takes up to 64
+//      tokens, one KV head and a part of the blocks; a wave splits 16 means into their parts once for all tokens.
 //   2. |s - f| <= B = kBound |qbar| max_j |mean_j| + 2^-8 max_j |f_j|: the parts leave 2^-16 of a channel each
 //      and the product of the low ones, 3 D additions 2^-23 of their sum each, together below 2^-13 of the
 //      norms' product (Cauchy-Schwarz); bf16 rounds by 2^-8 of a value.  The norms of the means are the diagonal of a
 //      matrix product too.
-//   3. A wave finds the K-th largest f of a row (histograms that narrow down on it) to lie within [lo, hi].  Blocks
-//      with f - 2 B > hi have fewer than K others at or above them: in.  Blocks with f + 2 B < lo: out.
-//   4. The others, a dozen or so, are scored in fp64 and ranked, ties to the lower block.
+//   3. chunk_choose_kernel, a wave a row and KV head: the K-th largest f (histograms that narrow down on it) lies
+//      within [lo, hi].  Blocks with f - 2 B > hi have fewer than K others at or above them: in.  Blocks with
+//      f + 2 B < lo: out.
+//   4. The others, two dozen or so, are scored in fp64 and ranked, ties to the lower block.
 // Rows with more than kMostOpen of them (many equal scores), and rows where a norm is not finite or so small that
 // its square is lost, select by digits of the exact scores alone, which they compute anew for every digit.
+// One kernel that kept the scores of 32 tokens in LDS took 388 us for 4096 tokens over 2048 blocks and 55 us for a few
+// users' drafted tokens: a row's passes waited with two waves a SIMD, and few tokens left most of the chip idle.
 #include <algorithm>
 
 #include "chunk_tile.h"
@@ -22,19 +26,49 @@ namespace vx {
 using namespace chunk;
 namespace {
 
-constexpr int kThreads = 512, kWaves = kThreads / kWave;
+constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr int kBins = 256;
 constexpr int kMostOpen = 128;
+constexpr int kFewInBin = 32;
+constexpr int kTogether = 4;               // times 8 open blocks whose means travel together
+constexpr int kScoreWgs = 1024;            // workgroups of the scores that fill the chip
+constexpr int kUnit = 32;                  // blocks that a wave looks up at a time
+constexpr size_t kScoreBytes = (size_t)128 << 20;        // of scores at a time: half of the last cache
 constexpr float kBound = 1.f / 4096.f;                   // twice the bound above
 constexpr float kTinySquare = 7.9e-31f;                  // 2^-100
 
 struct SelectArgs {
   const float* mean;
   const int32_t* budget;
-  int n_sink, n_local, r, stride;          // stride: scores of a token in LDS
+  int n_sink, n_local, r;
   int32_t* sel_pages;
   int32_t* sel_count;
+  uint16_t* scores;                        // [tile][H][tokens][stride]
+  float* norms;                            // [tile][H][parts]: largest square of the means' norms
+  int stride, part, parts;                 // of a row; blocks of a part
+  int tile0;                               // first tile of the launch
 };
+
+// What a tile's tokens select among.
+struct Scope {
+  int total;                               // the budget
+  int nb_all;                              // blocks of the request
+  int c0, c1;                              // candidates of the last token
+  bool scored;
+};
+__device__ __forceinline__ int blocks_of(const ChunkArgs& a, const Tile& t, const Scope& c, int x) {
+  return t.p0 + x < 0 ? 0 : min(((t.p0 + x) >> a.bs_shift) + 1, c.nb_all);
+}
+__device__ __forceinline__ Scope scope_of(const ChunkArgs& a, const SelectArgs& s, const Tile& t) {
+  Scope c;
+  c.total = min(max(s.budget[t.i], 0), a.max_sel);
+  c.nb_all = min((t.len + a.bs - 1) >> a.bs_shift, a.max_blocks);
+  const int nb = blocks_of(a, t, c, t.n - 1);
+  c.c0 = min(s.n_sink, nb);
+  c.c1 = max(nb - s.n_local, c.c0);
+  c.scored = c.total < nb && c.total > 0 && c.c1 > c.c0;
+  return c;
+}
 
 // A wave's own LDS: a histogram, then the row's query.
 struct WaveLds {
@@ -60,30 +94,34 @@ __device__ __forceinline__ int wave_sum(int x) {
   return x;
 }
 
-// Keys of the exact scores of 8 blocks: block j8 of lane / 8 (below 0: none), qbar in LDS.  Every lane of the 8 gets
-// its block's key.
-template <int D>
-__device__ __forceinline__ uint32_t exact_keys(const ChunkArgs& a, const SelectArgs& s, const Tile& t, int h, int j8,
-                                               const double* qbar) {
+// Keys of the exact scores of N times 8 blocks, qbar in LDS: row8[z] is the summary row of the block of this lane's 8
+// (below 0: none), and every lane of the 8 gets its key.
+template <int D, int N>
+__device__ __forceinline__ void exact_keys(const ChunkArgs& a, const SelectArgs& s, int h, const int (&row8)[N],
+                                           const double* qbar, uint32_t (&key)[N]) {
   const int x = lane_id() & 7;
-  double dot = 0.0;
-  if (j8 >= 0) {
-    const float* m = s.mean + (block_row(t.pages, j8, s.r, a.num_phys) * a.H + h) * D;
-    float4 v[D / 32];
+  float4 v[N][D / 32];
 #pragma unroll
-    for (int c = 0; c < D / 32; c++) v[c] = *reinterpret_cast<const float4*>(m + 32 * c + 4 * x);
+  for (int z = 0; z < N; z++) {
+    const float* m = s.mean + ((int64_t)max(row8[z], 0) * a.H + h) * D;
+#pragma unroll
+    for (int c = 0; c < D / 32; c++) v[z][c] = *reinterpret_cast<const float4*>(m + 32 * c + 4 * x);
+  }
+#pragma unroll
+  for (int z = 0; z < N; z++) {
+    double dot = 0.0;
 #pragma unroll
     for (int c = 0; c < D / 32; c++) {
       const double* q = qbar + 32 * c + 4 * x;
-      dot = fma(q[0], (double)v[c].x, dot);
-      dot = fma(q[1], (double)v[c].y, dot);
-      dot = fma(q[2], (double)v[c].z, dot);
-      dot = fma(q[3], (double)v[c].w, dot);
+      dot = fma(q[0], (double)v[z][c].x, dot);
+      dot = fma(q[1], (double)v[z][c].y, dot);
+      dot = fma(q[2], (double)v[z][c].z, dot);
+      dot = fma(q[3], (double)v[z][c].w, dot);
     }
-  }
 #pragma unroll
-  for (int y = 1; y < 8; y <<= 1) dot += __shfl_xor(dot, y, kWave);
-  return float_key((float)dot);
+    for (int y = 1; y < 8; y <<= 1) dot += __shfl_xor(dot, y, kWave);
+    key[z] = float_key((float)dot);
+  }
 }
 
 // The row's K best candidates of [c0, c1) by their exact scores alone: flags[j] = 1 or 0.
@@ -91,6 +129,12 @@ template <int D>
 __device__ __forceinline__ void select_by_digits(const ChunkArgs& a, const SelectArgs& s, const Tile& t, int h, int c0,
                                                  int c1, int want, const double* qbar, uint16_t* flags) {
   const int lane = lane_id(), sub = lane >> 3;
+  auto key_of = [&](int j) {
+    const int row8[1] = {(int)block_row(t.pages, min(j, c1 - 1), s.r, a.num_phys)};
+    uint32_t k[1];
+    exact_keys<D, 1>(a, s, h, row8, qbar, k);
+    return k[0];
+  };
   uint32_t T = 0;
   int ties = want;
   for (int bit = 31; bit >= 0; bit -= 4) {               // 16 bins a digit, a lane each
@@ -99,7 +143,7 @@ __device__ __forceinline__ void select_by_digits(const ChunkArgs& a, const Selec
     int bin = 0;                                         // lane d < 16: candidates of digit d
     for (int j0 = c0; j0 < c1; j0 += 8) {
       const int j = j0 + sub;
-      const uint32_t k = exact_keys<D>(a, s, t, h, j < c1 ? j : -1, qbar);
+      const uint32_t k = key_of(j);
       const bool on = j < c1 && (lane & 7) == 0 && (k & above) == T;
       const int d = (int)(k >> shift) & 15;
 #pragma unroll
@@ -119,7 +163,7 @@ __device__ __forceinline__ void select_by_digits(const ChunkArgs& a, const Selec
   int seen = 0;
   for (int j0 = c0; j0 < c1; j0 += 8) {
     const int j = j0 + sub;
-    const uint32_t k = exact_keys<D>(a, s, t, h, j < c1 ? j : -1, qbar);
+    const uint32_t k = key_of(j);
     const uint64_t eq = __ballot(j < c1 && (lane & 7) == 0 && k == T);
     const int before = seen + __popcll(eq & ((1ull << (lane & 56)) - 1));
     seen += __popcll(eq);
@@ -127,183 +171,232 @@ __device__ __forceinline__ void select_by_digits(const ChunkArgs& a, const Selec
   }
 }
 
+// CG groups of 16 tokens.
 template <int D, int CG>
-__global__ __launch_bounds__(kThreads) void chunk_select_kernel(const ChunkArgs a, const SelectArgs s) {
-  constexpr int KS = D / 32, TOK = 16 * CG;
-  extern __shared__ __attribute__((aligned(16))) uint16_t slab[];          // [token][stride]
-  __shared__ WaveLds wave_lds[kWaves];
-  __shared__ uint32_t key_lo[TOK], key_hi[TOK], norm_q[TOK], norm_m;       // ordered bits of floats
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void chunk_score_kernel(const ChunkArgs a, const SelectArgs s) {
+  constexpr int KS = D / 32;
+  __shared__ bf16x8_t parts[CG][KS][2][kWave];           // qh and ql, operand B
+  __shared__ uint32_t norm_m;                            // of a float that is not negative: ordered as its bits
   const int tid = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, grp = lane >> 4;
-  const int h = (int)blockIdx.x % a.H;
+  const int h = (int)blockIdx.x % a.H, xt = (int)blockIdx.x / a.H, part = (int)blockIdx.y;
   Tile t;
-  if (!find_tile(a, (int)blockIdx.x / a.H, t)) return;
-  const int total = min(max(s.budget[t.i], 0), a.max_sel);
-  const int nb_all = min((t.len + a.bs - 1) >> a.bs_shift, a.max_blocks);
-  auto blocks_of = [&](int x) { return t.p0 + x < 0 ? 0 : min(((t.p0 + x) >> a.bs_shift) + 1, nb_all); };
-  const int nb_last = blocks_of(t.n - 1);
-  const int c0 = min(s.n_sink, nb_last), c1_last = max(nb_last - s.n_local, c0);       // candidates of the last token
-  const bool scored = total < nb_last && total > 0 && c1_last > c0;
-
-  if (tid < TOK) {
-    key_lo[tid] = 0xffffffffu;
-    key_hi[tid] = 0u;
-    norm_q[tid] = 0u;
-  }
+  if (!find_tile(a, s.tile0 + xt, t)) return;
+  const Scope c = scope_of(a, s, t);
+  const int j_lo = max(c.c0 & ~(kUnit - 1), part * s.part), j_hi = min((c.c1 + kUnit - 1) & ~(kUnit - 1), (part + 1) * s.part);
   if (tid == 0) norm_m = 0u;
+  if (!c.scored) return;
+  float* norm_out = s.norms + ((int64_t)xt * a.H + h) * s.parts + part;
+  if (j_lo >= j_hi) {
+    if (tid == 0) *norm_out = 0.f;
+    return;
+  }
+  for (int y = wave; y < CG; y += kWaves) {
+    const int x = 16 * y + col;
+    const bool there = x < t.n;
+    const uint16_t* q = a.q + (t.row0 + (there ? x : 0)) * a.q_row + (int64_t)h * a.g * a.q_head;
+#pragma unroll
+    for (int kk = 0; kk < KS; kk++) {
+      float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      for (int g = 0; g < a.g; g++) {
+        const uint4 w = *reinterpret_cast<const uint4*>(q + g * a.q_head + 32 * kk + 8 * grp);
+        const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          v[2 * e] += bf16lo(ws[e]);
+          v[2 * e + 1] += bf16hi(ws[e]);
+        }
+      }
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        const float u = v[2 * e] / a.g, z = v[2 * e + 1] / a.g;
+        hi[e] = pack_bf16(u, z);
+        lo[e] = pack_bf16(u - bf16lo(hi[e]), z - bf16hi(hi[e]));
+      }
+      parts[y][kk][0][lane] = __builtin_bit_cast(bf16x8_t, u32x4_t{hi[0], hi[1], hi[2], hi[3]});
+      parts[y][kk][1][lane] = __builtin_bit_cast(bf16x8_t, u32x4_t{lo[0], lo[1], lo[2], lo[3]});
+    }
+  }
   __syncthreads();
-  if (scored) {
-    bf16x8_t qh[CG][KS], ql[CG][KS];
-    int c1[CG];
+  bf16x8_t qh[CG][KS], ql[CG][KS];
 #pragma unroll
-    for (int y = 0; y < CG; y++) {
-      const int x = 16 * y + col;
-      const bool there = x < t.n;
-      c1[y] = there ? max(blocks_of(x) - s.n_local, 0) : 0;
-      const uint16_t* q = a.q + (t.row0 + (there ? x : 0)) * a.q_row + (int64_t)h * a.g * a.q_head;
-      float square = 0.f;
+  for (int y = 0; y < CG; y++)
 #pragma unroll
-      for (int kk = 0; kk < KS; kk++) {
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        for (int g = 0; g < a.g; g++) {
-          const uint4 w = *reinterpret_cast<const uint4*>(q + g * a.q_head + 32 * kk + 8 * grp);
-          const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-          for (int e = 0; e < 4; e++) {
-            v[2 * e] += bf16lo(ws[e]);
-            v[2 * e + 1] += bf16hi(ws[e]);
-          }
-        }
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-          const float u = v[2 * e] / a.g, z = v[2 * e + 1] / a.g;
-          square = fmaf(u, u, fmaf(z, z, square));
-          hi[e] = pack_bf16(u, z);
-          lo[e] = pack_bf16(u - bf16lo(hi[e]), z - bf16hi(hi[e]));
-        }
-        qh[y][kk] = __builtin_bit_cast(bf16x8_t, u32x4_t{hi[0], hi[1], hi[2], hi[3]});
-        ql[y][kk] = __builtin_bit_cast(bf16x8_t, u32x4_t{lo[0], lo[1], lo[2], lo[3]});
-      }
-      square = column_sum(square);
-      if (wave == 0 && grp == 0) norm_q[x] = __float_as_uint(square);
+    for (int kk = 0; kk < KS; kk++) {
+      qh[y][kk] = parts[y][kk][0][lane];
+      ql[y][kk] = parts[y][kk][1][lane];
     }
-    float least[CG], most[CG], norm = 0.f;
+  uint16_t* out = s.scores + (((int64_t)xt * a.H + h) * a.tokens) * s.stride;
+  float norm = 0.f;
+  struct Means {
+    float4 v[KS][2];
+  };
+  // a lane finds the summary row of one of the unit's blocks, then two groups of 16 are scored
+  auto find = [&](int j0) {
+    const int j = min(max(j0 + (lane & (kUnit - 1)), c.c0), c.c1 - 1);
+    return (int)block_row(t.pages, j, s.r, a.num_phys);
+  };
+  auto fetch = [&](int found, int q, Means& m) {         // this lane: block 16 q + col of the unit
+    const float* src = s.mean + ((int64_t)__shfl(found, 16 * q + col, kWave) * a.H + h) * D + 8 * grp;
 #pragma unroll
-    for (int y = 0; y < CG; y++) {
-      least[y] = INFINITY;
-      most[y] = -INFINITY;
+    for (int kk = 0; kk < KS; kk++) {
+      m.v[kk][0] = *reinterpret_cast<const float4*>(src + 32 * kk);
+      m.v[kk][1] = *reinterpret_cast<const float4*>(src + 32 * kk + 4);
     }
-    bool odd = false;                                    // a score that is not finite
-    struct Means {
-      float4 v[KS][2];
-    };
-    auto fetch = [&](int j0, Means& m) {                 // this lane: block j0 + col
-      const int j = min(max(j0 + col, c0), c1_last - 1);
-      const float* src = s.mean + (block_row(t.pages, j, s.r, a.num_phys) * a.H + h) * D + 8 * grp;
+  };
+  auto score = [&](int j0, const Means& m) {
+    f32x4_t sc[CG], gram = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int kk = 0; kk < KS; kk++) {
-        m.v[kk][0] = *reinterpret_cast<const float4*>(src + 32 * kk);
-        m.v[kk][1] = *reinterpret_cast<const float4*>(src + 32 * kk + 4);
+    for (int y = 0; y < CG; y++) sc[y] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kk = 0; kk < KS; kk++) {
+      const float v[8] = {m.v[kk][0].x, m.v[kk][0].y, m.v[kk][0].z, m.v[kk][0].w,
+                          m.v[kk][1].x, m.v[kk][1].y, m.v[kk][1].z, m.v[kk][1].w};
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        hi[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+        lo[e] = pack_bf16(v[2 * e] - bf16lo(hi[e]), v[2 * e + 1] - bf16hi(hi[e]));
       }
-    };
-    auto score = [&](int j0, const Means& m) {
-      f32x4_t sc[CG], gram = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int y = 0; y < CG; y++) sc[y] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int kk = 0; kk < KS; kk++) {
-        const float v[8] = {m.v[kk][0].x, m.v[kk][0].y, m.v[kk][0].z, m.v[kk][0].w,
-                            m.v[kk][1].x, m.v[kk][1].y, m.v[kk][1].z, m.v[kk][1].w};
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-          hi[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
-          lo[e] = pack_bf16(v[2 * e] - bf16lo(hi[e]), v[2 * e + 1] - bf16hi(hi[e]));
-        }
-        const bf16x8_t mh = __builtin_bit_cast(bf16x8_t, u32x4_t{hi[0], hi[1], hi[2], hi[3]});
-        const bf16x8_t ml = __builtin_bit_cast(bf16x8_t, u32x4_t{lo[0], lo[1], lo[2], lo[3]});
-        gram = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mh, mh, gram, 0, 0, 0);
-#pragma unroll
-        for (int y = 0; y < CG; y++) {
-          sc[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ml, qh[y][kk], sc[y], 0, 0, 0);
-          sc[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mh, ql[y][kk], sc[y], 0, 0, 0);
-          sc[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mh, qh[y][kk], sc[y], 0, 0, 0);
-        }
-      }
-      // lane (grp, col): scores of blocks j0 + 4 grp + i and token 16 y + col; blocks' own products on the diagonal
-      if ((col >> 2) == grp && j0 + col >= c0 && j0 + col < c1_last) {
-        const float d = (col & 2) ? ((col & 1) ? gram[3] : gram[2]) : ((col & 1) ? gram[1] : gram[0]);
-        norm = d != d ? INFINITY : fmaxf(norm, d);
-      }
+      const bf16x8_t mh = __builtin_bit_cast(bf16x8_t, u32x4_t{hi[0], hi[1], hi[2], hi[3]});
+      const bf16x8_t ml = __builtin_bit_cast(bf16x8_t, u32x4_t{lo[0], lo[1], lo[2], lo[3]});
+      gram = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mh, mh, gram, 0, 0, 0);
 #pragma unroll
       for (int y = 0; y < CG; y++) {
-        const uint2 w = make_uint2(pack_bf16(sc[y][0], sc[y][1]), pack_bf16(sc[y][2], sc[y][3]));
-        if (CG > 1 || col < a.tokens) *reinterpret_cast<uint2*>(slab + (16 * y + col) * s.stride + j0 + 4 * grp) = w;
-        const float f[4] = {bf16lo(w.x), bf16hi(w.x), bf16lo(w.y), bf16hi(w.y)};
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-          const int j = j0 + 4 * grp + i;
-          const bool on = j >= c0 && j < c1[y];
-          least[y] = on ? fminf(least[y], f[i]) : least[y];
-          most[y] = on ? fmaxf(most[y], f[i]) : most[y];
-          odd = odd || (on && !(fabsf(f[i]) < INFINITY));
-        }
+        sc[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ml, qh[y][kk], sc[y], 0, 0, 0);
+        sc[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mh, ql[y][kk], sc[y], 0, 0, 0);
+        sc[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mh, qh[y][kk], sc[y], 0, 0, 0);
       }
-    };
-    const int g0 = c0 >> 4, g1 = (c1_last + 15) >> 4;    // groups of 16 blocks
-    Means ma, mb;
-    int g = g0 + wave;
-    if (g < g1) fetch(16 * g, ma);
-    for (; g < g1; g += 2 * kWaves) {
-      fetch(16 * min(g + kWaves, g1 - 1), mb);
-      score(16 * g, ma);
-      if (g + kWaves >= g1) break;
-      fetch(16 * min(g + 2 * kWaves, g1 - 1), ma);
-      score(16 * (g + kWaves), mb);
     }
-    norm = __any(odd) ? INFINITY : wave_max(norm);
-    if (lane == 0) atomicMax(&norm_m, __float_as_uint(norm));              // not negative: ordered as its bits
+    // lane (grp, col): scores of blocks j0 + 4 grp + i and token 16 y + col; blocks' own products on the diagonal
+    if ((col >> 2) == grp && j0 + col >= c.c0 && j0 + col < c.c1) {
+      const float d = (col & 2) ? ((col & 1) ? gram[3] : gram[2]) : ((col & 1) ? gram[1] : gram[0]);
+      norm = d != d ? INFINITY : fmaxf(norm, d);
+    }
 #pragma unroll
     for (int y = 0; y < CG; y++) {
-      const float hi = column_max(most[y]), lo = -column_max(-least[y]);
-      if (grp == 0 && hi >= lo) {
-        atomicMax(&key_hi[16 * y + col], float_key(hi));
-        atomicMin(&key_lo[16 * y + col], float_key(lo));
-      }
+      if (16 * y + col < t.n)
+        *reinterpret_cast<uint2*>(out + (int64_t)(16 * y + col) * s.stride + j0 + 4 * grp) =
+            make_uint2(pack_bf16(sc[y][0], sc[y][1]), pack_bf16(sc[y][2], sc[y][3]));
+    }
+  };
+  int j0 = j_lo + kUnit * wave;
+  if (j0 < j_hi) {
+    int found = find(j0);
+    Means ma, mb;
+    fetch(found, 0, ma);
+    for (; j0 < j_hi; j0 += kUnit * kWaves) {
+      const int next = find(min(j0 + kUnit * kWaves, j_hi - kUnit));
+      fetch(found, 1, mb);
+      score(j0, ma);
+      fetch(next, 0, ma);
+      score(j0 + 16, mb);
+      found = next;
     }
   }
+  norm = wave_max(norm);
+  if (lane == 0) atomicMax(&norm_m, __float_as_uint(norm));
   __syncthreads();
+  if (tid == 0) *norm_out = __uint_as_float(norm_m);
+}
 
-  auto from_key = [](uint32_t k) { return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k); };
+// A wave a row.
+template <int D>
+__global__ __launch_bounds__(kThreads) void chunk_choose_kernel(const ChunkArgs a, const SelectArgs s) {
+  extern __shared__ __attribute__((aligned(16))) uint16_t slab[];          // [wave][stride]
+  __shared__ WaveLds wave_lds[kWaves];
+  const int tid = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int groups = (a.tokens + kWaves - 1) / kWaves;   // of a tile's rows, one a wave
+  const int h = (int)blockIdx.x % a.H, xt = (int)blockIdx.x / a.H / groups;
+  const int x = ((int)blockIdx.x / a.H - xt * groups) * kWaves + wave;
+  Tile t;
+  if (!find_tile(a, s.tile0 + xt, t) || x >= t.n) return;
+  const Scope c = scope_of(a, s, t);
+  const int total = c.total;
   WaveLds& mine = wave_lds[wave];
-  for (int x = wave; x < t.n; x += kWaves) {
+  {
     const int64_t row = t.row0 + x;
-    const int nb = blocks_of(x), forced = min(nb, s.n_sink + s.n_local);
+    const int nb = blocks_of(a, t, c, x), forced = min(nb, s.n_sink + s.n_local);
     const int k0 = min(s.n_sink, nb), k1 = max(nb - s.n_local, k0);        // the row's candidates
     const bool all = total >= nb;
     const int want = all ? k1 - k0 : min(max(total - forced, 0), k1 - k0);
-    uint16_t* f16 = slab + x * s.stride;
+    uint16_t* f16 = slab + wave * s.stride;
     const bool choose = want > 0 && want < k1 - k0;
+    // lane's 8 blocks from j on: which of them are in [lo, hi), and their scores
+    auto inside = [&](int j, int lo, int hi) {
+      return (int)((1u << min(max(hi - j, 0), 8)) - 1) & ~(int)((1u << min(max(lo - j, 0), 8)) - 1);
+    };
+    auto eight = [&](int j, float (&f)[8]) {
+      const uint4 w = *reinterpret_cast<const uint4*>(f16 + j);
+      const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        f[2 * e] = bf16lo(ws[e]);
+        f[2 * e + 1] = bf16hi(ws[e]);
+      }
+    };
     if (choose) {
-      const float square = __uint_as_float(norm_q[x]), norm = __uint_as_float(norm_m);
-      float lo = from_key(key_lo[x]), hi = from_key(key_hi[x]);
-      bool exact = !(square < INFINITY) || !(norm < INFINITY) || square < kTinySquare || norm < kTinySquare;
+      // the row's scores into LDS; their ends, and the largest norm of the means
+      const uint16_t* src = s.scores + (((int64_t)xt * a.H + h) * a.tokens + x) * s.stride;
+      float lo = INFINITY, hi = -INFINITY, norm = 0.f;
+      bool odd = false;
+      for (int y = lane; y < s.parts; y += kWave) norm = fmaxf(norm, s.norms[((int64_t)xt * a.H + h) * s.parts + y]);
+      for (int j = 8 * lane; j < k1; j += 8 * kWave) {
+        const uint4 w = *reinterpret_cast<const uint4*>(src + j);
+        *reinterpret_cast<uint4*>(f16 + j) = w;
+        const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+        const int on = inside(j, k0, k1);
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+          const float f = (e & 1) ? bf16hi(ws[e >> 1]) : bf16lo(ws[e >> 1]);
+          if ((on >> e) & 1) {
+            lo = fminf(lo, f);
+            hi = fmaxf(hi, f);
+            odd = odd || !(fabsf(f) < INFINITY);
+          }
+        }
+      }
+      hi = wave_max(hi);
+      lo = -wave_max(-lo);
+      norm = wave_max(norm);
       int open = 0, in = 0;
+      // the row's query in fp64, on its way while the scores are looked at
+      double qsum[D / kWave];
+#pragma unroll
+      for (int y = 0; y < D / kWave; y++) qsum[y] = 0.0;
+      for (int g = 0; g < a.g; g++) {
+        const uint16_t* q = a.q + row * a.q_row + (int64_t)(h * a.g + g) * a.q_head + lane;
+#pragma unroll
+        for (int y = 0; y < D / kWave; y++) qsum[y] += (double)bf16_to_f32(q[y * kWave]);
+      }
+      float square = 0.f;
+#pragma unroll
+      for (int y = 0; y < D / kWave; y++) {
+        qsum[y] /= a.g;
+        square = fmaf((float)qsum[y], (float)qsum[y], square);
+      }
+#pragma unroll
+      for (int y = 1; y < kWave; y <<= 1) square += xor_shfl(square, y);
+      bool exact = __any(odd) || !(square < INFINITY) || !(norm < INFINITY) || square < kTinySquare || norm < kTinySquare;
+      wave_fence();
       if (!exact) {
         const float bound = 2.f * (kBound * sqrtf(square) * sqrtf(norm) + 0.00392f * fmaxf(fabsf(lo), fabsf(hi)));
         // narrow [lo, hi] down around the K-th largest
         int left = want;
         for (int level = 0; level < 4 && hi > lo; level++) {
-          const float scale = kBins / (hi - lo);
-          for (int b = lane; b < kBins; b += kWave) mine.hist[b] = 0;
+          const float scale = kBins / (hi - lo), base = -lo * scale;
+#pragma unroll
+          for (int b = 0; b < kBins; b += kWave) mine.hist[b + lane] = 0;
           wave_fence();
-          auto bin_of = [&](float f) { return min(max((int)((f - lo) * scale), 0), kBins - 1); };
-          for (int p = lane; 2 * p < k1; p += kWave) {
-            const uint32_t w = reinterpret_cast<const uint32_t*>(f16)[p];
-            const float f0 = bf16lo(w), f1 = bf16hi(w);
-            if (2 * p >= k0 && f0 >= lo && f0 <= hi) atomicAdd(&mine.hist[bin_of(f0)], 1u);
-            if (2 * p + 1 >= k0 && 2 * p + 1 < k1 && f1 >= lo && f1 <= hi) atomicAdd(&mine.hist[bin_of(f1)], 1u);
+          auto bin_of = [&](float f) { return min(max((int)fmaf(f, scale, base), 0), kBins - 1); };
+          for (int j = 8 * lane; j < k1; j += 8 * kWave) {
+            float f[8];
+            eight(j, f);
+            const int on = inside(j, k0, k1);
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+              if (((on >> e) & 1) && f[e] >= lo && f[e] <= hi) atomicAdd(&mine.hist[bin_of(f[e])], 1u);
           }
           wave_fence();
           // lane y: bins 255 - 4 y .. 252 - 4 y, from the top
@@ -317,72 +410,107 @@ __global__ __launch_bounds__(kThreads) void chunk_select_kernel(const ChunkArgs 
             if (lane >= y) upto += z;
           }
           const int src = __builtin_ctzll(__ballot(upto >= left) | (1ull << 63));
-          int before = upto - sum, bin = kBins - 1 - 4 * lane;
+          int before = upto - sum, down = 0;
 #pragma unroll
           for (int e = 0; e < 3; e++)
-            if (before + c[e] < left && bin == kBins - 1 - 4 * lane - e) {
+            if (down == e && before + c[e] < left) {
               before += c[e];
-              bin--;
+              down++;
             }
-          bin = __builtin_amdgcn_readlane(bin, src);
+          const int here = __builtin_amdgcn_readlane(down == 0 ? c[0] : down == 1 ? c[1] : down == 2 ? c[2] : c[3], src);
+          const int bin = __builtin_amdgcn_readlane(kBins - 1 - 4 * lane - down, src);
           before = __builtin_amdgcn_readlane(before, src);
-          const int here = (int)mine.hist[bin];
+          if (here <= kFewInBin) {
+            // the bin's ends, moved apart by more than the rounding of bin_of
+            const float width = (hi - lo) * (1.f / kBins), slack = (hi - lo) * (1.f / 65536.f) + fmaxf(fabsf(lo), fabsf(hi)) * (1.f / 1048576.f);
+            hi = fmaf((float)(bin + 1), width, lo) + slack;
+            lo = fmaf((float)bin, width, lo) - slack;
+            break;
+          }
           float top = -INFINITY, low = INFINITY;
-          for (int p = lane; 2 * p < k1; p += kWave) {
-            const uint32_t w = reinterpret_cast<const uint32_t*>(f16)[p];
-            const float f0 = bf16lo(w), f1 = bf16hi(w);
-            if (2 * p >= k0 && f0 >= lo && f0 <= hi && bin_of(f0) == bin) {
-              top = fmaxf(top, f0);
-              low = fminf(low, f0);
-            }
-            if (2 * p + 1 >= k0 && 2 * p + 1 < k1 && f1 >= lo && f1 <= hi && bin_of(f1) == bin) {
-              top = fmaxf(top, f1);
-              low = fminf(low, f1);
-            }
+          for (int j = 8 * lane; j < k1; j += 8 * kWave) {
+            float f[8];
+            eight(j, f);
+            const int on = inside(j, k0, k1);
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+              if (((on >> e) & 1) && f[e] >= lo && f[e] <= hi && bin_of(f[e]) == bin) {
+                top = fmaxf(top, f[e]);
+                low = fminf(low, f[e]);
+              }
           }
           hi = wave_max(top);
           lo = -wave_max(-low);
           left -= before;
-          if (here <= 16) break;
         }
         // in, out, or open
-        for (int j0 = 0; j0 < k1; j0 += kWave) {
-          const int j = j0 + lane;
-          const bool cand = j >= k0 && j < k1;
-          const float f = cand ? __uint_as_float((uint32_t)f16[j] << 16) : 0.f;
-          const bool yes = cand && f - bound > hi, no = f + bound < lo;
-          const bool ask = cand && !yes && !no;
-          int n;
-          const int at = open + wave_excl_count(ask, &n);
-          if (ask && at < kMostOpen) mine.id[at] = (uint16_t)j;
-          if (cand) f16[j] = yes ? 1 : 0;
-          open += n;
-          in += __popcll(__ballot(yes));
+        for (int j0 = 0; j0 < k1; j0 += 8 * kWave) {
+          const int j = j0 + 8 * lane;
+          int yes = 0, ask = 0;
+          if (j < k1) {
+            float f[8];
+            eight(j, f);
+            const int on = inside(j, k0, k1);
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+              yes |= (f[e] - bound > hi) << e;
+              ask |= (!(f[e] + bound < lo)) << e;
+            }
+            yes &= on;
+            ask &= on & ~yes;
+            // flags in the scores' place: 1 is in
+            *reinterpret_cast<uint4*>(f16 + j) = make_uint4((yes & 1) | (yes & 2) << 15, (yes >> 2 & 1) | (yes >> 2 & 2) << 15,
+                                                            (yes >> 4 & 1) | (yes >> 4 & 2) << 15, (yes >> 6 & 1) | (yes >> 6 & 2) << 15);
+          }
+          in += __popc(yes);
+          if (__any(ask)) {
+            const int c = __popc(ask);
+            int at = c;
+#pragma unroll
+            for (int y = 1; y < kWave; y <<= 1) {
+              const int z = __shfl_up(at, y, kWave);
+              if (lane >= y) at += z;
+            }
+            const int n = __builtin_amdgcn_readlane(at, kWave - 1);
+            at += open - c;
+            for (int m = ask; m; m &= m - 1, at++)
+              if (at < kMostOpen) mine.id[at] = (uint16_t)(j + __builtin_ctz(m));
+            open += n;
+          }
         }
+        in = wave_sum(in);
         exact = open > kMostOpen;
       }
       wave_fence();
-      // the row's query in fp64
-      for (int c = lane; c < D; c += kWave) {
-        double sum = 0.0;
-        for (int g = 0; g < a.g; g++)
-          sum += (double)bf16_to_f32(a.q[row * a.q_row + (int64_t)(h * a.g + g) * a.q_head + c]);
-        mine.qbar[c] = sum / a.g;
-      }
+#pragma unroll
+      for (int y = 0; y < D / kWave; y++) mine.qbar[y * kWave + lane] = qsum[y];
       wave_fence();
       if (exact) {
         select_by_digits<D>(a, s, t, h, k0, k1, want, mine.qbar, f16);
       } else {
-        for (int u = 0; u < open; u += 8) {
-          const int y = u + (lane >> 3);
-          const uint32_t k = exact_keys<D>(a, s, t, h, y < open ? (int)mine.id[y] : -1, mine.qbar);
-          if (y < open && (lane & 7) == 0) mine.key[y] = k;
+        for (int u = 0; u < open; u += 8 * kTogether) {
+          int row8[kTogether];
+#pragma unroll
+          for (int z = 0; z < kTogether; z++) {
+            const int y = u + 8 * z + (lane >> 3);
+            row8[z] = y < open ? (int)block_row(t.pages, (int)mine.id[y], s.r, a.num_phys) : -1;
+          }
+          uint32_t k[kTogether];
+          exact_keys<D, kTogether>(a, s, h, row8, mine.qbar, k);
+#pragma unroll
+          for (int z = 0; z < kTogether; z++) {
+            const int y = u + 8 * z + (lane >> 3);
+            if (y < open && (lane & 7) == 0) mine.key[y] = k[z];
+          }
         }
         wave_fence();
         for (int u = lane; u < open; u += kWave) {       // ids ascend: of equal scores the earlier entry
           const uint32_t k = mine.key[u];
           int rank = 0;
-          for (int y = 0; y < open; y++) rank += mine.key[y] > k || (mine.key[y] == k && y < u);
+          for (int y = 0; y < open; y++) {
+            const uint32_t o = mine.key[y];
+            rank += o > k || (o == k && y < u);
+          }
           if (rank < want - in) f16[mine.id[u]] = 1;
         }
       }
@@ -391,13 +519,29 @@ __global__ __launch_bounds__(kThreads) void chunk_select_kernel(const ChunkArgs 
     // the list, ascending
     int32_t* sel = s.sel_pages + (row * a.H + h) * a.max_sel;
     int at = 0;
-    for (int j0 = 0; j0 < nb; j0 += kWave) {
-      const int j = j0 + lane;
-      const bool must = j < s.n_sink || j >= nb - s.n_local;
-      const bool take = j < nb && (must || want == k1 - k0 || (choose && f16[j] == 1));
-      int n;
-      const int place = at + wave_excl_count(take, &n);
-      if (take && place < a.max_sel) sel[place] = j;
+    const bool every = want == k1 - k0;
+    for (int j0 = 0; j0 < nb; j0 += 8 * kWave) {
+      const int j = j0 + 8 * lane, real = inside(j, 0, nb);
+      int take = every ? real : real & ~inside(j, s.n_sink, nb - s.n_local);
+      if (choose && j < k1) {
+        const uint4 w = *reinterpret_cast<const uint4*>(f16 + j);
+        const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+        int flags = 0;
+#pragma unroll
+        for (int e = 0; e < 4; e++) flags |= (int)((ws[e] & 1) | (ws[e] >> 15 & 2)) << (2 * e);
+        take |= flags & inside(j, k0, k1);
+      }
+      const int c = __popc(take);
+      int place = c;
+#pragma unroll
+      for (int y = 1; y < kWave; y <<= 1) {
+        const int z = __shfl_up(place, y, kWave);
+        if (lane >= y) place += z;
+      }
+      const int n = __builtin_amdgcn_readlane(place, kWave - 1);
+      place += at - c;
+      for (int m = take; m; m &= m - 1, place++)
+        if (place < a.max_sel) sel[place] = j + __builtin_ctz(m);
       at += n;
     }
     for (int y = at + lane; y < a.max_sel; y += kWave) sel[y] = -1;
@@ -405,25 +549,54 @@ __global__ __launch_bounds__(kThreads) void chunk_select_kernel(const ChunkArgs 
   }
 }
 
+// Tokens of a tile, and what the workspace holds of a launch.
+struct SelectPlan {
+  int tokens, stride, part, parts;
+  int64_t tiles;                           // of all rows (an upper bound)
+  int at_once;                             // of a launch
+  size_t scores, bytes;
+};
+SelectPlan plan_of(const Geometry& g, int n) {
+  SelectPlan p{};
+  const int64_t batch = std::max(g.batch, 1);
+  p.tokens = (int64_t)n <= 16 * batch ? 16 : 64;
+  p.tiles = (int64_t)n / p.tokens + batch;
+  p.stride = (g.max_pages + 63) & ~63;
+  const size_t tile = (size_t)p.tokens * g.H * p.stride * sizeof(uint16_t);
+  p.at_once = (int)std::max<int64_t>(1, std::min<int64_t>(p.tiles, (int64_t)(kScoreBytes / tile)));
+  // parts of at least a unit a wave
+  const int64_t work = std::max<int64_t>(1, std::min<int64_t>(p.at_once, std::max<int64_t>(batch, (n + p.tokens - 1) / p.tokens)) * g.H);
+  const int least = kUnit * kWaves, most = (p.stride + least - 1) / least;
+  const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(most, kScoreWgs / work));
+  p.part = ((p.stride + parts - 1) / parts + least - 1) / least * least;
+  p.parts = (p.stride + p.part - 1) / p.part;
+  p.scores = (tile * p.at_once + 255) / 256 * 256;
+  p.bytes = p.scores + sizeof(float) * (size_t)p.at_once * g.H * p.parts;
+  return p;
+}
+
 template <int D>
-hipError_t launch(ChunkArgs& a, SelectArgs& s, hipStream_t stream) {
-  // tokens of a workgroup: as many as leave their scores room in LDS.  Rows are 16 bytes past a multiple of 64, so
-  // that the 16 tokens of a store spread over the banks.
-  s.stride = ((a.max_blocks + 31) & ~31) + 8;
-  int tokens = 32;
-  while (tokens > 4 && (size_t)tokens * s.stride * sizeof(uint16_t) > 136 * 1024) tokens /= 2;
-  a.tokens = tokens;
-  const int64_t tiles = (int64_t)a.num_rows / tokens + a.batch;
-  const dim3 grid((unsigned)(tiles * a.H));
-  const size_t lds = sizeof(uint16_t) * (size_t)tokens * s.stride;
-  if (tokens == 32) hipLaunchKernelGGL((chunk_select_kernel<D, 2>), grid, dim3(kThreads), lds, stream, a, s);
-  else hipLaunchKernelGGL((chunk_select_kernel<D, 1>), grid, dim3(kThreads), lds, stream, a, s);
-  return hipGetLastError();
+hipError_t launch(const ChunkArgs& a, SelectArgs& s, const SelectPlan& p, hipStream_t stream) {
+  const size_t lds = sizeof(uint16_t) * (size_t)kWaves * s.stride;
+  const int groups = (p.tokens + kWaves - 1) / kWaves;
+  for (int64_t x = 0; x < p.tiles; x += p.at_once) {
+    const unsigned tiles = (unsigned)std::min<int64_t>(p.at_once, p.tiles - x);
+    s.tile0 = (int)x;
+    const dim3 grid(tiles * a.H, (unsigned)p.parts);
+    if (p.tokens == 64) hipLaunchKernelGGL((chunk_score_kernel<D, 4>), grid, dim3(kThreads), 0, stream, a, s);
+    else hipLaunchKernelGGL((chunk_score_kernel<D, 1>), grid, dim3(kThreads), 0, stream, a, s);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((chunk_choose_kernel<D>), dim3(tiles * groups * a.H), dim3(kThreads), lds, stream, a, s);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace
 
-size_t chunk_select_workspace(const Geometry& g, int n, int Hq) { return 16; }
+size_t chunk_select_workspace(const Geometry& g, int n, int Hq) { return plan_of(g, n).bytes; }
 
 hipError_t launch_chunk_select(const Geometry& g, const ChunkRows& rows, const float* mean, const int32_t* budget,
                                int n_sink, int n_local, int max_sel, int32_t* sel_pages, int32_t* sel_count, void* ws,
@@ -451,8 +624,11 @@ hipError_t launch_chunk_select(const Geometry& g, const ChunkRows& rows, const f
   a.bs_shift = __builtin_ctz((unsigned)g.bs);
   a.max_sel = max_sel;
   a.max_blocks = g.max_pages;
-  SelectArgs s{mean, budget, n_sink, n_local, g.r, 0, sel_pages, sel_count};
-  return g.Dqk == 128 ? launch<128>(a, s, stream) : launch<64>(a, s, stream);
+  const SelectPlan p = plan_of(g, rows.n);
+  a.tokens = p.tokens;
+  SelectArgs s{mean, budget, n_sink, n_local, g.r, sel_pages, sel_count, static_cast<uint16_t*>(ws),
+               reinterpret_cast<float*>(static_cast<char*>(ws) + p.scores), p.stride, p.part, p.parts, 0};
+  return g.Dqk == 128 ? launch<128>(a, s, p, stream) : launch<64>(a, s, p, stream);
 }
 
 }  // namespace vx
