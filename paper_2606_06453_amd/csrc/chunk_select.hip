@@ -76,21 +76,30 @@ struct WaveLds {
     uint32_t hist[kBins];
     double qbar[128];
   };
-  uint32_t key[kMostOpen];
+  __attribute__((aligned(16))) uint32_t key[kMostOpen];
   uint16_t id[kMostOpen];
 };
 
 // LDS of a wave is written and read in order; the compiler keeps the order too.
 __device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
+// Over the wave, in registers (row_ror within 16 lanes, then swaps of 16 and 32): a row takes a dozen of these one
+// after the other, and each through LDS costs six of its round trips.
 __device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int s = 1; s < kWave; s <<= 1) x = fmaxf(x, xor_shfl(x, s));
-  return x;
+  x = fmaxf(x, dpp_f32<0x128>(x));
+  x = fmaxf(x, dpp_f32<0x124>(x));
+  x = fmaxf(x, dpp_f32<0x122>(x));
+  x = fmaxf(x, dpp_f32<0x121>(x));
+  return column_max(x);
 }
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-  for (int s = 1; s < kWave; s <<= 1) x += __shfl_xor(x, s, kWave);
+// Sum over this lane and those below it: row_shr 1, 2, 4, 8, then the sums of the rows before (row_bcast 15 and 31).
+__device__ __forceinline__ int wave_prefix(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
   return x;
 }
 
@@ -337,6 +346,22 @@ __global__ __launch_bounds__(kThreads) void chunk_choose_kernel(const ChunkArgs 
       }
     };
     if (choose) {
+      // the row's query in fp64
+      double qsum[D / kWave];
+#pragma unroll
+      for (int y = 0; y < D / kWave; y++) qsum[y] = 0.0;
+      for (int g = 0; g < a.g; g += 4) {
+        uint16_t q[4][D / kWave];
+#pragma unroll
+        for (int z = 0; z < 4; z++)
+#pragma unroll
+          for (int y = 0; y < D / kWave; y++)
+            q[z][y] = a.q[row * a.q_row + (int64_t)(h * a.g + min(g + z, a.g - 1)) * a.q_head + y * kWave + lane];
+#pragma unroll
+        for (int z = 0; z < 4; z++)
+#pragma unroll
+          for (int y = 0; y < D / kWave; y++) qsum[y] += g + z < a.g ? (double)bf16_to_f32(q[z][y]) : 0.0;
+      }
       // the row's scores into LDS; their ends, and the largest norm of the means
       const uint16_t* src = s.scores + (((int64_t)xt * a.H + h) * a.tokens + x) * s.stride;
       float lo = INFINITY, hi = -INFINITY, norm = 0.f;
@@ -350,35 +375,24 @@ __global__ __launch_bounds__(kThreads) void chunk_choose_kernel(const ChunkArgs 
 #pragma unroll
         for (int e = 0; e < 8; e++) {
           const float f = (e & 1) ? bf16hi(ws[e >> 1]) : bf16lo(ws[e >> 1]);
-          if ((on >> e) & 1) {
-            lo = fminf(lo, f);
-            hi = fmaxf(hi, f);
-            odd = odd || !(fabsf(f) < INFINITY);
-          }
+          const bool mine_ = (on >> e) & 1;
+          odd = odd || (mine_ && f != f);
+          lo = fminf(lo, mine_ ? f : INFINITY);
+          hi = fmaxf(hi, mine_ ? f : -INFINITY);
         }
       }
       hi = wave_max(hi);
       lo = -wave_max(-lo);
       norm = wave_max(norm);
       int open = 0, in = 0;
-      // the row's query in fp64, on its way while the scores are looked at
-      double qsum[D / kWave];
-#pragma unroll
-      for (int y = 0; y < D / kWave; y++) qsum[y] = 0.0;
-      for (int g = 0; g < a.g; g++) {
-        const uint16_t* q = a.q + row * a.q_row + (int64_t)(h * a.g + g) * a.q_head + lane;
-#pragma unroll
-        for (int y = 0; y < D / kWave; y++) qsum[y] += (double)bf16_to_f32(q[y * kWave]);
-      }
       float square = 0.f;
 #pragma unroll
       for (int y = 0; y < D / kWave; y++) {
         qsum[y] /= a.g;
         square = fmaf((float)qsum[y], (float)qsum[y], square);
       }
-#pragma unroll
-      for (int y = 1; y < kWave; y <<= 1) square += xor_shfl(square, y);
-      bool exact = __any(odd) || !(square < INFINITY) || !(norm < INFINITY) || square < kTinySquare || norm < kTinySquare;
+      square = column_sum(row16_sum_f32(square));
+      bool exact = __any(odd) || !(fmaxf(fabsf(lo), fabsf(hi)) < INFINITY) || !(square < INFINITY) || !(norm < INFINITY) || square < kTinySquare || norm < kTinySquare;
       wave_fence();
       if (!exact) {
         const float bound = 2.f * (kBound * sqrtf(square) * sqrtf(norm) + 0.00392f * fmaxf(fabsf(lo), fabsf(hi)));
@@ -394,6 +408,11 @@ __global__ __launch_bounds__(kThreads) void chunk_choose_kernel(const ChunkArgs 
             float f[8];
             eight(j, f);
             const int on = inside(j, k0, k1);
+            if (level == 0 && __all(on == 255)) {        // lo and hi are the row's ends
+#pragma unroll
+              for (int e = 0; e < 8; e++) atomicAdd(&mine.hist[bin_of(f[e])], 1u);
+              continue;
+            }
 #pragma unroll
             for (int e = 0; e < 8; e++)
               if (((on >> e) & 1) && f[e] >= lo && f[e] <= hi) atomicAdd(&mine.hist[bin_of(f[e])], 1u);
@@ -403,12 +422,7 @@ __global__ __launch_bounds__(kThreads) void chunk_choose_kernel(const ChunkArgs 
           int c[4], sum = 0;
 #pragma unroll
           for (int e = 0; e < 4; e++) sum += c[e] = (int)mine.hist[kBins - 1 - 4 * lane - e];
-          int upto = sum;
-#pragma unroll
-          for (int y = 1; y < kWave; y <<= 1) {
-            const int z = __shfl_up(upto, y, kWave);
-            if (lane >= y) upto += z;
-          }
+          const int upto = wave_prefix(sum);
           const int src = __builtin_ctzll(__ballot(upto >= left) | (1ull << 63));
           int before = upto - sum, down = 0;
 #pragma unroll
@@ -465,12 +479,7 @@ __global__ __launch_bounds__(kThreads) void chunk_choose_kernel(const ChunkArgs 
           in += __popc(yes);
           if (__any(ask)) {
             const int c = __popc(ask);
-            int at = c;
-#pragma unroll
-            for (int y = 1; y < kWave; y <<= 1) {
-              const int z = __shfl_up(at, y, kWave);
-              if (lane >= y) at += z;
-            }
+            int at = wave_prefix(c);
             const int n = __builtin_amdgcn_readlane(at, kWave - 1);
             at += open - c;
             for (int m = ask; m; m &= m - 1, at++)
@@ -478,7 +487,7 @@ __global__ __launch_bounds__(kThreads) void chunk_choose_kernel(const ChunkArgs 
             open += n;
           }
         }
-        in = wave_sum(in);
+        in = __builtin_amdgcn_readlane(wave_prefix(in), kWave - 1);
         exact = open > kMostOpen;
       }
       wave_fence();
@@ -507,9 +516,11 @@ __global__ __launch_bounds__(kThreads) void chunk_choose_kernel(const ChunkArgs 
         for (int u = lane; u < open; u += kWave) {       // ids ascend: of equal scores the earlier entry
           const uint32_t k = mine.key[u];
           int rank = 0;
-          for (int y = 0; y < open; y++) {
-            const uint32_t o = mine.key[y];
-            rank += o > k || (o == k && y < u);
+          for (int y = 0; y < open; y += 4) {            // entries behind the last one count for none
+            const uint4 o = *reinterpret_cast<const uint4*>(&mine.key[y]);
+            const uint32_t os[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+            for (int z = 0; z < 4; z++) rank += y + z < open && (os[z] > k || (os[z] == k && y + z < u));
           }
           if (rank < want - in) f16[mine.id[u]] = 1;
         }
@@ -532,12 +543,7 @@ __global__ __launch_bounds__(kThreads) void chunk_choose_kernel(const ChunkArgs 
         take |= flags & inside(j, k0, k1);
       }
       const int c = __popc(take);
-      int place = c;
-#pragma unroll
-      for (int y = 1; y < kWave; y <<= 1) {
-        const int z = __shfl_up(place, y, kWave);
-        if (lane >= y) place += z;
-      }
+      int place = wave_prefix(c);
       const int n = __builtin_amdgcn_readlane(place, kWave - 1);
       place += at - c;
       for (int m = take; m; m &= m - 1, place++)
