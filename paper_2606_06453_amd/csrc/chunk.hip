@@ -281,9 +281,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 
 // Four waves of 16 RT rows each share the tokens of their tile through LDS (chunk_wide.h).  A wave passes over
 // runs that none of its rows attends.
+// Tokens of a buffer.  Listed blocks are short runs in any place, which take longest to arrive: half the tokens let
+// twice the workgroups wait side by side (4096 tokens over 128 blocks each 1069 -> 923 us; dense prompts are 1% slower
+// with them).  The latent's rows are 4.5 times longer.
+template <int D, int DV, bool SPARSE>
+constexpr int kTokens = SPARSE || D != DV ? 32 : 64;
+
 template <int D, int DV, int KT, int RT, bool SPARSE>
 __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int h, int split, uint32_t* lds) {
-  using G = Wide<D, DV, KT>;
+  constexpr int TK = kTokens<D, DV, SPARSE>;
+  using G = Wide<D, DV, KT, TK>;
   constexpr int KS = D / 32, NJ = DV / 16;
   const int tid = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, grp = lane >> 4;
@@ -299,62 +306,82 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
   // the tile tokens of this wave's rows, and what they attend between them
   const int x0 = min(r0 / a.g, t.n), x1 = min((r0 + 16 * RT - 1) / a.g, t.n - 1);
   const int wave_from = first_key(a, t.p0 + x0), wave_to = r0 < rows ? end_key(a, t, t.p0 + x1) : 0;
-  const int wave_mask = r0 < rows ? (2 << (x1 & 15)) - (1 << (x0 & 15)) : 0;
+  const int wave_mask = r0 >= rows ? 0 : SPARSE ? (2 << x1) - (1 << x0) : 0xffff;
 
   const int n16 = (runs.hi - runs.lo) << shift16, steps = (n16 + G::UNITS - 1) / G::UNITS;
-  auto run_at = [&](int x, int& mask) {                  // first token of run x of the part
-    const int e = runs.lo + (x >> shift16);
-    int id = e;
-    mask = 0xffff;
-    if constexpr (SPARSE) {
-      id = runs.ids[e];
-      mask = runs.masks[id];
-    }
-    return (id << runs.shift) + 16 * (x & ((1 << shift16) - 1));
+  // The runs that a lane looks up for all (listed blocks), or for its wave (a range): first token, page, and the tile
+  // tokens that list it.  Listed: lane u holds run 64 w + u, the next 64 are on their way meanwhile.  A range: lane u
+  // holds the run that this wave loads in step 64 w + u.
+  struct Found {
+    int tok, page, mask;
   };
-  // this wave's runs of the next 64 steps, a lane each: page, and first token
   const int unit = wave / G::WPU;
-  int my_page = 0, my_tok = 0;
-  auto look_up = [&](int s0) {
-    const int x = min(G::UNITS * (s0 + lane) + unit, n16 - 1);           // past the end: the last run again
-    int mask;
-    if (x >= 0) {
-      my_tok = run_at(x, mask);
-      my_page = (int)clamp_page(t.pages[my_tok >> a.ps_shift], a.num_phys);
+  auto look_up = [&](int w) {
+    Found f{0, 0, 0};
+    const int x = SPARSE ? 64 * w + lane : G::UNITS * (64 * w + lane) + unit, y = min(x, n16 - 1);
+    if (y >= 0) {                                        // past the end: the last run again, for no row
+      const int e = runs.lo + (y >> shift16);
+      int id = e;
+      if constexpr (SPARSE) {
+        id = runs.ids[e];
+        f.mask = x < n16 ? runs.masks[id] : 0;
+      }
+      f.tok = (id << runs.shift) + 16 * (y & ((1 << shift16) - 1));
+      f.page = (int)clamp_page(t.pages[f.tok >> a.ps_shift], a.num_phys);
     }
+    return f;
   };
-  Travel<D, DV, KT> travel;
+  Found now = look_up(0), after = now;
+  if constexpr (SPARSE) after = look_up(1);
+  Travel<D, DV, KT, TK> travel;
+  // runs of the step that is on its way: first tokens and masks
+  int toks[G::UNITS], masks[G::UNITS], mine = 0;
   auto send = [&](int s) {
-    if ((s & 63) == 0) look_up(s);
-    const int page = __builtin_amdgcn_readlane(my_page, s & 63), tok = __builtin_amdgcn_readlane(my_tok, s & 63);
+    int page;
+    if constexpr (SPARSE) {
+      const int at = G::UNITS * s & 63;
+      if (at == 0 && s > 0) {
+        now = after;
+        after = look_up(G::UNITS * s / 64 + 1);
+      }
+#pragma unroll
+      for (int u = 0; u < G::UNITS; u++) {
+        toks[u] = __builtin_amdgcn_readlane(now.tok, at + u);
+        masks[u] = __builtin_amdgcn_readlane(now.mask, at + u);
+      }
+      page = __builtin_amdgcn_readlane(now.page, at + unit);
+      mine = __builtin_amdgcn_readlane(now.tok, at + unit);
+    } else {
+      if ((s & 63) == 0 && s > 0) now = look_up(s / 64);
+      page = __builtin_amdgcn_readlane(now.page, s & 63);
+      mine = __builtin_amdgcn_readlane(now.tok, s & 63);
+#pragma unroll
+      for (int u = 0; u < G::UNITS; u++) {
+        const int x = G::UNITS * s + u;
+        toks[u] = (runs.lo + min(x, n16 - 1)) << 4;
+        masks[u] = x < n16 ? 0xffff : 0;
+      }
+    }
     const uint8_t* ks = slice_of<D, KT>(a, a.k, page, h);
-    send_run<D, DV, KT>(a, ks, G::kAlias ? ks : slice_of<D, KT>(a, a.v, page, h), tok & (a.ps - 1), last - tok, wave, lane,
-                        bufs + (s & 1) * G::BUF, travel);
+    send_run<D, DV, KT, TK>(a, ks, G::kAlias ? ks : slice_of<D, KT>(a, a.v, page, h), mine & (a.ps - 1), last - mine, wave, lane,
+                            bufs + (s & 1) * G::BUF, travel);
   };
-  int tok_sent = 0;                                      // of the run on its way
-  if (steps > 0) {
-    send(0);
-    tok_sent = __builtin_amdgcn_readlane(my_tok, 0);
-  }
+  if (steps > 0) send(0);
   for (int s = 0; s < steps; s++) {
     uint8_t* buf = bufs + (s & 1) * G::BUF;
-    land_run<D, DV, KT>(wave, lane, last - tok_sent, buf, travel);
+    land_run<D, DV, KT, TK>(wave, lane, last - mine, buf, travel);
     lds_barrier();                                       // every wave's part is there, and the other buffer is free
-    if (s + 1 < steps) {
-      send(s + 1);
-      tok_sent = __builtin_amdgcn_readlane(my_tok, (s + 1) & 63);
+    int tok[G::UNITS], mask[G::UNITS];
+#pragma unroll
+    for (int u = 0; u < G::UNITS; u++) {
+      tok[u] = toks[u];
+      mask[u] = masks[u];
     }
+    if (s + 1 < steps) send(s + 1);
     const uint8_t* vt = G::kAlias ? buf : buf + G::TILE;
 #pragma unroll
     for (int y = 0; y < G::UNITS; y += 2) {
-      const int x = G::UNITS * s + y;
-      int mask0 = 0, mask1 = 0, tok0 = 0, tok1 = 0;
-      if (x < n16) {
-        tok0 = __builtin_amdgcn_readfirstlane(run_at(x, mask0));
-        tok1 = __builtin_amdgcn_readfirstlane(run_at(min(x + 1, n16 - 1), mask1));
-        mask0 = __builtin_amdgcn_readfirstlane(mask0);
-        mask1 = x + 1 < n16 ? __builtin_amdgcn_readfirstlane(mask1) : 0;
-      }
+      const int tok0 = tok[y], tok1 = tok[y + 1], mask0 = mask[y], mask1 = mask[y + 1];
       if (((mask0 | mask1) & wave_mask) != 0 && min(tok0, tok1) < wave_to && max(tok0, tok1) + 16 > wave_from) {
         const bool whole = min(tok0, tok1) >= w.all_from && max(tok0, tok1) + 16 <= w.all_to && (mask0 & mask1) == 0xffff;
         f32x4_t sc[RT][2];
@@ -536,7 +563,7 @@ void launch_narrow(const ChunkArgs& a, dim3 grid, size_t lists, hipStream_t stre
 }
 template <int D, int DV, int KT, int RT, bool SPARSE>
 void launch_wide(const ChunkArgs& a, dim3 grid, size_t lists, hipStream_t stream) {
-  const size_t lds = 2 * (size_t)Wide<D, DV, KT>::BUF + lists;
+  const size_t lds = 2 * (size_t)Wide<D, DV, KT, kTokens<D, DV, SPARSE>>::BUF + lists;
   hipLaunchKernelGGL((chunk_wide_kernel<D, DV, KT, RT, SPARSE>), grid, dim3(kThreads), lds, stream, a);
 }
 

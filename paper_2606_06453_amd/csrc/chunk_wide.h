@@ -1,5 +1,5 @@
-// The wide tile kernel: four waves of 16 RT query rows each share every 64 (latent: 32) tokens of K and V
-// in LDS.
+// The wide tile kernel: four waves of 16 RT query rows each share every 64 (listed blocks, latent: 32) tokens of K and
+// V in LDS.
 //
 // LDS holds bf16 rows of 16-byte chunks.  bf16 rows go there straight from memory (each lane of a load picks
 // its source, so the swizzle costs nothing), other types pass through registers, where they are widened.
@@ -43,10 +43,10 @@ __device__ __forceinline__ int swizzle(int token) {
   else return (((token >> 1) & 3) << 1) | ((token >> 3) & 1);
 }
 
-template <int D, int DV, int KT>
+template <int D, int DV, int KT, int TOKENS>
 struct Wide {
   static constexpr bool kAlias = D != DV;
-  static constexpr int TK = kAlias ? 32 : 64;            // tokens of a buffer
+  static constexpr int TK = TOKENS;                      // tokens of a buffer
   static constexpr int UNITS = TK / 16;                  // runs of 16 tokens
   static constexpr int CH = D / 8;                       // chunks of a row
   static constexpr int WPU = 4 / UNITS;                  // waves that load a run
@@ -56,9 +56,9 @@ struct Wide {
 };
 
 // Element chunk of lane `lane` in piece k of the wave's part of a run: token and logical chunk.
-template <int D, int DV, int KT>
+template <int D, int DV, int KT, int TOKENS>
 __device__ __forceinline__ void piece(int wave, int k, int lane, int& token, int& c) {
-  using G = Wide<D, DV, KT>;
+  using G = Wide<D, DV, KT, TOKENS>;
   const int slot = 64 * ((wave % G::WPU) * G::NI + k) + lane;
   token = slot / G::CH;
   c = (slot % G::CH) ^ swizzle<D>(token);
@@ -66,19 +66,22 @@ __device__ __forceinline__ void piece(int wave, int k, int lane, int& token, int
 
 // A wave's part of a run on its way through registers: fp8, 16 codes a lane and piece; mxfp4, a lane's D / 4 codes of
 // one K row and the codes of D / 16 channels of four V rows, and their scales.
-template <int D, int DV, int KT>
+template <int D, int DV, int KT, int TOKENS>
 struct Travel {
   static constexpr bool kMx = KT == kKvMxFp4;
-  static constexpr int N = kMx ? 1 : (D + 64 * Wide<D, DV, KT>::WPU - 1) / (64 * Wide<D, DV, KT>::WPU);
+  static constexpr int N = kMx ? 1 : (D + 64 * Wide<D, DV, KT, TOKENS>::WPU - 1) / (64 * Wide<D, DV, KT, TOKENS>::WPU);
   static constexpr int W = kMx ? D / 32 : 4;
-  uint32_t k[N][W], v[Wide<D, DV, KT>::kAlias ? 1 : N][W], k_scale, v_scale;
+  // mxfp4: of two waves that load a run one takes K, the other V
+  static __device__ __forceinline__ bool takes_k(int wave) { return Wide<D, DV, KT, TOKENS>::WPU == 1 || (wave & 1) == 0; }
+  static __device__ __forceinline__ bool takes_v(int wave) { return Wide<D, DV, KT, TOKENS>::WPU == 1 || (wave & 1) == 1; }
+  uint32_t k[N][W], v[Wide<D, DV, KT, TOKENS>::kAlias ? 1 : N][W], k_scale, v_scale;
 };
 
 // fp8: lane's piece x of a run, token and 16 channels; false past the run.
-template <int D, int DV, int KT>
+template <int D, int DV, int KT, int TOKENS>
 __device__ __forceinline__ bool codes_piece(int wave, int x, int lane, int& token, int& c16) {
-  using G = Wide<D, DV, KT>;
-  const int slot = 64 * ((wave % G::WPU) * Travel<D, DV, KT>::N + x) + lane;
+  using G = Wide<D, DV, KT, TOKENS>;
+  const int slot = 64 * ((wave % G::WPU) * Travel<D, DV, KT, TOKENS>::N + x) + lane;
   token = slot / (D / 16);
   c16 = slot % (D / 16);
   return slot < D;
@@ -86,35 +89,39 @@ __device__ __forceinline__ bool codes_piece(int wave, int x, int lane, int& toke
 
 // Starts a run's way into the buffer (bf16), or into registers.  t: its first token's place in the page; left: its
 // tokens before the last one that any row attends (other types: what lies behind arrives as zeros).
-template <int D, int DV, int KT>
+template <int D, int DV, int KT, int TOKENS>
 __device__ __forceinline__ void send_run(const ChunkArgs& a, const uint8_t* ks, const uint8_t* vs, int t, int left, int wave,
-                                         int lane, uint8_t* buf, Travel<D, DV, KT>& r) {
-  using G = Wide<D, DV, KT>;
-  using T = Travel<D, DV, KT>;
+                                         int lane, uint8_t* buf, Travel<D, DV, KT, TOKENS>& r) {
+  using G = Wide<D, DV, KT, TOKENS>;
+  using T = Travel<D, DV, KT, TOKENS>;
   if constexpr (KT == kKvBf16) {
     const uint32_t dst = lds_address(buf) + (wave / G::WPU) * 16 * D * 2;
 #pragma unroll
     for (int k = 0; k < G::NI; k++) {
       int token, c;
-      piece<D, DV, KT>(wave, k, lane, token, c);
+      piece<D, DV, KT, TOKENS>(wave, k, lane, token, c);
       const uint32_t to = dst + 1024 * ((wave % G::WPU) * G::NI + k), at = 2 * (token * D + 8 * c);
       send16(ks + 2 * t * D, at, to);
       if constexpr (!G::kAlias) send16(vs + 2 * t * D, at, to + G::TILE);
     }
   } else if constexpr (T::kMx) {
     const int col = lane & 15, grp = lane >> 4;
-    load_words<T::W>(rows_of<D, KT>(a, ks, t, 16), lane * (D / 8), r.k[0]);
-    r.k_scale = __builtin_amdgcn_raw_buffer_load_b8(scales_of<D>(a, ks, t), (lane >> 2) * (D / 32) + (lane & 3) * D / 128, 0, 0);
-    load_words<T::W>(rows_of<D, KT>(a, vs, t, 16), lane * (D / 8), r.v[0]);
-    r.v_scale = __builtin_amdgcn_raw_buffer_load_b32(scales_of<D>(a, vs, t), (grp * (D / 32) + col * (D / 16) / 32) * 4, 0, 0);
-    const int n = left - 4 * grp;                        // byte x: token 4 grp + x; a scale of 0 is 2^-127
-    r.v_scale &= n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1;
+    if (T::takes_k(wave)) {
+      load_words<T::W>(rows_of<D, KT>(a, ks, t, 16), lane * (D / 8), r.k[0]);
+      r.k_scale = __builtin_amdgcn_raw_buffer_load_b8(scales_of<D>(a, ks, t), (lane >> 2) * (D / 32) + (lane & 3) * D / 128, 0, 0);
+    }
+    if (T::takes_v(wave)) {
+      load_words<T::W>(rows_of<D, KT>(a, vs, t, 16), lane * (D / 8), r.v[0]);
+      r.v_scale = __builtin_amdgcn_raw_buffer_load_b32(scales_of<D>(a, vs, t), (grp * (D / 32) + col * (D / 16) / 32) * 4, 0, 0);
+      const int n = left - 4 * grp;                      // byte x: token 4 grp + x; a scale of 0 is 2^-127
+      r.v_scale &= n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1;
+    }
   } else {
     const int n = min(left, 16);
 #pragma unroll
     for (int x = 0; x < T::N; x++) {
       int token, c16;
-      codes_piece<D, DV, KT>(wave, x, lane, token, c16);
+      codes_piece<D, DV, KT, TOKENS>(wave, x, lane, token, c16);
       const int off = token * D + 16 * c16;              // past the run it is past the resource too
       load_words<4>(rows_of<D, KT>(a, ks, t, n), off, r.k[x]);
       if constexpr (!G::kAlias) load_words<4>(rows_of<D, KT>(a, vs, t, n), off, r.v[x]);
@@ -137,44 +144,46 @@ __device__ __forceinline__ uint4 widen_mx(uint32_t w, float s) {
 
 // Ends it: widened rows into the buffer; of bf16 rows, those of V behind the last token that any row attends (which may
 // hold anything) are set to zero.
-template <int D, int DV, int KT>
-__device__ __forceinline__ void land_run(int wave, int lane, int left, uint8_t* buf, const Travel<D, DV, KT>& r) {
-  using G = Wide<D, DV, KT>;
-  using T = Travel<D, DV, KT>;
+template <int D, int DV, int KT, int TOKENS>
+__device__ __forceinline__ void land_run(int wave, int lane, int left, uint8_t* buf, const Travel<D, DV, KT, TOKENS>& r) {
+  using G = Wide<D, DV, KT, TOKENS>;
+  using T = Travel<D, DV, KT, TOKENS>;
   uint8_t* run = buf + (wave / G::WPU) * 16 * D * 2;
   if constexpr (KT == kKvBf16) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if (left < 16) {
       for (int k = 0; k < G::NI; k++) {
         int token, c;
-        piece<D, DV, KT>(wave, k, lane, token, c);
+        piece<D, DV, KT, TOKENS>(wave, k, lane, token, c);
         uint8_t* dst = run + 1024 * ((wave % G::WPU) * G::NI + k) + 16 * lane + (G::kAlias ? 0 : G::TILE);
         if (token >= left) *reinterpret_cast<uint4*>(dst) = make_uint4(0, 0, 0, 0);
       }
     }
   } else if constexpr (T::kMx) {
-    // K: lane holds D / 4 channels of token lane / 4
-    const float s = mx::scale_operand(r.k_scale);
+    if (T::takes_k(wave)) {                              // lane holds D / 4 channels of token lane / 4
+      const float s = mx::scale_operand(r.k_scale);
 #pragma unroll
-    for (int x = 0; x < D / 32; x++) *chunk_place<D>(run, lane >> 2, (lane & 3) * (D / 32) + x) = widen_mx(r.k[0][x], s);
-    // V: channels col D / 16 .. of tokens 4 grp + x
-    const int col = lane & 15, grp = lane >> 4;
+      for (int x = 0; x < D / 32; x++) *chunk_place<D>(run, lane >> 2, (lane & 3) * (D / 32) + x) = widen_mx(r.k[0][x], s);
+    }
+    if (T::takes_v(wave)) {                              // channels col D / 16 .. of tokens 4 grp + x
+      const int col = lane & 15, grp = lane >> 4;
 #pragma unroll
-    for (int x = 0; x < 4; x++) {
-      const float f = mx::scale_operand((r.v_scale >> (8 * x)) & 255);
-      if constexpr (D == 128) {
-        *chunk_place<D>(run + G::TILE, 4 * grp + x, col) = widen_mx(r.v[0][x], f);
-      } else {
-        const uint32_t w = r.v[0][x >> 1];
-        uint2* p = reinterpret_cast<uint2*>(chunk_place<D>(run + G::TILE, 4 * grp + x, col >> 1)) + (col & 1);
-        *p = (x & 1) ? make_uint2(mx::pair_bf16<2>(w, f), mx::pair_bf16<3>(w, f)) : make_uint2(mx::pair_bf16<0>(w, f), mx::pair_bf16<1>(w, f));
+      for (int x = 0; x < 4; x++) {
+        const float f = mx::scale_operand((r.v_scale >> (8 * x)) & 255);
+        if constexpr (D == 128) {
+          *chunk_place<D>(run + G::TILE, 4 * grp + x, col) = widen_mx(r.v[0][x], f);
+        } else {
+          const uint32_t w = r.v[0][x >> 1];
+          uint2* p = reinterpret_cast<uint2*>(chunk_place<D>(run + G::TILE, 4 * grp + x, col >> 1)) + (col & 1);
+          *p = (x & 1) ? make_uint2(mx::pair_bf16<2>(w, f), mx::pair_bf16<3>(w, f)) : make_uint2(mx::pair_bf16<0>(w, f), mx::pair_bf16<1>(w, f));
+        }
       }
     }
   } else {
 #pragma unroll
     for (int x = 0; x < T::N; x++) {
       int token, c16;
-      if (!codes_piece<D, DV, KT>(wave, x, lane, token, c16)) continue;
+      if (!codes_piece<D, DV, KT, TOKENS>(wave, x, lane, token, c16)) continue;
 #pragma unroll
       for (int e = 0; e < 2; e++) {
         *chunk_place<D>(run, token, 2 * c16 + e) = widen_codes<KT>(r.k[x][2 * e], r.k[x][2 * e + 1]);
