@@ -6,9 +6,11 @@
 // and products are fp64; a row's angles are computed once for all its heads and held in LDS.  A
 // workgroup takes a few rows, or a part of one row's heads where there are few.
 //
-// Tasks of a row, 8 channels each: the K chunks (a thread reads its chunk and the one that holds its
-// partners, so that the four lanes of a 4-bit group hold neighbouring chunks whatever the pairing), the V
-// chunks, then the queries: both chunks of a pair by one thread, which makes q_out == q safe.
+// Tasks, 8 channels each: the K chunks (a thread reads its chunk and the one that holds its partners, so that the four
+// lanes of a 4-bit group hold neighbouring chunks whatever the pairing), the V chunks, then the queries: both chunks of
+// a pair of halves by one thread, which makes q_out == q safe, and the chunks that pass.  A thread sends for the
+// chunks of a few tasks before it works on the first, for the kernel is bound by memory: 100003 rows of 36 heads of 128
+// channels into E4M3 NNN us (N.N TB/s; one task at a time 384), 8192 rows of 48 heads into mxfp4 NN us.
 #include "cache_rows.h"
 #include "mxfp4.h"
 #include "vx_device.h"
@@ -18,7 +20,7 @@ namespace vx {
 namespace {
 
 constexpr int kRopeThreads = 256;
-constexpr int kRopeRows = 4;               // most rows of a workgroup
+constexpr int kRopeRows = 2;               // most rows of a workgroup
 
 struct RopeArgs {
   uint8_t* k;
@@ -37,8 +39,9 @@ struct RopeArgs {
   int first, half;                         // first rotated channel, pairs
   int interleaved;
   int rows;                                // rows of a workgroup
-  int k_tasks, kv_tasks, tasks;            // of a row, up to the K, the V and the query tasks' end; tasks: whole quads
-  int q_tasks, q_per_head;
+  int k_tasks, v_tasks;                    // of a row
+  int turned, passed;                      // query tasks of a head
+  uint32_t turned_inv, passed_inv;         // 2^32 / them, rounded up
   float scale, k_scale, v_scale;
 };
 
@@ -149,10 +152,8 @@ __device__ __forceinline__ void store_v(const RopeArgs& a, int64_t page, int t, 
   }
 }
 
-// The row's K chunk c8 rotated: its own 8 channels, from them and their partners.
-__device__ __forceinline__ void rotated_chunk(const RopeArgs& a, const uint16_t* row, int c8, const double2* cs,
-                                              float (&x)[8]) {
-  widen8(*reinterpret_cast<const uint4*>(row + 8 * c8), x);
+// Chunk c8 of a row rotated: its own 8 channels x, from them and their partners y (halves).
+__device__ __forceinline__ void turn_chunk(const RopeArgs& a, int c8, const double2* cs, float (&x)[8], const float (&y)[8]) {
   const int c = 8 * c8 - a.first;                      // channel inside the rotated part
   if (c < 0 || c >= 2 * a.half) return;
   if (a.interleaved) {
@@ -164,45 +165,39 @@ __device__ __forceinline__ void rotated_chunk(const RopeArgs& a, const uint16_t*
       x[2 * e + 1] = turn_b(p, r, w);
     }
   } else {
-    float y[8];
     const bool low = c < a.half;
-    widen8(*reinterpret_cast<const uint4*>(row + 8 * c8 + (low ? a.half : -a.half)), y);
     const double2* w = cs + (low ? c : c - a.half);
 #pragma unroll
     for (int e = 0; e < 8; e++) x[e] = low ? turn_a(x[e], y[e], w[e]) : turn_b(y[e], x[e], w[e]);
   }
 }
 
-// Query task z of a head: a pair of chunks (halves), a rotated chunk (neighbours) or a chunk that passes.
-__device__ __forceinline__ void query_task(const RopeArgs& a, const uint16_t* src, uint16_t* dst, int z,
-                                           const double2* cs) {
-  const int turned = a.interleaved ? a.half / 4 : a.half / 8;
-  if (z >= turned) {
-    int c = 8 * (z - turned);
-    if (c >= a.first) c += 2 * a.half;
-    if (src != dst) *reinterpret_cast<uint4*>(dst + c) = *reinterpret_cast<const uint4*>(src + c);
-    return;
-  }
-  float x[8];
-  const int c = a.first + 8 * z;
-  if (a.interleaved) {
-    rotated_chunk(a, src, c >> 3, cs, x);
-    *reinterpret_cast<uint4*>(dst + c) = narrow8(x);
-    return;
-  }
-  float y[8];
-  widen8(*reinterpret_cast<const uint4*>(src + c), x);
-  widen8(*reinterpret_cast<const uint4*>(src + c + a.half), y);
-#pragma unroll
-  for (int e = 0; e < 8; e++) {
-    const double2 w = cs[8 * z + e];
-    const float p = x[e], r = y[e];
-    x[e] = turn_a(p, r, w);
-    y[e] = turn_b(p, r, w);
-  }
-  *reinterpret_cast<uint4*>(dst + c) = narrow8(x);
-  *reinterpret_cast<uint4*>(dst + c + a.half) = narrow8(y);
+// Chunk that holds the partners of chunk c8 (itself, where there are none or they lie in it).
+__device__ __forceinline__ int partner_chunk(const RopeArgs& a, int c8) {
+  const int c = 8 * c8 - a.first;
+  if (a.interleaved || c < 0 || c >= 2 * a.half) return c8;
+  return c < a.half ? c8 + a.half / 8 : c8 - a.half / 8;
 }
+
+// `count` tasks of the workgroups of a row group, N at a time: load(x) sends for task x's chunks, use(x, chunks) does it.
+template <int N, class Load, class Use>
+__device__ __forceinline__ void tasks_of(int count, Load load, Use use) {
+  const int step = (int)(gridDim.y * kRopeThreads);
+  for (int x = (int)(blockIdx.y * kRopeThreads + threadIdx.x); x < count; x += N * step) {
+    decltype(load(0)) got[N];
+#pragma unroll
+    for (int n = 0; n < N; n++)
+      if (x + n * step < count) got[n] = load(x + n * step);
+#pragma unroll
+    for (int n = 0; n < N; n++)
+      if (x + n * step < count) use(x + n * step, got[n]);
+  }
+}
+
+struct TwoChunks {
+  uint4 own, other;
+};
+__device__ __forceinline__ uint4 chunk_at(const uint16_t* p) { return *reinterpret_cast<const uint4*>(p); }
 
 template <int D, int KT>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(const RopeArgs a) {
@@ -219,30 +214,118 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(const RopeArgs a) {
     angles[x] = w;
   }
   __syncthreads();
-  const int total = rows * a.tasks;
-  for (int x = (int)(blockIdx.y * kRopeThreads + threadIdx.x); x < total; x += (int)(gridDim.y * kRopeThreads)) {
-    const int r = x / a.tasks, y = x - r * a.tasks;
-    const int64_t n = n0 + r;
-    const double2* cs = angles + r * a.half;
-    if (y < a.kv_tasks) {
-      const bool v = y >= a.k_tasks;
-      const int z = v ? y - a.k_tasks : y;
-      const int h = z / CH, c8 = z - h * CH;
-      const int64_t slot = a.slots[n], page = slot >> a.ps_shift;
-      const int t = (int)(slot & (a.ps - 1));
-      const bool ok = slot >= 0 && page < a.num_phys;
-      if (v) {
-        store_v<D, KT>(a, page, t, h, c8, ok, load_stream_u4(a.v_in + n * a.v_row + h * a.v_head + 8 * c8));
-      } else {
-        float w[8];
-        rotated_chunk(a, a.k_in + n * a.k_row + h * a.k_head, c8, cs, w);
-        store_k<D, KT>(a, page, t, h, c8, ok, w);
-      }
-    } else if (y < a.q_tasks) {
-      const int z = y - a.kv_tasks, h = z / a.q_per_head;
-      query_task(a, a.q_in + n * a.q_row + h * a.q_head, a.q_out + n * a.o_row + h * a.o_head, z - h * a.q_per_head, cs);
-    }
-  }
+  // row of task x, at most kRopeRows of them
+  auto row_of = [&](int x, int per_row, int& z) {
+    int r = 0;
+#pragma unroll
+    for (int y = 1; y < kRopeRows; y++) r += x >= y * per_row;
+    z = x - r * per_row;
+    return r;
+  };
+  auto place = [&](int64_t n, int64_t& page, int& t) {
+    const int64_t slot = a.slots[n];
+    page = slot >> a.ps_shift;
+    t = (int)(slot & (a.ps - 1));
+    return slot >= 0 && page < a.num_phys;
+  };
+  tasks_of<2>(rows * a.k_tasks,
+      [&](int x) {
+        int z;
+        const int64_t n = n0 + row_of(x, a.k_tasks, z);
+        const int h = z / CH, c8 = z - h * CH;
+        const uint16_t* row = a.k_in + n * a.k_row + h * a.k_head;
+        return TwoChunks{chunk_at(row + 8 * c8), chunk_at(row + 8 * partner_chunk(a, c8))};
+      },
+      [&](int x, const TwoChunks& got) {
+        int z, t;
+        const int r = row_of(x, a.k_tasks, z), h = z / CH, c8 = z - h * CH;
+        int64_t page;
+        const bool ok = place(n0 + r, page, t);
+        float own[8], other[8];
+        widen8(got.own, own);
+        widen8(got.other, other);
+        turn_chunk(a, c8, angles + r * a.half, own, other);
+        store_k<D, KT>(a, page, t, h, c8, ok, own);
+      });
+  tasks_of<4>(rows * a.v_tasks,
+      [&](int x) {
+        int z;
+        const int64_t n = n0 + row_of(x, a.v_tasks, z);
+        const int h = z / CH, c8 = z - h * CH;
+        return load_stream_u4(a.v_in + n * a.v_row + h * a.v_head + 8 * c8);
+      },
+      [&](int x, const uint4& got) {
+        int z, t;
+        const int r = row_of(x, a.v_tasks, z), h = z / CH, c8 = z - h * CH;
+        int64_t page;
+        const bool ok = place(n0 + r, page, t);
+        store_v<D, KT>(a, page, t, h, c8, ok, got);
+      });
+  if (!a.q_in) return;
+  // source and destination of a head's rows, and the channel of task z of it
+  auto query = [&](int x, int per_head, uint32_t inv, int& r, int& z, const uint16_t*& src, uint16_t*& dst) {
+    r = row_of(x, a.Hq * per_head, z);
+    const int h = per_head == 1 ? z : (int)__umulhi((uint32_t)z, inv);
+    z -= h * per_head;
+    src = a.q_in + (n0 + r) * a.q_row + h * a.q_head;
+    dst = a.q_out + (n0 + r) * a.o_row + h * a.o_head;
+  };
+  tasks_of<2>(rows * a.Hq * a.turned,
+      [&](int x) {
+        int r, z;
+        const uint16_t* src;
+        uint16_t* dst;
+        query(x, a.turned, a.turned_inv, r, z, src, dst);
+        src += a.first + 8 * z;
+        return TwoChunks{chunk_at(src), a.interleaved ? uint4{} : chunk_at(src + a.half)};
+      },
+      [&](int x, const TwoChunks& got) {
+        int r, z;
+        const uint16_t* src;
+        uint16_t* dst;
+        query(x, a.turned, a.turned_inv, r, z, src, dst);
+        dst += a.first + 8 * z;
+        const double2* cs = angles + r * a.half;
+        float p[8], q[8];
+        widen8(got.own, p);
+        if (a.interleaved) {
+#pragma unroll
+          for (int e = 0; e < 4; e++) {
+            const double2 w = cs[4 * z + e];
+            const float u = p[2 * e], v = p[2 * e + 1];
+            p[2 * e] = turn_a(u, v, w);
+            p[2 * e + 1] = turn_b(u, v, w);
+          }
+        } else {
+          widen8(got.other, q);
+#pragma unroll
+          for (int e = 0; e < 8; e++) {
+            const double2 w = cs[8 * z + e];
+            const float u = p[e], v = q[e];
+            p[e] = turn_a(u, v, w);
+            q[e] = turn_b(u, v, w);
+          }
+          *reinterpret_cast<uint4*>(dst + a.half) = narrow8(q);
+        }
+        *reinterpret_cast<uint4*>(dst) = narrow8(p);
+      });
+  if (a.passed == 0 || (a.q_in == a.q_out)) return;      // in place they are there
+  auto passing = [&](int z) { return 8 * z < a.first ? 8 * z : 8 * z + 2 * a.half; };
+  tasks_of<4>(rows * a.Hq * a.passed,
+      [&](int x) {
+        int r, z;
+        const uint16_t* src;
+        uint16_t* dst;
+        query(x, a.passed, a.passed_inv, r, z, src, dst);
+        return load_stream_u4(src + passing(z));
+      },
+      [&](int x, const uint4& got) {
+        int r, z;
+        const uint16_t* src;
+        uint16_t* dst;
+        query(x, a.passed, a.passed_inv, r, z, src, dst);
+        *reinterpret_cast<uint4*>(dst + passing(z)) = got;
+      });
 }
 
 template <int D, int KT>
@@ -258,7 +341,7 @@ hipError_t launch(const RopeArgs& all, hipStream_t stream) {
     a.pos = all.pos + done;
     a.slots = all.slots + done;
     const int groups = (a.n + a.rows - 1) / a.rows;
-    const int whole = (a.rows * a.tasks + kRopeThreads - 1) / kRopeThreads;
+    const int whole = (a.rows * (a.k_tasks + a.v_tasks + a.Hq * (a.turned + a.passed)) + kRopeThreads - 1) / kRopeThreads;
     int parts = 1;
     while (groups * parts < 1024 && parts < whole) parts *= 2;
     hipLaunchKernelGGL((rope_kernel<D, KT>), dim3((unsigned)groups, (unsigned)parts), dim3(kRopeThreads),
@@ -318,10 +401,11 @@ hipError_t launch_rope_kv_write(const Geometry& g, const Rotation& rope, const R
   a.v_scale = g.v_scale;
   a.rows = n >= 1024 * kRopeRows ? kRopeRows : 1;
   a.k_tasks = g.H * (g.Dqk / 8);
-  a.kv_tasks = a.k_tasks + (g.v ? g.H * (g.Dv / 8) : 0);
-  a.q_per_head = (rope.interleaved ? a.half / 4 : a.half / 8) + (g.Dqk - rope.dim) / 8;
-  a.q_tasks = a.kv_tasks + (q.rows ? Hq * a.q_per_head : 0);
-  a.tasks = (a.q_tasks + 3) & ~3;
+  a.v_tasks = g.v ? g.H * (g.Dv / 8) : 0;
+  a.turned = rope.interleaved ? a.half / 4 : a.half / 8;
+  a.passed = (g.Dqk - rope.dim) / 8;
+  a.turned_inv = (uint32_t)(((1ull << 32) + a.turned - 1) / a.turned);
+  a.passed_inv = a.passed ? (uint32_t)(((1ull << 32) + a.passed - 1) / a.passed) : 0;
   if (g.Dqk == 128) return launch_kt<128>(a, g.kv_dtype, stream);
   if (g.Dqk == 64) return launch_kt<64>(a, g.kv_dtype, stream);
   return launch_kt<576>(a, g.kv_dtype, stream);

@@ -160,6 +160,10 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
+# The current device, without the check that the runtime has started (a tensor on a GPU has seen to that).
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _stream(stream, device: Optional[int] = None) -> Optional[int]:
     if stream is None:
         return _raw_stream(torch.cuda.current_device() if device is None else device)
@@ -267,6 +271,17 @@ class BatchSpec:
         self._ref = None
         return self.ref()
 
+    def kept(self):
+        """A by-reference argument holding this batch as it is now: built again where a tensor has other memory or
+        another length, or the bound has changed, since."""
+        lens = self.seq_lens
+        at = (self.page_indptr.data_ptr(), self.page_indices.data_ptr(), lens.data_ptr(), lens.numel(), self.max_pages_per_seq)
+        kept = self.__dict__.get("_kept")
+        if kept is None or kept[0] != at:
+            st = self.struct()
+            kept = self.__dict__["_kept"] = (at, ctypes.byref(st))
+        return kept[1]
+
 
 @dataclass
 class PagePool:
@@ -322,7 +337,7 @@ def _gpu_of(t: torch.Tensor) -> int:
     """The current GPU, which t has to be on: the kernels take addresses, and another device's or the
     host's would fault it."""
     d = t.get_device()
-    if d < 0 or d != torch.cuda.current_device():
+    if d < 0 or d != _current_device():
         raise ValueError(f"tensors must be on the current GPU (got one on {t.device})")
     return d
 
@@ -450,13 +465,20 @@ class Rope:
     def current(self, d: int):
         """A by-reference argument holding this rotation as it is now, on GPU d."""
         f, ax = self.inv_freq, self.axis
+        at = (f.data_ptr(), f.numel(), f.dtype, d, None if ax is None else (ax.data_ptr(), ax.numel(), ax.dtype), self.num_axes, self.first,
+              self.interleaved, self.scale)
+        kept = self.__dict__.get("_kept")
+        if kept is not None and kept[0] == at:
+            return kept[1]
         if f.dtype is not torch.float32 or f.get_device() != d or not f.is_contiguous():
             _refuse(f, torch.float32, None, "inv_freq")
         if ax is not None and (ax.dtype is not torch.int32 or ax.numel() != f.numel() or ax.get_device() != d
                                or not ax.is_contiguous()):
             _refuse(ax, torch.int32, f.numel(), "axis")
-        return ctypes.byref(_Rope(f.data_ptr(), None if ax is None else ax.data_ptr(), int(self.num_axes), int(self.first),
-                                  2 * f.numel(), int(bool(self.interleaved)), float(self.scale)))
+        kept = self.__dict__["_kept"] = (at, ctypes.byref(
+            _Rope(f.data_ptr(), None if ax is None else ax.data_ptr(), int(self.num_axes), int(self.first), 2 * f.numel(),
+                  int(bool(self.interleaved)), float(self.scale))))
+        return kept[1]
 
 
 def rope_kv_write(kv: PagedKV, rope: Rope, q: Optional[torch.Tensor], k_new: torch.Tensor,
@@ -498,7 +520,7 @@ def chunk_workspace_size(stage: int, kv: PagedKV, batch: BatchSpec, num_rows: in
     """Workspace bytes of chunk_attention, chunk_score_topk or sparse_chunk_attention (stage CHUNK_ATTENTION,
     CHUNK_SCORE_TOPK, CHUNK_SPARSE) for num_rows rows of queries."""
     out = ctypes.c_size_t(0)
-    _check(lib().vx_chunk_workspace_size(stage, kv.current(), batch.current(), int(num_rows), int(num_q_heads), int(max_sel),
+    _check(lib().vx_chunk_workspace_size(stage, kv.current(), batch.kept(), int(num_rows), int(num_q_heads), int(max_sel),
                                          ctypes.byref(out)))
     return int(out.value)
 
@@ -507,22 +529,32 @@ def _chunk_args(q: torch.Tensor, kv: PagedKV, batch: BatchSpec, q_indptr: torch.
                 q_lens: Optional[torch.Tensor], workspace: torch.Tensor):
     """What the chunk calls share: the device, the query's arguments, the cache, the batch and the chunk."""
     d, c, i32 = _gpu_of(kv.k), kv.current(), torch.int32
-    B = batch.seq_lens.numel()
-    for t, n, name in ((batch.seq_lens, B, "seq_lens"), (batch.page_indptr, B + 1, "page_indptr"),
-                       (batch.page_indices, None, "page_indices"), (q_indptr, B + 1, "q_indptr"), (q_lens, B, "q_lens")):
-        if t is not None and (t.dtype is not i32 or t.get_device() != d or not t.is_contiguous()
-                              or (n is not None and t.numel() != n)):
-            _refuse(t, i32, n, name)
+    lens, indptr, pages = batch.seq_lens, batch.page_indptr, batch.page_indices
+    B = lens.numel()
+    if not (lens.dtype is i32 and indptr.dtype is i32 and pages.dtype is i32 and q_indptr.dtype is i32
+            and indptr.numel() == B + 1 and q_indptr.numel() == B + 1
+            and lens.get_device() == d and indptr.get_device() == d and pages.get_device() == d and q_indptr.get_device() == d
+            and lens.is_contiguous() and indptr.is_contiguous() and pages.is_contiguous() and q_indptr.is_contiguous()):
+        for t, n, name in ((lens, B, "seq_lens"), (indptr, B + 1, "page_indptr"), (pages, None, "page_indices"),
+                           (q_indptr, B + 1, "q_indptr")):
+            if t.dtype is not i32 or (n is not None and t.numel() != n) or t.get_device() != d or not t.is_contiguous():
+                _refuse(t, i32, n, name)
+    if q_lens is not None and (q_lens.dtype is not i32 or q_lens.numel() != B or q_lens.get_device() != d
+                               or not q_lens.is_contiguous()):
+        _refuse(q_lens, i32, B, "q_lens")
     if workspace.get_device() != d or not workspace.is_contiguous():
         _refuse(workspace, workspace.dtype, None, "workspace")
     if q.dim() != 3:
         raise ValueError(f"q must be [rows][heads][dim] (got {tuple(q.shape)})")
-    n, heads = q.shape[0], q.shape[1]
+    n, heads, dim = q.shape
     if n > _MOST:
         raise ValueError(f"at most {_MOST} rows a call (got {n})")
-    q_args = _row_args(q, n, heads, kv._dims[1], d, "q")
-    chunk = _Chunk(q_indptr.data_ptr(), None if q_lens is None else q_lens.data_ptr(), n)
-    return d, q_args + (heads, c, batch.current(), ctypes.byref(chunk))
+    address, row, head = _row_args(q, n, heads, kv._dims[1], d, "q")
+    at = (q_indptr.data_ptr(), None if q_lens is None else q_lens.data_ptr(), n)
+    kept = batch.__dict__.get("_chunk")
+    if kept is None or kept[0] != at:
+        kept = batch.__dict__["_chunk"] = (at, ctypes.byref(_Chunk(*at)))
+    return d, (address, row, head, heads, c, batch.kept(), kept[1])
 
 
 def _result(t: Optional[torch.Tensor], dtype: torch.dtype, shape, d: int, name: str):
@@ -530,7 +562,7 @@ def _result(t: Optional[torch.Tensor], dtype: torch.dtype, shape, d: int, name: 
         return None
     if t.dtype is not dtype or t.get_device() != d or not t.is_contiguous():
         _refuse(t, dtype, None, name)
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)} (got {list(t.shape)})")
     return t.data_ptr()
 
