@@ -194,7 +194,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     for (int u = 0; u < count; u++) {
       const int tok0 = __builtin_amdgcn_readlane(my_tok, 2 * u), tok1 = __builtin_amdgcn_readlane(my_tok, 2 * u + 1);
       const int mask0 = __builtin_amdgcn_readlane(my_mask, 2 * u), mask1 = __builtin_amdgcn_readlane(my_mask, 2 * u + 1);
-      const bool whole = min(tok0, tok1) >= w.all_from && max(tok0, tok1) + 16 <= w.all_to && (mask0 & mask1) == 0xffff;
+      const bool inner = min(tok0, tok1) >= w.all_from && max(tok0, tok1) + 16 <= w.all_to;
       const int next = min(u + 1, count - 1);
       f32x4_t s[1][2];
 #pragma unroll
@@ -205,7 +205,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
           s[0][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand<D, KT>(k[e], kk), w.q[0][kk], s[0][e], 0, 0, 0);
       }
       fetch_k(next);
-      if (!whole) mask_scores<D, D, 1>(0, s[0], tok0, tok1, mask0, mask1, grp, w);
+      if (!inner || (mask0 & mask1) != 0xffff) mask_scores<D, D, 1>(0, s[0], tok0, tok1, mask0, mask1, inner, grp, w);
       uint32_t p[1][4];
       softmax_step<D, D, 1>(a.scale_log2, s, w, p);
       uint32_t v0[4][W], v1[4][W];
@@ -383,7 +383,7 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
     for (int y = 0; y < G::UNITS; y += 2) {
       const int tok0 = tok[y], tok1 = tok[y + 1], mask0 = mask[y], mask1 = mask[y + 1];
       if (((mask0 | mask1) & wave_mask) != 0 && min(tok0, tok1) < wave_to && max(tok0, tok1) + 16 > wave_from) {
-        const bool whole = min(tok0, tok1) >= w.all_from && max(tok0, tok1) + 16 <= w.all_to && (mask0 & mask1) == 0xffff;
+        const bool inner = min(tok0, tok1) >= w.all_from && max(tok0, tok1) + 16 <= w.all_to;
         f32x4_t sc[RT][2];
 #pragma unroll
         for (int rt = 0; rt < RT; rt++) sc[rt][0] = sc[rt][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -404,9 +404,9 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
                 if (k0 + kk < KS)
                   sc[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[kk][e], w.q[rt][k0 + kk], sc[rt][e], 0, 0, 0);
         }
-        if (!whole) {
+        if (!inner || (mask0 & mask1) != 0xffff) {
 #pragma unroll
-          for (int rt = 0; rt < RT; rt++) mask_scores<D, DV, RT>(rt, sc[rt], tok0, tok1, mask0, mask1, grp, w);
+          for (int rt = 0; rt < RT; rt++) mask_scores<D, DV, RT>(rt, sc[rt], tok0, tok1, mask0, mask1, inner, grp, w);
         }
         uint32_t p[RT][4];
         softmax_step<D, DV, RT>(a.scale_log2, sc, w, p);

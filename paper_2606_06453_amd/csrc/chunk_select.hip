@@ -30,7 +30,7 @@ constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr int kBins = 256;
 constexpr int kMostOpen = 128;
 constexpr int kFewInBin = 32;
-constexpr int kTogether = 4;               // times 8 open blocks whose means travel together
+constexpr int kTogether = 2;               // times 8 open blocks whose means travel together
 constexpr int kScoreWgs = 1024;            // workgroups of the scores that fill the chip
 constexpr int kUnit = 32;                  // blocks that a wave looks up at a time
 constexpr size_t kScoreBytes = (size_t)128 << 20;        // of scores at a time: half of the last cache
@@ -312,7 +312,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 
 // A wave a row.
 template <int D>
-__global__ __launch_bounds__(kThreads) void chunk_choose_kernel(const ChunkArgs a, const SelectArgs s) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6))) void chunk_choose_kernel(const ChunkArgs a, const SelectArgs s) {
   extern __shared__ __attribute__((aligned(16))) uint16_t slab[];          // [wave][stride]
   __shared__ WaveLds wave_lds[kWaves];
   const int tid = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);

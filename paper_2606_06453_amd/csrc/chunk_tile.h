@@ -233,12 +233,21 @@ __device__ __forceinline__ void begin_rows(const ChunkArgs& a, const Tile& t, in
 }
 
 // Scores of tokens that a row does not attend: s holds 16 tokens from tok0 and 16 from tok1, of the tile tokens in
-// mask0 and mask1.
+// mask0 and mask1.  inner: every row that lists the runs attends all their tokens.
 template <int D, int DV, int RT>
-__device__ __forceinline__ void mask_scores(int rt, f32x4_t (&s)[2], int tok0, int tok1, int mask0, int mask1, int grp,
-                                            const Rows<D, DV, RT>& w) {
+__device__ __forceinline__ void mask_scores(int rt, f32x4_t (&s)[2], int tok0, int tok1, int mask0, int mask1, bool inner,
+                                            int grp, const Rows<D, DV, RT>& w) {
+  const bool on0 = (mask0 >> w.bit[rt]) & 1, on1 = (mask1 >> w.bit[rt]) & 1;
+  if (inner) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      s[0][i] = on0 ? s[0][i] : -INFINITY;
+      s[1][i] = on1 ? s[1][i] : -INFINITY;
+    }
+    return;
+  }
   const int t0 = tok0 + 4 * grp, t1 = tok1 + 4 * grp;
-  const int to0 = ((mask0 >> w.bit[rt]) & 1) ? w.to[rt] : 0, to1 = ((mask1 >> w.bit[rt]) & 1) ? w.to[rt] : 0;
+  const int to0 = on0 ? w.to[rt] : 0, to1 = on1 ? w.to[rt] : 0;
 #pragma unroll
   for (int i = 0; i < 4; i++) {
     s[0][i] = t0 + i < to0 && t0 + i >= w.from[rt] ? s[0][i] : -INFINITY;
