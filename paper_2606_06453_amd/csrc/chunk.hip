@@ -303,10 +303,16 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
   const int r0 = wave * 16 * RT;
   Rows<D, DV, RT> w;
   begin_rows<D, DV, kKvBf16, RT>(a, t, h, r0, col, grp, w);
+  if constexpr (!SPARSE) {                               // what lies behind the part is for the others
+    const int end = min(runs.hi, INT_MAX >> 4) << 4;
+    w.all_to = min(w.all_to, end);
+#pragma unroll
+    for (int rt = 0; rt < RT; rt++) w.to[rt] = min(w.to[rt], end);
+  }
   // the tile tokens of this wave's rows, and what they attend between them
   const int x0 = min(r0 / a.g, t.n), x1 = min((r0 + 16 * RT - 1) / a.g, t.n - 1);
   const int wave_from = first_key(a, t.p0 + x0), wave_to = r0 < rows ? end_key(a, t, t.p0 + x1) : 0;
-  const int wave_mask = r0 >= rows ? 0 : SPARSE ? (2 << x1) - (1 << x0) : 0xffff;
+  const int wave_mask = SPARSE && r0 < rows ? (2 << x1) - (1 << x0) : 0;
 
   const int n16 = (runs.hi - runs.lo) << shift16, steps = (n16 + G::UNITS - 1) / G::UNITS;
   // The runs that a lane looks up for all (listed blocks), or for its wave (a range): first token, page, and the tile
@@ -355,12 +361,6 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
       if ((s & 63) == 0 && s > 0) now = look_up(s / 64);
       page = __builtin_amdgcn_readlane(now.page, s & 63);
       mine = __builtin_amdgcn_readlane(now.tok, s & 63);
-#pragma unroll
-      for (int u = 0; u < G::UNITS; u++) {
-        const int x = G::UNITS * s + u;
-        toks[u] = (runs.lo + min(x, n16 - 1)) << 4;
-        masks[u] = x < n16 ? 0xffff : 0;
-      }
     }
     const uint8_t* ks = slice_of<D, KT>(a, a.k, page, h);
     send_run<D, DV, KT, TK>(a, ks, G::kAlias ? ks : slice_of<D, KT>(a, a.v, page, h), mine & (a.ps - 1), last - mine, wave, lane,
@@ -374,16 +374,18 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
     int tok[G::UNITS], mask[G::UNITS];
 #pragma unroll
     for (int u = 0; u < G::UNITS; u++) {
-      tok[u] = toks[u];
-      mask[u] = masks[u];
+      tok[u] = SPARSE ? toks[u] : (runs.lo + G::UNITS * s + u) << 4;
+      mask[u] = SPARSE ? masks[u] : 0xffff;
     }
     if (s + 1 < steps) send(s + 1);
     const uint8_t* vt = G::kAlias ? buf : buf + G::TILE;
 #pragma unroll
     for (int y = 0; y < G::UNITS; y += 2) {
       const int tok0 = tok[y], tok1 = tok[y + 1], mask0 = mask[y], mask1 = mask[y + 1];
-      if (((mask0 | mask1) & wave_mask) != 0 && min(tok0, tok1) < wave_to && max(tok0, tok1) + 16 > wave_from) {
-        const bool inner = min(tok0, tok1) >= w.all_from && max(tok0, tok1) + 16 <= w.all_to;
+      const bool some = SPARSE ? ((mask0 | mask1) & wave_mask) != 0 : tok0 < wave_to && tok0 + 32 > wave_from;
+      if (some) {
+        // of a list the last blocks alone may reach past a row's own token
+        const bool inner = SPARSE ? max(tok0, tok1) + 16 <= w.all_to : tok0 >= w.all_from && tok0 + 32 <= w.all_to;
         f32x4_t sc[RT][2];
 #pragma unroll
         for (int rt = 0; rt < RT; rt++) sc[rt][0] = sc[rt][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};

@@ -17,9 +17,9 @@ typedef __attribute__((address_space(3))) uint8_t lds_u8;
 __device__ __forceinline__ uint32_t lds_address(const uint8_t* p) { return (uint32_t)(uintptr_t)(lds_u8*)p; }
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short v4i16_t;
 
-// One direct-to-LDS load: lane l's 16 bytes at base + off go to LDS address lds + 16 l.  In assembly, for the
-// compiler would wait for loads that it sees before every read of LDS; `land_run` waits instead.  M0 holds the
-// LDS address; the compiler reserves it, so its value is saved and restored here.
+// Direct-to-LDS loads: lane l's 16 bytes at base + off go to LDS address lds + 16 l; the second form also loads base2 +
+// off to lds + GAP.  In assembly, for the compiler would wait for loads that it sees before every read of LDS;
+// `land_run` waits instead.  M0 holds the LDS address; the compiler reserves it, so its value is saved and restored.
 __device__ __forceinline__ void send16(const uint8_t* base, uint32_t off, uint32_t lds) {
   uint32_t saved;
   asm volatile(
@@ -31,6 +31,22 @@ __device__ __forceinline__ void send16(const uint8_t* base, uint32_t off, uint32
       : "=&s"(saved)
       : "s"(lds), "v"(off), "s"(base)
       : "memory");
+}
+template <int GAP>
+__device__ __forceinline__ void send16(const uint8_t* base, const uint8_t* base2, uint32_t off, uint32_t lds) {
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %2, %3\n\t"
+      "s_add_u32 m0, m0, %5\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %2, %4\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "s"(lds), "v"(off), "s"(base), "s"(base2), "n"(GAP)
+      : "memory", "scc");
 }
 
 // A barrier that completes this wave's LDS accesses first.
@@ -101,8 +117,8 @@ __device__ __forceinline__ void send_run(const ChunkArgs& a, const uint8_t* ks, 
       int token, c;
       piece<D, DV, KT, TOKENS>(wave, k, lane, token, c);
       const uint32_t to = dst + 1024 * ((wave % G::WPU) * G::NI + k), at = 2 * (token * D + 8 * c);
-      send16(ks + 2 * t * D, at, to);
-      if constexpr (!G::kAlias) send16(vs + 2 * t * D, at, to + G::TILE);
+      if constexpr (G::kAlias) send16(ks + 2 * t * D, at, to);
+      else send16<G::TILE>(ks + 2 * t * D, vs + 2 * t * D, at, to);
     }
   } else if constexpr (T::kMx) {
     const int col = lane & 15, grp = lane >> 4;
