@@ -28,9 +28,10 @@ constexpr int kAtOnce = 4;                 // K operands of a run that are sent 
 constexpr float kLn2 = 0.693147180559945309f;
 
 // The blocks listed for the tile's tokens: masks[id] holds a bit for each token that lists block id, ids the
-// listed ones in ascending order.  Returns their count.  Every thread of the workgroup takes part.
-__device__ __forceinline__ int listed_blocks(const ChunkArgs& a, const Tile& t, int h, uint32_t* words, uint16_t* ids) {
-  __shared__ int wave_total[kWaves];
+// listed ones in ascending order; wave_total: kWaves words.  Returns their count.  Every thread of the workgroup takes
+// part.
+__device__ __forceinline__ int listed_blocks(const ChunkArgs& a, const Tile& t, int h, uint32_t* words, uint16_t* ids,
+                                             int* wave_total) {
   const int tid = (int)threadIdx.x, lane = lane_id(), wave = tid >> 6;
   const int p_last = t.p0 + t.n - 1;
   const int nb = p_last < 0 ? 0 : min((min(p_last + 1, t.len) + a.bs - 1) >> a.bs_shift, a.max_blocks);
@@ -109,13 +110,14 @@ __device__ __forceinline__ bool empty_part(const ChunkArgs& a, const Tile& t, in
   return true;
 }
 
-// The runs of a workgroup's part; shift16: log2 of the 16-token runs of an entry.
+// The runs of a workgroup's part; shift16: log2 of the 16-token runs of an entry.  scratch: kWaves words.
 template <bool SPARSE>
-__device__ __forceinline__ Runs part_runs(const ChunkArgs& a, const Tile& t, int h, int split, uint32_t* lds, int& shift16) {
+__device__ __forceinline__ Runs part_runs(const ChunkArgs& a, const Tile& t, int h, int split, uint32_t* lds, uint32_t* scratch,
+                                          int& shift16) {
   Runs runs;
   if constexpr (SPARSE) {
     uint16_t* ids = reinterpret_cast<uint16_t*>(lds + (a.max_blocks + 1) / 2);
-    const int all = __builtin_amdgcn_readfirstlane(listed_blocks(a, t, h, lds, ids));
+    const int all = __builtin_amdgcn_readfirstlane(listed_blocks(a, t, h, lds, ids, reinterpret_cast<int*>(scratch)));
     runs.ids = ids;
     runs.masks = reinterpret_cast<const uint16_t*>(lds);
     runs.shift = a.bs_shift;
@@ -145,7 +147,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   Tile t;
   if (!find_tile(a, (int)blockIdx.x / a.H, t)) return;
   int shift16;
-  const Runs runs = part_runs<SPARSE>(a, t, h, split, lds, shift16);
+  const Runs runs = part_runs<SPARSE>(a, t, h, split, lds, lds + 2 * ((a.max_blocks + 1) / 2), shift16);
   if (empty_part(a, t, h, split, runs)) return;
   const int rows = t.n * a.g, last = end_key(a, t, t.p0 + t.n - 1);        // past every row's tokens
   Rows<D, D, 1> w;
@@ -205,9 +207,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
           s[0][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand<D, KT>(k[e], kk), w.q[0][kk], s[0][e], 0, 0, 0);
       }
       fetch_k(next);
-      if (!inner || (mask0 & mask1) != 0xffff) mask_scores<D, D, 1>(0, s[0], tok0, tok1, mask0, mask1, inner, grp, w);
+      if (!inner) mask_scores<D, D, 1>(s, tok0, tok1, grp, w);
       uint32_t p[1][4];
-      softmax_step<D, D, 1>(a.scale_log2, s, w, p);
+      softmax_step<D, D, 1, true>(a.scale_log2, s, mask0, mask1, w, p);
       uint32_t v0[4][W], v1[4][W];
       v_rows<D, KT>(v[0], v0);
       v_rows<D, KT>(v[1], v1);
@@ -274,7 +276,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     }
   }
   if (__syncthreads_or(orow < rows && !fine)) {
-    if constexpr (SPARSE) listed_blocks(a, t, h, lds, const_cast<uint16_t*>(runs.ids));
+    if constexpr (SPARSE) listed_blocks(a, t, h, lds, const_cast<uint16_t*>(runs.ids), reinterpret_cast<int*>(lds + 2 * ((a.max_blocks + 1) / 2)));
     attend_rows<D, D, KT>(a, t, h, runs, split);
   }
 }
@@ -297,7 +299,7 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
   uint8_t* bufs = reinterpret_cast<uint8_t*>(lds);
   uint32_t* lists = lds + 2 * G::BUF / sizeof(uint32_t);
   int shift16;
-  const Runs runs = part_runs<SPARSE>(a, t, h, split, lists, shift16);
+  const Runs runs = part_runs<SPARSE>(a, t, h, split, lists, lds, shift16);
   if (empty_part(a, t, h, split, runs)) return;
   const int rows = t.n * a.g, last = end_key(a, t, t.p0 + t.n - 1);
   const int r0 = wave * 16 * RT;
@@ -406,12 +408,9 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
                 if (k0 + kk < KS)
                   sc[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[kk][e], w.q[rt][k0 + kk], sc[rt][e], 0, 0, 0);
         }
-        if (!inner || (mask0 & mask1) != 0xffff) {
-#pragma unroll
-          for (int rt = 0; rt < RT; rt++) mask_scores<D, DV, RT>(rt, sc[rt], tok0, tok1, mask0, mask1, inner, grp, w);
-        }
+        if (!inner) mask_scores<D, DV, RT>(sc, tok0, tok1, grp, w);
         uint32_t p[RT][4];
-        softmax_step<D, DV, RT>(a.scale_log2, sc, w, p);
+        softmax_step<D, DV, RT, SPARSE>(a.scale_log2, sc, mask0, mask1, w, p);
 #pragma unroll
         for (int j = 0; j < NJ; j++) {
           const bf16x8_t v = v_from_lds<D>(vt, 16 * y, j, col, grp);
@@ -561,7 +560,7 @@ Plan plan_of(const Geometry& g, int n, int Hq, bool sparse, int max_sel) {
 template <int D, int KT, bool SPARSE>
 void launch_narrow(const ChunkArgs& a, dim3 grid, size_t lists, hipStream_t stream) {
   const size_t states = sizeof(float) * kWaves * 16 * (D + 4) + sizeof(float2) * kWaves * 16;
-  hipLaunchKernelGGL((chunk_narrow_kernel<D, KT, SPARSE>), grid, dim3(kThreads), std::max(lists, states), stream, a);
+  hipLaunchKernelGGL((chunk_narrow_kernel<D, KT, SPARSE>), grid, dim3(kThreads), std::max(lists + kWaves * sizeof(int), states), stream, a);
 }
 template <int D, int DV, int KT, int RT, bool SPARSE>
 void launch_wide(const ChunkArgs& a, dim3 grid, size_t lists, hipStream_t stream) {

@@ -232,40 +232,37 @@ __device__ __forceinline__ void begin_rows(const ChunkArgs& a, const Tile& t, in
   w.all_to = end_key(a, t, t.p0);
 }
 
-// Scores of tokens that a row does not attend: s holds 16 tokens from tok0 and 16 from tok1, of the tile tokens in
-// mask0 and mask1.  inner: every row that lists the runs attends all their tokens.
+// Scores of tokens that a row does not attend: s holds 16 tokens from tok0 and 16 from tok1.  Few steps need it: the
+// statement without instructions keeps its comparisons, which the compiler would make ahead of the branch around
+// it for every step, inside.
 template <int D, int DV, int RT>
-__device__ __forceinline__ void mask_scores(int rt, f32x4_t (&s)[2], int tok0, int tok1, int mask0, int mask1, bool inner,
-                                            int grp, const Rows<D, DV, RT>& w) {
-  const bool on0 = (mask0 >> w.bit[rt]) & 1, on1 = (mask1 >> w.bit[rt]) & 1;
-  if (inner) {
+__device__ __forceinline__ void mask_scores(f32x4_t (&s)[RT][2], int tok0, int tok1, int grp, const Rows<D, DV, RT>& w) {
+  asm volatile("" : "+s"(tok0), "+s"(tok1));
+  const int t0 = tok0 + 4 * grp, t1 = tok1 + 4 * grp;
+#pragma unroll
+  for (int rt = 0; rt < RT; rt++)
 #pragma unroll
     for (int i = 0; i < 4; i++) {
-      s[0][i] = on0 ? s[0][i] : -INFINITY;
-      s[1][i] = on1 ? s[1][i] : -INFINITY;
+      s[rt][0][i] = t0 + i < w.to[rt] && t0 + i >= w.from[rt] ? s[rt][0][i] : -INFINITY;
+      s[rt][1][i] = t1 + i < w.to[rt] && t1 + i >= w.from[rt] ? s[rt][1][i] : -INFINITY;
     }
-    return;
-  }
-  const int t0 = tok0 + 4 * grp, t1 = tok1 + 4 * grp;
-  const int to0 = on0 ? w.to[rt] : 0, to1 = on1 ? w.to[rt] : 0;
-#pragma unroll
-  for (int i = 0; i < 4; i++) {
-    s[0][i] = t0 + i < to0 && t0 + i >= w.from[rt] ? s[0][i] : -INFINITY;
-    s[1][i] = t1 + i < to1 && t1 + i >= w.from[rt] ? s[1][i] : -INFINITY;
-  }
 }
 
 // One step of the softmax: the scores s of 32 tokens become weights p, bf16, operand B of O^T = V^T P^T.  The
 // weights are taken at the present references first and seldom reach 2 (bit 14 of a bf16 number; infinities and
 // NaN have it too); only then the references move.  The sum takes the weights before their rounding, which is to the
 // nearest (2^-9 of each at most, without a bias) and halves the matrix work that two parts would need.
-template <int D, int DV, int RT>
-__device__ __forceinline__ void softmax_step(float scale_log2, const f32x4_t (&s)[RT][2], Rows<D, DV, RT>& w,
-                                             uint32_t (&p)[RT][4]) {
+// LISTED: mask0 and mask1 hold the tile tokens that list the first and the last 16 tokens; another's reference for
+// them is infinite, and their weights are zero.
+template <int D, int DV, int RT, bool LISTED>
+__device__ __forceinline__ void softmax_step(float scale_log2, const f32x4_t (&s)[RT][2], int mask0, int mask1,
+                                             Rows<D, DV, RT>& w, uint32_t (&p)[RT][4]) {
   float x[RT][8];
+  auto on = [&](int rt, int e) { return !LISTED || ((e ? mask1 : mask0) >> w.bit[rt] & 1) != 0; };
   auto weigh = [&](int rt) {
+    const float m[2] = {on(rt, 0) ? w.m[rt] : INFINITY, on(rt, 1) ? w.m[rt] : INFINITY};
 #pragma unroll
-    for (int i = 0; i < 8; i++) x[rt][i] = __builtin_amdgcn_exp2f(fmaf(s[rt][i >> 2][i & 3], scale_log2, -w.m[rt]));
+    for (int i = 0; i < 8; i++) x[rt][i] = __builtin_amdgcn_exp2f(fmaf(s[rt][i >> 2][i & 3], scale_log2, -m[i >> 2]));
 #pragma unroll
     for (int i = 0; i < 4; i++) p[rt][i] = pack_bf16(x[rt][2 * i], x[rt][2 * i + 1]);
   };
@@ -278,9 +275,10 @@ __device__ __forceinline__ void softmax_step(float scale_log2, const f32x4_t (&s
   if (__builtin_expect(__any((seen & 0x40004000u) != 0), 0)) {
 #pragma unroll
     for (int rt = 0; rt < RT; rt++) {
-      const float top = fmaxf(fmaxf(fmaxf(s[rt][0][0], s[rt][0][1]), fmaxf(s[rt][0][2], s[rt][0][3])),
-                              fmaxf(fmaxf(s[rt][1][0], s[rt][1][1]), fmaxf(s[rt][1][2], s[rt][1][3]))) *
-                        scale_log2;
+      float top = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 2; e++)
+        if (on(rt, e)) top = fmaxf(top, fmaxf(fmaxf(s[rt][e][0], s[rt][e][1]), fmaxf(s[rt][e][2], s[rt][e][3])) * scale_log2);
       const float c = column_max(top), next = c > w.m[rt] ? c + kAhead : w.m[rt];
       const float alpha = __builtin_amdgcn_exp2f(w.m[rt] - next);
       w.m[rt] = next;
