@@ -52,11 +52,13 @@ __device__ __forceinline__ void send16(const uint8_t* base, const uint8_t* base2
 // A barrier that completes this wave's LDS accesses first.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// Place of a row's chunks: XOR within groups of 16 (D = 128) or 8 chunks.
+// Place of a row's chunks: XOR within groups of 16 (D = 128) or 8 chunks.  Chosen among the linear maps of the token's
+// bits by timing both kinds of read over 8 KiB: 36 cycles of a CU for K and 41 for V; without one 258 and 264.
 template <int D>
 __device__ __forceinline__ int swizzle(int token) {
-  if constexpr (D == 128) return ((token & 7) << 1) | ((token >> 3) & 1);
-  else return (((token >> 1) & 3) << 1) | ((token >> 3) & 1);
+  if constexpr (D == 128) return (token & 7) << 1;
+  else if constexpr (D == 64) return token & 7;
+  else return (token & 4) | (((token ^ (token >> 1) ^ (token >> 3)) & 1) << 1);
 }
 
 template <int D, int DV, int KT, int TOKENS>
@@ -145,6 +147,14 @@ __device__ __forceinline__ void send_run(const ChunkArgs& a, const uint8_t* ks, 
   }
 }
 
+// The place of chunk 'most + c' of a row with swizzle f, as a part that differs between lanes and one that is a constant
+// where `most` is: a row's group of chunks.
+template <int D>
+__device__ __forceinline__ int place(int most, int c, int f) {
+  constexpr int kGroup = D == 128 ? 16 : 8;
+  return 16 * (most / kGroup * kGroup) + 16 * ((most % kGroup + c) ^ f);
+}
+
 // Chunk c of token `token` of a run at `run`.
 template <int D>
 __device__ __forceinline__ uint4* chunk_place(uint8_t* run, int token, int c) {
@@ -212,8 +222,7 @@ __device__ __forceinline__ void land_run(int wave, int lane, int left, uint8_t* 
 // Operand A of S^T: 16 tokens from t0, k-step kk (channels 32 kk + 8 grp ..).
 template <int D>
 __device__ __forceinline__ bf16x8_t k_from_lds(const uint8_t* tile, int t0, int kk, int col, int grp) {
-  const int token = t0 + col, c = (4 * kk + grp) ^ swizzle<D>(col);
-  return *reinterpret_cast<const bf16x8_t*>(tile + token * D * 2 + 16 * c);
+  return *reinterpret_cast<const bf16x8_t*>(tile + (t0 + col) * D * 2 + place<D>(4 * kk, grp, swizzle<D>(col)));
 }
 
 // Operand A of O^T: channels 16 j + col of tokens t0 + 4 grp + 0..3 and t0 + 16 + 4 grp + 0..3.  Lane 4 r + x of
@@ -221,8 +230,7 @@ __device__ __forceinline__ bf16x8_t k_from_lds(const uint8_t* tile, int t0, int 
 template <int D>
 __device__ __forceinline__ bf16x8_t v_from_lds(const uint8_t* tile, int t0, int j, int col, int grp) {
   const int row = 4 * grp + (col >> 2), x = col & 3;
-  const int c = (2 * j + (x >> 1)) ^ swizzle<D>(row);
-  lds_u8* p = (lds_u8*)(tile + (t0 + row) * D * 2 + 16 * c + 8 * (x & 1));
+  lds_u8* p = (lds_u8*)(tile + (t0 + row) * D * 2 + place<D>(2 * j, x >> 1, swizzle<D>(row)) + 8 * (x & 1));
   const v4i16_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16_t*)p);
   const v4i16_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16_t*)(p + 16 * D * 2));
   typedef short s16x8_t __attribute__((ext_vector_type(8)));
