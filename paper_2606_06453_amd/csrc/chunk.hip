@@ -398,7 +398,7 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
           for (int kk = 0; kk < kAtOnce; kk++)
 #pragma unroll
             for (int e = 0; e < 2; e++)
-              if (k0 + kk < KS) k[kk][e] = k_from_lds<D>(buf, 16 * (y + e), k0 + kk, col, grp);
+              if (k0 + kk < KS) k[kk][e] = k_from_lds<G::PLANE>(buf, 16 * (y + e), k0 + kk, col, grp);
 #pragma unroll
           for (int kk = 0; kk < kAtOnce; kk++)
 #pragma unroll
@@ -413,7 +413,7 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
         softmax_step<D, DV, RT, SPARSE>(a.scale_log2, sc, mask0, mask1, w, p);
 #pragma unroll
         for (int j = 0; j < NJ; j++) {
-          const bf16x8_t v = v_from_lds<D>(vt, 16 * y, j, col, grp);
+          const bf16x8_t v = v_from_lds<G::PLANE>(vt, 16 * y, j, col, grp);
 #pragma unroll
           for (int rt = 0; rt < RT; rt++)
             w.acc[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_operand(p[rt]), w.acc[rt][j], 0, 0, 0);
@@ -455,8 +455,9 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
   if (__syncthreads_or(bad)) attend_rows<D, DV, KT>(a, t, h, runs, split);
 }
 
+// The latent's rows take 250 registers of two waves a SIMD; as fp8 they need more and have one.
 template <int D, int DV, int KT, int RT, bool SPARSE>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(D == DV ? 2 : 1))) void chunk_wide_kernel(const ChunkArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(D == DV || KT == kKvBf16 ? 2 : 1))) void chunk_wide_kernel(const ChunkArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
   const int h = (int)blockIdx.x % a.H, split = (int)blockIdx.y;
   Tile t;
@@ -548,7 +549,10 @@ Plan plan_of(const Geometry& g, int n, int Hq, bool sparse, int max_sel) {
   const int64_t tiles = std::max<int64_t>(batch, (n + p.tokens - 1) / p.tokens) * g.H;
   const int64_t list = std::min<int64_t>((int64_t)g.max_pages * g.bs, sparse ? (int64_t)max_sel * p.tokens * g.bs : INT64_MAX);
   const int64_t most = std::min<int64_t>(kMaxParts, (list + kPartTokens - 1) / kPartTokens);
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, kTargetWgs / tiles));
+  // a little more than one workgroup a CU: as halves, most CUs take three in place of two wholes (350 tiles of the
+  // latent 470 -> 377 us)
+  const bool halves = tiles > kTargetWgs / 2 && tiles <= kTargetWgs * 3 / 4;
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, halves ? 2 : kTargetWgs / tiles));
   if (p.splits > 1) {
     p.o_bytes = (size_t)n * Hq * p.splits * g.Dv * sizeof(float);
     p.bytes = p.o_bytes + (size_t)n * Hq * p.splits * sizeof(float2);

@@ -1,11 +1,12 @@
 // The wide tile kernel: four waves of 16 RT query rows each share every 64 (listed blocks, latent: 32) tokens of K and
 // V in LDS.
 //
-// LDS holds bf16 rows of 16-byte chunks.  bf16 rows go there straight from memory (each lane of a load picks
-// its source, so the swizzle costs nothing), other types pass through registers, where they are widened.
-// Operands of S^T = K Q^T are 16-byte reads of a row; those of O^T = V^T P^T are transposing reads of four
-// tokens by 16 channels.  Chunk c of token t lies at place c ^ f(t) of its row (f: `swizzle`), which spreads the 16
-// rows that a K read touches, and the 8 rows of half a V read, over all banks.
+// LDS holds bf16 channels in D / 64 planes of 128 bytes a token, chunks of 16 bytes.  bf16 rows go there straight from
+// memory (each lane of a load picks its source, so the swizzle costs nothing), other types pass through registers,
+// where they are widened.  Operands of S^T = K Q^T are 16-byte reads of a token; those of O^T = V^T P^T are transposing
+// reads of four tokens by 16 channels.  Chunk c of token t of a plane lies at place c ^ (t & 7), where neither kind of
+// read collides: 36 and 41 cycles of a CU for 8 KiB (without the swizzle 131 and 136).  A read's plane is a constant of
+// its address, so that few registers hold addresses.
 // Two buffers: the next tokens travel while the present ones are multiplied.
 #pragma once
 #include "chunk_tile.h"
@@ -52,34 +53,25 @@ __device__ __forceinline__ void send16(const uint8_t* base, const uint8_t* base2
 // A barrier that completes this wave's LDS accesses first.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// Place of a row's chunks: XOR within groups of 16 (D = 128) or 8 chunks.  Chosen among the linear maps of the token's
-// bits by timing both kinds of read over 8 KiB: 36 cycles of a CU for K and 41 for V; without one 258 and 264.
-template <int D>
-__device__ __forceinline__ int swizzle(int token) {
-  if constexpr (D == 128) return (token & 7) << 1;
-  else if constexpr (D == 64) return token & 7;
-  else return (token & 4) | (((token ^ (token >> 1) ^ (token >> 3)) & 1) << 1);
-}
-
 template <int D, int DV, int KT, int TOKENS>
 struct Wide {
   static constexpr bool kAlias = D != DV;
   static constexpr int TK = TOKENS;                      // tokens of a buffer
   static constexpr int UNITS = TK / 16;                  // runs of 16 tokens
-  static constexpr int CH = D / 8;                       // chunks of a row
+  static constexpr int PLANE = TK * 128;                 // bytes of 64 channels
   static constexpr int WPU = 4 / UNITS;                  // waves that load a run
-  static constexpr int NI = 16 * CH / 64 / WPU;          // 64-chunk pieces of a wave
+  static constexpr int NI = D / 32 / WPU;                // pieces of a wave: 8 tokens of a plane
   static constexpr int TILE = TK * D * 2;                // bytes of K
   static constexpr int BUF = kAlias ? TILE : 2 * TILE;
 };
 
-// Element chunk of lane `lane` in piece k of the wave's part of a run: token and logical chunk.
+// Piece k of a wave's part of a run: its first token, and its plane.
 template <int D, int DV, int KT, int TOKENS>
-__device__ __forceinline__ void piece(int wave, int k, int lane, int& token, int& c) {
+__device__ __forceinline__ void piece(int wave, int k, int& token, int& plane) {
   using G = Wide<D, DV, KT, TOKENS>;
-  const int slot = 64 * ((wave % G::WPU) * G::NI + k) + lane;
-  token = slot / G::CH;
-  c = (slot % G::CH) ^ swizzle<D>(token);
+  const int x = G::NI * (wave % G::WPU) + k;
+  token = 8 * (x & 1);
+  plane = x >> 1;
 }
 
 // A wave's part of a run on its way through registers: fp8, 16 codes a lane and piece; mxfp4, a lane's D / 4 codes of
@@ -113,14 +105,16 @@ __device__ __forceinline__ void send_run(const ChunkArgs& a, const uint8_t* ks, 
   using G = Wide<D, DV, KT, TOKENS>;
   using T = Travel<D, DV, KT, TOKENS>;
   if constexpr (KT == kKvBf16) {
-    const uint32_t dst = lds_address(buf) + (wave / G::WPU) * 16 * D * 2;
+    const uint32_t dst = lds_address(buf) + (wave / G::WPU) * 16 * 128;
+    const uint32_t at = 2 * ((lane >> 3) * D + 8 * ((lane & 7) ^ (lane >> 3)));
 #pragma unroll
     for (int k = 0; k < G::NI; k++) {
-      int token, c;
-      piece<D, DV, KT, TOKENS>(wave, k, lane, token, c);
-      const uint32_t to = dst + 1024 * ((wave % G::WPU) * G::NI + k), at = 2 * (token * D + 8 * c);
-      if constexpr (G::kAlias) send16(ks + 2 * t * D, at, to);
-      else send16<G::TILE>(ks + 2 * t * D, vs + 2 * t * D, at, to);
+      int token, plane;
+      piece<D, DV, KT, TOKENS>(wave, k, token, plane);
+      const uint32_t to = dst + plane * G::PLANE + token * 128;
+      const int from = 2 * ((t + token) * D + 64 * plane);
+      if constexpr (G::kAlias) send16(ks + from, at, to);
+      else send16<G::TILE>(ks + from, vs + from, at, to);
     }
   } else if constexpr (T::kMx) {
     const int col = lane & 15, grp = lane >> 4;
@@ -147,18 +141,10 @@ __device__ __forceinline__ void send_run(const ChunkArgs& a, const uint8_t* ks, 
   }
 }
 
-// The place of chunk 'most + c' of a row with swizzle f, as a part that differs between lanes and one that is a constant
-// where `most` is: a row's group of chunks.
-template <int D>
-__device__ __forceinline__ int place(int most, int c, int f) {
-  constexpr int kGroup = D == 128 ? 16 : 8;
-  return 16 * (most / kGroup * kGroup) + 16 * ((most % kGroup + c) ^ f);
-}
-
-// Chunk c of token `token` of a run at `run`.
-template <int D>
+// Chunk c of token `token` of a run whose first plane is at `run`.
+template <int PLANE>
 __device__ __forceinline__ uint4* chunk_place(uint8_t* run, int token, int c) {
-  return reinterpret_cast<uint4*>(run + token * D * 2 + 16 * (c ^ swizzle<D>(token)));
+  return reinterpret_cast<uint4*>(run + (c >> 3) * PLANE + token * 128 + 16 * ((c ^ token) & 7));
 }
 template <int KT>
 __device__ __forceinline__ uint4 widen_codes(uint32_t lo, uint32_t hi) {
@@ -174,22 +160,22 @@ template <int D, int DV, int KT, int TOKENS>
 __device__ __forceinline__ void land_run(int wave, int lane, int left, uint8_t* buf, const Travel<D, DV, KT, TOKENS>& r) {
   using G = Wide<D, DV, KT, TOKENS>;
   using T = Travel<D, DV, KT, TOKENS>;
-  uint8_t* run = buf + (wave / G::WPU) * 16 * D * 2;
+  uint8_t* run = buf + (wave / G::WPU) * 16 * 128;
   if constexpr (KT == kKvBf16) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if (left < 16) {
       for (int k = 0; k < G::NI; k++) {
-        int token, c;
-        piece<D, DV, KT, TOKENS>(wave, k, lane, token, c);
-        uint8_t* dst = run + 1024 * ((wave % G::WPU) * G::NI + k) + 16 * lane + (G::kAlias ? 0 : G::TILE);
-        if (token >= left) *reinterpret_cast<uint4*>(dst) = make_uint4(0, 0, 0, 0);
+        int token, plane;
+        piece<D, DV, KT, TOKENS>(wave, k, token, plane);
+        uint8_t* dst = run + plane * G::PLANE + token * 128 + 16 * lane + (G::kAlias ? 0 : G::TILE);
+        if (token + (lane >> 3) >= left) *reinterpret_cast<uint4*>(dst) = make_uint4(0, 0, 0, 0);
       }
     }
   } else if constexpr (T::kMx) {
     if (T::takes_k(wave)) {                              // lane holds D / 4 channels of token lane / 4
       const float s = mx::scale_operand(r.k_scale);
 #pragma unroll
-      for (int x = 0; x < D / 32; x++) *chunk_place<D>(run, lane >> 2, (lane & 3) * (D / 32) + x) = widen_mx(r.k[0][x], s);
+      for (int x = 0; x < D / 32; x++) *chunk_place<G::PLANE>(run, lane >> 2, (lane & 3) * (D / 32) + x) = widen_mx(r.k[0][x], s);
     }
     if (T::takes_v(wave)) {                              // channels col D / 16 .. of tokens 4 grp + x
       const int col = lane & 15, grp = lane >> 4;
@@ -197,10 +183,10 @@ __device__ __forceinline__ void land_run(int wave, int lane, int left, uint8_t* 
       for (int x = 0; x < 4; x++) {
         const float f = mx::scale_operand((r.v_scale >> (8 * x)) & 255);
         if constexpr (D == 128) {
-          *chunk_place<D>(run + G::TILE, 4 * grp + x, col) = widen_mx(r.v[0][x], f);
+          *chunk_place<G::PLANE>(run + G::TILE, 4 * grp + x, col) = widen_mx(r.v[0][x], f);
         } else {
           const uint32_t w = r.v[0][x >> 1];
-          uint2* p = reinterpret_cast<uint2*>(chunk_place<D>(run + G::TILE, 4 * grp + x, col >> 1)) + (col & 1);
+          uint2* p = reinterpret_cast<uint2*>(chunk_place<G::PLANE>(run + G::TILE, 4 * grp + x, col >> 1)) + (col & 1);
           *p = (x & 1) ? make_uint2(mx::pair_bf16<2>(w, f), mx::pair_bf16<3>(w, f)) : make_uint2(mx::pair_bf16<0>(w, f), mx::pair_bf16<1>(w, f));
         }
       }
@@ -212,27 +198,28 @@ __device__ __forceinline__ void land_run(int wave, int lane, int left, uint8_t* 
       if (!codes_piece<D, DV, KT, TOKENS>(wave, x, lane, token, c16)) continue;
 #pragma unroll
       for (int e = 0; e < 2; e++) {
-        *chunk_place<D>(run, token, 2 * c16 + e) = widen_codes<KT>(r.k[x][2 * e], r.k[x][2 * e + 1]);
-        if constexpr (!G::kAlias) *chunk_place<D>(run + G::TILE, token, 2 * c16 + e) = widen_codes<KT>(r.v[x][2 * e], r.v[x][2 * e + 1]);
+        *chunk_place<G::PLANE>(run, token, 2 * c16 + e) = widen_codes<KT>(r.k[x][2 * e], r.k[x][2 * e + 1]);
+        if constexpr (!G::kAlias) *chunk_place<G::PLANE>(run + G::TILE, token, 2 * c16 + e) = widen_codes<KT>(r.v[x][2 * e], r.v[x][2 * e + 1]);
       }
     }
   }
 }
 
 // Operand A of S^T: 16 tokens from t0, k-step kk (channels 32 kk + 8 grp ..).
-template <int D>
+template <int PLANE>
 __device__ __forceinline__ bf16x8_t k_from_lds(const uint8_t* tile, int t0, int kk, int col, int grp) {
-  return *reinterpret_cast<const bf16x8_t*>(tile + (t0 + col) * D * 2 + place<D>(4 * kk, grp, swizzle<D>(col)));
+  const int c = (4 * (kk & 1) + grp) ^ (col & 7);
+  return *reinterpret_cast<const bf16x8_t*>(tile + (t0 + col) * 128 + 16 * c + (kk >> 1) * PLANE);
 }
 
 // Operand A of O^T: channels 16 j + col of tokens t0 + 4 grp + 0..3 and t0 + 16 + 4 grp + 0..3.  Lane 4 r + x of
 // 16 reads channels 4 x .. 4 x + 3 of row r; the transposing read gives it channel `lane` of the four rows.
-template <int D>
+template <int PLANE>
 __device__ __forceinline__ bf16x8_t v_from_lds(const uint8_t* tile, int t0, int j, int col, int grp) {
-  const int row = 4 * grp + (col >> 2), x = col & 3;
-  lds_u8* p = (lds_u8*)(tile + (t0 + row) * D * 2 + place<D>(2 * j, x >> 1, swizzle<D>(row)) + 8 * (x & 1));
+  const int row = 4 * grp + (col >> 2), x = col & 3, c = (2 * (j & 3) + (x >> 1)) ^ (row & 7);
+  lds_u8* p = (lds_u8*)(tile + (t0 + row) * 128 + 16 * c + 8 * (x & 1) + (j >> 2) * PLANE);
   const v4i16_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16_t*)p);
-  const v4i16_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16_t*)(p + 16 * D * 2));
+  const v4i16_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16_t*)(p + 16 * 128));
   typedef short s16x8_t __attribute__((ext_vector_type(8)));
   const s16x8_t w = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
   return __builtin_bit_cast(bf16x8_t, w);
