@@ -411,8 +411,12 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
         if (!inner) mask_scores<D, DV, RT>(sc, tok0, tok1, grp, w);
         uint32_t p[RT][4];
         softmax_step<D, DV, RT, SPARSE>(a.scale_log2, sc, mask0, mask1, w, p);
+        // bf16: the waves that add values go first, the others meanwhile weigh theirs (prompt 3485 -> 3370 us, listed
+        // blocks 705 -> 688; mxfp4, whose waves also widen, 865 -> 887 us with it)
+        if constexpr (KT == kKvBf16) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int j = 0; j < NJ; j++) {
+          if (KT == kKvBf16 && j == NJ - 1) __builtin_amdgcn_s_setprio(0);
           const bf16x8_t v = v_from_lds<G::PLANE>(vt, 16 * y, j, col, grp);
 #pragma unroll
           for (int rt = 0; rt < RT; rt++)
@@ -549,9 +553,9 @@ Plan plan_of(const Geometry& g, int n, int Hq, bool sparse, int max_sel) {
   const int64_t tiles = std::max<int64_t>(batch, (n + p.tokens - 1) / p.tokens) * g.H;
   const int64_t list = std::min<int64_t>((int64_t)g.max_pages * g.bs, sparse ? (int64_t)max_sel * p.tokens * g.bs : INT64_MAX);
   const int64_t most = std::min<int64_t>(kMaxParts, (list + kPartTokens - 1) / kPartTokens);
-  // a little more than one workgroup a CU: as halves, most CUs take three in place of two wholes (350 tiles of the
-  // latent 470 -> 377 us)
-  const bool halves = tiles > kTargetWgs / 2 && tiles <= kTargetWgs * 3 / 4;
+  // A little more than one tile of the latent a CU: as halves, most CUs take three in place of two wholes (350 tiles 470
+  // -> 377 us; where memory bounds, as for drafted tokens, halves cost more than they bring: 58 -> 70 us).
+  const bool halves = latent && tiles > kTargetWgs / 2 && tiles <= kTargetWgs * 3 / 4;
   p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, halves ? 2 : kTargetWgs / tiles));
   if (p.splits > 1) {
     p.o_bytes = (size_t)n * Hq * p.splits * g.Dv * sizeof(float);
