@@ -577,24 +577,32 @@ void launch_wide(const ChunkArgs& a, dim3 grid, size_t lists, hipStream_t stream
 }
 
 template <int D, int DV, int KT>
-hipError_t launch_kt(const ChunkArgs& a, int operands, hipStream_t stream) {
-  const int64_t tiles = (int64_t)a.num_rows / a.tokens + a.batch;
-  const dim3 grid((unsigned)(tiles * a.H), (unsigned)a.splits);
+void launch_tiles(const ChunkArgs& a, int operands, dim3 grid, hipStream_t stream) {
   if constexpr (D == DV) {
     const size_t lists = a.sel_pages ? 2 * sizeof(uint32_t) * ((a.max_blocks + 1) / 2) : 0;    // at most 64 KiB
-    if (operands == 0) {
-      if (a.sel_pages) launch_narrow<D, KT, true>(a, grid, lists, stream);
-      else launch_narrow<D, KT, false>(a, grid, 0, stream);
-    } else if (a.sel_pages) {
-      launch_wide<D, DV, KT, 1, true>(a, grid, lists, stream);
-    } else if (operands == 1) {
-      launch_wide<D, DV, KT, 1, false>(a, grid, 0, stream);
-    } else {
-      launch_wide<D, DV, KT, 2, false>(a, grid, 0, stream);
+    if constexpr (KT != kKvBf16) {
+      if (operands == 0) {
+        if (a.sel_pages) launch_narrow<D, KT, true>(a, grid, lists, stream);
+        else launch_narrow<D, KT, false>(a, grid, 0, stream);
+        return;
+      }
     }
-  } else {
-    launch_wide<D, DV, KT, 1, false>(a, grid, 0, stream);
+    if (a.sel_pages) {
+      launch_wide<D, DV, KT, 1, true>(a, grid, lists, stream);
+      return;
+    }
+    if (operands == 2) {
+      launch_wide<D, DV, KT, 2, false>(a, grid, 0, stream);
+      return;
+    }
   }
+  launch_wide<D, DV, KT, 1, false>(a, grid, 0, stream);
+}
+
+template <int D, int DV, int KT>
+hipError_t launch_kt(const ChunkArgs& a, int operands, hipStream_t stream) {
+  const int64_t tiles = (int64_t)a.num_rows / a.tokens + a.batch;
+  launch_tiles<D, DV, KT>(a, operands, dim3((unsigned)(tiles * a.H), (unsigned)a.splits), stream);
   if (a.splits > 1) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -4,8 +4,8 @@
 // S^T = K Q^T is a 16x16x32 product: operand A is 16 tokens (row = lane & 15), operand B 16 query rows.  Lane
 // (grp, col) then holds S[token 4 grp + i][row col], which, as bf16, is operand B of O^T = V^T P^T if the
 // contraction's slot (grp, j) is token 4 grp + j of the first 16 tokens (j < 4) or of the second: no value
-// changes lanes between the two products.  Row `col` of V^T operand j is channel col * D / 16 + j, so that a
-// lane's channels are neighbours in a V row.
+// changes lanes between the two products.  Operands straight from the cache (RawV): row `col` of V^T operand j is channel
+// col * D / 16 + j, so that a lane's channels are neighbours in a V row.
 #pragma once
 #include "chunk_common.h"
 
@@ -35,15 +35,15 @@ __device__ __forceinline__ int k_channel(int kk, int grp) {
   return KT == kKvBf16 ? 32 * kk + 8 * grp : D / 4 * grp + 8 * kk;
 }
 
-// 16 tokens of K, and of V, as loaded.
+// 16 tokens of K, and of V, as loaded: fp8 or mxfp4.
 template <int D, int KT>
 struct RawK {
-  static constexpr int W = KT == kKvBf16 ? D / 8 : KT == kKvMxFp4 ? D / 32 : D / 16;     // words of a lane's part
+  static constexpr int W = KT == kKvMxFp4 ? D / 32 : D / 16;     // words of a lane's part
   uint32_t w[W], scale;                    // scale: mxfp4
 };
 template <int D, int KT>
 struct RawV {
-  static constexpr int W = KT == kKvBf16 ? D / 32 : KT == kKvMxFp4 ? D / 128 : D / 64;   // words of a row's
+  static constexpr int W = D / 64;         // words of an fp8 row's part
   static constexpr int N = KT == kKvMxFp4 ? D / 32 : 4 * W;
   uint32_t w[N], scale;
 };
@@ -61,7 +61,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const uint8_t* base, int 
 // Tokens t .. t + 15 (t a multiple of 16, the same in all lanes) of a page, the first n of which are looked at.
 template <int D, int KT>
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const ChunkArgs& a, const uint8_t* slice, int t, int n) {
-  constexpr int kRow = KT == kKvBf16 ? 2 * D : KT == kKvMxFp4 ? D / 2 : D;
+  constexpr int kRow = KT == kKvMxFp4 ? D / 2 : D;
   // mxfp4: four tokens of V share their codes' bytes; what is not looked at goes by its scale
   return rsrc(slice + t * kRow, (KT == kKvMxFp4 ? 16 : n) * kRow);
 }
@@ -97,9 +97,6 @@ __device__ __forceinline__ void load_k(const ChunkArgs& a, const uint8_t* slice,
   if constexpr (KT == kKvMxFp4) {
     load_words<D / 32>(k, col * (D / 2) + D / 8 * grp, r.w);
     r.scale = __builtin_amdgcn_raw_buffer_load_b8(scales_of<D>(a, slice, t), col * (D / 32) + D / 4 * grp / 32, 0, 0);
-  } else if constexpr (KT == kKvBf16) {
-#pragma unroll
-    for (int kk = 0; kk < D / 32; kk++) load_words<4>(k, 2 * (col * D + 8 * grp) + 64 * kk, r.w + 4 * kk);
   } else {
     load_words<D / 16>(k, col * D + D / 4 * grp, r.w);
   }
@@ -113,9 +110,9 @@ __device__ __forceinline__ void load_v(const ChunkArgs& a, const uint8_t* slice,
     const int left = n - 4 * grp;                        // byte x: token 4 grp + x; a scale of 0 is 2^-127
     r.scale &= left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1;
   } else {
-    constexpr int B = KT == kKvBf16 ? 2 : 1, W = RawV<D, KT>::W;
+    constexpr int W = RawV<D, KT>::W;
 #pragma unroll
-    for (int x = 0; x < 4; x++) load_words<W>(v, B * (4 * grp * D + col * (D / 16)) + B * x * D, r.w + x * W);
+    for (int x = 0; x < 4; x++) load_words<W>(v, (4 * grp + x) * D + col * (D / 16), r.w + x * W);
   }
 }
 
@@ -123,9 +120,7 @@ __device__ __forceinline__ void load_v(const ChunkArgs& a, const uint8_t* slice,
 template <int D, int KT>
 __device__ __forceinline__ bf16x8_t k_operand(const RawK<D, KT>& r, int kk) {
   u32x4_t w;
-  if constexpr (KT == kKvBf16) {
-    w = u32x4_t{r.w[4 * kk], r.w[4 * kk + 1], r.w[4 * kk + 2], r.w[4 * kk + 3]};
-  } else if constexpr (KT == kKvMxFp4) {
+  if constexpr (KT == kKvMxFp4) {
     const float s = mx::scale_operand(r.scale);
     const uint32_t c = r.w[kk];
     w = u32x4_t{mx::pair_bf16<0>(c, s), mx::pair_bf16<1>(c, s), mx::pair_bf16<2>(c, s), mx::pair_bf16<3>(c, s)};
@@ -141,10 +136,7 @@ template <int D, int KT>
 __device__ __forceinline__ void v_rows(const RawV<D, KT>& r, uint32_t (&v)[4][D / 32]) {
 #pragma unroll
   for (int x = 0; x < 4; x++) {
-    if constexpr (KT == kKvBf16) {
-#pragma unroll
-      for (int w = 0; w < D / 32; w++) v[x][w] = r.w[x * (D / 32) + w];
-    } else if constexpr (KT == kKvMxFp4) {
+    if constexpr (KT == kKvMxFp4) {
       const float s = mx::scale_operand((r.scale >> (8 * x)) & 255);
       if constexpr (D == 128) {
         v[x][0] = mx::pair_bf16<0>(r.w[x], s);
