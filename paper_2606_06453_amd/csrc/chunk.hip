@@ -136,7 +136,11 @@ __device__ __forceinline__ Runs part_runs(const ChunkArgs& a, const Tile& t, int
 }
 
 // Four waves share a tile of 16 query rows; each takes every fourth pair of 16-token runs of the tile's list,
-// straight from the cache into matrix operands, and the waves' states meet in LDS.
+// straight from the cache into matrix operands, and the waves' states meet in LDS.  For few rows over fp8 or mxfp4 caches,
+// which memory bounds: no barrier stands between loads and their use, and codes widen once for 16 rows (drafted tokens of
+// 32 users over 64 listed blocks of 32 tokens, E4M3: 57 us, 6.4 TB/s of the 7.05 that a stream reads; in wide tiles 124).
+// bf16 rows take wide tiles from the first row: straight to LDS they need no register on their way (4 users' drafted
+// tokens 92 us, here 125).
 template <int D, int KT, bool SPARSE>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void chunk_narrow_kernel(const ChunkArgs a) {
   constexpr int KS = D / 32, NJ = D / 16, W = D / 32;
@@ -281,14 +285,22 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   }
 }
 
-// Four waves of 16 RT rows each share the tokens of their tile through LDS (chunk_wide.h).  A wave passes over
-// runs that none of its rows attends.
 // Tokens of a buffer.  Listed blocks are short runs in any place, which take longest to arrive: half the tokens let
 // twice the workgroups wait side by side (4096 tokens over 128 blocks each 1069 -> 923 us; dense prompts are 1% slower
-// with them).  The latent's rows are 4.5 times longer.
+// with them).  The latent's rows are 4.5 times longer, and two workgroups of 72 KB share a CU.
 template <int D, int DV, bool SPARSE>
 constexpr int kTokens = SPARSE || D != DV ? 32 : 64;
 
+// Four waves of 16 RT rows each share the tokens of their tile through LDS (chunk_wide.h).  A wave passes over
+// runs that none of its rows attends.  Two operands of rows a wave halve the reads of LDS a product; one serves tiles of
+// up to 64 rows, listed blocks (16 tokens a mask) and the latent, whose 512 output channels fill the registers.
+//   a prompt's last 8192 of 32768 tokens, 32 heads over 8, bf16: 3310 us, 1160 TFLOP/s (a library product of 16384^3
+//     1356); matrix instructions 52% and vector ones 49% of the time, which hardly overlap within two waves a SIMD
+//   prompts and drafts of 48 requests, mxfp4: 860 us, 770 TFLOP/s; 35% and 45%, and the widened rows' way to LDS
+//   prompts under a window of 1000 tokens, 64 channels, E4M3: 94 us; 31% and 69%: the softmax, which D does not shorten
+//   the latent, eight prompts' chunks: 287 us with the join, 735 TFLOP/s; 37% and 18%, LDS 37%
+//   4096 tokens over 128 listed blocks of 16 each: 680 us; 30% and 47%.  A wave's four tokens list 2.3 times the blocks
+//     of one, so 203 TFLOP/s of what the tokens list are 600 of products
 template <int D, int DV, int KT, int RT, bool SPARSE>
 __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int h, int split, uint32_t* lds) {
   constexpr int TK = kTokens<D, DV, SPARSE>;
@@ -476,7 +488,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(D == D
 }
 
 // Joins the parts of every row, a wave a row and a token a workgroup (a.tokens is 1): each part's weight is its
-// sum at the row's largest reference.
+// sum at the row's largest reference.  Memory bounds it: 16 heads of 1241 tokens in two parts of 512 channels 23 us
+// (4.5 TB/s), 16 parts of drafted tokens 6 us.
 template <int DV>
 __global__ __launch_bounds__(kThreads) void chunk_merge_kernel(const ChunkArgs a) {
   constexpr int N = DV / kWave, kBatch = 8;              // channels of a lane; parts on their way at a time
@@ -601,14 +614,14 @@ void launch_tiles(const ChunkArgs& a, int operands, dim3 grid, hipStream_t strea
 
 template <int D, int DV, int KT>
 hipError_t launch_kt(const ChunkArgs& a, int operands, hipStream_t stream) {
-  const int64_t tiles = (int64_t)a.num_rows / a.tokens + a.batch;
+  const int64_t tiles = most_tiles(a.num_rows, a.tokens, a.batch);
   launch_tiles<D, DV, KT>(a, operands, dim3((unsigned)(tiles * a.H), (unsigned)a.splits), stream);
   if (a.splits > 1) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     ChunkArgs m = a;
     m.tokens = 1;
-    const int64_t rows = (int64_t)a.num_rows + a.batch;
+    const int64_t rows = most_tiles(a.num_rows, 1, a.batch);
     hipLaunchKernelGGL((chunk_merge_kernel<DV>), dim3((unsigned)(rows * a.H)), dim3(kThreads), 0, stream, m);
   }
   return hipGetLastError();

@@ -108,6 +108,11 @@ __device__ __forceinline__ bool find_tile(const ChunkArgs& a, int x, Tile& t) {
   return true;
 }
 
+// Tiles that n rows of a batch can have: the grid of find_tile.
+inline int64_t most_tiles(int64_t n, int tokens, int64_t batch) {
+  return batch <= kWave ? (n + batch * (tokens - 1)) / tokens : (n + tokens - 1) / tokens + batch - 1;
+}
+
 // The tokens [lo, hi) that the token at position p attends.
 __device__ __forceinline__ int first_key(const ChunkArgs& a, int p) {
   return a.window > 0 ? max(p - a.window + 1, 0) : 0;

@@ -18,6 +18,8 @@
 // its square is lost, select by digits of the exact scores alone, which they compute anew for every digit.
 // One kernel that kept the scores of 32 tokens in LDS took 388 us for 4096 tokens over 2048 blocks and 55 us for a few
 // users' drafted tokens: a row's passes waited with two waves a SIMD, and few tokens left most of the chip idle.
+// Now 234 and 38 us: 4096 tokens take 98 us of scores and 122 us of choosing, which vector instructions bound (2200 a
+// row); eight users' 4 tokens each 19 us and 17 us, which are the latencies of a few dependent passes.
 #include <algorithm>
 
 #include "chunk_tile.h"
@@ -180,7 +182,9 @@ __device__ __forceinline__ void select_by_digits(const ChunkArgs& a, const Selec
   }
 }
 
-// CG groups of 16 tokens.
+// CG groups of 16 tokens, all of whose queries stay in registers, and a part of the blocks.  4096 tokens over 2048
+// blocks of 8 heads, 98 us: matrix instructions 25% and vector ones, which split the means (once for 64 tokens), 34% of
+// the time; the means come from the caches, 8 MB for every 64 tokens.
 template <int D, int CG>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void chunk_score_kernel(const ChunkArgs a, const SelectArgs s) {
   constexpr int KS = D / 32;
@@ -310,7 +314,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   if (tid == 0) *norm_out = __uint_as_float(norm_m);
 }
 
-// A wave a row.
+// A wave a row; six waves a SIMD, for a row's passes depend on one another (two: 264 -> 238 us for 4096 tokens,
+// scores included).  Vector instructions bound it.
 template <int D>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6))) void chunk_choose_kernel(const ChunkArgs a, const SelectArgs s) {
   extern __shared__ __attribute__((aligned(16))) uint16_t slab[];          // [wave][stride]
@@ -566,7 +571,7 @@ SelectPlan plan_of(const Geometry& g, int n) {
   SelectPlan p{};
   const int64_t batch = std::max(g.batch, 1);
   p.tokens = (int64_t)n <= 16 * batch ? 16 : 64;
-  p.tiles = (int64_t)n / p.tokens + batch;
+  p.tiles = most_tiles(n, p.tokens, batch);
   p.stride = (g.max_pages + 63) & ~63;
   const size_t tile = (size_t)p.tokens * g.H * p.stride * sizeof(uint16_t);
   p.at_once = (int)std::max<int64_t>(1, std::min<int64_t>(p.tiles, (int64_t)(kScoreBytes / tile)));
@@ -602,7 +607,7 @@ hipError_t launch(const ChunkArgs& a, SelectArgs& s, const SelectPlan& p, hipStr
 
 }  // namespace
 
-size_t chunk_select_workspace(const Geometry& g, int n, int Hq) { return plan_of(g, n).bytes; }
+size_t chunk_select_workspace(const Geometry& g, int n) { return plan_of(g, n).bytes; }
 
 hipError_t launch_chunk_select(const Geometry& g, const ChunkRows& rows, const float* mean, const int32_t* budget,
                                int n_sink, int n_local, int max_sel, int32_t* sel_pages, int32_t* sel_count, void* ws,

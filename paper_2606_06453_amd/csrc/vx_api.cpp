@@ -870,7 +870,7 @@ vx_status vx_chunk_workspace_size(vx_chunk_stage stage, const vx_paged_cache* kv
   if (stage != VX_CHUNK_ATTENTION && max_sel < 1) return fail(VX_ERR_INVALID_ARG, "max_sel must be >= 1");
   const vx::Geometry g = geometry(kv, b);
   *bytes = stage == VX_CHUNK_SCORE_TOPK
-               ? vx::chunk_select_workspace(g, num_rows, num_q_heads)
+               ? vx::chunk_select_workspace(g, num_rows)
                : vx::chunk_attention_workspace(g, num_rows, num_q_heads, stage == VX_CHUNK_SPARSE, max_sel);
   return VX_OK;
 }
@@ -905,7 +905,7 @@ vx_status vx_chunk_score_topk(const void* q, int64_t q_row_stride, int64_t q_hea
   if ((int64_t)n_sink + n_local > max_sel) return fail(VX_ERR_INVALID_ARG, "n_sink + n_local must be <= max_sel");
   if (chunk->num_rows == 0 || b->batch == 0) return VX_OK;
   const vx::Geometry g = geometry(kv, b);
-  const size_t need = vx::chunk_select_workspace(g, chunk->num_rows, num_q_heads);
+  const size_t need = vx::chunk_select_workspace(g, chunk->num_rows);
   if ((s = check_workspace("vx_chunk_score_topk", workspace, workspace_bytes, need)) != VX_OK) return s;
   if (!mean || !pages_budget || !sel_pages || !sel_count)
     return fail(VX_ERR_INVALID_ARG, "mean, pages_budget, sel_pages and sel_count must be non-NULL");

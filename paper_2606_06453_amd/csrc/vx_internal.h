@@ -142,7 +142,7 @@ size_t chunk_attention_workspace(const Geometry& g, int n, int Hq, bool sparse, 
 hipError_t launch_chunk_attention(const Geometry& g, const ChunkRows& rows, const ChunkSelection& sel, int window,
                                   bool causal, float sm_scale, uint16_t* out, float* lse, void* ws, hipStream_t stream);
 
-size_t chunk_select_workspace(const Geometry& g, int n, int Hq);
+size_t chunk_select_workspace(const Geometry& g, int n);
 hipError_t launch_chunk_select(const Geometry& g, const ChunkRows& rows, const float* mean, const int32_t* budget,
                                int n_sink, int n_local, int max_sel, int32_t* sel_pages, int32_t* sel_count, void* ws,
                                hipStream_t stream);
