@@ -286,16 +286,19 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 }
 
 // Tokens of a buffer.  Listed blocks are short runs in any place, which take longest to arrive: half the tokens let
-// twice the workgroups wait side by side (4096 tokens over 128 blocks each 1069 -> 923 us; dense prompts are 1% slower
-// with them).  The latent's rows are 4.5 times longer, and two workgroups of 72 KB share a CU.
-template <int D, int DV, bool SPARSE>
-constexpr int kTokens = SPARSE || D != DV ? 32 : 64;
+// twice the workgroups wait side by side (4096 tokens over 128 blocks each 1069 -> 923 us).  bf16 rows of 128 channels:
+// with 32 the prompt kernel has room for three waves a SIMD (3290 -> 3215 us; with two 3390); the types that pass
+// through registers want 64 (mxfp4 864, with 32 1160 us).  The latent's rows are 4.5 times longer, and two workgroups of
+// 72 KB share a CU.
+template <int D, int DV, int KT, bool SPARSE>
+constexpr int kTokens = SPARSE || D != DV || (KT == kKvBf16 && D == 128) ? 32 : 64;
 
 // Four waves of 16 RT rows each share the tokens of their tile through LDS (chunk_wide.h).  A wave passes over
 // runs that none of its rows attends.  Two operands of rows a wave halve the reads of LDS a product; one serves tiles of
 // up to 64 rows, listed blocks (16 tokens a mask) and the latent, whose 512 output channels fill the registers.
-//   a prompt's last 8192 of 32768 tokens, 32 heads over 8, bf16: 3310 us, 1160 TFLOP/s (a library product of 16384^3
-//     1356); matrix instructions 52% and vector ones 49% of the time, which hardly overlap within two waves a SIMD
+//   a prompt's last 8192 of 32768 tokens, 32 heads over 8, bf16: 3275 us, 1176 TFLOP/s (a library product of 16384^3
+//     1356); matrix instructions 59% and vector ones 56% of the cycles, at 1.9 GHz: 11% fewer cycles by a third wave a
+//     SIMD were 2% less time
 //   prompts and drafts of 48 requests, mxfp4: 860 us, 770 TFLOP/s; 35% and 45%, and the widened rows' way to LDS
 //   prompts under a window of 1000 tokens, 64 channels, E4M3: 94 us; 31% and 69%: the softmax, which D does not shorten
 //   the latent, eight prompts' chunks: 287 us with the join, 735 TFLOP/s; 37% and 18%, LDS 37%
@@ -303,7 +306,7 @@ constexpr int kTokens = SPARSE || D != DV ? 32 : 64;
 //     of one, so 203 TFLOP/s of what the tokens list are 600 of products
 template <int D, int DV, int KT, int RT, bool SPARSE>
 __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int h, int split, uint32_t* lds) {
-  constexpr int TK = kTokens<D, DV, SPARSE>;
+  constexpr int TK = kTokens<D, DV, KT, SPARSE>;
   using G = Wide<D, DV, KT, TK>;
   constexpr int KS = D / 32, NJ = DV / 16;
   const int tid = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -317,15 +320,17 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
   const int r0 = wave * 16 * RT;
   Rows<D, DV, RT> w;
   begin_rows<D, DV, kKvBf16, RT>(a, t, h, r0, col, grp, w);
+  // the tile tokens of this wave's rows, and what they attend between them
+  const int x0 = min(r0 / a.g, t.n), x1 = min((r0 + 16 * RT - 1) / a.g, t.n - 1);
+  const int wave_from = first_key(a, t.p0 + x0);
+  int wave_to = r0 < rows ? end_key(a, t, t.p0 + x1) : 0;
   if constexpr (!SPARSE) {                               // what lies behind the part is for the others
     const int end = min(runs.hi, INT_MAX >> 4) << 4;
+    wave_to = min(wave_to, end);
     w.all_to = min(w.all_to, end);
 #pragma unroll
     for (int rt = 0; rt < RT; rt++) w.to[rt] = min(w.to[rt], end);
   }
-  // the tile tokens of this wave's rows, and what they attend between them
-  const int x0 = min(r0 / a.g, t.n), x1 = min((r0 + 16 * RT - 1) / a.g, t.n - 1);
-  const int wave_from = first_key(a, t.p0 + x0), wave_to = r0 < rows ? end_key(a, t, t.p0 + x1) : 0;
   const int wave_mask = SPARSE && r0 < rows ? (2 << x1) - (1 << x0) : 0;
 
   const int n16 = (runs.hi - runs.lo) << shift16, steps = (n16 + G::UNITS - 1) / G::UNITS;
@@ -471,9 +476,13 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
   if (__syncthreads_or(bad)) attend_rows<D, DV, KT>(a, t, h, runs, split);
 }
 
-// The latent's rows take 250 registers of two waves a SIMD; as fp8 they need more and have one.
+// The latent's rows take 250 registers of two waves a SIMD; as fp8 they need more and have one.  Prompts of bf16 rows
+// keep nine words of the setup in scratch for a third wave.
+template <int D, int DV, int KT, int RT>
+constexpr int kWavesPerSimd = D != DV ? (KT == kKvBf16 ? 2 : 1) : KT == kKvBf16 && D == 128 && RT == 2 ? 3 : 2;
+
 template <int D, int DV, int KT, int RT, bool SPARSE>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(D == DV || KT == kKvBf16 ? 2 : 1))) void chunk_wide_kernel(const ChunkArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd<D, DV, KT, RT>))) void chunk_wide_kernel(const ChunkArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
   const int h = (int)blockIdx.x % a.H, split = (int)blockIdx.y;
   Tile t;
@@ -585,7 +594,7 @@ void launch_narrow(const ChunkArgs& a, dim3 grid, size_t lists, hipStream_t stre
 }
 template <int D, int DV, int KT, int RT, bool SPARSE>
 void launch_wide(const ChunkArgs& a, dim3 grid, size_t lists, hipStream_t stream) {
-  const size_t lds = 2 * (size_t)Wide<D, DV, KT, kTokens<D, DV, SPARSE>>::BUF + lists;
+  const size_t lds = 2 * (size_t)Wide<D, DV, KT, kTokens<D, DV, KT, SPARSE>>::BUF + lists;
   hipLaunchKernelGGL((chunk_wide_kernel<D, DV, KT, RT, SPARSE>), grid, dim3(kThreads), lds, stream, a);
 }
 

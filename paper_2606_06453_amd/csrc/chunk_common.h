@@ -202,8 +202,6 @@ __device__ void attend_row(const ChunkArgs& a, const Tile& t, int h, int r, int 
   const int p = t.p0 + x, from = first_key(a, p), to = end_key(a, t, p);
   const uint16_t* q = a.q + (t.row0 + x) * a.q_row + (int64_t)(h * a.g + r) * a.q_head;
   const void* vbase = a.v ? a.v : a.k;
-  const int vD = a.v ? DV : D;
-  (void)vD;
   st.m = -INFINITY;
   st.l = 0.f;
 #pragma unroll

@@ -243,7 +243,7 @@ __device__ __forceinline__ void mask_scores(f32x4_t (&s)[RT][2], int tok0, int t
 // One step of the softmax: the scores s of 32 tokens become weights p, bf16, operand B of O^T = V^T P^T.  The
 // weights are taken at the present references first and seldom reach 2 (bit 14 of a bf16 number; infinities and
 // NaN have it too); only then the references move.  The sum takes the weights before their rounding, which is to the
-// nearest (2^-9 of each at most, without a bias) and halves the matrix work that two parts would need.
+// nearest (2^-8 of each at most, without a bias) and halves the matrix work that two parts would need.
 // LISTED: mask0 and mask1 hold the tile tokens that list the first and the last 16 tokens; another's reference for
 // them is infinite, and their weights are zero.
 template <int D, int DV, int RT, bool LISTED>

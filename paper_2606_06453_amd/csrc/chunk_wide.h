@@ -1,5 +1,4 @@
-// The wide tile kernel: four waves of 16 RT query rows each share every 64 (listed blocks, latent: 32) tokens of K and
-// V in LDS.
+// The wide tile kernel: four waves of 16 RT query rows each share every 64 or 32 tokens of K and V in LDS.
 //
 // LDS holds bf16 channels in D / 64 planes of 128 bytes a token, chunks of 16 bytes.  bf16 rows go there straight from
 // memory (each lane of a load picks its source, so the swizzle costs nothing), other types pass through registers,

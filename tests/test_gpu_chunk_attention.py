@@ -54,6 +54,24 @@ def test_latent(kind, before, new):
     _check(c, *_run(c))
 
 
+@pytest.mark.parametrize("kind", KINDS[:2])
+@pytest.mark.parametrize("before,new", [([3000, 40, 1500], [3, 70, 1]), ([1100, 0, 600, 900, 300, 1050, 20, 800], [161, 160, 150, 170, 155, 165, 149, 163])])
+def test_latent_in_parts(kind, before, new):
+    """Long lists of few tiles, and a little more than one tile a CU, which is cut into two parts."""
+    c = Chunk([13, len(before)], before, new, 16, 1, MLA_D, ps=64, kv=kind, sigma=0.5)
+    _check(c, *_run(c))
+
+
+@pytest.mark.parametrize("D,new", [(128, 33), (64, 65), (128, 1)])
+def test_requests_that_fill_the_grid(D, new):
+    """As many tiles as rows can have: every request one row past whole tiles; and the same with refused requests."""
+    for n in (3, 64, 67):
+        c = Chunk([n, new], [(17 * i) % 90 for i in range(n)], [new] * n, 8, 2, D)
+        _check(c, *_run(c))
+        c.q_lens = np.array([0 if i % 3 == 1 else new for i in range(n)], np.int32)
+        _check(c, *_run(c))
+
+
 @pytest.mark.parametrize("before,new", [([0], [1]), ([15], [1]), ([16], [1]), ([0], [16]), ([63], [2]), ([1000], [1]), ([2047, 5], [2, 1]),
                                         ([0], [257]), ([100], [300]), ([511], [129]), ([0] * 9, [1, 2, 3, 15, 16, 17, 31, 32, 33]),
                                         (list(range(0, 130, 2)), [1] * 65), (list(range(0, 70)), [1 + i % 3 for i in range(70)])])

@@ -67,6 +67,16 @@ def test_lengths(before, new, M):
     _check(c, *_attend(c, sel, count), sel, count)
 
 
+@pytest.mark.parametrize("n,new", [(3, 17), (64, 17), (67, 17), (70, 1)])
+def test_requests_that_fill_the_grid(n, new):
+    """As many tiles as rows can have, and the same with refused requests."""
+    c = Chunk([n, new, 5], [(37 * i) % 200 for i in range(n)], [new] * n, 8, 2, 64)
+    sel, count = _lists(c, [n, 3], 8)
+    _check(c, *_attend(c, sel, count), sel, count)
+    c.q_lens = np.array([0 if i % 3 == 1 else new for i in range(n)], np.int32)
+    _check(c, *_attend(c, sel, count), sel, count)
+
+
 def test_lists_as_they_come():
     """Any order, blocks listed twice, ids outside the row's blocks, counts of zero, below zero and past the lists,
     rows of no token."""
@@ -154,6 +164,15 @@ def test_select_layouts(D, H, g, ps, block):
 def test_select_lengths(before, new, M, n_sink, n_local):
     c = Chunk([len(before), 4], before, new, 4, 2, 64)
     _same(c, _mean(c, [M, 6]), [M] * len(before), n_sink, n_local, M)
+
+
+@pytest.mark.parametrize("n,new", [(3, 17), (64, 17), (67, 17), (5, 65), (70, 1)])
+def test_select_requests_that_fill_the_grid(n, new):
+    c = Chunk([n, new, 6], [(137 * i) % 600 for i in range(n)], [new] * n, 4, 2, 64)
+    mean, budget = _mean(c, [n, 8]), [7] * n
+    _same(c, mean, budget, 1, 2, 7)
+    c.q_lens = np.array([0 if i % 3 == 1 else new for i in range(n)], np.int32)
+    _same(c, mean, budget, 1, 2, 7)
 
 
 @pytest.mark.parametrize("what", ["equal", "two_values", "signed_zeros", "close", "huge", "bf16_ties", "nan", "inf"])
