@@ -18,8 +18,8 @@
 // its square is lost, select by digits of the exact scores alone, which they compute anew for every digit.
 // One kernel that kept the scores of 32 tokens in LDS took 388 us for 4096 tokens over 2048 blocks and 55 us for a few
 // users' drafted tokens: a row's passes waited with two waves a SIMD, and few tokens left most of the chip idle.
-// Now 234 and 38 us: 4096 tokens take 98 us of scores and 122 us of choosing, which vector instructions bound (2200 a
-// row); eight users' 4 tokens each 19 us and 17 us, which are the latencies of a few dependent passes.
+// Now 230 and 36 us: 4096 tokens take 95 us of scores and 122 us of choosing, which vector instructions bound (2200 a
+// row); eight users' 4 tokens each 17 us and 17 us, which are the latencies of a few dependent passes.
 #include <algorithm>
 
 #include "chunk_tile.h"
@@ -33,7 +33,7 @@ constexpr int kBins = 256;
 constexpr int kMostOpen = 128;
 constexpr int kFewInBin = 32;
 constexpr int kTogether = 2;               // times 8 open blocks whose means travel together
-constexpr int kScoreWgs = 1024;            // workgroups of the scores that fill the chip
+constexpr int kScoreWgs = 512;             // workgroups of the scores that fill the chip (1024: 234 and 38 us where 230 and 36 are, at the top)
 constexpr int kUnit = 32;                  // blocks that a wave looks up at a time
 constexpr size_t kScoreBytes = (size_t)128 << 20;        // of scores at a time: half of the last cache
 constexpr float kBound = 1.f / 4096.f;                   // twice the bound above
@@ -183,7 +183,7 @@ __device__ __forceinline__ void select_by_digits(const ChunkArgs& a, const Selec
 }
 
 // CG groups of 16 tokens, all of whose queries stay in registers, and a part of the blocks.  4096 tokens over 2048
-// blocks of 8 heads, 98 us: matrix instructions 25% and vector ones, which split the means (once for 64 tokens), 34% of
+// blocks of 8 heads, 95 us: matrix instructions 25% and vector ones, which split the means (once for 64 tokens), 34% of
 // the time; the means come from the caches, 8 MB for every 64 tokens.
 template <int D, int CG>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void chunk_score_kernel(const ChunkArgs a, const SelectArgs s) {
