@@ -476,10 +476,11 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
   if (__syncthreads_or(bad)) attend_rows<D, DV, KT>(a, t, h, runs, split);
 }
 
-// The latent's rows take 250 registers of two waves a SIMD; as fp8 they need more and have one.  Prompts of bf16 rows
+// The latent's rows just fit two waves a SIMD; as fp8 30 words go to scratch, and yet one wave takes longer (44 requests'
+// drafted tokens 326 us, 412 with one; prompts 273 and 386).  Prompts of bf16 rows
 // keep nine words of the setup in scratch for a third wave.
 template <int D, int DV, int KT, int RT>
-constexpr int kWavesPerSimd = D != DV ? (KT == kKvBf16 ? 2 : 1) : KT == kKvBf16 && D == 128 && RT == 2 ? 3 : 2;
+constexpr int kWavesPerSimd = KT == kKvBf16 && D == 128 && RT == 2 ? 3 : 2;
 
 template <int D, int DV, int KT, int RT, bool SPARSE>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd<D, DV, KT, RT>))) void chunk_wide_kernel(const ChunkArgs a) {

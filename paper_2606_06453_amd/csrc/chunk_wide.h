@@ -78,7 +78,7 @@ __device__ __forceinline__ void piece(int wave, int k, int& token, int& plane) {
 template <int D, int DV, int KT, int TOKENS>
 struct Travel {
   static constexpr bool kMx = KT == kKvMxFp4;
-  static constexpr int N = kMx ? 1 : (D + 64 * Wide<D, DV, KT, TOKENS>::WPU - 1) / (64 * Wide<D, DV, KT, TOKENS>::WPU);
+  static constexpr int N = kMx ? 1 : (D / 64 + Wide<D, DV, KT, TOKENS>::WPU - 1) / Wide<D, DV, KT, TOKENS>::WPU;
   static constexpr int W = kMx ? D / 32 : 4;
   // mxfp4: of two waves that load a run one takes K, the other V
   static __device__ __forceinline__ bool takes_k(int wave) { return Wide<D, DV, KT, TOKENS>::WPU == 1 || (wave & 1) == 0; }
@@ -86,14 +86,11 @@ struct Travel {
   uint32_t k[N][W], v[Wide<D, DV, KT, TOKENS>::kAlias ? 1 : N][W], k_scale, v_scale;
 };
 
-// fp8: lane's piece x of a run, token and 16 channels; false past the run.
+// fp8: the plane of a wave's piece x of a run (none: D / 64), of which lane l takes the l % 4th 16 channels of token l / 4.
 template <int D, int DV, int KT, int TOKENS>
-__device__ __forceinline__ bool codes_piece(int wave, int x, int lane, int& token, int& c16) {
+__device__ __forceinline__ int codes_plane(int wave, int x) {
   using G = Wide<D, DV, KT, TOKENS>;
-  const int slot = 64 * ((wave % G::WPU) * Travel<D, DV, KT, TOKENS>::N + x) + lane;
-  token = slot / (D / 16);
-  c16 = slot % (D / 16);
-  return slot < D;
+  return min(G::WPU * x + wave % G::WPU, D / 64);
 }
 
 // Starts a run's way into the buffer (bf16), or into registers.  t: its first token's place in the page; left: its
@@ -131,9 +128,9 @@ __device__ __forceinline__ void send_run(const ChunkArgs& a, const uint8_t* ks, 
     const int n = min(left, 16);
 #pragma unroll
     for (int x = 0; x < T::N; x++) {
-      int token, c16;
-      codes_piece<D, DV, KT, TOKENS>(wave, x, lane, token, c16);
-      const int off = token * D + 16 * c16;              // past the run it is past the resource too
+      const int plane = codes_plane<D, DV, KT, TOKENS>(wave, x);
+      if (plane == D / 64) continue;
+      const int off = (lane >> 2) * D + 16 * (lane & 3) + 64 * plane;
       load_words<4>(rows_of<D, KT>(a, ks, t, n), off, r.k[x]);
       if constexpr (!G::kAlias) load_words<4>(rows_of<D, KT>(a, vs, t, n), off, r.v[x]);
     }
@@ -193,13 +190,18 @@ __device__ __forceinline__ void land_run(int wave, int lane, int left, uint8_t* 
   } else {
 #pragma unroll
     for (int x = 0; x < T::N; x++) {
-      int token, c16;
-      if (!codes_piece<D, DV, KT, TOKENS>(wave, x, lane, token, c16)) continue;
+      const int plane = codes_plane<D, DV, KT, TOKENS>(wave, x), token = lane >> 2;
+      if (plane == D / 64) continue;
+      // every other pair of tokens begins with its second chunk: first chunks alone leave half of the banks idle
+      const int odd = (token >> 1) & 1;
+      auto put = [&](uint8_t* to, const uint32_t (&w)[T::W]) {
 #pragma unroll
-      for (int e = 0; e < 2; e++) {
-        *chunk_place<G::PLANE>(run, token, 2 * c16 + e) = widen_codes<KT>(r.k[x][2 * e], r.k[x][2 * e + 1]);
-        if constexpr (!G::kAlias) *chunk_place<G::PLANE>(run + G::TILE, token, 2 * c16 + e) = widen_codes<KT>(r.v[x][2 * e], r.v[x][2 * e + 1]);
-      }
+        for (int e = 0; e < 2; e++)
+          *chunk_place<G::PLANE>(to + plane * G::PLANE, token, 2 * (lane & 3) + (e ^ odd)) =
+              widen_codes<KT>(odd ? w[2 - 2 * e] : w[2 * e], odd ? w[3 - 2 * e] : w[2 * e + 1]);
+      };
+      put(run, r.k[x]);
+      if constexpr (!G::kAlias) put(run + G::TILE, r.v[x]);
     }
   }
 }
