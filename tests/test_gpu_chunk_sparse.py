@@ -77,6 +77,15 @@ def test_requests_that_fill_the_grid(n, new):
     _check(c, *_attend(c, sel, count), sel, count)
 
 
+@pytest.mark.parametrize("kind", KINDS[:2] + KINDS[3:])
+@pytest.mark.parametrize("new,D", [(3, 64), (70, 128)])
+def test_most_blocks_of_a_request(kind, new, D):
+    """16384 blocks: the lists' largest marks, in narrow and wide tiles."""
+    c = Chunk([new, D, 7], [(1 << 18) - new], [new], 2, 1, D, kv=kind)
+    sel, count = _lists(c, [new, 4], 40)
+    _check(c, *_attend(c, sel, count), sel, count)
+
+
 def test_lists_as_they_come():
     """Any order, blocks listed twice, ids outside the row's blocks, counts of zero, below zero and past the lists,
     rows of no token."""
@@ -173,6 +182,12 @@ def test_select_requests_that_fill_the_grid(n, new):
     _same(c, mean, budget, 1, 2, 7)
     c.q_lens = np.array([0 if i % 3 == 1 else new for i in range(n)], np.int32)
     _same(c, mean, budget, 1, 2, 7)
+
+
+@pytest.mark.parametrize("new", [2, 19])
+def test_select_among_most_blocks(new):
+    c = Chunk([new, 9], [(1 << 18) - new], [new], 4, 2, 64)
+    _same(c, _mean(c, [new, 10]), [100], 1, 2, 100)
 
 
 @pytest.mark.parametrize("what", ["equal", "two_values", "signed_zeros", "close", "huge", "bf16_ties", "nan", "inf"])
