@@ -7,8 +7,6 @@
 // A tile whose sums are not finite is done again row by row (attend_rows).
 #include <algorithm>
 #include <climits>
-#include <cmath>
-#include <type_traits>
 
 #include "chunk_common.h"
 #include "chunk_tile.h"

@@ -60,7 +60,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const uint8_t* base, int 
 
 // Tokens t .. t + 15 (t a multiple of 16, the same in all lanes) of a page, the first n of which are looked at.
 template <int D, int KT>
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const ChunkArgs& a, const uint8_t* slice, int t, int n) {
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const uint8_t* slice, int t, int n) {
   constexpr int kRow = KT == kKvMxFp4 ? D / 2 : D;
   // mxfp4: four tokens of V share their codes' bytes; what is not looked at goes by its scale
   return rsrc(slice + t * kRow, (KT == kKvMxFp4 ? 16 : n) * kRow);
@@ -93,7 +93,7 @@ __device__ __forceinline__ void load_words(__amdgpu_buffer_rsrc_t r, int off, ui
 // n: tokens of the run that some row may attend.
 template <int D, int KT>
 __device__ __forceinline__ void load_k(const ChunkArgs& a, const uint8_t* slice, int t, int n, int col, int grp, RawK<D, KT>& r) {
-  const __amdgpu_buffer_rsrc_t k = rows_of<D, KT>(a, slice, t, n);
+  const __amdgpu_buffer_rsrc_t k = rows_of<D, KT>(slice, t, n);
   if constexpr (KT == kKvMxFp4) {
     load_words<D / 32>(k, col * (D / 2) + D / 8 * grp, r.w);
     r.scale = __builtin_amdgcn_raw_buffer_load_b8(scales_of<D>(a, slice, t), col * (D / 32) + D / 4 * grp / 32, 0, 0);
@@ -103,7 +103,7 @@ __device__ __forceinline__ void load_k(const ChunkArgs& a, const uint8_t* slice,
 }
 template <int D, int KT>
 __device__ __forceinline__ void load_v(const ChunkArgs& a, const uint8_t* slice, int t, int n, int col, int grp, RawV<D, KT>& r) {
-  const __amdgpu_buffer_rsrc_t v = rows_of<D, KT>(a, slice, t, n);
+  const __amdgpu_buffer_rsrc_t v = rows_of<D, KT>(slice, t, n);
   if constexpr (KT == kKvMxFp4) {
     load_words<D / 32>(v, (grp * 16 + col) * (D / 8), r.w);
     r.scale = __builtin_amdgcn_raw_buffer_load_b32(scales_of<D>(a, slice, t), (grp * (D / 32) + col * (D / 16) / 32) * 4, 0, 0);

@@ -115,11 +115,11 @@ __device__ __forceinline__ void send_run(const ChunkArgs& a, const uint8_t* ks, 
   } else if constexpr (T::kMx) {
     const int col = lane & 15, grp = lane >> 4;
     if (T::takes_k(wave)) {
-      load_words<T::W>(rows_of<D, KT>(a, ks, t, 16), lane * (D / 8), r.k[0]);
+      load_words<T::W>(rows_of<D, KT>(ks, t, 16), lane * (D / 8), r.k[0]);
       r.k_scale = __builtin_amdgcn_raw_buffer_load_b8(scales_of<D>(a, ks, t), (lane >> 2) * (D / 32) + (lane & 3) * D / 128, 0, 0);
     }
     if (T::takes_v(wave)) {
-      load_words<T::W>(rows_of<D, KT>(a, vs, t, 16), lane * (D / 8), r.v[0]);
+      load_words<T::W>(rows_of<D, KT>(vs, t, 16), lane * (D / 8), r.v[0]);
       r.v_scale = __builtin_amdgcn_raw_buffer_load_b32(scales_of<D>(a, vs, t), (grp * (D / 32) + col * (D / 16) / 32) * 4, 0, 0);
       const int n = left - 4 * grp;                      // byte x: token 4 grp + x; a scale of 0 is 2^-127
       r.v_scale &= n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1;
@@ -131,8 +131,8 @@ __device__ __forceinline__ void send_run(const ChunkArgs& a, const uint8_t* ks, 
       const int plane = codes_plane<D, DV, KT, TOKENS>(wave, x);
       if (plane == D / 64) continue;
       const int off = (lane >> 2) * D + 16 * (lane & 3) + 64 * plane;
-      load_words<4>(rows_of<D, KT>(a, ks, t, n), off, r.k[x]);
-      if constexpr (!G::kAlias) load_words<4>(rows_of<D, KT>(a, vs, t, n), off, r.v[x]);
+      load_words<4>(rows_of<D, KT>(ks, t, n), off, r.k[x]);
+      if constexpr (!G::kAlias) load_words<4>(rows_of<D, KT>(vs, t, n), off, r.v[x]);
     }
   }
 }
