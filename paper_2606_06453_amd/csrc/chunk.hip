@@ -210,14 +210,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       }
       fetch_k(next);
       if (!inner) mask_scores<D, D, 1>(s, tok0, tok1, grp, w);
-      uint32_t p[1][4];
+      uint32_t p[1][2][4];
       softmax_step<D, D, 1, true>(a.scale_log2, s, mask0, mask1, w, p);
       uint32_t v0[4][W], v1[4][W];
       v_rows<D, KT>(v[0], v0);
       v_rows<D, KT>(v[1], v1);
 #pragma unroll
       for (int j = 0; j < NJ; j++)
-        w.acc[0][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_operand<W>(v0, v1, j), p_operand(p[0]), w.acc[0][j], 0, 0, 0);
+#pragma unroll
+        for (int e = 0; e < 2; e++)
+          w.acc[0][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_operand<W>(v0, v1, j), p_operand(p[0][e]), w.acc[0][j], 0, 0, 0);
       fetch_v(next);
     }
   }
@@ -424,18 +426,22 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
                   sc[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[kk][e], w.q[rt][k0 + kk], sc[rt][e], 0, 0, 0);
         }
         if (!inner) mask_scores<D, DV, RT>(sc, tok0, tok1, grp, w);
-        uint32_t p[RT][4];
+        uint32_t p[RT][2][4];
         softmax_step<D, DV, RT, SPARSE>(a.scale_log2, sc, mask0, mask1, w, p);
         // bf16: the waves that add values go first, the others meanwhile weigh theirs (prompt 3485 -> 3370 us, listed
         // blocks 705 -> 688; mxfp4, whose waves also widen, 865 -> 887 us with it)
         if constexpr (KT == kKvBf16) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int j = 0; j < NJ; j++) {
-          if (KT == kKvBf16 && j == NJ - 1) __builtin_amdgcn_s_setprio(0);
-          const bf16x8_t v = v_from_lds<G::PLANE>(vt, 16 * y, j, col, grp);
+        for (int j = 0; j < NJ; j += 2) {                // two channels' operands: a weight's parts add to one sum in turn
+          if (KT == kKvBf16 && j == NJ - 2) __builtin_amdgcn_s_setprio(0);
+          const bf16x8_t v[2] = {v_from_lds<G::PLANE>(vt, 16 * y, j, col, grp), v_from_lds<G::PLANE>(vt, 16 * y, j + 1, col, grp)};
 #pragma unroll
-          for (int rt = 0; rt < RT; rt++)
-            w.acc[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_operand(p[rt]), w.acc[rt][j], 0, 0, 0);
+          for (int e = 0; e < 2; e++)
+#pragma unroll
+            for (int rt = 0; rt < RT; rt++)
+#pragma unroll
+              for (int x = 0; x < 2; x++)
+                w.acc[rt][j + x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[x], p_operand(p[rt][e]), w.acc[rt][j + x], 0, 0, 0);
         }
       }
     }

@@ -240,15 +240,16 @@ __device__ __forceinline__ void mask_scores(f32x4_t (&s)[RT][2], int tok0, int t
     }
 }
 
-// One step of the softmax: the scores s of 32 tokens become weights p, bf16, operand B of O^T = V^T P^T.  The
-// weights are taken at the present references first and seldom reach 2 (bit 14 of a bf16 number; infinities and
-// NaN have it too); only then the references move.  The sum takes the weights before their rounding, which is to the
-// nearest (2^-8 of each at most, without a bias) and halves the matrix work that two parts would need.
+// One step of the softmax: the scores s of 32 tokens become weights p, operand B of O^T = V^T P^T.  The weights are
+// taken at the present references first and seldom reach 2 (bit 14 of a bf16 number; infinities and NaN have it too);
+// only then the references move.  A weight is the sum of two bf16 parts, p[.][0] and what it leaves, p[.][1], each to
+// the nearest: 2^-16 of it at most, as in the decode step.  One part alone (2^-8) would be as large an error as the
+// rounding of the output.  The sum takes the weights before their rounding.
 // LISTED: mask0 and mask1 hold the tile tokens that list the first and the last 16 tokens; another's reference for
 // them is infinite, and their weights are zero.
 template <int D, int DV, int RT, bool LISTED>
 __device__ __forceinline__ void softmax_step(float scale_log2, const f32x4_t (&s)[RT][2], int mask0, int mask1,
-                                             Rows<D, DV, RT>& w, uint32_t (&p)[RT][4]) {
+                                             Rows<D, DV, RT>& w, uint32_t (&p)[RT][2][4]) {
   float x[RT][8];
   auto on = [&](int rt, int e) { return !LISTED || ((e ? mask1 : mask0) >> w.bit[rt] & 1) != 0; };
   auto weigh = [&](int rt) {
@@ -256,13 +257,13 @@ __device__ __forceinline__ void softmax_step(float scale_log2, const f32x4_t (&s
 #pragma unroll
     for (int i = 0; i < 8; i++) x[rt][i] = __builtin_amdgcn_exp2f(fmaf(s[rt][i >> 2][i & 3], scale_log2, -m[i >> 2]));
 #pragma unroll
-    for (int i = 0; i < 4; i++) p[rt][i] = pack_bf16(x[rt][2 * i], x[rt][2 * i + 1]);
+    for (int i = 0; i < 4; i++) p[rt][0][i] = pack_bf16(x[rt][2 * i], x[rt][2 * i + 1]);
   };
   uint32_t seen = 0;
 #pragma unroll
   for (int rt = 0; rt < RT; rt++) {
     weigh(rt);
-    seen |= (p[rt][0] | p[rt][1]) | (p[rt][2] | p[rt][3]);
+    seen |= (p[rt][0][0] | p[rt][0][1]) | (p[rt][0][2] | p[rt][0][3]);
   }
   if (__builtin_expect(__any((seen & 0x40004000u) != 0), 0)) {
 #pragma unroll
@@ -283,8 +284,12 @@ __device__ __forceinline__ void softmax_step(float scale_log2, const f32x4_t (&s
     }
   }
 #pragma unroll
-  for (int rt = 0; rt < RT; rt++)
+  for (int rt = 0; rt < RT; rt++) {
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+      p[rt][1][i] = pack_bf16(x[rt][2 * i] - bf16lo(p[rt][0][i]), x[rt][2 * i + 1] - bf16hi(p[rt][0][i]));
     w.l[rt] += ((x[rt][0] + x[rt][1]) + (x[rt][2] + x[rt][3])) + ((x[rt][4] + x[rt][5]) + (x[rt][6] + x[rt][7]));
+  }
 }
 
 __device__ __forceinline__ bf16x8_t p_operand(const uint32_t (&p)[4]) {
