@@ -1,15 +1,15 @@
 // The blocks that each token of a chunk attends (vx_chunk_score_topk): block-mean scores of every block before
 // its own, then the sink and local blocks and the best others.
 //
-// A score is sum_c qbar_c mean_jc in fp64, rounded to fp32 (qbar: the mean of the group's queries), and the
+// A score is sum_c qbar_c mean_jc in fp64, rounded to fp32 (qbar: the mean of the group's queries, summed in fp64), and the
 // selection is by these scores exactly.  Few of them are computed so:
 //   1. chunk_score_kernel: scores s' from matrix products of bf16 parts, qbar = qh + ql and mean = mh + ml
 //      (s' = qh mh + ql mh + qh ml in fp32), kept as bf16 numbers f in the workspace.  A workgroup takes up to 64
 //      tokens, one KV head and a part of the blocks; a wave splits 16 means into their parts once for all tokens.
 //   2. |s - f| <= B = kBound |qbar| max_j |mean_j| + 2^-8 max_j |f_j|: the parts leave 2^-16 of a channel each
-//      and the product of the low ones, 3 D additions 2^-23 of their sum each, together below 2^-13 of the
-//      norms' product (Cauchy-Schwarz); bf16 rounds by 2^-8 of a value.  The norms of the means are the diagonal of a
-//      matrix product too.
+//      (of qbar itself, however its heads cancel) and the product of the low ones, 3 D additions 2^-23 of their sum
+//      each, together below 2^-13 of the norms' product (Cauchy-Schwarz); bf16 rounds by 2^-8 of a value.  The
+//      norms of the means are the diagonal of a matrix product too.
 //   3. chunk_choose_kernel, a wave a row and KV head: the K-th largest f (histograms that narrow down on it) lies
 //      within [lo, hi].  Blocks with f - 2 B > hi have fewer than K others at or above them: in.  Blocks with
 //      f + 2 B < lo: out.
@@ -204,28 +204,30 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     if (tid == 0) *norm_out = 0.f;
     return;
   }
+  const double share = 1.0 / a.g;
   for (int y = wave; y < CG; y += kWaves) {
     const int x = 16 * y + col;
     const bool there = x < t.n;
     const uint16_t* q = a.q + (t.row0 + (there ? x : 0)) * a.q_row + (int64_t)h * a.g * a.q_head;
 #pragma unroll
     for (int kk = 0; kk < KS; kk++) {
-      float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      // in fp64: where a group's queries cancel, an fp32 sum is off by more than the bound of what is left
+      double v[8] = {0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0};
       for (int g = 0; g < a.g; g++) {
         const uint4 w = *reinterpret_cast<const uint4*>(q + g * a.q_head + 32 * kk + 8 * grp);
         const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-          v[2 * e] += bf16lo(ws[e]);
-          v[2 * e + 1] += bf16hi(ws[e]);
+          v[2 * e] += (double)bf16lo(ws[e]);
+          v[2 * e + 1] += (double)bf16hi(ws[e]);
         }
       }
       uint32_t hi[4], lo[4];
 #pragma unroll
       for (int e = 0; e < 4; e++) {
-        const float u = v[2 * e] / a.g, z = v[2 * e + 1] / a.g;
-        hi[e] = pack_bf16(u, z);
-        lo[e] = pack_bf16(u - bf16lo(hi[e]), z - bf16hi(hi[e]));
+        const double u = v[2 * e] * share, z = v[2 * e + 1] * share;
+        hi[e] = pack_bf16((float)u, (float)z);
+        lo[e] = pack_bf16((float)(u - (double)bf16lo(hi[e])), (float)(z - (double)bf16hi(hi[e])));
       }
       parts[y][kk][0][lane] = __builtin_bit_cast(bf16x8_t, u32x4_t{hi[0], hi[1], hi[2], hi[3]});
       parts[y][kk][1][lane] = __builtin_bit_cast(bf16x8_t, u32x4_t{lo[0], lo[1], lo[2], lo[3]});
