@@ -465,7 +465,8 @@ class Rope:
     def current(self, d: int):
         """A by-reference argument holding this rotation as it is now, on GPU d."""
         f, ax = self.inv_freq, self.axis
-        at = (f.data_ptr(), f.numel(), f.dtype, d, None if ax is None else (ax.data_ptr(), ax.numel(), ax.dtype), self.num_axes, self.first,
+        at = (f.data_ptr(), f.numel(), f.dtype, f.is_contiguous(), d,
+              None if ax is None else (ax.data_ptr(), ax.numel(), ax.dtype, ax.is_contiguous()), self.num_axes, self.first,
               self.interleaved, self.scale)
         kept = self.__dict__.get("_kept")
         if kept is not None and kept[0] == at:
