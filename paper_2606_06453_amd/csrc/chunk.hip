@@ -158,7 +158,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   const int n16 = (runs.hi - runs.lo) << shift16, pairs = (n16 + 1) >> 1;
   // 32 pairs of the wave at a time: lane 2 u + e finds run e of its pair u
   for (int w0 = wave; w0 < pairs; w0 += 32 * kWaves) {
-    int my_page = 0, my_tok = 0, my_mask = 0;
+    int my_page = 0, my_tok = 0, my_mask = 0, my_n = 0;    // my_n: of its 16 tokens, those that some row may attend
     {
       const int x = 2 * (w0 + (lane >> 1) * kWaves) + (lane & 1), y = min(x, n16 - 1);
       if (y >= 0) {                                      // past the end: the last run again, for no row
@@ -172,6 +172,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         if (x >= n16) my_mask = 0;
         my_tok = (id << runs.shift) + 16 * (y & ((1 << shift16) - 1));
         my_page = (int)clamp_page(t.pages[my_tok >> a.ps_shift], a.num_phys);
+        my_n = min(max(last - my_tok, 0), 16);           // a listed block may end in runs behind the last token
       }
     }
     const int count = min(32, (pairs - w0 + kWaves - 1) / kWaves);
@@ -183,14 +184,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
       for (int e = 0; e < 2; e++) {
         const int page = __builtin_amdgcn_readlane(my_page, 2 * u + e), tok = __builtin_amdgcn_readlane(my_tok, 2 * u + e);
-        load_k<D, KT>(a, slice_of<D, KT>(a, a.k, page, h), tok & (a.ps - 1), min(last - tok, 16), col, grp, k[e]);
+        load_k<D, KT>(a, slice_of<D, KT>(a, a.k, page, h), tok & (a.ps - 1), __builtin_amdgcn_readlane(my_n, 2 * u + e), col, grp, k[e]);
       }
     };
     auto fetch_v = [&](int u) {
 #pragma unroll
       for (int e = 0; e < 2; e++) {
         const int page = __builtin_amdgcn_readlane(my_page, 2 * u + e), tok = __builtin_amdgcn_readlane(my_tok, 2 * u + e);
-        load_v<D, KT>(a, slice_of<D, KT>(a, a.v, page, h), tok & (a.ps - 1), min(last - tok, 16), col, grp, v[e]);
+        load_v<D, KT>(a, slice_of<D, KT>(a, a.v, page, h), tok & (a.ps - 1), __builtin_amdgcn_readlane(my_n, 2 * u + e), col, grp, v[e]);
       }
     };
     fetch_k(0);
@@ -382,8 +383,8 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
       mine = __builtin_amdgcn_readlane(now.tok, s & 63);
     }
     const uint8_t* ks = slice_of<D, KT>(a, a.k, page, h);
-    send_run<D, DV, KT, TK>(a, ks, G::kAlias ? ks : slice_of<D, KT>(a, a.v, page, h), mine & (a.ps - 1), last - mine, wave, lane,
-                            bufs + (s & 1) * G::BUF, travel);
+    send_run<D, DV, KT, TK>(a, ks, G::kAlias ? ks : slice_of<D, KT>(a, a.v, page, h), mine & (a.ps - 1),
+                            SPARSE ? max(last - mine, 0) : last - mine, wave, lane, bufs + (s & 1) * G::BUF, travel);
   };
   if (steps > 0) send(0);
   for (int s = 0; s < steps; s++) {

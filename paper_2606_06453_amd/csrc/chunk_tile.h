@@ -58,7 +58,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const uint8_t* base, int 
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, bytes, 0x00020000);
 }
 
-// Tokens t .. t + 15 (t a multiple of 16, the same in all lanes) of a page, the first n of which are looked at.
+// Tokens t .. t + 15 (t a multiple of 16, the same in all lanes) of a page, the first n of which are looked at (0 to 16).
 template <int D, int KT>
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const uint8_t* slice, int t, int n) {
   constexpr int kRow = KT == kKvMxFp4 ? D / 2 : D;
