@@ -745,7 +745,7 @@ vx_status vx_rope_kv_write(const vx_paged_cache* kv, const vx_rope* rope, const 
     const bool same = q == q_out && (n == 1 || q_row_stride == q_out_row_stride) &&
                       (Hq == 1 || q_head_stride == q_out_head_stride);
     for (const Lattice& x : in) {
-      if (x.p == q && same) continue;
+      if (&x == in && same) continue;                    // q itself; other rows at its address are another input
       if (rows_meet(out, x)) return fail(VX_ERR_INVALID_ARG, "q_out and %s overlap", x.name);
     }
     if (rows_touch(out, kv->k, cache_bytes(kv, D)) || rows_touch(out, kv->v, kv->v ? cache_bytes(kv, kv->head_dim_v) : 0))
