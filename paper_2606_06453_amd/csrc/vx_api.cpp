@@ -681,6 +681,26 @@ bool rows_touch(const Lattice& x, const void* p, size_t bytes) {
   return a < c + bytes && c < b;
 }
 
+// Whether rows of x may share a byte with the positions of n rows along any of `axes` axes, whose stride is within 2^40.
+bool axes_touch(const Lattice& x, const int64_t* p, int64_t stride, int axes, int n) {
+  if (!x.p || x.n == 0 || n == 0) return false;
+  if (axes == 1 || stride == 0) return rows_touch(x, p, (size_t)n * 8);
+  uintptr_t a, b;
+  reach(x, &a, &b);
+  // axis k touches where below < k * step < above; a negative step is turned round
+  const int64_t at = (int64_t)reinterpret_cast<uintptr_t>(p);
+  int64_t below = (int64_t)a - at - (int64_t)n * 8, above = (int64_t)b - at, step = stride * 8;
+  if (step < 0) {
+    const int64_t x0 = below;
+    below = -above;
+    above = -x0;
+    step = -step;
+  }
+  if (above <= 0) return false;
+  const int64_t first = below < 0 ? 0 : below / step + 1, last = std::min<int64_t>((above - 1) / step, axes - 1);
+  return first <= last;
+}
+
 // Bytes of a cache of head dim D (checked caches only).
 size_t cache_bytes(const vx_paged_cache* kv, int D) {
   const size_t n = (size_t)kv->num_phys_pages * kv->num_kv_heads * kv->page_size * D;
@@ -736,6 +756,8 @@ vx_status vx_rope_kv_write(const vx_paged_cache* kv, const vx_rope* rope, const 
                         {"v_new", v_new, n, H, kv->head_dim_v, v_row_stride, v_head_stride}};
   for (const Lattice& x : in)
     if (x.p && (s = check_strides(x.name, x.row, x.head, n, x.heads)) != VX_OK) return s;
+  if (rope->num_axes > 1 && (positions_stride > ((int64_t)1 << 40) || positions_stride < -((int64_t)1 << 40)))
+    return fail(VX_ERR_INVALID_ARG, "positions_stride is beyond 2^40");
   if (q) {
     if ((s = check_rows("q", q, n, Hq, q_row_stride, q_head_stride)) != VX_OK) return s;
     if ((s = check_rows("q_out", q_out, n, Hq, q_out_row_stride, q_out_head_stride)) != VX_OK) return s;
@@ -750,11 +772,12 @@ vx_status vx_rope_kv_write(const vx_paged_cache* kv, const vx_rope* rope, const 
     }
     if (rows_touch(out, kv->k, cache_bytes(kv, D)) || rows_touch(out, kv->v, kv->v ? cache_bytes(kv, kv->head_dim_v) : 0))
       return fail(VX_ERR_INVALID_ARG, "q_out and the caches overlap");
-    if (rows_touch(out, slots, (size_t)n * 8) || rows_touch(out, positions, (size_t)n * 8))
+    if (rows_touch(out, slots, (size_t)n * 8) || axes_touch(out, positions, positions_stride, rope->num_axes, n))
       return fail(VX_ERR_INVALID_ARG, "q_out and positions or slots overlap");
+    const size_t pairs = (size_t)rope->dim / 2;
+    if (rows_touch(out, rope->inv_freq, pairs * 4)) return fail(VX_ERR_INVALID_ARG, "q_out and inv_freq overlap");
+    if (rows_touch(out, rope->axis, pairs * 4)) return fail(VX_ERR_INVALID_ARG, "q_out and axis overlap");
   }
-  if (rope->num_axes > 1 && (positions_stride > ((int64_t)1 << 40) || positions_stride < -((int64_t)1 << 40)))
-    return fail(VX_ERR_INVALID_ARG, "positions_stride is beyond 2^40");
   vx_batch none{};
   const vx::Rotation rot{rope->inv_freq, rope->axis, rope->num_axes, rope->first, rope->dim, rope->interleaved,
                          rope->scale};
