@@ -580,8 +580,9 @@ vx_status vx_chunk_workspace_size(vx_chunk_stage stage, const vx_paged_cache* kv
  * q [num_rows][num_q_heads][head_dim_qk] bf16 at element strides (multiples of 8, 16-byte aligned; the
  * stride of a dimension of one entry is not looked at); out [num_rows][num_q_heads][head_dim_v] bf16,
  * contiguous, rounded to nearest even from fp32 sums of weights held to 2^-16 of each (two bf16 parts, as in
- * vx_sparse_paged_decode); lse fp32 [num_rows][num_q_heads] or NULL.  A row with no token gives zeros.  Tokens that a row does not attend do
- * not reach it, whatever their values (infinities and NaN too).  sm_scale > 0.  out and lse overlap no
+ * vx_sparse_paged_decode); lse fp32 [num_rows][num_q_heads] or NULL.  A row with no token gives zeros; a
+ * row whose tokens all score -inf gives NaN (0 / 0), and an lse of -inf.  Tokens that a row does not attend
+ * do not reach it, whatever their values (infinities and NaN too).  sm_scale > 0.  out and lse overlap no
  * other array of the call. */
 vx_status vx_chunk_attention(const void* q, int64_t q_row_stride, int64_t q_head_stride, int32_t num_q_heads,
                              const vx_paged_cache* kv, const vx_batch* b, const vx_chunk* chunk, int32_t window,

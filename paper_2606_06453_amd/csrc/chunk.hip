@@ -156,6 +156,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   begin_rows<D, D, KT, 1>(a, t, h, 0, col, grp, w);
 
   const int n16 = (runs.hi - runs.lo) << shift16, pairs = (n16 + 1) >> 1;
+  int listed = 0;                                        // tile tokens that list one of the wave's runs
   // 32 pairs of the wave at a time: lane 2 u + e finds run e of its pair u
   for (int w0 = wave; w0 < pairs; w0 += 32 * kWaves) {
     int my_page = 0, my_tok = 0, my_mask = 0, my_n = 0;    // my_n: of its 16 tokens, those that some row may attend
@@ -199,6 +200,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     for (int u = 0; u < count; u++) {
       const int tok0 = __builtin_amdgcn_readlane(my_tok, 2 * u), tok1 = __builtin_amdgcn_readlane(my_tok, 2 * u + 1);
       const int mask0 = __builtin_amdgcn_readlane(my_mask, 2 * u), mask1 = __builtin_amdgcn_readlane(my_mask, 2 * u + 1);
+      if constexpr (SPARSE) listed |= mask0 | mask1;
       const bool inner = min(tok0, tok1) >= w.all_from && max(tok0, tok1) + 16 <= w.all_to;
       const int next = min(u + 1, count - 1);
       f32x4_t s[1][2];
@@ -233,7 +235,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   const int orow = tid / (D / CPT), oc = (tid % (D / CPT)) * CPT;
   __syncthreads();
   const float sum = column_sum(w.l[0]);
-  if (grp == 0) mbuf[wave * 16 + col] = make_float2(w.m[0], sum);
+  if (grp == 0) mbuf[wave * 16 + col] = make_float2(SPARSE && !(listed >> w.bit[0] & 1) ? -INFINITY : w.m[0], sum);
 #pragma unroll
   for (int i = 0; i < 4; i++)
 #pragma unroll
@@ -260,6 +262,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   }
   const float inv = total > 0.f ? 1.f / total : 0.f;
   bool fine = fabsf(total) < INFINITY;
+  if (total == 0.f) {                                    // a row that attends tokens and has no weight: every score is -inf
+    bool some = false;
+    if constexpr (SPARSE) {
+#pragma unroll
+      for (int x = 0; x < kWaves; x++) some = some || ml[x].x > -INFINITY;
+    } else if (orow < rows) {
+      const int p = t.p0 + orow / a.g;
+      some = max(first_key(a, p), runs.lo << 4) < min(end_key(a, t, p), min(runs.hi, INT_MAX >> 4) << 4);
+    }
+    fine = !some;
+  }
 #pragma unroll
   for (int c = 0; c < CPT; c++) {
     fine = fine && fabsf(o[c]) < INFINITY;
@@ -386,6 +399,7 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
     send_run<D, DV, KT, TK>(a, ks, G::kAlias ? ks : slice_of<D, KT>(a, a.v, page, h), mine & (a.ps - 1),
                             SPARSE ? max(last - mine, 0) : last - mine, wave, lane, bufs + (s & 1) * G::BUF, travel);
   };
+  int listed = 0;                                        // tile tokens that list a run of the part
   if (steps > 0) send(0);
   for (int s = 0; s < steps; s++) {
     uint8_t* buf = bufs + (s & 1) * G::BUF;
@@ -402,6 +416,7 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
 #pragma unroll
     for (int y = 0; y < G::UNITS; y += 2) {
       const int tok0 = tok[y], tok1 = tok[y + 1], mask0 = mask[y], mask1 = mask[y + 1];
+      if constexpr (SPARSE) listed |= mask0 | mask1;
       const bool some = SPARSE ? ((mask0 | mask1) & wave_mask) != 0 : tok0 < wave_to && tok0 + 32 > wave_from;
       if (some) {
         // of a list the last blocks alone may reach past a row's own token
@@ -456,7 +471,9 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
     const int r = r0 + 16 * rt + col;
     const bool there = r < rows;
     const int64_t at = (t.row0 + (there ? r / a.g : 0)) * a.Hq + h * a.g + (there ? r % a.g : 0);
-    bool fine = fabsf(total) < INFINITY;
+    // a row that attends tokens and has no weight: every score is -inf
+    const bool some = SPARSE ? (listed >> w.bit[rt] & 1) != 0 : max(w.from[rt], runs.lo << 4) < w.to[rt];
+    bool fine = fabsf(total) < INFINITY && !(total == 0.f && some);
 #pragma unroll
     for (int j = 0; j < NJ; j++) {
       float o[4];
@@ -522,9 +539,10 @@ __global__ __launch_bounds__(kThreads) void chunk_merge_kernel(const ChunkArgs a
 #pragma unroll
     for (int s = 1; s < kWave; s <<= 1) total += xor_shfl(total, s);
     w = total != 0.f ? w / total : 0.f;
+    const bool bare = total == 0.f && __any(ml.x > -INFINITY);           // tokens, and no weight
     float o[N];
 #pragma unroll
-    for (int c = 0; c < N; c++) o[c] = 0.f;
+    for (int c = 0; c < N; c++) o[c] = bare ? NAN : 0.f;
     const float* src = a.part_o + at * S * DV + N * lane;
     for (int s0 = 0; s0 < S; s0 += kBatch) {
       float v[kBatch][N];

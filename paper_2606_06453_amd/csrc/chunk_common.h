@@ -183,13 +183,17 @@ struct Runs {
   int shift;                               // log2 tokens of a run (at most 6)
 };
 
-// State of a row: reference and sum of the weights in the log2 domain, and channels 8 c8 + j of the
-// weighted mean in the lanes c8 = lane, lane + 64 below DV / 8.
+// State of a row: reference and sum of the weights in the log2 domain, channels 8 c8 + j of the weighted mean in the
+// lanes c8 = lane, lane + 64 below DV / 8, and whether the row attends a token at all.
 template <int DV>
 struct RowState {
   static constexpr int N = (DV / 8 + kWave - 1) / kWave;
   float m, l, o[N][8];
+  bool any;
 };
+// The reference of a part whose tokens all score -inf (a part without a token: -inf).  A row of such parts alone has no
+// weights, 0 / 0, and gives NaN; a row without a token gives zeros.
+constexpr float kNoWeight = -3.0e38f;
 
 // A wave's attention of query head r of tile token x over the runs, without matrix operands: a token that
 // the row does not attend is not multiplied by a zero weight but left out, so that its infinities and NaN
@@ -204,6 +208,7 @@ __device__ void attend_row(const ChunkArgs& a, const Tile& t, int h, int r, int 
   const void* vbase = a.v ? a.v : a.k;
   st.m = -INFINITY;
   st.l = 0.f;
+  st.any = false;
 #pragma unroll
   for (int u = 0; u < RowState<DV>::N; u++)
 #pragma unroll
@@ -221,6 +226,7 @@ __device__ void attend_row(const ChunkArgs& a, const Tile& t, int h, int r, int 
     }
     const uint64_t some = __ballot(ok);
     if (!some) continue;
+    st.any = true;
     int page = 0;
     float z = -INFINITY;
     const int at = tok & (a.ps - 1);
@@ -278,7 +284,7 @@ template <int DV>
 __device__ __forceinline__ void store_row(const ChunkArgs& a, int64_t row, int head, int s, const RowState<DV>& st) {
   const int lane = lane_id();
   const int64_t at = row * a.Hq + head;
-  const bool parts = a.splits > 1;
+  const bool parts = a.splits > 1, bare = st.any && st.l == 0.f;
 #pragma unroll
   for (int u = 0; u < RowState<DV>::N; u++) {
     const int c8 = lane + kWave * u;
@@ -291,12 +297,12 @@ __device__ __forceinline__ void store_row(const ChunkArgs& a, int64_t row, int h
       uint32_t w[4];
 #pragma unroll
       for (int e = 0; e < 4; e++)
-        w[e] = f32_to_bf16_rne(st.o[u][2 * e] * a.v_scale) | (f32_to_bf16_rne(st.o[u][2 * e + 1] * a.v_scale) << 16);
+        w[e] = bare ? 0x7fc07fc0u : f32_to_bf16_rne(st.o[u][2 * e] * a.v_scale) | (f32_to_bf16_rne(st.o[u][2 * e + 1] * a.v_scale) << 16);
       *reinterpret_cast<uint4*>(a.out + at * DV + 8 * c8) = make_uint4(w[0], w[1], w[2], w[3]);
     }
   }
   if (lane == 0) {
-    if (parts) a.part_ml[at * a.splits + s] = make_float2(st.m, st.l);
+    if (parts) a.part_ml[at * a.splits + s] = make_float2(bare ? kNoWeight : st.m, st.l);
     else if (a.lse) a.lse[at] = st.l > 0.f ? (st.m + log2f(st.l)) * 0.693147180559945309f : st.l == 0.f ? -INFINITY : st.l;
   }
 }
