@@ -567,8 +567,10 @@ typedef enum {
   VX_CHUNK_SPARSE = 2
 } vx_chunk_stage;
 
-/* Host-only: workspace bytes of a chunk call for num_rows rows of queries (max_sel: of the two calls with
- * selections, else not looked at).  The buffer needs no filling and is 16-byte aligned. */
+/* Host-only: workspace bytes of chunk calls of up to num_rows rows of queries, over batches of up to b->batch requests
+ * and b->max_pages_per_seq pages and lists of up to max_sel blocks (of the two calls with selections, else not looked
+ * at): a prompt's short last chunk may need more than its long ones do.  A call asks for what it needs itself.  The
+ * buffer needs no filling and is 16-byte aligned. */
 vx_status vx_chunk_workspace_size(vx_chunk_stage stage, const vx_paged_cache* kv, const vx_batch* b, int32_t num_rows,
                                   int32_t num_q_heads, int32_t max_sel, size_t* bytes);
 

@@ -587,25 +587,33 @@ struct Plan {
   int tokens, splits;
   size_t o_bytes, bytes;
 };
+int tile_tokens(int operands, int group, bool sparse) {
+  const int rows = operands == 0 ? kTileRows : 4 * kTileRows * operands;
+  return std::max(1, sparse ? std::min(16, rows / group) : rows / group);
+}
+int64_t most_parts(const Geometry& g, int tokens, bool sparse, int max_sel) {
+  const int64_t list = std::min<int64_t>((int64_t)g.max_pages * g.bs, sparse ? (int64_t)max_sel * tokens * g.bs : INT64_MAX);
+  return std::min<int64_t>(kMaxParts, (list + kPartTokens - 1) / kPartTokens);
+}
+size_t part_bytes(const Geometry& g) { return g.Dv * sizeof(float) + sizeof(float2); }
+constexpr int kHalvesFrom = kTargetWgs / 2, kHalvesTo = kTargetWgs * 3 / 4;        // tiles of the latent: see plan_of
 Plan plan_of(const Geometry& g, int n, int Hq, bool sparse, int max_sel) {
   Plan p{};
   const int group = Hq / g.H;
   const bool latent = g.Dqk != g.Dv;
   const int64_t batch = std::max(g.batch, 1);
-  auto tokens = [&](int rows) { return std::max(1, sparse ? std::min(16, rows / group) : rows / group); };
   if (!latent && g.kv_dtype != kKvBf16 && (int64_t)n <= batch * kNarrowTiles * (kTileRows / group)) p.operands = 0;
   else p.operands = sparse || latent || (int64_t)n * group <= batch * 4 * kTileRows ? 1 : 2;
-  p.tokens = tokens(p.operands == 0 ? kTileRows : 4 * kTileRows * p.operands);
+  p.tokens = tile_tokens(p.operands, group, sparse);
   const int64_t tiles = std::max<int64_t>(batch, (n + p.tokens - 1) / p.tokens) * g.H;
-  const int64_t list = std::min<int64_t>((int64_t)g.max_pages * g.bs, sparse ? (int64_t)max_sel * p.tokens * g.bs : INT64_MAX);
-  const int64_t most = std::min<int64_t>(kMaxParts, (list + kPartTokens - 1) / kPartTokens);
+  const int64_t most = most_parts(g, p.tokens, sparse, max_sel);
   // A little more than one tile of the latent a CU: as halves, most CUs take three in place of two wholes (350 tiles 470
   // -> 377 us; where memory bounds, as for drafted tokens, halves cost more than they bring: 58 -> 70 us).
-  const bool halves = latent && tiles > kTargetWgs / 2 && tiles <= kTargetWgs * 3 / 4;
+  const bool halves = latent && tiles > kHalvesFrom && tiles <= kHalvesTo;
   p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, halves ? 2 : kTargetWgs / tiles));
   if (p.splits > 1) {
     p.o_bytes = (size_t)n * Hq * p.splits * g.Dv * sizeof(float);
-    p.bytes = p.o_bytes + (size_t)n * Hq * p.splits * sizeof(float2);
+    p.bytes = (size_t)n * Hq * p.splits * part_bytes(g);
   }
   p.bytes = std::max<size_t>(p.bytes, 16);
   return p;
@@ -674,6 +682,23 @@ hipError_t launch_d(const ChunkArgs& a, int kt, int operands, hipStream_t stream
 
 size_t chunk_attention_workspace(const Geometry& g, int n, int Hq, bool sparse, int max_sel) {
   return plan_of(g, n, Hq, sparse, max_sel).bytes;
+}
+
+// The same for any call of at most n rows, g.batch requests and max_sel blocks a list.  Tiles of T tokens and H heads number at
+// least rows H / T, so that rows times parts is at most T kTargetWgs / H (or rows times `most`), and of halves 2 T kHalvesTo / H.
+size_t chunk_attention_workspace_up_to(const Geometry& g, int n, int Hq, bool sparse, int max_sel) {
+  const int group = Hq / g.H;
+  const bool latent = g.Dqk != g.Dv;
+  int64_t most = 0;
+  for (int operands = 0; operands <= 2; operands++) {
+    if ((operands == 0 && (latent || g.kv_dtype == kKvBf16)) || (operands == 2 && (latent || sparse))) continue;
+    const int T = tile_tokens(operands, group, sparse);
+    const int64_t parts = most_parts(g, T, sparse, max_sel);
+    if (parts <= 1) continue;
+    most = std::max(most, std::min<int64_t>(n * parts, (int64_t)T * kTargetWgs / g.H));
+    if (latent) most = std::max(most, 2 * std::min<int64_t>(n, (int64_t)T * kHalvesTo / g.H));
+  }
+  return std::max<size_t>((size_t)most * Hq * part_bytes(g), 16);
 }
 
 hipError_t launch_chunk_attention(const Geometry& g, const ChunkRows& rows, const ChunkSelection& sel, int window,

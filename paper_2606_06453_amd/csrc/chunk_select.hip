@@ -611,6 +611,22 @@ hipError_t launch(const ChunkArgs& a, SelectArgs& s, const SelectPlan& p, hipStr
 
 size_t chunk_select_workspace(const Geometry& g, int n) { return plan_of(g, n).bytes; }
 
+// The same for any call of at most n rows and g.batch requests: the larger of both tiles' scores, and norms of as many parts as a
+// row can have.
+size_t chunk_select_workspace_up_to(const Geometry& g, int n) {
+  const int64_t batch = std::max(g.batch, 1);
+  const int stride = (g.max_pages + 63) & ~63;
+  const int parts = (stride + kUnit * kWaves - 1) / (kUnit * kWaves);
+  size_t most = 0;
+  for (const int tokens : {16, 64}) {
+    const int64_t rows = tokens == 16 ? std::min<int64_t>(n, 16 * batch) : n;
+    const size_t tile = (size_t)tokens * g.H * stride * sizeof(uint16_t);
+    const int64_t tiles = std::max<int64_t>(1, std::min<int64_t>(most_tiles(rows, tokens, batch), (int64_t)(kScoreBytes / tile)));
+    most = std::max(most, (tile * tiles + 255) / 256 * 256 + sizeof(float) * (size_t)tiles * g.H * parts);
+  }
+  return most;
+}
+
 hipError_t launch_chunk_select(const Geometry& g, const ChunkRows& rows, const float* mean, const int32_t* budget,
                                int n_sink, int n_local, int max_sel, int32_t* sel_pages, int32_t* sel_count, void* ws,
                                hipStream_t stream) {

@@ -893,8 +893,8 @@ vx_status vx_chunk_workspace_size(vx_chunk_stage stage, const vx_paged_cache* kv
   if (stage != VX_CHUNK_ATTENTION && max_sel < 1) return fail(VX_ERR_INVALID_ARG, "max_sel must be >= 1");
   const vx::Geometry g = geometry(kv, b);
   *bytes = stage == VX_CHUNK_SCORE_TOPK
-               ? vx::chunk_select_workspace(g, num_rows)
-               : vx::chunk_attention_workspace(g, num_rows, num_q_heads, stage == VX_CHUNK_SPARSE, max_sel);
+               ? vx::chunk_select_workspace_up_to(g, num_rows)
+               : vx::chunk_attention_workspace_up_to(g, num_rows, num_q_heads, stage == VX_CHUNK_SPARSE, max_sel);
   return VX_OK;
 }
 

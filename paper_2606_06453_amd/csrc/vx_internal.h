@@ -138,11 +138,14 @@ struct ChunkSelection {
   const int32_t* count = nullptr;
   int max_sel = 0;
 };
+// Of this call; and of any call of at most as many rows, requests and blocks a list.
 size_t chunk_attention_workspace(const Geometry& g, int n, int Hq, bool sparse, int max_sel);
+size_t chunk_attention_workspace_up_to(const Geometry& g, int n, int Hq, bool sparse, int max_sel);
 hipError_t launch_chunk_attention(const Geometry& g, const ChunkRows& rows, const ChunkSelection& sel, int window,
                                   bool causal, float sm_scale, uint16_t* out, float* lse, void* ws, hipStream_t stream);
 
 size_t chunk_select_workspace(const Geometry& g, int n);
+size_t chunk_select_workspace_up_to(const Geometry& g, int n);
 hipError_t launch_chunk_select(const Geometry& g, const ChunkRows& rows, const float* mean, const int32_t* budget,
                                int n_sink, int n_local, int max_sel, int32_t* sel_pages, int32_t* sel_count, void* ws,
                                hipStream_t stream);

@@ -519,7 +519,8 @@ CHUNK_ATTENTION, CHUNK_SCORE_TOPK, CHUNK_SPARSE = 0, 1, 2
 def chunk_workspace_size(stage: int, kv: PagedKV, batch: BatchSpec, num_rows: int, num_q_heads: int,
                          max_sel: int = 1) -> int:
     """Workspace bytes of chunk_attention, chunk_score_topk or sparse_chunk_attention (stage CHUNK_ATTENTION,
-    CHUNK_SCORE_TOPK, CHUNK_SPARSE) for num_rows rows of queries."""
+    CHUNK_SCORE_TOPK, CHUNK_SPARSE) for up to num_rows rows of queries, over up to as many requests and pages
+    as the batch has and lists of up to max_sel blocks: one buffer serves all chunks of a prompt."""
     out = ctypes.c_size_t(0)
     _check(lib().vx_chunk_workspace_size(stage, kv.current(), batch.kept(), int(num_rows), int(num_q_heads), int(max_sel),
                                          ctypes.byref(out)))
