@@ -278,6 +278,7 @@ class BatchSpec:
         at = (self.page_indptr.data_ptr(), self.page_indices.data_ptr(), lens.data_ptr(), lens.numel(), self.max_pages_per_seq)
         kept = self.__dict__.get("_kept")
         if kept is None or kept[0] != at:
+            _counts(max_pages_per_seq=self.max_pages_per_seq)
             st = self.struct()
             kept = self.__dict__["_kept"] = (at, ctypes.byref(st))
         return kept[1]
@@ -331,6 +332,13 @@ class PagePool:
 
 
 _MOST = 2 ** 31 - 1      # what the calls' 32-bit counts hold
+
+
+def _counts(**values) -> None:
+    """Refuses what a call's 32-bit argument would hold the low bits of."""
+    for name, x in values.items():
+        if not -_MOST <= x <= _MOST:
+            raise ValueError(f"{name} must fit 32 bits (got {x})")
 
 
 def _gpu_of(t: torch.Tensor) -> int:
@@ -476,6 +484,7 @@ class Rope:
         if ax is not None and (ax.dtype is not torch.int32 or ax.numel() != f.numel() or ax.get_device() != d
                                or not ax.is_contiguous()):
             _refuse(ax, torch.int32, f.numel(), "axis")
+        _counts(num_axes=self.num_axes, first=self.first)
         kept = self.__dict__["_kept"] = (at, ctypes.byref(
             _Rope(f.data_ptr(), None if ax is None else ax.data_ptr(), int(self.num_axes), int(self.first), 2 * f.numel(),
                   int(bool(self.interleaved)), float(self.scale))))
@@ -522,6 +531,7 @@ def chunk_workspace_size(stage: int, kv: PagedKV, batch: BatchSpec, num_rows: in
     CHUNK_SCORE_TOPK, CHUNK_SPARSE) for up to num_rows rows of queries, over up to as many requests and pages
     as the batch has and lists of up to max_sel blocks: one buffer serves all chunks of a prompt."""
     out = ctypes.c_size_t(0)
+    _counts(stage=stage, num_rows=num_rows, num_q_heads=num_q_heads, max_sel=max_sel)
     _check(lib().vx_chunk_workspace_size(stage, kv.current(), batch.kept(), int(num_rows), int(num_q_heads), int(max_sel),
                                          ctypes.byref(out)))
     return int(out.value)
@@ -584,6 +594,10 @@ def chunk_attention(q: torch.Tensor, kv: PagedKV, batch: BatchSpec, q_indptr: to
     n, heads = q.shape[:2]
     o = _result(out, torch.bfloat16, (n, heads, kv._dims[2]), d, "out")
     e = _result(lse, torch.float32, (n, heads), d, "lse")
+    if window > _MOST:
+        window = _MOST                                       # longer than any request
+    elif window < -_MOST:
+        _counts(window=window)
     _check(lib().vx_chunk_attention(*args, int(window), int(bool(causal)), float(sm_scale), o, e, workspace.data_ptr(),
                                     _bytes(workspace), _stream(stream, d)))
 
@@ -596,6 +610,7 @@ def chunk_score_topk(q: torch.Tensor, kv: PagedKV, batch: BatchSpec, q_indptr: t
     sel_pages [n][H][max_sel] and sel_count [n] (int32).  kind: MEAN_DOT; n_local >= 1."""
     d, args = _chunk_args(q, kv, batch, q_indptr, q_lens, workspace)
     n, H, D = q.shape[0], kv._dims[0], kv._dims[1]
+    _counts(kind=kind, n_sink=n_sink, n_local=n_local)
     blocks = kv.k.shape[0] * (kv.k.shape[2] // kv.block_size if kv.block_size else 1)
     m = _result(mean, torch.float32, (blocks, H, D), d, "mean")
     budget = _result(pages_budget, torch.int32, (batch.seq_lens.numel(),), d, "pages_budget")
