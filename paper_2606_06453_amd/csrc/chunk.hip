@@ -300,12 +300,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 }
 
 // Tokens of a buffer.  Listed blocks are short runs in any place, which take longest to arrive: half the tokens let
-// twice the workgroups wait side by side (4096 tokens over 128 blocks each 1069 -> 923 us).  bf16 rows of 128 channels:
-// with 32 the prompt kernel has room for three waves a SIMD (3290 -> 3215 us; with two 3390); the types that pass
-// through registers want 64 (mxfp4 864, with 32 1160 us).  The latent's rows are 4.5 times longer, and two workgroups of
-// 72 KB share a CU.
+// twice the workgroups wait side by side (4096 tokens over 128 blocks each 790 us, with 64 880).  Lists of everything
+// want 64 (prompts: bf16 4380, with 32 and two waves a SIMD 4590, with 32 and three 4470; mxfp4 1000 and 1228).  The
+// latent's rows are 4.5 times longer, and two workgroups of 72 KB share a CU.
 template <int D, int DV, int KT, bool SPARSE>
-constexpr int kTokens = SPARSE || D != DV || (KT == kKvBf16 && D == 128) ? 32 : 64;
+constexpr int kTokens = SPARSE || D != DV ? 32 : 64;
 
 // Four waves of 16 RT rows each share the tokens of their tile through LDS (chunk_wide.h).  A wave passes over
 // runs that none of its rows attends.  Two operands of rows a wave halve the reads of LDS a product; one serves tiles of
@@ -498,14 +497,10 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
   if (__syncthreads_or(bad)) attend_rows<D, DV, KT>(a, t, h, runs, split);
 }
 
-// The latent's rows just fit two waves a SIMD; as fp8 30 words go to scratch, and yet one wave takes longer (44 requests'
-// drafted tokens 326 us, 412 with one; prompts 273 and 386).  Prompts of bf16 rows
-// keep nine words of the setup in scratch for a third wave.
-template <int D, int DV, int KT, int RT>
-constexpr int kWavesPerSimd = KT == kKvBf16 && D == 128 && RT == 2 ? 3 : 2;
-
+// The latent's rows just fit two waves a SIMD, with some words in scratch (15, as fp8 50); one wave takes longer (44
+// requests' drafted tokens 280 and 399 us, 440 and 432 with one).
 template <int D, int DV, int KT, int RT, bool SPARSE>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd<D, DV, KT, RT>))) void chunk_wide_kernel(const ChunkArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void chunk_wide_kernel(const ChunkArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
   const int h = (int)blockIdx.x % a.H, split = (int)blockIdx.y;
   Tile t;
@@ -607,8 +602,11 @@ Plan plan_of(const Geometry& g, int n, int Hq, bool sparse, int max_sel) {
   p.tokens = tile_tokens(p.operands, group, sparse);
   const int64_t tiles = std::max<int64_t>(batch, (n + p.tokens - 1) / p.tokens) * g.H;
   const int64_t most = most_parts(g, p.tokens, sparse, max_sel);
-  // A little more than one tile of the latent a CU: as halves, most CUs take three in place of two wholes (350 tiles 470
-  // -> 377 us; where memory bounds, as for drafted tokens, halves cost more than they bring: 58 -> 70 us).
+  // A little more than one tile of the latent a CU: as halves, which are cut from the longest list and so spare the short
+  // ones, the long lists end earlier.  40 batches of 260 to 384 tiles with contexts of 0-2048 to 16000-30000 tokens take
+  // 0.62 to 1.10 times as long as wholes, 0.83 on average (8 requests of 2048-8192: 350 and 493 us), 8 batches of equal
+  // contexts 1.07 to 1.33 times; how even a batch is the host does not know.  Where memory bounds, as for drafted tokens,
+  // halves cost more than they bring (58 -> 70 us).
   const bool halves = latent && tiles > kHalvesFrom && tiles <= kHalvesTo;
   p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, halves ? 2 : kTargetWgs / tiles));
   if (p.splits > 1) {
