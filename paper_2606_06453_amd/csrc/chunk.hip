@@ -136,7 +136,7 @@ __device__ __forceinline__ Runs part_runs(const ChunkArgs& a, const Tile& t, int
 // Four waves share a tile of 16 query rows; each takes every fourth pair of 16-token runs of the tile's list,
 // straight from the cache into matrix operands, and the waves' states meet in LDS.  For few rows over fp8 or mxfp4 caches,
 // which memory bounds: no barrier stands between loads and their use, and codes widen once for 16 rows (drafted tokens of
-// 32 users over 64 listed blocks of 32 tokens, E4M3: 57 us, 6.4 TB/s of the 7.05 that a stream reads; in wide tiles 124).
+// 32 users over 64 listed blocks of 32 tokens, E4M3: 57 us, 6.3 TB/s of the 7.05 that a stream reads; in wide tiles 114).
 // bf16 rows take wide tiles from the first row: straight to LDS they need no register on their way (4 users' drafted
 // tokens 92 us, here 125).
 template <int D, int KT, bool SPARSE>
@@ -309,14 +309,14 @@ constexpr int kTokens = SPARSE || D != DV ? 32 : 64;
 // Four waves of 16 RT rows each share the tokens of their tile through LDS (chunk_wide.h).  A wave passes over
 // runs that none of its rows attends.  Two operands of rows a wave halve the reads of LDS a product; one serves tiles of
 // up to 64 rows, listed blocks (16 tokens a mask) and the latent, whose 512 output channels fill the registers.
-//   a prompt's last 8192 of 32768 tokens, 32 heads over 8, bf16: 3275 us, 1176 TFLOP/s (a library product of 16384^3
-//     1356); matrix instructions 59% and vector ones 56% of the cycles, at 1.9 GHz: 11% fewer cycles by a third wave a
-//     SIMD were 2% less time
-//   prompts and drafts of 48 requests, mxfp4: 860 us, 770 TFLOP/s; 35% and 45%, and the widened rows' way to LDS
-//   prompts under a window of 1000 tokens, 64 channels, E4M3: 94 us; 31% and 69%: the softmax, which D does not shorten
-//   the latent, eight prompts' chunks: 287 us with the join, 735 TFLOP/s; 37% and 18%, LDS 37%
-//   4096 tokens over 128 listed blocks of 16 each: 680 us; 30% and 47%.  A wave's four tokens list 2.3 times the blocks
-//     of one, so 203 TFLOP/s of what the tokens list are 600 of products
+//   a prompt's last 8192 of 32768 tokens, 32 heads over 8, bf16: 4420 us, 1300 TFLOP/s with the weights' second part
+//     counted (a library product of 16384^3 1356); matrix instructions 61% and vector ones up to 55% of the cycles, at 1.9
+//     to 2 GHz.  With weights in one part 3200 us at the same rate
+//   prompts and drafts of 48 requests, mxfp4: 1000 us; 45% and up to 51%, and the widened rows' way to LDS
+//   prompts under a window of 1000 tokens, 64 channels, E4M3: 118 us; 37% and 75%: the softmax, which D does not shorten
+//   the latent, eight prompts' chunks: 348 us with the join; 51% and 24%, LDS 35%
+//   4096 tokens over 128 listed blocks of 16 each: 790 us; 38% and 52%.  A wave's four tokens list 2.3 times the blocks
+//     of one, and pairs of runs in the order of blocks make that 3.3
 template <int D, int DV, int KT, int RT, bool SPARSE>
 __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int h, int split, uint32_t* lds) {
   constexpr int TK = kTokens<D, DV, KT, SPARSE>;
@@ -443,8 +443,8 @@ __device__ __forceinline__ void wide_tile(const ChunkArgs& a, const Tile& t, int
         if (!inner) mask_scores<D, DV, RT>(sc, tok0, tok1, grp, w);
         uint32_t p[RT][2][4];
         softmax_step<D, DV, RT, SPARSE>(a.scale_log2, sc, mask0, mask1, w, p);
-        // bf16: the waves that add values go first, the others meanwhile weigh theirs (prompt 3485 -> 3370 us, listed
-        // blocks 705 -> 688; mxfp4, whose waves also widen, 865 -> 887 us with it)
+        // bf16: the waves that add values go first, the others meanwhile weigh theirs (prompt 4500 -> 4470 us, listed
+        // blocks 796 -> 785, the latent 346 -> 351; mxfp4, whose waves also widen, 1000 -> 1046 us with it)
         if constexpr (KT == kKvBf16) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int j = 0; j < NJ; j += 2) {                // two channels' operands: a weight's parts add to one sum in turn

@@ -18,8 +18,9 @@
 // its square is lost, select by digits of the exact scores alone, which they compute anew for every digit.
 // One kernel that kept the scores of 32 tokens in LDS took 388 us for 4096 tokens over 2048 blocks and 55 us for a few
 // users' drafted tokens: a row's passes waited with two waves a SIMD, and few tokens left most of the chip idle.
-// Now 230 and 36 us: 4096 tokens take 95 us of scores and 122 us of choosing, which vector instructions bound (2200 a
-// row); eight users' 4 tokens each 17 us and 17 us, which are the latencies of a few dependent passes.
+// Now 231 and 37 us: 4096 tokens take 95 us of scores and 123 us of choosing, which vector instructions bound (2200 a
+// row); eight users' 4 tokens each 17 us and 17 us, which are the latencies of a few dependent passes.  With equal means
+// every row selects by digits: 17 ms and 2 ms.
 #include <algorithm>
 
 #include "chunk_tile.h"
@@ -183,7 +184,7 @@ __device__ __forceinline__ void select_by_digits(const ChunkArgs& a, const Selec
 }
 
 // CG groups of 16 tokens, all of whose queries stay in registers, and a part of the blocks.  4096 tokens over 2048
-// blocks of 8 heads, 95 us: matrix instructions 25% and vector ones, which split the means (once for 64 tokens), 34% of
+// blocks of 8 heads, 95 us: matrix instructions 27% and vector ones, which split the means (once for 64 tokens), 34% of
 // the time; the means come from the caches, 8 MB for every 64 tokens.
 template <int D, int CG>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void chunk_score_kernel(const ChunkArgs a, const SelectArgs s) {
